@@ -236,6 +236,99 @@ qsl_status qsl_debug_units(qsl_ctx *ctx, uint32_t *out_host, uint32_t max_units,
 qsl_status qsl_timing_enable(qsl_ctx *ctx, int enabled);
 qsl_status qsl_timing_read(qsl_ctx *ctx, double *total_ms, uint32_t *launches);
 
+/* ---- what stands before and behind the synchronisation: a model's logits -----------------------------------------------
+ * The local step of Algorithm 1 starts from the gradient of a loss in the model's logits, and the plots of Section 5 (loss,
+ * top-1 and top-5 error against bits) from the log probabilities of the right classes and the best alternatives.  The calls below
+ * work on `rows` rows of `vocab` logits each (a row: a sample, a position; a class: a label, a token).  With the factor c = scale,
+ * logp_i = c z_i - ln sum_j exp(c z_j) and p_i = exp(logp_i), natural logarithms throughout.
+ *   - They have no context, keep nothing from one call for the next, and may run at the same time: all state is in the caller's
+ *     arrays and `workspace`, which belongs to one call at a time (two captured graphs that may run side by side need one each).
+ *     They enqueue kernels on `hip_stream` (NULL = the default stream) of the current HIP device, whose memory all device
+ *     pointers are, and can be captured into a graph.
+ *   - All arithmetic is in 32 bits or more, whatever the type of the logits; a gradient is rounded to that type once.  Results do not
+ *     depend on anything but the inputs: no atomics decide an order of additions.
+ *   - A logit of -inf is a class left out: its probability and gradient are 0, its log probability -inf.  A row of nothing else has
+ *     lse and log probabilities -inf, entropy 0 and gradient 0.  A NaN or +inf makes the row's results NaN (indices: -1).
+ *   - rows = 0 does nothing.  What lies between two rows (stride > vocab) is neither read nor written.
+ */
+enum { QSL_F32 = 0, QSL_BF16 = 1, QSL_F16 = 2 };
+#define QSL_TOP_MAX 128      /* alternatives per row at most */
+#define QSL_TEACHER_MAX 256  /* entries of a teacher's row at most */
+
+typedef struct {
+  const void *data;          /* device; row n starts at element n * stride                              */
+  uint64_t stride;           /* elements from one row to the next, >= vocab                             */
+  uint32_t rows;             /* < 2^31                                                                  */
+  uint32_t vocab;            /* classes, 1 <= vocab < 2^31                                              */
+  uint32_t dtype;            /* QSL_F32, QSL_BF16, QSL_F16; data is aligned to it                       */
+  float scale;               /* c, 2^-100 <= c <= 2^100 (1: the logits as they are; 1 / temperature)    */
+} qsl_logits;
+
+/* Bytes of device memory that the calls below need for such rows (0 for most), a multiple of 256; pass `top` = 0 for all calls but
+ * qsl_token_logprobs with alternatives.  0 for invalid arguments too. */
+size_t qsl_logits_workspace_bytes(const qsl_logits *z, uint32_t top);
+
+/* Log probabilities of given classes, with the entropy and the best alternatives of every row.
+ *   target       device, const int64 [rows], or NULL; target < 0: none is given (logprob 0); >= vocab: logprob NaN
+ *   top          alternatives per row, 0 .. min(vocab, QSL_TOP_MAX)
+ *   logprob      device, float [rows] or NULL (needs target): logp of the given class
+ *   entropy      device, float [rows] or NULL: -sum_i p_i logp_i
+ *   lse          device, float [rows] or NULL: ln sum_i exp(c z_i)
+ *   top_index    device, int32 [rows, top] or NULL: the classes of the largest logits, largest first, ties to the lower index
+ *   top_logprob  device, float [rows, top] or NULL: their logp
+ *   stats        device, float [rows, 4] or NULL: for qsl_token_logprobs_backward on the same logits and scale
+ *   workspace    device, qsl_logits_workspace_bytes() bytes, 256-byte aligned, or NULL if that is 0 */
+qsl_status qsl_token_logprobs(const qsl_logits *z, const int64_t *target, uint32_t top, float *logprob, float *entropy,
+                              float *lse, int32_t *top_index, float *top_logprob, float *stats, void *workspace,
+                              size_t workspace_bytes, void *hip_stream);
+
+/* The gradient in the logits of  sum_n grad_logprob[n] logprob[n] + grad_entropy[n] entropy[n]:
+ *   dlogits[n, i] = c ( [i = target] grad_logprob - p_i (grad_logprob + grad_entropy (logp_i + entropy)) )
+ *   target        as above; NULL if grad_logprob is NULL.  target < 0: no gradient from the log probability; >= vocab: a row of NaN
+ *   grad_logprob  device, const float [rows] or NULL (zeros)
+ *   grad_entropy  device, const float [rows] or NULL (zeros); one of the two has to be there
+ *   stats         device, const float [rows, 4], as qsl_token_logprobs left them; NULL: formed here.  With stats = NULL a training step whose
+ *                 weights are known beforehand needs this call alone: it can also hand out
+ *   logprob, entropy  device, float [rows] or NULL, only with stats = NULL; logprob needs target
+ *   dlogits       device, [rows] rows of vocab values of the logits' type, row n at element n * dstride; every value is written.  May be
+ *                 the logits themselves (same pointer and stride); may not overlap them otherwise */
+qsl_status qsl_token_logprobs_backward(const qsl_logits *z, const int64_t *target, const float *grad_logprob,
+                                       const float *grad_entropy, const float *stats, float *logprob, float *entropy,
+                                       void *dlogits, uint64_t dstride, void *workspace, size_t workspace_bytes,
+                                       void *hip_stream);
+
+/* A teacher's top logits (as qsl_token_logprobs hands them out: top_index, top_logprob with scale 1). */
+typedef struct {
+  const int32_t *index;      /* device, [rows, top]: classes; < 0: no entry; >= vocab: the row's results are NaN; a class that stands in a row
+                                more than once counts where it stands first                              */
+  const float *value;        /* device, [rows, top]: the teacher's logits (or log probabilities) there   */
+  const float *lse;          /* device, [rows]: ln of the sum of exp(scale * logit) over all the teacher's classes, or NULL */
+  uint32_t top;              /* entries per row, 1 .. QSL_TEACHER_MAX                                    */
+  float scale;               /* the factor of `value`, in the range of qsl_logits' scale                 */
+} qsl_teacher;
+
+/* The Kullback-Leibler divergence of the student's rows from a teacher's.
+ *   lse == NULL:  q_k = exp(scale value_k) / sum_j exp(scale value_j),        loss = sum_k q_k (ln q_k - logp_{index_k})
+ *   lse != NULL:  q_k = exp(scale value_k - lse); what the entries leave over, q_r = max(0, 1 - sum_k q_k), is one more class, which the
+ *                 student gives p_r = 1 - sum_k p_{index_k}:                     loss as above + q_r (ln q_r - ln p_r)
+ *                 (without that term where no class is left outside the entries, or all of them have logit -inf)
+ * Terms with q = 0 are 0; a class with q > 0 and logit -inf makes the loss +inf.  A row without entries has loss 0 and gradient 0.
+ *   loss   device, float [rows] or NULL
+ *   stats  device, float [rows, 8] or NULL: for qsl_distill_backward on the same arguments; one of the two has to be there */
+qsl_status qsl_distill(const qsl_logits *z, const qsl_teacher *teacher, float *loss, float *stats, void *workspace,
+                       size_t workspace_bytes, void *hip_stream);
+
+/* The gradient in the logits of  sum_n grad_loss[n] loss[n]:
+ *   dlogits[n, i] = c grad_loss (p_i - q_i) for the entries' classes; for the others c grad_loss p_i (lse == NULL), or
+ *                   c grad_loss p_i (1 - q_r / p_r)
+ *   grad_loss  device, const float [rows] or NULL (ones)
+ *   stats      device, const float [rows, 8], as qsl_distill left them; NULL: formed here, and then
+ *   loss       device, float [rows] or NULL, receives the loss (only with stats = NULL)
+ *   dlogits, dstride   as for qsl_token_logprobs_backward */
+qsl_status qsl_distill_backward(const qsl_logits *z, const qsl_teacher *teacher, const float *grad_loss, const float *stats,
+                                float *loss, void *dlogits, uint64_t dstride, void *workspace, size_t workspace_bytes,
+                                void *hip_stream);
+
 const char *qsl_status_string(qsl_status st);
 
 #ifdef __cplusplus

@@ -22,6 +22,10 @@ FLAG_OWN_V = 4
 FLAG_NO_WARM_START = 8
 FLAG_DENSE_FORMAT = 16
 
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # QSL_F32, QSL_BF16, QSL_F16
+TOP_MAX = 128
+TEACHER_MAX = 256
+
 OK, ERR_INVALID_ARG, ERR_BUFFER_TOO_SMALL, ERR_NONFINITE_INPUT, ERR_DEVICE, ERR_UNSUPPORTED = range(6)
 
 
@@ -35,6 +39,15 @@ class _Config(C.Structure):
     _fields_ = [("d", C.c_uint64), ("num_segments", C.c_uint32), ("seg_offset", C.POINTER(C.c_uint64)),
                 ("seg_k", C.POINTER(C.c_uint32)), ("s", C.c_uint32), ("sparsifier", C.c_uint32),
                 ("quantizer", C.c_uint32), ("seed", C.c_uint64), ("max_workers", C.c_uint32), ("flags", C.c_uint32)]
+
+
+class _Logits(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_uint64), ("rows", C.c_uint32), ("vocab", C.c_uint32), ("dtype", C.c_uint32),
+                ("scale", C.c_float)]
+
+
+class _Teacher(C.Structure):
+    _fields_ = [("index", C.c_void_p), ("value", C.c_void_p), ("lse", C.c_void_p), ("top", C.c_uint32), ("scale", C.c_float)]
 
 
 def _load():
@@ -61,6 +74,13 @@ def _load():
     lib.qsl_timing_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(u32)]; lib.qsl_timing_read.restype = C.c_int
     lib.qsl_bits_index_free.argtypes = [C.POINTER(_Config), C.POINTER(u64)]; lib.qsl_bits_index_free.restype = C.c_int
     lib.qsl_plan_paths.argtypes = [C.POINTER(_Config), C.POINTER(u32)]; lib.qsl_plan_paths.restype = C.c_int
+    zp, tp, sz = C.POINTER(_Logits), C.POINTER(_Teacher), C.c_size_t
+    lib.qsl_logits_workspace_bytes.argtypes = [zp, u32]; lib.qsl_logits_workspace_bytes.restype = sz
+    lib.qsl_token_logprobs.argtypes = [zp, vp, u32, vp, vp, vp, vp, vp, vp, vp, sz, vp]; lib.qsl_token_logprobs.restype = C.c_int
+    lib.qsl_token_logprobs_backward.argtypes = [zp, vp, vp, vp, vp, vp, vp, vp, u64, vp, sz, vp]
+    lib.qsl_token_logprobs_backward.restype = C.c_int
+    lib.qsl_distill.argtypes = [zp, tp, vp, vp, vp, sz, vp]; lib.qsl_distill.restype = C.c_int
+    lib.qsl_distill_backward.argtypes = [zp, tp, vp, vp, vp, vp, u64, vp, sz, vp]; lib.qsl_distill_backward.restype = C.c_int
     return lib
 
 
@@ -69,7 +89,8 @@ _lib = _load()
 EXPORTED = ["qsl_create", "qsl_destroy", "qsl_set_stream", "qsl_msg_capacity_bytes", "qsl_compress",
             "qsl_compress_diff", "qsl_error_update", "qsl_aggregate", "qsl_aggregate_static", "qsl_bits_sent", "qsl_bits_index_free", "qsl_plan_paths",
             "qsl_device_status", "qsl_debug_units",
-            "qsl_timing_enable", "qsl_timing_read", "qsl_status_string"]
+            "qsl_timing_enable", "qsl_timing_read", "qsl_status_string", "qsl_logits_workspace_bytes", "qsl_token_logprobs",
+            "qsl_token_logprobs_backward", "qsl_distill", "qsl_distill_backward"]
 
 
 def _check(status, where):
@@ -125,6 +146,121 @@ def aggregate_static(d, k, s, sparsifier, quantizer, msg, out, scale, worker_lis
     stream = C.c_void_p(torch.cuda.current_stream(msg.device).cuda_stream)
     _check(_lib.qsl_aggregate_static(C.byref(cfg), stream, _ptr(msg, torch.uint8), lst, R, float(scale),
                                      int(bool(accumulate)), _ptr(out, torch.float32)), "qsl_aggregate_static")
+
+
+def _rows_of(t, what):
+    """Address and row stride of a [rows, vocab] tensor whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in DTYPES or (t.shape[1] != 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected a device tensor [rows, vocab] of float32, bfloat16 or float16 with contiguous rows")
+    rows, vocab = t.shape
+    stride = t.stride(0) if rows > 1 else vocab
+    if stride < vocab:
+        raise ValueError(f"{what}: rows overlap (stride {stride}, {vocab} classes)")
+    return t.data_ptr(), stride
+
+
+def _beside(t, what, z, dtype, *shape):
+    """Address of an argument that goes with the logits `z`: on their device, contiguous, of that type and shape; 0 for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != z.device:
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor {list(shape)} on {z.device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+class _LogitsCall:
+    """The arguments that all calls on logits share: the rows, the workspace, the stream; and the device they run on."""
+
+    def __init__(self, logits, scale, top=0, workspace=None):
+        data, stride = _rows_of(logits, "logits")
+        rows, vocab = logits.shape
+        self.z = _Logits(data, stride, rows, vocab, DTYPES[logits.dtype], scale)
+        self.ref = C.byref(self.z)
+        need = _lib.qsl_logits_workspace_bytes(self.ref, top)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+        elif workspace is not None:
+            _beside(workspace, "workspace", logits, torch.uint8, workspace.numel())
+        self.workspace, self.bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        self._keep = workspace
+        self.index = logits.device.index
+        self.stream = torch.cuda.current_stream(logits.device).cuda_stream
+
+    def run(self, where, fn, *args):
+        if self.index == torch.cuda.current_device():
+            st = fn(self.ref, *args, self.workspace, self.bytes, self.stream)
+        else:
+            with torch.cuda.device(self.index):
+                st = fn(self.ref, *args, self.workspace, self.bytes, self.stream)
+        if st != OK:
+            raise QslError(st, where)
+
+
+def logits_workspace_bytes(logits, top=0):
+    """`qsl_logits_workspace_bytes` of these rows: what `workspace=` of the calls below has to hold (they allocate it if it is not given)."""
+    data, stride = _rows_of(logits, "logits")
+    return int(_lib.qsl_logits_workspace_bytes(C.byref(_Logits(data, stride, logits.shape[0], logits.shape[1], DTYPES[logits.dtype], 1.0)), top))
+
+
+def token_logprobs(logits, target=None, scale=1.0, logprob=None, entropy=None, lse=None, top_index=None, top_logprob=None,
+                   stats=None, workspace=None):
+    """`qsl_token_logprobs`: log probabilities of the given classes, entropy and best alternatives of every row of
+    logits [rows, vocab], into those of the output tensors that are given."""
+    N = logits.shape[0]
+    some = top_index if top_index is not None else top_logprob
+    top = 0 if some is None else some.shape[-1]
+    c = _LogitsCall(logits, scale, top, workspace)
+    f32 = torch.float32
+    c.run("qsl_token_logprobs", _lib.qsl_token_logprobs, _beside(target, "target", logits, torch.int64, N), top,
+          _beside(logprob, "logprob", logits, f32, N), _beside(entropy, "entropy", logits, f32, N), _beside(lse, "lse", logits, f32, N),
+          _beside(top_index, "top_index", logits, torch.int32, N, top), _beside(top_logprob, "top_logprob", logits, f32, N, top),
+          _beside(stats, "stats", logits, f32, N, 4))
+
+
+def _gradient_rows(dlogits, logits):
+    if dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.device != logits.device:
+        raise ValueError("dlogits: expected the logits' type, shape and device")
+    return _rows_of(dlogits, "dlogits")
+
+
+def token_logprobs_backward(logits, target, dlogits, scale=1.0, grad_logprob=None, grad_entropy=None, stats=None, logprob=None,
+                            entropy=None, workspace=None):
+    """`qsl_token_logprobs_backward`: the gradient of sum(grad_logprob * logprob) + sum(grad_entropy * entropy) in the logits."""
+    N = logits.shape[0]
+    c = _LogitsCall(logits, scale, 0, workspace)
+    f32 = torch.float32
+    out, dstride = _gradient_rows(dlogits, logits)
+    c.run("qsl_token_logprobs_backward", _lib.qsl_token_logprobs_backward, _beside(target, "target", logits, torch.int64, N),
+          _beside(grad_logprob, "grad_logprob", logits, f32, N), _beside(grad_entropy, "grad_entropy", logits, f32, N),
+          _beside(stats, "stats", logits, f32, N, 4), _beside(logprob, "logprob", logits, f32, N),
+          _beside(entropy, "entropy", logits, f32, N), out, dstride)
+
+
+def _teacher(logits, index, value, lse, scale):
+    N, top = logits.shape[0], index.shape[-1]
+    return _Teacher(_beside(index, "teacher_index", logits, torch.int32, N, top), _beside(value, "teacher_value", logits, torch.float32, N, top),
+                    _beside(lse, "teacher_lse", logits, torch.float32, N), top, scale)
+
+
+def distill(logits, teacher_index, teacher_value, scale=1.0, teacher_scale=1.0, teacher_lse=None, loss=None, stats=None, workspace=None):
+    """`qsl_distill`: the Kullback-Leibler divergence of every row from a teacher's top logits [rows, top]."""
+    N = logits.shape[0]
+    c = _LogitsCall(logits, scale, 0, workspace)
+    t = _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale)
+    c.run("qsl_distill", _lib.qsl_distill, C.byref(t), _beside(loss, "loss", logits, torch.float32, N),
+          _beside(stats, "stats", logits, torch.float32, N, 8))
+
+
+def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, teacher_scale=1.0, teacher_lse=None, grad_loss=None,
+                     stats=None, loss=None, workspace=None):
+    """`qsl_distill_backward`: the gradient of sum(grad_loss * loss) in the logits."""
+    N = logits.shape[0]
+    c = _LogitsCall(logits, scale, 0, workspace)
+    t = _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale)
+    f32 = torch.float32
+    out, dstride = _gradient_rows(dlogits, logits)
+    c.run("qsl_distill_backward", _lib.qsl_distill_backward, C.byref(t), _beside(grad_loss, "grad_loss", logits, f32, N),
+          _beside(stats, "stats", logits, f32, N, 8), _beside(loss, "loss", logits, f32, N), out, dstride)
 
 
 class Qsl:

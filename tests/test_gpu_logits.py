@@ -1,0 +1,432 @@
+"""The operators on logits on the GPU against their definitions in 64 bits (logits_util), at the sizes, masks, layouts and
+calls where they can go wrong."""
+import pytest
+import torch
+
+import logits_util as X
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+SIZES = [(3, 1), (5, 2), (17, 10), (4, 63), (3, 64), (6, 65), (2, 255), (5, 1000), (3, 2047), (2, 2049), (3, 4100), (2, 8191), (1, 16385),
+         (2, 20000), (3, 32768), (1, 65537), (2, 131075), (1, 300007)]
+dev = torch.device("cuda")
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1906_02367_amd import binding
+    return binding
+
+
+def logits_of(N, V, dtype, seed=0, pad=0, masked=False, spread=2.0):
+    g = torch.Generator().manual_seed(seed * 1009 + V)
+    z = spread * torch.randn(N, V, generator=g)
+    if masked:
+        z[:, torch.rand(V, generator=g) < 0.3] = -INF
+        if V > 1:
+            z[:, V // 2] = 0.5
+    held = torch.full((N, V + pad), float("nan"), dtype=dtype)
+    held[:, :V] = z.to(dtype)
+    return held.to(dev)[:, :V]
+
+
+def targets_of(N, V, seed=0):
+    g = torch.Generator().manual_seed(seed + 77)
+    t = torch.randint(0, V, (N,), generator=g)
+    if N > 2:
+        t[1] = -100
+    return t.to(dev)
+
+
+def new(*shape, dtype=torch.float32):
+    return torch.full(shape, 77, dtype=dtype, device=dev)
+
+
+def run_score(B, z, t, K, c, **kw):
+    N = z.shape[0]
+    o = dict(logprob=new(N), entropy=new(N), lse=new(N), stats=new(N, 4))
+    if K:
+        o.update(top_index=new(N, K, dtype=torch.int32), top_logprob=new(N, K))
+    B.token_logprobs(z, t, scale=c, **o, **kw)
+    return o
+
+
+def check_score(z, t, K, c, o, what):
+    r = X.rows_of(z, c)
+    X.check(o["logprob"], *X.target_logprob(r, t), f"{what}: logprob")
+    X.check(o["lse"], *X.lse(r), f"{what}: lse")
+    H, tol = X.entropy(r)
+    X.check(o["entropy"], H.squeeze(1), tol.squeeze(1), f"{what}: entropy")
+    if K:
+        index, lp, tol = X.top(r, K)
+        assert torch.equal(o["top_index"].cpu().long(), index), f"{what}: alternatives"
+        X.check(o["top_logprob"], lp, tol, f"{what}: top_logprob")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N,V", SIZES)
+def test_log_probabilities(B, N, V, dtype):
+    for K, c, pad, masked in ((0, 1.0, 0, False), (min(V, 5), 1.25, 1, True), (min(V, 128), 0.5, 3, False)):
+        z, t = logits_of(N, V, TYPES[dtype], seed=K, pad=pad, masked=masked), targets_of(N, V)
+        check_score(z, t, K, c, run_score(B, z, t, K, c), f"{dtype} {N} x {V}, K = {K}")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N,V", SIZES)
+def test_gradient_of_log_probabilities(B, N, V, dtype):
+    dt = TYPES[dtype]
+    for c, pad, masked, with_g, with_h in ((1.0, 0, False, True, False), (0.5, 1, True, True, True), (1.25, 3, False, False, True)):
+        z, t = logits_of(N, V, dt, seed=3, pad=pad, masked=masked), targets_of(N, V)
+        gen = torch.Generator().manual_seed(5)
+        g = torch.randn(N, generator=gen).to(dev) if with_g else None
+        h = torch.randn(N, generator=gen).to(dev) if with_h else None
+        r = X.rows_of(z, c)
+        want, tol = X.logprob_gradient(r, t, g, h, dt)
+        held = new(N, V + 5, dtype=dt)
+        lp, H = new(N), new(N)
+        B.token_logprobs_backward(z, t, held[:, :V], scale=c, grad_logprob=g, grad_entropy=h, logprob=lp, entropy=H)
+        what = f"{dtype} {N} x {V}, c = {c}"
+        X.check(held[:, :V], want, tol, what)
+        assert (held[:, V:] == 77).all(), "written behind a row"
+        X.check(lp, *X.target_logprob(r, t), f"{what}: logprob")
+        X.check(H, *(x.squeeze(1) for x in X.entropy(r)), f"{what}: entropy")
+        # from the statistics of the forward call, in place
+        o = run_score(B, z, t, 0, c)
+        z2 = z.clone()
+        B.token_logprobs_backward(z2, t, z2, scale=c, grad_logprob=g, grad_entropy=h, stats=o["stats"])
+        X.check(z2, want, tol, f"{what}: from statistics, in place")
+        z3 = z.clone()
+        B.token_logprobs_backward(z3, t, z3, scale=c, grad_logprob=g, grad_entropy=h)
+        assert torch.equal(z3, held[:, :V]), "in place differs"
+
+
+def teacher_of(N, V, K, seed=0, ragged=False):
+    g = torch.Generator().manual_seed(seed * 31 + K)
+    t = 2.0 * torch.randn(N, V, generator=g)
+    value, index = torch.topk(t, K, dim=1)
+    index = index.to(torch.int32)
+    if ragged and N > 1:
+        for n in range(N):
+            keep = int(torch.randint(0, K + 1, (1,), generator=g))
+            index[n, keep:] = -1
+        index[0] = -1                                                  # a row without entries
+        value[index < 0] = float("nan")                               # what stands there is not looked at
+    return index.to(dev), value.to(dev), torch.logsumexp(t.double(), 1).float().to(dev)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N,V", SIZES)
+def test_distillation(B, N, V, dtype, rest):
+    dt = TYPES[dtype]
+    for K, c, c_t, pad, masked, ragged in ((1, 1.0, 1.0, 0, False, False), (min(V, 7), 0.5, 0.5, 1, False, True), (min(V, 64), 1.25, 1.0, 3, True, True),
+                                           (min(V, 256), 1.0, 1.0, 0, False, False)):
+        z = logits_of(N, V, dt, seed=K, pad=pad, masked=masked)
+        index, value, t_lse = teacher_of(N, V, K, seed=1, ragged=ragged)
+        if c_t != 1.0:
+            t_lse = t_lse * 0 + 3.0                                    # any normaliser that leaves something over
+        if not rest:
+            t_lse = None
+        g = torch.randn(N, generator=torch.Generator().manual_seed(5)).to(dev)
+        r = X.rows_of(z, c)
+        loss, tol_loss, dz, tol = X.distill(r, index.cpu(), value.cpu(), c_t, None if t_lse is None else t_lse.cpu(), g.cpu(), dt)
+        what = f"{dtype} {N} x {V}, K = {K}"
+        kw = dict(scale=c, teacher_scale=c_t, teacher_lse=t_lse)
+        got, stats = new(N), new(N, 8)
+        B.distill(z, index, value, loss=got, stats=stats, **kw)
+        X.check(got, loss, tol_loss, f"{what}: loss")
+        held, got2 = new(N, V + 5, dtype=dt), new(N)
+        B.distill_backward(z, index, value, held[:, :V], grad_loss=g, loss=got2, **kw)
+        X.check(got2, loss, tol_loss, f"{what}: loss with the gradient")
+        X.check(held[:, :V], dz, tol, f"{what}: gradient")
+        assert (held[:, V:] == 77).all(), "written behind a row"
+        z2 = z.clone()
+        B.distill_backward(z2, index, value, z2, grad_loss=g, stats=stats, **kw)
+        X.check(z2, dz, tol, f"{what}: gradient from statistics, in place")
+        z3 = z.clone()
+        B.distill_backward(z3, index, value, z3, grad_loss=g, **kw)
+        assert torch.equal(z3, held[:, :V]), "in place differs"
+
+
+def special_rows(V, dtype):
+    """Rows whose mask leaves nothing or one class, the type's extremes, ties, orders."""
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    rows = [torch.full((V,), -INF), torch.full((V,), low), torch.full((V,), high), torch.zeros(V), torch.full((V,), -INF), torch.full((V,), low),
+            torch.arange(V).float() / V * 8, -torch.arange(V).float() / V * 8, torch.randint(0, 3, (V,)).float(), torch.full((V,), -INF), torch.zeros(V)]
+    rows[4][V - 1] = 1.5                                               # one class left
+    rows[5][V // 3] = 2.0                                              # all others at the type's lowest value
+    rows[9][V // 2] = low                                              # the only class is at the lowest value
+    rows[10][::2] = -0.0                                               # both zeros are equal
+    return torch.stack(rows).to(dtype).to(dev)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("V", [2, 40, 700, 5000, 40000, 140000])
+def test_special_rows(B, V, dtype):
+    torch.manual_seed(1)
+    dt = TYPES[dtype]
+    z = special_rows(V, dt)
+    N = z.shape[0]
+    t = torch.full((N,), V // 2, device=dev)
+    for K in (0, min(V, 20), min(V, 128)):
+        check_score(z, t, K, 1.0, run_score(B, z, t, K, 1.0), f"{dtype} V = {V}, K = {K}")
+    g, h = torch.linspace(-1, 1, N, device=dev), torch.full((N,), 0.25, device=dev)
+    r = X.rows_of(z, 1.0)
+    want, tol = X.logprob_gradient(r, t, g, h, dt)
+    dz = torch.empty_like(z)
+    B.token_logprobs_backward(z, t, dz, grad_logprob=g, grad_entropy=h)
+    X.check(dz, want, tol, f"{dtype} V = {V}: gradient")
+    K = min(V, 30)
+    index, value, t_lse = teacher_of(N, V, K)
+    for lse in (None, t_lse):
+        loss, tol_loss, want, tol = X.distill(r, index.cpu(), value.cpu(), 1.0, None if lse is None else lse.cpu(), g.cpu(), dt)
+        got = new(N)
+        B.distill_backward(z, index, value, dz, teacher_lse=lse, grad_loss=g, loss=got)
+        X.check(got, loss, tol_loss, f"{dtype} V = {V}, rest {lse is not None}: loss")
+        X.check(dz, want, tol, f"{dtype} V = {V}, rest {lse is not None}: gradient")
+
+
+@pytest.mark.parametrize("V", [9, 300, 30000, 200000])
+def test_nan_and_infinity(B, V):
+    z = logits_of(4, V, torch.float32)
+    z[0, V // 2], z[1, V - 1], z[2, 0] = float("nan"), INF, -INF
+    t = torch.tensor([0, 1, 0, V - 1], device=dev)
+    o = run_score(B, z, t, 5, 1.0)
+    for k in ("logprob", "entropy", "lse", "top_logprob"):
+        assert torch.isnan(o[k][:2]).all() and not torch.isnan(o[k][2:]).any(), k
+    assert (o["top_index"][:2] == -1).all() and float(o["logprob"][2]) == -INF
+    dz = torch.empty_like(z)
+    B.token_logprobs_backward(z, t, dz, grad_logprob=torch.ones(4, device=dev))
+    assert torch.isnan(dz[:2]).all() and torch.isfinite(dz[2:]).all()
+    index, value, lse = teacher_of(4, V, 5)
+    for l in (None, lse):
+        loss = new(4)
+        B.distill_backward(z, index, value, dz, loss=loss, teacher_lse=l)
+        assert torch.isnan(loss[:2]).all() and torch.isnan(dz[:2]).all() and not torch.isnan(loss[2:]).any() and torch.isfinite(dz[2:]).all()
+    value[3, 2] = float("nan")
+    B.distill(z, index, value, loss=loss)
+    assert torch.isnan(loss[3]) and not torch.isnan(loss[2])
+
+
+@pytest.mark.parametrize("V", [12, 1000, 50000])
+def test_indices_outside_and_twice(B, V):
+    z = logits_of(5, V, torch.float32)
+    t = torch.tensor([V, -1, 2 ** 40, -2 ** 40, V - 1], device=dev)
+    lp, dz = new(5), torch.empty_like(z)
+    B.token_logprobs(z, t, logprob=lp)
+    assert torch.isnan(lp[[0, 2]]).all() and (lp[[1, 3]] == 0).all() and torch.isfinite(lp[4])
+    g = torch.ones(5, device=dev)
+    B.token_logprobs_backward(z, t, dz, grad_logprob=g)
+    assert torch.isnan(dz[[0, 2]]).all() and (dz[[1, 3]] == 0).all() and torch.isfinite(dz[4]).all()
+    index, value, lse = teacher_of(5, V, 8)
+    index[0, 3] = V                                                    # outside: the row is NaN
+    index[1, 5] = index[1, 2]                                          # twice: counts where it stands first
+    index[2, :] = index[2, 0]
+    index[3, 6] = -2 ** 31
+    for l in (None, lse):
+        loss, tol_loss, want, tol = X.distill(X.rows_of(z, 1.0), index.cpu(), value.cpu(), 1.0, None if l is None else l.cpu(), None, torch.float32)
+        got = new(5)
+        B.distill_backward(z, index, value, dz, loss=got, teacher_lse=l)
+        X.check(got, loss, tol_loss, f"loss, rest {l is not None}")
+        X.check(dz, want, tol, f"gradient, rest {l is not None}")
+
+
+def test_a_teacher_that_puts_no_mass_on_its_entries(B):
+    z = logits_of(3, 500, torch.float32)
+    index, value, lse = teacher_of(3, 500, 6)
+    value[0] = -INF                                                    # nothing to learn from
+    value[1, 2:] = -INF                                                # entries without mass among others
+    for l in (None, lse):
+        loss, tol_loss, want, tol = X.distill(X.rows_of(z, 1.0), index.cpu(), value.cpu(), 1.0, None if l is None else l.cpu(), None, torch.float32)
+        got, dz = new(3), torch.empty_like(z)
+        B.distill_backward(z, index, value, dz, loss=got, teacher_lse=l)
+        X.check(got, loss, tol_loss, f"loss, rest {l is not None}")
+        X.check(dz, want, tol, f"gradient, rest {l is not None}")
+
+
+def test_offsets_beyond_32_bits(B):
+    N, V, stride = 3, 1000, 2 ** 31 + 24
+    held = torch.empty(2 * stride + V, dtype=torch.bfloat16, device=dev)
+    z = held.as_strided((N, V), (stride, 1))
+    z.copy_(logits_of(N, V, torch.bfloat16))
+    t = targets_of(N, V)
+    check_score(z, t, 5, 1.0, run_score(B, z, t, 5, 1.0), "long strides")
+    g = torch.ones(N, device=dev)
+    want, tol = X.logprob_gradient(X.rows_of(z, 1.0), t, g, None, torch.bfloat16)
+    B.token_logprobs_backward(z, t, z, grad_logprob=g)
+    X.check(z, want, tol, "long strides: gradient in place")
+    del held, z
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("N,V", [(70000, 3), (3000, 257), (1500, 4096)])
+def test_many_rows(B, N, V):
+    z, t = logits_of(N, V, torch.bfloat16), targets_of(N, V)
+    check_score(z, t, min(V, 4), 1.0, run_score(B, z, t, min(V, 4), 1.0), f"{N} x {V}")
+    g = torch.randn(N, device=dev)
+    dz = torch.empty_like(z)
+    B.token_logprobs_backward(z, t, dz, grad_logprob=g)
+    X.check(dz, *X.logprob_gradient(X.rows_of(z, 1.0), t, g, None, torch.bfloat16), f"{N} x {V}: gradient")
+
+
+@pytest.mark.parametrize("N,V", [(1, 5), (9, 700), (1, 130000), (40, 33000)])
+def test_gradients_against_differences(B, N, V):
+    """(f(z + e) - f(z - e)) / 2e along a direction d: off by e^2 / 6 times the third derivative (for |d_i| <= 1 at most 8 for logprob and loss, 32
+    for the entropy term weighed with 1/4: 16 in all) and by the values' own error over e."""
+    gen = torch.Generator().manual_seed(V)
+    d = (torch.rand(N, V, generator=gen) * 2 - 1).to(dev)
+    z, t = logits_of(N, V, torch.float32), torch.randint(0, V, (N,), generator=gen).to(dev)
+    index, value, lse = teacher_of(N, V, min(V, 20))
+    e = 2.0 ** -6
+
+    def nll(x):
+        lp, H = new(N), new(N)
+        B.token_logprobs(x, t, logprob=lp, entropy=H)
+        return lp.double() + 0.25 * H.double()
+
+    def kl(l):
+        def f(x):
+            loss = new(N)
+            B.distill(x, index, value, loss=loss, teacher_lse=l)
+            return loss.double()
+        return f
+
+    r = X.rows_of(z, 1.0)
+    H, tol_H = X.entropy(r)
+    values = float(tol_H.max()) + float(r["tol_L"].max()) + X.U * 8 * 40
+    tol = e * e / 6 * 16 + 2 * values / e + 2.0 ** -20
+    dz = torch.empty_like(z)
+    ones = torch.ones(N, device=dev)
+    for f, grad in ((nll, lambda: B.token_logprobs_backward(z, t, dz, grad_logprob=ones, grad_entropy=0.25 * ones)),
+                    (kl(None), lambda: B.distill_backward(z, index, value, dz)),
+                    (kl(lse), lambda: B.distill_backward(z, index, value, dz, teacher_lse=lse))):
+        grad()
+        along = (dz.double() * d.double()).sum(1)
+        diff = (f(z + e * d) - f(z - e * d)) / (2 * e)
+        assert float((along - diff).abs().max()) <= tol, (float((along - diff).abs().max()), tol)
+
+
+@pytest.mark.parametrize("N,V", [(2, 100000), (37, 2000), (600, 9000)])
+def test_captured_and_replayed(B, N, V):
+    """One graph of the forward and the backward calls, replayed on changed inputs, with eager calls in between."""
+    K = 10
+    z, t = logits_of(N, V, torch.bfloat16), targets_of(N, V)
+    index, value, lse = teacher_of(N, V, K)
+    g = torch.randn(N, generator=torch.Generator().manual_seed(5)).to(dev)
+
+    def outputs():
+        o = dict(logprob=new(N), entropy=new(N), stats=new(N, 4), top_index=new(N, K, dtype=torch.int32), top_logprob=new(N, K))
+        return o, torch.zeros_like(z), torch.zeros_like(z), new(N)
+
+    def calls(o, dz, dz2, loss):
+        B.token_logprobs(z, t, **o)
+        B.token_logprobs_backward(z, t, dz, grad_logprob=g, grad_entropy=g, stats=o["stats"])
+        B.distill_backward(z, index, value, dz2, grad_loss=g, teacher_lse=lse, loss=loss)
+
+    a, b = outputs(), outputs()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls(*a)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(*a)
+    for k in range(4):
+        z.copy_(logits_of(N, V, torch.bfloat16, seed=10 + k))
+        graph.replay()
+        calls(*b)
+        torch.cuda.synchronize()
+        for n in a[0]:
+            assert torch.equal(a[0][n], b[0][n]), (k, n)
+        assert all(torch.equal(x, y) for x, y in zip(a[1:], b[1:])), k
+
+
+def test_two_graphs_and_two_streams_at_once(B):
+    """Calls on two streams, and two graphs replayed side by side: no call knows of the other."""
+    N, V, K = 3, 120000, 12
+    zs = [logits_of(N, V, torch.bfloat16, seed=s) for s in (1, 2)]
+    t = targets_of(N, V)
+    want = [run_score(B, z, t, K, 1.0) for z in zs]
+    streams = [torch.cuda.Stream() for _ in zs]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for z, s in zip(zs, streams):
+        o = dict(logprob=new(N), entropy=new(N), lse=new(N), stats=new(N, 4), top_index=new(N, K, dtype=torch.int32), top_logprob=new(N, K))
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr, stream=s):
+            B.token_logprobs(z, t, **o)
+        graphs.append(gr); outs.append(o)
+    for k in range(5):
+        for o in outs:
+            for x in o.values():
+                x.zero_()
+        torch.cuda.synchronize()
+        for gr, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                gr.replay()
+        direct = []
+        for z, s in zip(zs, reversed(streams)):
+            with torch.cuda.stream(s):
+                direct.append(run_score(B, z, t, K, 1.0))
+        torch.cuda.synchronize()
+        for o, d, w in zip(outs, direct, want):
+            for n in w:
+                assert torch.equal(o[n], w[n]) and torch.equal(d[n], w[n]), (k, n)
+
+
+def test_the_same_call_gives_the_same_bits(B):
+    N, V, K = 5, 70001, 40
+    z, t = logits_of(N, V, torch.float16), targets_of(N, V)
+    index, value, lse = teacher_of(N, V, K)
+    first = None
+    for _ in range(4):
+        o = run_score(B, z, t, K, 0.5)
+        dz, loss = torch.empty_like(z), new(N)
+        B.distill_backward(z, index, value, dz, loss=loss, teacher_lse=lse)
+        now = [x.clone() for x in o.values()] + [dz, loss]
+        if first is None:
+            first = now
+        assert all(torch.equal(x, y) for x, y in zip(first, now))
+
+
+def test_no_rows(B):
+    z = torch.empty(0, 50, device=dev)
+    B.token_logprobs(z, torch.empty(0, dtype=torch.int64, device=dev), logprob=new(0), top_index=new(0, 3, dtype=torch.int32))
+    B.token_logprobs_backward(z, torch.empty(0, dtype=torch.int64, device=dev), torch.empty_like(z), grad_logprob=new(0))
+    B.distill_backward(z, new(0, 3, dtype=torch.int32), new(0, 3), torch.empty_like(z), loss=new(0))
+    torch.cuda.synchronize()
+
+
+def test_wrong_tensors_are_refused(B):
+    z, t = logits_of(4, 30, torch.float32), targets_of(4, 30)
+    dz = torch.empty_like(z)
+    one = torch.ones(4, device=dev)
+    index, value, lse = teacher_of(4, 30, 3)
+    bad = [lambda: B.token_logprobs(z.double(), t, logprob=new(4)), lambda: B.token_logprobs(z.cpu(), t, logprob=new(4)),
+           lambda: B.token_logprobs(z.t(), t, logprob=new(4)), lambda: B.token_logprobs(z[0], t, logprob=new(4)),
+           lambda: B.token_logprobs(z[:1].expand(4, 30), t, logprob=new(4)),
+           lambda: B.token_logprobs(z, t.int(), logprob=new(4)), lambda: B.token_logprobs(z, t[:3], logprob=new(4)),
+           lambda: B.token_logprobs(z, t, logprob=new(3)), lambda: B.token_logprobs(z, t, logprob=new(4).bfloat16()),
+           lambda: B.token_logprobs(z, t, logprob=new(8)[::2]), lambda: B.token_logprobs(z, t, top_index=new(4, 3, dtype=torch.int32), top_logprob=new(4, 2)),
+           lambda: B.token_logprobs_backward(z, t, dz.bfloat16(), grad_logprob=one), lambda: B.token_logprobs_backward(z, t, dz[:, :29], grad_logprob=one),
+           lambda: B.distill(z, index.long(), value, loss=new(4)), lambda: B.distill(z, index, value[:, :2], loss=new(4))]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    refused = [lambda: B.token_logprobs(z, t), lambda: B.token_logprobs(z, None, logprob=new(4)), lambda: B.token_logprobs(z, t, scale=0.0, logprob=new(4)),
+               lambda: B.token_logprobs(z, t, scale=float("nan"), logprob=new(4)), lambda: B.token_logprobs(z, t, top_index=new(4, 31, dtype=torch.int32)),
+               lambda: B.token_logprobs_backward(z, t, dz), lambda: B.token_logprobs_backward(z, None, dz, grad_logprob=one),
+               lambda: B.token_logprobs_backward(z, t, dz, grad_logprob=one, stats=new(4, 4), logprob=new(4)),
+               lambda: B.distill(z, index, value),
+               lambda: B.distill_backward(z, index, value, dz, stats=new(4, 8), loss=new(4)), lambda: B.distill(z, index, value, teacher_scale=-1.0, loss=new(4))]
+    for f in refused:
+        with pytest.raises(B.QslError):
+            f()
+    wide = torch.zeros(4, 60, device=dev)                                # dlogits that overlap the logits without being them
+    with pytest.raises(B.QslError):
+        B.token_logprobs_backward(wide[:, :30], t, wide[:, 10:40], grad_logprob=one)
+    torch.cuda.synchronize()
