@@ -150,50 +150,45 @@ def aggregate_static(d, k, s, sparsifier, quantizer, msg, out, scale, worker_lis
 
 def _rows_of(t, what):
     """Address and row stride of a [rows, vocab] tensor whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda or t.dtype not in DTYPES or (t.shape[1] != 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: expected a device tensor [rows, vocab] of float32, bfloat16 or float16 with contiguous rows")
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in DTYPES:
+        raise ValueError(f"{what}: expected a device tensor [rows, vocab] of float32, bfloat16 or float16")
     rows, vocab = t.shape
-    stride = t.stride(0) if rows > 1 else vocab
-    if stride < vocab:
-        raise ValueError(f"{what}: rows overlap (stride {stride}, {vocab} classes)")
-    return t.data_ptr(), stride
+    stride, step = t.stride()
+    if (step != 1 and vocab != 1) or (rows > 1 and stride < vocab):
+        raise ValueError(f"{what}: expected contiguous rows that do not overlap, got strides {t.stride()}")
+    return t.data_ptr(), stride if rows > 1 else vocab
 
 
-def _beside(t, what, z, dtype, *shape):
-    """Address of an argument that goes with the logits `z`: on their device, contiguous, of that type and shape; 0 for None."""
+def _beside(t, what, z, dtype, shape):
+    """Address of an argument that goes with the logits `z`: on their device, contiguous, of that type and shape; None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != z.device:
+    if t.dtype is not dtype or t.shape != shape or t.device != z.device or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor {list(shape)} on {z.device}, got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-class _LogitsCall:
-    """The arguments that all calls on logits share: the rows, the workspace, the stream; and the device they run on."""
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
-    def __init__(self, logits, scale, top=0, workspace=None):
-        data, stride = _rows_of(logits, "logits")
-        rows, vocab = logits.shape
-        self.z = _Logits(data, stride, rows, vocab, DTYPES[logits.dtype], scale)
-        self.ref = C.byref(self.z)
-        need = _lib.qsl_logits_workspace_bytes(self.ref, top)
-        if workspace is None and need:
+
+def _on_logits(where, fn, logits, scale, top, workspace, *args):
+    """Calls fn(rows, *args, workspace, its size, stream) on the logits' device and its current stream."""
+    data, stride = _rows_of(logits, "logits")
+    rows, vocab = logits.shape
+    z = C.byref(_Logits(data, stride, rows, vocab, DTYPES[logits.dtype], scale))
+    if workspace is None:
+        need = _lib.qsl_logits_workspace_bytes(z, top)
+        if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
-        elif workspace is not None:
-            _beside(workspace, "workspace", logits, torch.uint8, workspace.numel())
-        self.workspace, self.bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-        self._keep = workspace
-        self.index = logits.device.index
-        self.stream = torch.cuda.current_stream(logits.device).cuda_stream
-
-    def run(self, where, fn, *args):
-        if self.index == torch.cuda.current_device():
-            st = fn(self.ref, *args, self.workspace, self.bytes, self.stream)
-        else:
-            with torch.cuda.device(self.index):
-                st = fn(self.ref, *args, self.workspace, self.bytes, self.stream)
-        if st != OK:
-            raise QslError(st, where)
+    at, size = (None, 0) if workspace is None else (_beside(workspace, "workspace", logits, torch.uint8, (workspace.numel(),)), workspace.numel())
+    device = logits.get_device()
+    if device == _current_device():
+        st = fn(z, *args, at, size, _raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            st = fn(z, *args, at, size, _raw_stream(device))
+    if st != OK:
+        raise QslError(st, where)
 
 
 def logits_workspace_bytes(logits, top=0):
@@ -209,12 +204,11 @@ def token_logprobs(logits, target=None, scale=1.0, logprob=None, entropy=None, l
     N = logits.shape[0]
     some = top_index if top_index is not None else top_logprob
     top = 0 if some is None else some.shape[-1]
-    c = _LogitsCall(logits, scale, top, workspace)
     f32 = torch.float32
-    c.run("qsl_token_logprobs", _lib.qsl_token_logprobs, _beside(target, "target", logits, torch.int64, N), top,
-          _beside(logprob, "logprob", logits, f32, N), _beside(entropy, "entropy", logits, f32, N), _beside(lse, "lse", logits, f32, N),
-          _beside(top_index, "top_index", logits, torch.int32, N, top), _beside(top_logprob, "top_logprob", logits, f32, N, top),
-          _beside(stats, "stats", logits, f32, N, 4))
+    _on_logits("qsl_token_logprobs", _lib.qsl_token_logprobs, logits, scale, top, workspace, _beside(target, "target", logits, torch.int64, (N,)), top,
+               _beside(logprob, "logprob", logits, f32, (N,)), _beside(entropy, "entropy", logits, f32, (N,)), _beside(lse, "lse", logits, f32, (N,)),
+               _beside(top_index, "top_index", logits, torch.int32, (N, top)), _beside(top_logprob, "top_logprob", logits, f32, (N, top)),
+               _beside(stats, "stats", logits, f32, (N, 4)))
 
 
 def _gradient_rows(dlogits, logits):
@@ -227,40 +221,38 @@ def token_logprobs_backward(logits, target, dlogits, scale=1.0, grad_logprob=Non
                             entropy=None, workspace=None):
     """`qsl_token_logprobs_backward`: the gradient of sum(grad_logprob * logprob) + sum(grad_entropy * entropy) in the logits."""
     N = logits.shape[0]
-    c = _LogitsCall(logits, scale, 0, workspace)
     f32 = torch.float32
     out, dstride = _gradient_rows(dlogits, logits)
-    c.run("qsl_token_logprobs_backward", _lib.qsl_token_logprobs_backward, _beside(target, "target", logits, torch.int64, N),
-          _beside(grad_logprob, "grad_logprob", logits, f32, N), _beside(grad_entropy, "grad_entropy", logits, f32, N),
-          _beside(stats, "stats", logits, f32, N, 4), _beside(logprob, "logprob", logits, f32, N),
-          _beside(entropy, "entropy", logits, f32, N), out, dstride)
+    _on_logits("qsl_token_logprobs_backward", _lib.qsl_token_logprobs_backward, logits, scale, 0, workspace,
+               _beside(target, "target", logits, torch.int64, (N,)), _beside(grad_logprob, "grad_logprob", logits, f32, (N,)),
+               _beside(grad_entropy, "grad_entropy", logits, f32, (N,)), _beside(stats, "stats", logits, f32, (N, 4)),
+               _beside(logprob, "logprob", logits, f32, (N,)), _beside(entropy, "entropy", logits, f32, (N,)), out, dstride)
 
 
 def _teacher(logits, index, value, lse, scale):
     N, top = logits.shape[0], index.shape[-1]
-    return _Teacher(_beside(index, "teacher_index", logits, torch.int32, N, top), _beside(value, "teacher_value", logits, torch.float32, N, top),
-                    _beside(lse, "teacher_lse", logits, torch.float32, N), top, scale)
+    return C.byref(_Teacher(_beside(index, "teacher_index", logits, torch.int32, (N, top)),
+                            _beside(value, "teacher_value", logits, torch.float32, (N, top)),
+                            _beside(lse, "teacher_lse", logits, torch.float32, (N,)), top, scale))
 
 
 def distill(logits, teacher_index, teacher_value, scale=1.0, teacher_scale=1.0, teacher_lse=None, loss=None, stats=None, workspace=None):
     """`qsl_distill`: the Kullback-Leibler divergence of every row from a teacher's top logits [rows, top]."""
     N = logits.shape[0]
-    c = _LogitsCall(logits, scale, 0, workspace)
-    t = _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale)
-    c.run("qsl_distill", _lib.qsl_distill, C.byref(t), _beside(loss, "loss", logits, torch.float32, N),
-          _beside(stats, "stats", logits, torch.float32, N, 8))
+    _on_logits("qsl_distill", _lib.qsl_distill, logits, scale, teacher_index.shape[-1], workspace,
+               _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(loss, "loss", logits, torch.float32, (N,)),
+               _beside(stats, "stats", logits, torch.float32, (N, 8)))
 
 
 def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, teacher_scale=1.0, teacher_lse=None, grad_loss=None,
                      stats=None, loss=None, workspace=None):
     """`qsl_distill_backward`: the gradient of sum(grad_loss * loss) in the logits."""
     N = logits.shape[0]
-    c = _LogitsCall(logits, scale, 0, workspace)
-    t = _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale)
     f32 = torch.float32
     out, dstride = _gradient_rows(dlogits, logits)
-    c.run("qsl_distill_backward", _lib.qsl_distill_backward, C.byref(t), _beside(grad_loss, "grad_loss", logits, f32, N),
-          _beside(stats, "stats", logits, f32, N, 8), _beside(loss, "loss", logits, f32, N), out, dstride)
+    _on_logits("qsl_distill_backward", _lib.qsl_distill_backward, logits, scale, teacher_index.shape[-1], workspace,
+               _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(grad_loss, "grad_loss", logits, f32, (N,)),
+               _beside(stats, "stats", logits, f32, (N, 8)), _beside(loss, "loss", logits, f32, (N,)), out, dstride)
 
 
 class Qsl:

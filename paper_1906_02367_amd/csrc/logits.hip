@@ -13,14 +13,17 @@
 #include "qsl_logits.h"
 
 static_assert(TOP_MAX == QSL_TOP_MAX && TEACHER_MAX == QSL_TEACHER_MAX, "the header's limits");
-static_assert(CAND_CAP >= 2 * TOP_MAX, "a full list must hold more than the alternatives");
-static_assert(HASH_SIZE >= 2 * TEACHER_MAX && HASH_SIZE == 1u << 10, "teacher_entries takes the upper 10 bits of the hash");
+static_assert(REFINE >= 2 * TOP_MAX && CAND_CAP >= REFINE, "a bound from the first candidates must leave some of them out");
 
 namespace {
 
-constexpr uint32_t MAX_ROW_BLOCKS = 1u << 20;      // blocks of a launch; further rows are taken by the same blocks
+constexpr uint64_t GRID_X = 1u << 20;              // blocks in a row of the grid (a launch counts its threads in 32 bits)
+constexpr uint32_t FEW_ROWS = 256;                 // fewer rows than this leave compute units without a block
+constexpr uint32_t WANTED_BLOCKS = 1024;           // blocks of 256 threads that keep the chip busy
+constexpr uint64_t MIN_SLICE = 4096;               // bytes: 16 a thread
 
 bool scale_ok(float c) { return c >= 0x1p-100f && c <= 0x1p100f; }
+uint64_t align_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 uint32_t elem_size(uint32_t dtype) { return dtype == QSL_F32 ? 4 : 2; }
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -48,46 +51,117 @@ bool teacher_ok(const qsl_logits* z, const qsl_teacher* t) {
   return t->index && t->value && aligned(t->index, 4) && aligned(t->value, 4) && aligned(t->lse, 4);
 }
 
-bool workspace_ok(const qsl_logits* z, uint32_t top, const void* workspace, size_t bytes, qsl_status* st) {
-  const size_t need = qsl_logits_workspace_bytes(z, top);
-  *st = QSL_OK;
-  if (need == 0) return true;
-  if (!workspace || !aligned(workspace, 256)) *st = QSL_ERR_INVALID_ARG;
-  else if (bytes < need) *st = QSL_ERR_BUFFER_TOO_SMALL;
-  return *st == QSL_OK;
-}
-
-// f(the element type, the threads of a block) as types
+// f(the element type) as a type
 template <class F>
-void pick(const qsl_logits* z, F&& f) {
-  auto by_threads = [&](auto e) {
-    const uint32_t nvec = z->vocab / Elem<decltype(e)>::N;
-    if (nvec <= 256) f(e, std::integral_constant<int, 64>());
-    else if (nvec <= 2048) f(e, std::integral_constant<int, 256>());
-    else f(e, std::integral_constant<int, 1024>());
-  };
-  if (z->dtype == QSL_F32) by_threads(float());
-  else if (z->dtype == QSL_BF16) by_threads(__bf16());
-  else by_threads(_Float16());
+void pick_type(const qsl_logits* z, F&& f) {
+  if (z->dtype == QSL_F32) f(float());
+  else if (z->dtype == QSL_BF16) f(__bf16());
+  else f(_Float16());
 }
-
 template <class F>
 void pick_bool(bool b, F&& f) {
   if (b) f(std::true_type());
   else f(std::false_type());
 }
+template <int V> using Int = std::integral_constant<int, V>;
 
-dim3 row_grid(uint32_t rows) { return dim3(std::min(rows, MAX_ROW_BLOCKS)); }
+constexpr uint64_t KB = 1024;
+constexpr uint64_t HELD_MAX = 256 * KB;            // bytes of a row that 1024 threads hold in registers, 16 vectors each
+constexpr uint64_t HELD_TOP_MAX = 64 * KB;         // ... that 256 threads hold
+
+uint64_t row_bytes(const qsl_logits* z) { return static_cast<uint64_t>(z->vocab) * elem_size(z->dtype); }
+
+// f(threads, vectors a thread holds) for rows of at most HELD_MAX bytes (and the values behind their last vector)
+template <class F>
+void pick_held(uint64_t nvec, F&& f) {
+  if (nvec <= 64) f(Int<64>(), Int<1>());
+  else if (nvec <= 64 * 4) f(Int<64>(), Int<4>());
+  else if (nvec <= 256 * 4) f(Int<256>(), Int<4>());
+  else if (nvec <= 256 * 8) f(Int<256>(), Int<8>());
+  else if (nvec <= 256 * 16) f(Int<256>(), Int<16>());
+  else if (nvec <= 1024 * 8) f(Int<1024>(), Int<8>());
+  else f(Int<1024>(), Int<16>());
+}
+
+// How a call splits its rows.
+struct Plan {
+  bool split;
+  uint32_t S, len;
+};
+
+Plan plan_slices(const qsl_logits* z, uint64_t most_bytes) {
+  const uint64_t bytes = row_bytes(z), es = elem_size(z->dtype);
+  uint64_t S = std::max<uint64_t>((bytes + most_bytes - 1) / most_bytes, WANTED_BLOCKS / std::max(z->rows, 1u));
+  S = std::min<uint64_t>({S, SLICES_MAX, (bytes + MIN_SLICE - 1) / MIN_SLICE});
+  Plan p;
+  p.split = S > 1;
+  // whole 4 KB: slices start where vectors do, and their threads are busy alike
+  p.len = static_cast<uint32_t>(align_up((z->vocab + S - 1) / S, 4 * KB / es));
+  p.S = (z->vocab + p.len - 1) / p.len;
+  return p;
+}
+
+// Alternatives: in a block's registers, or a slice of the row in each; rows of more than 64 slices are walked along.
+Plan plan_top(const qsl_logits* z) {
+  const uint64_t bytes = row_bytes(z);
+  if (bytes > SLICES_MAX * HELD_TOP_MAX || (bytes <= HELD_TOP_MAX && (z->rows >= FEW_ROWS || bytes <= 4 * MIN_SLICE))) return Plan{false, 0, 0};
+  return plan_slices(z, HELD_TOP_MAX);
+}
+// Statistics alone (no alternatives), and the gradients: split where there are few rows.
+Plan plan_few(const qsl_logits* z) {
+  const uint64_t bytes = row_bytes(z);
+  if (z->rows >= FEW_ROWS || bytes <= 4 * MIN_SLICE) return Plan{false, 0, 0};
+  return plan_slices(z, bytes);
+}
+Plan plan_gradient(const qsl_logits* z) {
+  return row_bytes(z) > HELD_MAX ? plan_slices(z, HELD_MAX) : plan_few(z);
+}
+
+struct Workspace {
+  uint64_t need;
+  Slices sl;
+  Taught w;
+};
+// the parts of a call's workspace at `base`
+Workspace lay_out(const qsl_logits* z, const Plan& p, uint32_t keys, uint32_t entries, void* base) {
+  Workspace w = {};
+  if (!p.split) return w;
+  char* at = static_cast<char*>(base);
+  auto take = [&](uint64_t bytes) { char* r = at + w.need; w.need += align_up(bytes, 256); return r; };
+  const uint64_t rows = z->rows;
+  w.sl.S = p.S; w.sl.len = p.len;
+  w.sl.part = reinterpret_cast<Stat4*>(take(rows * p.S * sizeof(Stat4)));
+  if (keys) w.sl.key = reinterpret_cast<uint64_t*>(take(rows * p.S * keys * 8));
+  if (entries) {
+    w.w.row = reinterpret_cast<Stat4*>(take(rows * sizeof(Stat4)));
+    w.w.index = reinterpret_cast<int32_t*>(take(rows * entries * 4));
+    w.w.value = reinterpret_cast<float*>(take(rows * entries * 4));
+  }
+  return w;
+}
+
+qsl_status check_workspace(const qsl_logits* z, uint32_t top, const void* workspace, size_t bytes) {
+  const size_t need = qsl_logits_workspace_bytes(z, top);
+  if (need == 0) return QSL_OK;
+  if (!workspace || !aligned(workspace, 256)) return QSL_ERR_INVALID_ARG;
+  return bytes < need ? QSL_ERR_BUFFER_TOO_SMALL : QSL_OK;
+}
+
+dim3 grid_of(uint64_t blocks) {
+  return dim3(static_cast<uint32_t>(std::min(blocks, GRID_X)), static_cast<uint32_t>((blocks + GRID_X - 1) / GRID_X));
+}
+
+uint64_t apply_blocks(const qsl_logits* z) { const uint64_t n = 1024 * 16 / elem_size(z->dtype); return z->rows * ((z->vocab + n - 1) / n); }
 
 qsl_status launched() { return hipGetLastError() == hipSuccess ? QSL_OK : QSL_ERR_DEVICE; }
-
-uint32_t mask_bytes(uint32_t vocab) { return (std::min(vocab, MASK_SPAN) + 31) / 32 * 4; }
 
 }  // namespace
 
 extern "C" size_t qsl_logits_workspace_bytes(const qsl_logits* z, uint32_t top) {
-  (void)z; (void)top;
-  return 0;
+  if (!logits_ok(z) || z->rows == 0 || top > std::max(QSL_TOP_MAX, QSL_TEACHER_MAX)) return 0;
+  uint64_t need = std::max(lay_out(z, plan_few(z), 0, 0, nullptr).need, lay_out(z, plan_gradient(z), 0, top, nullptr).need);
+  if (top) need = std::max(need, lay_out(z, plan_top(z), top, 0, nullptr).need);
+  return need;
 }
 
 extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* target, uint32_t top, float* logprob, float* entropy,
@@ -101,13 +175,37 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
   if (logprob && !target) return QSL_ERR_INVALID_ARG;
   if (!aligned(target, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4) || !aligned(top_index, 4) ||
       !aligned(top_logprob, 4) || !aligned(stats, 16)) return QSL_ERR_INVALID_ARG;
-  qsl_status st;
-  if (!workspace_ok(z, top, workspace, workspace_bytes, &st)) return st;
+  const qsl_status st = check_workspace(z, top, workspace, workspace_bytes);
+  if (st != QSL_OK) return st;
   const ScoreArgs a = {z->data, z->stride, z->rows, z->vocab, top, z->scale, target, logprob, entropy, lse, top_index, top_logprob, stats};
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  pick(z, [&](auto e, auto th) {
+  const Plan plan = top ? plan_top(z) : plan_few(z);
+  const Slices sl = lay_out(z, plan, top, 0, workspace).sl;
+  const dim3 rows = grid_of(z->rows);
+  pick_type(z, [&](auto e) {
+    typedef decltype(e) E;
+    const uint32_t nvec = z->vocab / Elem<E>::N;
     pick_bool(entropy || stats, [&](auto ent) {
-      pick_bool(top != 0, [&](auto tp) { k_score<decltype(e), th(), ent(), tp()><<<row_grid(z->rows), th(), 0, stream>>>(a); });
+      if (plan.split) {
+        const dim3 grid = grid_of(static_cast<uint64_t>(z->rows) * plan.S);
+        const uint32_t held = (plan.len / Elem<E>::N + 255) / 256;
+        if (!top) k_slice_stats<E, 0, ent()><<<grid, 256, 0, stream>>>(a, sl);
+        else if (held <= 4) k_slice_stats<E, 4, ent()><<<grid, 256, 0, stream>>>(a, sl);
+        else k_slice_stats<E, 16, ent()><<<grid, 256, 0, stream>>>(a, sl);
+        k_score_join<E, ent()><<<rows, 256, 0, stream>>>(a, sl);
+      } else if (top && row_bytes(z) <= HELD_TOP_MAX) {
+        pick_held(top > 64 ? std::max(nvec, 64 * 4 + 1u) : nvec, [&](auto th, auto nv) {
+          if constexpr (th() <= 256) k_score_held<E, th(), nv(), ent()><<<rows, th(), 0, stream>>>(a);
+        });
+      } else if (top) {
+        k_score<E, 1024, ent(), true><<<rows, 1024, 0, stream>>>(a);
+      } else if (nvec <= 256) {
+        k_score<E, 64, ent(), false><<<rows, 64, 0, stream>>>(a);
+      } else if (nvec <= 2048) {
+        k_score<E, 256, ent(), false><<<rows, 256, 0, stream>>>(a);
+      } else {
+        k_score<E, 1024, ent(), false><<<rows, 1024, 0, stream>>>(a);
+      }
     });
   });
   return launched();
@@ -123,30 +221,52 @@ extern "C" qsl_status qsl_token_logprobs_backward(const qsl_logits* z, const int
   if (stats && (logprob || entropy)) return QSL_ERR_INVALID_ARG;
   if (!aligned(target, 8) || !aligned(grad_logprob, 4) || !aligned(grad_entropy, 4) || !aligned(stats, 16) || !aligned(logprob, 4) ||
       !aligned(entropy, 4)) return QSL_ERR_INVALID_ARG;
-  qsl_status st;
-  if (!workspace_ok(z, 0, workspace, workspace_bytes, &st)) return st;
+  const qsl_status st = check_workspace(z, 0, workspace, workspace_bytes);
+  if (st != QSL_OK) return st;
   const GradArgs a = {z->data, dlogits, z->stride, dstride, z->rows, z->vocab, z->scale, target, grad_logprob, grad_entropy, stats, logprob, entropy};
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  pick(z, [&](auto e, auto th) {
+  const Plan plan = plan_gradient(z);
+  const Slices sl = lay_out(z, plan, 0, 0, workspace).sl;
+  pick_type(z, [&](auto e) {
+    typedef decltype(e) E;
     pick_bool(grad_entropy || entropy, [&](auto ent) {
-      k_logprob_gradient<decltype(e), th(), ent()><<<row_grid(z->rows), th(), 0, stream>>>(a);
+      if (!stats && !plan.split) {
+        pick_held(z->vocab / Elem<E>::N, [&](auto th, auto nv) { k_gradient_held<E, th(), nv(), ent()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
+        return;
+      }
+      if (!stats) {
+        ScoreArgs s = {};
+        s.z = z->data; s.stride = z->stride; s.rows = z->rows; s.vocab = z->vocab; s.c = z->scale;
+        k_slice_stats<E, 0, ent()><<<grid_of(static_cast<uint64_t>(z->rows) * plan.S), 256, 0, stream>>>(s, sl);
+      }
+      k_gradient_apply<E, ent()><<<grid_of(apply_blocks(z)), 256, 0, stream>>>(a, sl);
     });
   });
   return launched();
 }
 
-static qsl_status launch_distill(const qsl_logits* z, const qsl_teacher* t, const DistillArgs& a, bool grad, void* workspace,
-                                 size_t workspace_bytes, void* hip_stream) {
-  qsl_status st;
-  if (!workspace_ok(z, 0, workspace, workspace_bytes, &st)) return st;
+static qsl_status launch_distill(const qsl_logits* z, const qsl_teacher* t, const DistillArgs& a, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream) {
+  const qsl_status st = check_workspace(z, t->top, workspace, workspace_bytes);
+  if (st != QSL_OK) return st;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  pick(z, [&](auto e, auto th) {
+  const Plan plan = plan_gradient(z);
+  const Workspace ws = lay_out(z, plan, 0, t->top, workspace);
+  const Taught w = a.dz ? ws.w : Taught{nullptr, nullptr, nullptr};
+  pick_type(z, [&](auto e) {
+    typedef decltype(e) E;
     pick_bool(t->lse != nullptr, [&](auto rest) {
-      pick_bool(grad, [&](auto gr) {
-        const uint32_t lds = rest() && !a.stats_in ? mask_bytes(z->vocab) : 0;
-        k_distill<decltype(e), th(), rest(), gr()><<<row_grid(z->rows), th(), lds, stream>>>(a);
-      });
+      if (!plan.split) {
+        pick_held(z->vocab / Elem<E>::N, [&](auto th, auto nv) { k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
+        return;
+      }
+      if (!a.stats_in) {
+        const uint32_t lds = rest() ? 4 * (std::min(plan.len, MASK_SPAN) / 32 + 1) : 0;
+        k_distill_slices<E, rest()><<<grid_of(static_cast<uint64_t>(z->rows) * plan.S), 256, lds, stream>>>(a, ws.sl);
+      }
+      k_distill_join<E, rest()><<<grid_of(z->rows), 256, 0, stream>>>(a, ws.sl, w);
     });
+    if (plan.split && a.dz) k_distill_apply<E><<<grid_of(apply_blocks(z)), 256, 0, stream>>>(a, w);
   });
   return launched();
 }
@@ -158,7 +278,7 @@ extern "C" qsl_status qsl_distill(const qsl_logits* z, const qsl_teacher* teache
   if ((!loss && !stats) || !aligned(loss, 4) || !aligned(stats, 16)) return QSL_ERR_INVALID_ARG;
   const DistillArgs a = {z->data, nullptr, z->stride, 0, z->rows, z->vocab, teacher->top, z->scale, teacher->scale, teacher->index,
                          teacher->value, teacher->lse, nullptr, nullptr, loss, stats};
-  return launch_distill(z, teacher, a, false, workspace, workspace_bytes, hip_stream);
+  return launch_distill(z, teacher, a, workspace, workspace_bytes, hip_stream);
 }
 
 extern "C" qsl_status qsl_distill_backward(const qsl_logits* z, const qsl_teacher* teacher, const float* grad_loss,
@@ -169,5 +289,5 @@ extern "C" qsl_status qsl_distill_backward(const qsl_logits* z, const qsl_teache
   if ((stats && loss) || !aligned(grad_loss, 4) || !aligned(stats, 16) || !aligned(loss, 4)) return QSL_ERR_INVALID_ARG;
   const DistillArgs a = {z->data, dlogits, z->stride, dstride, z->rows, z->vocab, teacher->top, z->scale, teacher->scale, teacher->index,
                          teacher->value, teacher->lse, grad_loss, stats, loss, nullptr};
-  return launch_distill(z, teacher, a, true, workspace, workspace_bytes, hip_stream);
+  return launch_distill(z, teacher, a, workspace, workspace_bytes, hip_stream);
 }

@@ -22,11 +22,16 @@ namespace {
 
 constexpr float LOWEST = -FLT_MAX, LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
 constexpr float Y_MIN = -1e4f;             // exp2 of this is 0; keeps 0 * -inf out of w
+// Blocks are numbered over a grid of two dimensions, whose last row may be short of work.  (A loop over rows in the kernel would have its
+// offsets held in registers from row to row: 189 VGPRs instead of 101 for 16 vectors.)
+__device__ __forceinline__ uint64_t block_number() { return static_cast<uint64_t>(blockIdx.y) * gridDim.x + blockIdx.x; }
+
 constexpr uint32_t TOP_MAX = 128;          // alternatives of a row at most
 constexpr uint32_t TEACHER_MAX = 256;      // entries of a teacher's row at most
-constexpr uint32_t CAND_CAP = 1024;        // candidates for the alternatives that are ranked at once
+constexpr uint32_t CAND_CAP = 512;         // candidates for the alternatives that are ranked at once
+constexpr uint32_t REFINE = 256;           // ... of which so many give the next bound when there are more
 constexpr uint32_t GROUPS = 256;           // maxima of groups of threads that the threshold is taken from, at most
-constexpr uint32_t HASH_SIZE = 1024;       // slots in which a teacher's entries are looked up: at most a quarter is used
+constexpr uint32_t HASH_SIZE = 4 * TEACHER_MAX;   // slots in which a teacher's entries are looked up, at most
 constexpr uint32_t MASK_SPAN = 1u << 18;   // classes whose membership in the teacher's entries is held in LDS at once (32 KB)
 
 // ---------------------------------------------------------------------------------------------
@@ -45,6 +50,15 @@ template <> struct Elem<float> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
   }
+  static __device__ __forceinline__ float value(raw4 r, uint32_t q) {
+    const uint32_t w = q;
+    const uint32_t lo = w & 1 ? r[1] : r[0], hi = w & 1 ? r[3] : r[2], x = w & 2 ? hi : lo;
+    return __uint_as_float(x);
+  }
+  static __device__ __forceinline__ void erase(raw4& r, uint32_t bits) {      // -inf where a bit is set
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = bits >> i & 1 ? MINUS_INF : r[i];
+  }
   static __device__ __forceinline__ raw4 pack(const float* v) {
     raw4 r;
 #pragma unroll
@@ -59,6 +73,18 @@ template <> struct Elem<__bf16> {
   static __device__ __forceinline__ void unpack(raw4 r, float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(r[i] << 16); v[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u); }
+  }
+  static __device__ __forceinline__ float value(raw4 r, uint32_t q) {
+    const uint32_t w = q >> 1;
+    const uint32_t lo = w & 1 ? r[1] : r[0], hi = w & 1 ? r[3] : r[2], x = w & 2 ? hi : lo;
+    return __uint_as_float(q & 1 ? x & 0xFFFF0000u : x << 16);
+  }
+  static __device__ __forceinline__ void erase(raw4& r, uint32_t bits) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t m = (bits >> 2 * i & 1 ? 0x0000FFFFu : 0u) | (bits >> 2 * i & 2 ? 0xFFFF0000u : 0u);
+      r[i] = (r[i] & ~m) | (MINUS_INF & m);
+    }
   }
   static __device__ __forceinline__ raw4 pack(const float* v) {      // rounded once, to nearest even
     typedef __bf16 b2 __attribute__((ext_vector_type(2)));
@@ -77,6 +103,18 @@ template <> struct Elem<_Float16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { const h2 x = __builtin_bit_cast(h2, static_cast<uint32_t>(r[i])); v[2 * i] = static_cast<float>(x[0]); v[2 * i + 1] = static_cast<float>(x[1]); }
   }
+  static __device__ __forceinline__ float value(raw4 r, uint32_t q) {
+    const uint32_t w = q >> 1;
+    const uint32_t lo = w & 1 ? r[1] : r[0], hi = w & 1 ? r[3] : r[2], x = w & 2 ? hi : lo;
+    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(q & 1 ? x >> 16 : x)));
+  }
+  static __device__ __forceinline__ void erase(raw4& r, uint32_t bits) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t m = (bits >> 2 * i & 1 ? 0x0000FFFFu : 0u) | (bits >> 2 * i & 2 ? 0xFFFF0000u : 0u);
+      r[i] = (r[i] & ~m) | (MINUS_INF & m);
+    }
+  }
   static __device__ __forceinline__ raw4 pack(const float* v) {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
     raw4 r;
@@ -93,6 +131,7 @@ template <class E> __device__ __forceinline__ void store16(E* p, raw4 r) { *rein
 // statistics
 // ---------------------------------------------------------------------------------------------
 struct Stat { float m, s, w; };
+struct __align__(16) Stat4 { float m, s, w, pad; };
 
 __device__ __forceinline__ Stat stat_none() { return Stat{LOWEST, 0.0f, 0.0f}; }
 __device__ __forceinline__ float exp2_(float y) { return __builtin_amdgcn_exp2f(y); }
@@ -103,12 +142,10 @@ __device__ __forceinline__ void take(Stat& o, const float* v, float cl) {
   float vm = v[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) vm = fmaxf(vm, v[i]);
-  if (vm > o.m) {
-    const float dl = fmaxf((o.m - vm) * cl, Y_MIN), f = exp2_(dl);
-    if (ENT) o.w = (o.w + o.s * dl) * f;
-    o.s *= f;
-    o.m = vm;
-  }
+  const float m = fmaxf(o.m, vm), dl = fmaxf((o.m - m) * cl, Y_MIN), f = exp2_(dl);      // f = 1 where m stays: cheaper than a branch
+  if (ENT) o.w = (o.w + o.s * dl) * f;
+  o.s *= f;
+  o.m = m;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float y = (v[i] - o.m) * cl, e = exp2_(y);
@@ -140,15 +177,18 @@ __device__ __forceinline__ float wave_sum_f(float x) {
   x += dpp_keep<DPP_BCAST31, 0xC>(x, 0.0f);
   return lane_float(x, 63);
 }
-__device__ __forceinline__ double wave_sum_d(double x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o, 64);
-  return x;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_zero_d(double x) {
+  return __builtin_bit_cast(double, dpp_or_zero64<CTRL, ROWS>(__builtin_bit_cast(uint64_t, x)));
 }
-__device__ __forceinline__ double wave_max_d(double x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = fmax(x, __shfl_xor(x, o, 64));
-  return x;
+__device__ __forceinline__ double wave_sum_d(double x) {
+  x += dpp_zero_d<DPP_ROW_SHR + 1, 0xF>(x);
+  x += dpp_zero_d<DPP_ROW_SHR + 2, 0xF>(x);
+  x += dpp_zero_d<DPP_ROW_SHR + 4, 0xF>(x);
+  x += dpp_zero_d<DPP_ROW_SHR + 8, 0xF>(x);
+  x += dpp_zero_d<DPP_BCAST15, 0xA>(x);
+  x += dpp_zero_d<DPP_BCAST31, 0xC>(x);
+  return __builtin_bit_cast(double, lane_value64(__builtin_bit_cast(uint64_t, x), 63));
 }
 
 // (m, s, w) brought to a larger maximum
@@ -228,91 +268,238 @@ __device__ __forceinline__ Stat pass_stat(const E* z, uint32_t n, float cl) {
   return o;
 }
 
+// dz = p (A + B y) with y = (x - m) cl, p = exp2(y - l2): the gradient in a class that nothing is given for
+struct Gradient { float cl, m, l2, A, B; };
+template <bool ENT>
+__device__ __forceinline__ float gradient_value(const Gradient& f, float x) {
+  const float y = (x - f.m) * f.cl, p = exp2_(y - f.l2);
+  return ENT ? p * __builtin_fmaf(f.B, fmaxf(y, Y_MIN), f.A) : p * f.A;
+}
+
+// A piece of a row that the block holds in registers, NV vectors a thread and the values behind the last whole vector one a thread: it
+// is read from memory once, whatever is made of it.  load() only starts the loads; loads past the end go to the last vector, and
+// settle() makes -inf of them.
+template <class E, int TH, int NV>
+struct Held {
+  static constexpr int N = Elem<E>::N;
+  static constexpr uint32_t SIZE = TH * NV * N;                        // values in whole vectors
+  raw4 r[NV];
+  E last;
+  uint32_t nvec, n;
+  __device__ __forceinline__ uint32_t vec(int u) const { return threadIdx.x + u * TH; }
+  __device__ __forceinline__ uint32_t last_index() const { return nvec * N + threadIdx.x; }
+  __device__ __forceinline__ void load(const E* z, uint32_t n_) {
+    n = n_; nvec = n / N;
+    if (nvec) {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) r[u] = load16(z + static_cast<uint64_t>(min(vec(u), nvec - 1)) * N);
+    }
+    last = z[min(last_index(), n - 1)];
+  }
+  // What is made of vector u comes after `y` is known: keeps the compiler from waiting for all loads before the first sum, and from
+  // holding all values unpacked from one use to the next (16 vectors of bf16: 152 VGPRs without this, 101 with it).
+  __device__ __forceinline__ void in_order(int u, float& y) { asm volatile("" : "+v"(r[u]), "+v"(y)); }
+  __device__ __forceinline__ void settle(int u) {
+    const bool out = vec(u) >= nvec;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) r[u][q] = out ? Elem<E>::MINUS_INF : r[u][q];
+  }
+  // out(first index of vector u): the bits of the values that are left out
+  template <bool ENT, class F>
+  __device__ __forceinline__ Stat stat(float cl, F&& out) {
+    constexpr int U = NV < 16 / N ? NV : 16 / N;
+    Stat o = stat_none();
+#pragma unroll
+    for (int u0 = 0; u0 < NV; u0 += U) {
+      float v[U * N];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        in_order(u0 + u, o.s);
+        if (ENT) in_order(u0 + u, o.w);
+        settle(u0 + u);
+        const uint32_t bits = out(min(vec(u0 + u), nvec) * N);
+        if (bits) Elem<E>::erase(r[u0 + u], bits);
+        Elem<E>::unpack(r[u0 + u], v + u * N);
+      }
+      take<ENT, U * N>(o, v, cl);
+    }
+    const float x = last_index() < n && !(out(nvec * N) >> threadIdx.x % 32 & 1 && threadIdx.x < N) ? static_cast<float>(last) : -INFINITY;
+    take<ENT, 1>(o, &x, cl);
+    return o;
+  }
+  // f(index, value) for the values that are at least `tau`: few, so the code for one of them stands once per vector
+  template <class F>
+  __device__ __forceinline__ void at_least(float tau, F&& f) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      in_order(u, tau);
+      float v[N];
+      Elem<E>::unpack(r[u], v);
+      uint32_t hits = 0;
+#pragma unroll
+      for (int q = 0; q < N; ++q) hits |= v[q] >= tau ? 1u << q : 0u;
+      if (vec(u) >= nvec) hits = 0;
+      while (hits) {
+        const uint32_t q = __builtin_ctz(hits);
+        hits &= hits - 1;
+        f(vec(u) * N + q, Elem<E>::value(r[u], q));
+      }
+    }
+    if (last_index() < n && static_cast<float>(last) >= tau) f(last_index(), static_cast<float>(last));
+  }
+  // the gradient of the piece; where class t is in it, `add` comes on top and given(its logit) is called
+  template <bool ENT, class F>
+  __device__ __forceinline__ void gradient(E* dz, Gradient f, uint32_t t, float add, F&& given) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      in_order(u, f.A);
+      float v[N];
+      Elem<E>::unpack(r[u], v);
+      const uint32_t q0 = t - vec(u) * N;
+      if (q0 < static_cast<uint32_t>(N) && vec(u) < nvec) {
+        float x = v[0];
+#pragma unroll
+        for (int q = 0; q < N; ++q) x = q0 == static_cast<uint32_t>(q) ? v[q] : x;
+        given(x);
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = gradient_value<ENT>(f, v[q]) + (q0 == static_cast<uint32_t>(q) ? add : 0.0f);
+      } else {
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = gradient_value<ENT>(f, v[q]);
+      }
+      if (vec(u) < nvec) store16(dz + static_cast<uint64_t>(vec(u)) * N, Elem<E>::pack(v));
+    }
+    if (last_index() < n) {
+      const float x = static_cast<float>(last);
+      if (t == last_index()) given(x);
+      dz[last_index()] = static_cast<E>(gradient_value<ENT>(f, x) + (t == last_index() ? add : 0.0f));
+    }
+  }
+};
+struct NoneOut { __device__ __forceinline__ uint32_t operator()(uint32_t) const { return 0; } };
+
+// a barrier for what is in LDS: loads from memory stay under way
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // ---------------------------------------------------------------------------------------------
 // the K largest values of a row, ties to the lower index
 // ---------------------------------------------------------------------------------------------
 // orders like (value, lower index first); no two entries of a row have the same key, and 0 is none's
-__device__ __forceinline__ uint64_t top_key(float z, uint32_t i) {
+__device__ __forceinline__ uint32_t ordered(float z) {                // (not for NaN)
   const uint32_t u = __float_as_uint(z + 0.0f);                       // -0 counts as +0
-  const uint32_t o = u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
-  return static_cast<uint64_t>(o) << 32 | (0xFFFFFFFFu - i);
+  return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
-__device__ __forceinline__ float key_value(uint64_t k) {
-  const uint32_t o = static_cast<uint32_t>(k >> 32);
-  return __uint_as_float(o >> 31 ? o ^ 0x80000000u : ~o);
-}
+__device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o >> 31 ? o ^ 0x80000000u : ~o); }
+__device__ __forceinline__ uint64_t top_key(float z, uint32_t i) { return static_cast<uint64_t>(ordered(z)) << 32 | (0xFFFFFFFFu - i); }
+__device__ __forceinline__ float key_value(uint64_t k) { return from_ordered(static_cast<uint32_t>(k >> 32)); }
 __device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xFFFFFFFFu - static_cast<uint32_t>(k); }
 
+template <uint32_t CAP>
 struct TopBox {
-  uint64_t list[CAND_CAP];
-  float group[GROUPS];
-  float tau;
+  __align__(16) uint64_t list[CAP + 8];    // zeros behind the last one up to a multiple of 8
+  __align__(16) float group[GROUPS];
   uint32_t n;
   uint64_t kth;
 };
 
-// The K largest of a row whose threads have met `most` as their largest value (-inf: none), through out(rank, key).
-// Groups of threads hold distinct values, so the K-th largest of the groups' maxima is at most the K-th largest value: only what
-// reaches it is a candidate (for values in no particular order a few more than K, in the few threads whose maximum reaches it).  If
-// more than CAND_CAP do (many equal or ordered values), the K-th largest of those that found room is the next bound; keys differ,
-// so it is a larger one.
-template <class E, int TH, class F>
-__device__ __forceinline__ void block_top(const E* z, uint32_t n, uint32_t K, float most, TopBox& b, F&& out) {
-  constexpr int N = Elem<E>::N, U = 4;
-  constexpr uint32_t PER = TH > GROUPS ? TH / GROUPS : 1, G = TH / PER;
+// for i < held: f(i, list[i], how many of list[0 .. among) are larger); zeros stand behind list[held - 1] up to a multiple of 8
+template <int TH, class F>
+__device__ __forceinline__ void ranked(const uint64_t* list, uint32_t held, uint32_t among, F&& f) {
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x; i < held; i += TH) {
+    const uint64_t k = list[i];
+    uint32_t rank = 0;
+#pragma unroll 1
+    for (uint32_t j = 0; j < among; j += 8) {                         // 8 at a time: one at a time every comparison waits for its own read
+#pragma unroll
+      for (uint32_t q = 0; q < 8; q += 2) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(list + j + q);
+        rank += (o.x > k) + (o.y > k);
+      }
+    }
+    f(k, rank);
+  }
+}
+
+// The K largest of n entries that the threads of a block hold, through out(rank, key); `most`: the thread's largest value (-inf:
+// none); scan(tau, f): f(key) for each of the thread's entries whose value is at least tau.
+// Groups of threads hold distinct entries, so the K-th largest of the groups' maxima is at most the K-th largest value: only what
+// reaches it is a candidate (for values in no particular order a few more than K, in the few threads whose maximum reaches it).  Every
+// wave finds it for itself, 20 bits of it from the top, by counting the maxima that reach a trial value; less than it will do as
+// well.  If more than CAP entries are candidates (many equal or ordered values), the K-th largest of the first REFINE that found room
+// is the next bound: a larger one, since keys differ, and for entries in no particular order it leaves K / REFINE of them.
+template <int TH, uint32_t CAP, class S, class F>
+__device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, TopBox<CAP>& b, S&& scan, F&& out) {
+  constexpr uint32_t PER = TH > GROUPS ? TH / GROUPS : 1, G = TH / PER, M = G / 64;
+  static_assert(PER == 1 || PER == 4, "a group is a thread or the four lanes of a quad");
   float gm = most;
   if (PER == 4) {
     gm = fmaxf(gm, dpp_keep<0xB1, 0xF>(gm, gm));                      // the lanes of a quad: 1 0 3 2, then 2 3 0 1
     gm = fmaxf(gm, dpp_keep<0x4E, 0xF>(gm, gm));
   }
-  if (threadIdx.x % PER == 0) b.group[threadIdx.x / PER] = gm;
-  if (threadIdx.x == 0) { b.tau = -INFINITY; b.n = 0; }
+  if (TH > 64 && threadIdx.x % PER == 0) b.group[threadIdx.x / PER] = gm;
+  if (threadIdx.x == 0) b.n = 0;
   __syncthreads();
-  if (K <= G && threadIdx.x < G) {
-    const float mine = b.group[threadIdx.x];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < G; ++j) { const float o = b.group[j]; rank += o > mine || (o == mine && j < threadIdx.x); }
-    if (rank == K - 1) b.tau = mine;
-  }
-  __syncthreads();
-  const float tau = b.tau;
-  uint64_t bound = top_key(tau, 0xFFFFFFFFu);
-  for (;;) {
-    auto offer = [&](uint32_t i, float x) {
-      const uint64_t k = top_key(x, i);
-      if (k < bound) return;
-      const uint32_t at = atomicAdd(&b.n, 1u);
-      if (at < CAND_CAP) b.list[at] = k;
-    };
-    if (most >= tau)
-      walk<E, TH, U>(z, n,
-        [&](uint32_t v0, const raw4* r) {
+  float tau = -INFINITY;
+  if (K <= G && n > 2 * K) {
+    uint32_t o[M], T = 0;
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const uint32_t i = (v0 + u * TH) * N;
-            if (v0 + u * TH >= n / N) continue;
-            float v[N];
-            Elem<E>::unpack(r[u], v);
+    for (uint32_t j = 0; j < M; ++j) o[j] = ordered(TH > 64 ? b.group[lane_id() + 64 * j] : gm);
+#pragma unroll 1
+    for (uint32_t bit = 1u << 31; bit >= 1u << 12; bit >>= 1) {
+      uint32_t reach = 0;
 #pragma unroll
-            for (int q = 0; q < N; ++q) if (v[q] >= tau) offer(i + q, v[q]);
-          }
-        },
-        [&](uint32_t i, float x) { if (x >= tau) offer(i, x); });
-    __syncthreads();
-    const uint32_t found = b.n, held = min(found, CAND_CAP);
-    for (uint32_t i = threadIdx.x; i < held; i += TH) {
-      const uint64_t k = b.list[i];
-      uint32_t rank = 0;
-      for (uint32_t j = 0; j < held; ++j) rank += b.list[j] > k;
-      if (found <= CAND_CAP) { if (rank < K) out(rank, k); }
-      else if (rank == K - 1) b.kth = k;
+      for (uint32_t j = 0; j < M; ++j) reach += __popcll(__ballot(o[j] >= (T | bit)));
+      if (reach >= K) T |= bit;
     }
-    if (found <= CAND_CAP) break;
+    if (T > ordered(-INFINITY)) tau = from_ordered(T);
+  }
+  uint64_t bound = 0;
+  for (;;) {
+    if (most >= tau)
+      scan(tau, [&](uint64_t k) {
+        if (k < bound) return;
+        const uint32_t at = atomicAdd(&b.n, 1u);
+        if (at < CAP) b.list[at] = k;
+      });
+    __syncthreads();
+    const uint32_t found = b.n, held = min(found, CAP);
+    if (threadIdx.x < 8) b.list[held + threadIdx.x] = 0;
+    __syncthreads();
+    if (found <= CAP) {
+      ranked<TH>(b.list, held, held, [&](uint64_t k, uint32_t rank) { if (rank < K) out(rank, k); });
+      return;
+    }
+    ranked<TH>(b.list, REFINE, REFINE, [&](uint64_t k, uint32_t rank) { if (rank == K - 1) b.kth = k; });
     __syncthreads();
     bound = b.kth;
     if (threadIdx.x == 0) b.n = 0;
     __syncthreads();
   }
+}
+
+// the same for a row in memory
+template <class E, int TH, uint32_t CAP, class F>
+__device__ __forceinline__ void row_top(const E* z, uint32_t n, uint32_t K, float most, TopBox<CAP>& b, F&& out) {
+  constexpr int N = Elem<E>::N, U = 4;
+  block_top<TH, CAP>(n, K, most, b, [&](float tau, auto&& f) {
+    walk<E, TH, U>(z, n,
+      [&](uint32_t v0, const raw4* r) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (v0 + u * TH >= n / N) continue;
+          float v[N];
+          Elem<E>::unpack(r[u], v);
+#pragma unroll
+          for (int q = 0; q < N; ++q) if (v[q] >= tau) f(top_key(v[q], (v0 + u * TH) * N + q));
+        }
+      },
+      [&](uint32_t i, float x) { if (x >= tau) f(top_key(x, i)); });
+  }, out);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -334,69 +521,169 @@ __device__ __forceinline__ float log_prob(const RowStat& r, float z, float c) {
   return z == -INFINITY && r.L == r.L ? -INFINITY : (z - r.m) * c - r.L;       // also where the row holds nothing else (L = -inf)
 }
 
+// the given class and its logit, read by one thread ahead of the row: two reads, one behind the other
 template <class E>
-__device__ __forceinline__ float target_logprob(const RowStat& r, const E* z, uint32_t vocab, int64_t t, float c) {
-  if (t < 0) return 0.0f;
-  if (t >= static_cast<int64_t>(vocab)) return NAN;
-  return log_prob(r, static_cast<float>(z[t]), c);
+struct Given {
+  int64_t t;
+  E x;
+  __device__ __forceinline__ void load(const ScoreArgs& a, uint32_t row, const E* z) {
+    if (!a.logprob || threadIdx.x != 0) return;
+    t = a.target[row];
+    x = z[t >= 0 && t < static_cast<int64_t>(a.vocab) ? t : 0];
+  }
+  __device__ __forceinline__ float logprob(const ScoreArgs& a, const RowStat& r) const {
+    return t < 0 ? 0.0f : t >= static_cast<int64_t>(a.vocab) ? NAN : log_prob(r, static_cast<float>(x), a.c);
+  }
+};
+
+template <class E>
+__device__ __forceinline__ void score_outputs(const ScoreArgs& a, uint32_t row, const Given<E>& g, const Stat& o, const RowStat& r) {
+  if (a.logprob) a.logprob[row] = g.logprob(a, r);
+  if (a.entropy) a.entropy[row] = r.H;
+  if (a.lse) a.lse[row] = o.s == 0.0f ? -INFINITY : r.m * a.c + r.L;
+  if (a.stats) { float* s = a.stats + 4ull * row; s[0] = r.m; s[1] = r.L; s[2] = r.H; s[3] = 0.0f; }
+}
+// f(out) with out(rank, key) writing an alternative; where the row has no order (a NaN or +inf in it) the outputs say so instead
+template <int TH, class F>
+__device__ __forceinline__ void alternatives(const ScoreArgs& a, uint32_t row, const RowStat& r, F&& f) {
+  int32_t* ti = a.top_index ? a.top_index + static_cast<uint64_t>(row) * a.K : nullptr;
+  float* tl = a.top_logprob ? a.top_logprob + static_cast<uint64_t>(row) * a.K : nullptr;
+  if (r.L != r.L) {
+    for (uint32_t k = threadIdx.x; k < a.K; k += TH) { if (ti) ti[k] = -1; if (tl) tl[k] = NAN; }
+    return;
+  }
+  f([&](uint32_t rank, uint64_t k) {
+    if (ti) ti[rank] = static_cast<int32_t>(key_index(k));
+    if (tl) tl[rank] = log_prob(r, key_value(k), a.c);
+  });
 }
 
+// A block per row, which it walks along (with alternatives it reads the threads' shares that hold candidates again).
 template <class E, int TH, bool ENT, bool TOP>
 __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
   __shared__ Stat box[16];
-  __shared__ TopBox tb;
+  __shared__ TopBox<TOP ? CAND_CAP : 1> tb;
   const float cl = a.c * LOG2E;
-  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const E* z = static_cast<const E*>(a.z) + row * a.stride;
-    const Stat mine = pass_stat<E, TH, ENT>(z, a.vocab, cl);
-    const Stat o = block_stat<ENT, TH>(mine, cl, box);
-    const RowStat r = row_stat<ENT>(o);
-    if (threadIdx.x == 0) {
-      if (a.logprob) a.logprob[row] = target_logprob(r, z, a.vocab, a.target[row], a.c);
-      if (ENT && a.entropy) a.entropy[row] = r.H;
-      if (a.lse) a.lse[row] = o.s == 0.0f ? -INFINITY : r.m * a.c + r.L;
-      if (a.stats) { float* s = a.stats + 4ull * row; s[0] = r.m; s[1] = r.L; s[2] = r.H; s[3] = 0.0f; }
-    }
-    if (TOP) {
-      int32_t* ti = a.top_index ? a.top_index + static_cast<uint64_t>(row) * a.K : nullptr;
-      float* tl = a.top_logprob ? a.top_logprob + static_cast<uint64_t>(row) * a.K : nullptr;
-      if (r.L != r.L) {                                              // a NaN or +inf in the row: no order to speak of
-        for (uint32_t k = threadIdx.x; k < a.K; k += TH) { if (ti) ti[k] = -1; if (tl) tl[k] = NAN; }
-      } else {
-        block_top<E, TH>(z, a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb, [&](uint32_t rank, uint64_t k) {
-          if (ti) ti[rank] = static_cast<int32_t>(key_index(k));
-          if (tl) tl[rank] = log_prob(r, key_value(k), a.c);
-        });
-      }
-    }
-    __syncthreads();                                                  // box and tb are used again
+  const uint64_t row = block_number();
+  if (row >= a.rows) return;
+  const E* z = static_cast<const E*>(a.z) + row * a.stride;
+  Given<E> given;
+  given.load(a, row, z);
+  const Stat mine = pass_stat<E, TH, ENT>(z, a.vocab, cl);
+  const Stat o = block_stat<ENT, TH>(mine, cl, box);
+  const RowStat r = row_stat<ENT>(o);
+  if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
+  if (TOP)
+    alternatives<TH>(a, row, r, [&](auto&& out) {
+      row_top<E, TH, TOP ? CAND_CAP : 1>(z, a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb, out);
+    });
+}
+
+// Alternatives of a row that fits the block's registers.
+template <class E, int TH, int NV, bool ENT>
+__global__ __launch_bounds__(TH) void k_score_held(ScoreArgs a) {
+  constexpr uint32_t CAP = CAND_CAP;
+  __shared__ Stat box[16];
+  __shared__ TopBox<CAP> tb;
+  const float cl = a.c * LOG2E;
+  const uint64_t row = block_number();
+  if (row >= a.rows) return;
+  const E* z = static_cast<const E*>(a.z) + row * a.stride;
+  Given<E> given;
+  Held<E, TH, NV> h;
+  h.load(z, a.vocab);
+  given.load(a, row, z);
+  const Stat mine = h.template stat<ENT>(cl, NoneOut());
+  const Stat o = block_stat<ENT, TH>(mine, cl, box);
+  const RowStat r = row_stat<ENT>(o);
+  if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
+  alternatives<TH>(a, row, r, [&](auto&& out) {
+    block_top<TH, CAP>(a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb,
+                       [&](float tau, auto&& f) { h.at_least(tau, [&](uint32_t i, float x) { f(top_key(x, i)); }); }, out);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
+// rows split into slices, a block each, where there are few rows or they do not fit a block's registers
+// ---------------------------------------------------------------------------------------------
+constexpr uint32_t SLICES_MAX = 64;        // slices of a row at most: a wave joins them
+
+struct Slices {
+  uint32_t S, len;                         // slices of a row, values in each but the last
+  Stat4* part;                             // [rows, S]
+  uint64_t* key;                           // [rows, S, K] the slice's largest, largest first; 0: none
+};
+
+// NV = 0: the slice is walked along, without alternatives
+template <class E, int NV, bool ENT>
+__global__ __launch_bounds__(256) void k_slice_stats(ScoreArgs a, Slices sl) {
+  __shared__ Stat box[4];
+  __shared__ TopBox<NV ? CAND_CAP : 1> tb;
+  const float cl = a.c * LOG2E;
+  const uint64_t pieces = static_cast<uint64_t>(a.rows) * sl.S;
+  const uint64_t p = block_number();
+  if (p >= pieces) return;
+  const uint32_t row = static_cast<uint32_t>(p / sl.S), i0 = static_cast<uint32_t>(p % sl.S) * sl.len, n = min(a.vocab - i0, sl.len);
+  const E* z = static_cast<const E*>(a.z) + row * a.stride + i0;
+  auto hand_over = [&](const Stat& mine) {
+    const Stat o = block_stat<ENT, 256>(mine, cl, box);
+    if (threadIdx.x == 0) sl.part[p] = Stat4{o.m, o.s, o.w, 0.0f};
+  };
+  if constexpr (NV == 0) hand_over(pass_stat<E, 256, ENT>(z, n, cl));
+  else {
+    Held<E, 256, NV> h;
+    h.load(z, n);
+    const Stat mine = h.template stat<ENT>(cl, NoneOut());
+    hand_over(mine);
+    uint64_t* key = sl.key + p * a.K;
+    for (uint32_t k = threadIdx.x; k < a.K; k += 256) if (k >= n) key[k] = 0;      // (of a slice with a NaN nobody looks at the keys)
+    block_top<256, CAND_CAP>(n, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb,
+                             [&](float tau, auto&& f) { h.at_least(tau, [&](uint32_t i, float x) { f(top_key(x, i0 + i)); }); },
+                             [&](uint32_t rank, uint64_t k) { key[rank] = k; });
   }
 }
 
-// ---------------------------------------------------------------------------------------------
-// gradients: dz_i = p_i (A + B y_i) for every class, the given token's or the teacher's classes written again behind a barrier
-// ---------------------------------------------------------------------------------------------
-template <class E, int TH, bool ENT>
-__device__ __forceinline__ void pass_gradient(const E* z, E* dz, uint32_t n, float cl, float m, float l2, float A, float B) {
-  constexpr int N = Elem<E>::N, U = 4;
-  auto value = [&](float x) {
-    const float y = (x - m) * cl, p = exp2_(y - l2);
-    return ENT ? p * __builtin_fmaf(B, fmaxf(y, Y_MIN), A) : p * A;
-  };
-  walk<E, TH, U>(z, n,
-    [&](uint32_t v0, const raw4* r) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float v[N];
-        Elem<E>::unpack(r[u], v);
-#pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = value(v[q]);
-        if (v0 + u * TH < n / N) store16(dz + static_cast<uint64_t>(v0 + u * TH) * N, Elem<E>::pack(v));
-      }
-    },
-    [&](uint32_t i, float x) { dz[i] = static_cast<E>(value(x)); });
+// every wave: the statistics of a row from those of its slices
+template <bool ENT>
+__device__ __forceinline__ Stat joined(const Slices& sl, uint32_t row, float cl) {
+  Stat o = stat_none();
+  if (lane_id() < sl.S) { const Stat4 p = sl.part[static_cast<uint64_t>(row) * sl.S + lane_id()]; o = Stat{p.m, p.s, p.w}; }
+  return wave_stat<ENT>(o, cl);
 }
 
+template <class E, bool ENT>
+__global__ __launch_bounds__(256) void k_score_join(ScoreArgs a, Slices sl) {
+  __shared__ TopBox<CAND_CAP> tb;
+  const float cl = a.c * LOG2E;
+  const uint64_t row = block_number();
+  if (row >= a.rows) return;
+  const uint32_t n = sl.S * a.K;
+  const uint64_t* key = sl.key + row * n;
+  const uint64_t mine = threadIdx.x < n ? key[threadIdx.x] : 0;
+  Given<E> given;
+  given.load(a, row, static_cast<const E*>(a.z) + row * a.stride);
+  const Stat o = joined<ENT>(sl, row, cl);
+  const RowStat r = row_stat<ENT>(o);
+  if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
+  if (a.K == 0) return;
+  alternatives<256>(a, row, r, [&](auto&& out) {
+    if (n <= 256) {                                                   // no bound needed: rank them all
+      tb.list[threadIdx.x] = mine;
+      if (threadIdx.x < 8) tb.list[256 + threadIdx.x] = 0;
+      __syncthreads();
+      ranked<256>(tb.list, n, n, [&](uint64_t k, uint32_t rank) { if (k && rank < a.K) out(rank, k); });
+      return;
+    }
+    uint64_t most = mine;
+    for (uint32_t i = threadIdx.x + 256; i < n; i += 256) most = max(most, key[i]);
+    block_top<256, CAND_CAP>(n, a.K, most ? key_value(most) : -INFINITY, tb,
+      [&](float tau, auto&& f) { for (uint32_t i = threadIdx.x; i < n; i += 256) { const uint64_t k = key[i]; if (k && key_value(k) >= tau) f(k); } }, out);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
+// the gradient of log probabilities and entropies
+// ---------------------------------------------------------------------------------------------
 struct GradArgs {
   const void* z;
   void* dz;
@@ -409,43 +696,69 @@ struct GradArgs {
   float *logprob, *entropy;
 };
 
-// A block per row: without `stats` it walks along the row twice, the second time mostly through the caches.
-template <class E, int TH, bool ENT>
-__global__ __launch_bounds__(TH) void k_logprob_gradient(GradArgs a) {
+struct RowGradient {
+  Gradient f;
+  uint32_t t;                              // the given class, or 2^32 - 1
+  float add;                               // what it gets on top
+};
+
+template <bool ENT>
+__device__ __forceinline__ RowGradient row_gradient(const GradArgs& a, uint32_t row, const RowStat& r) {
+  const int64_t t = a.target ? a.target[row] : -1;
+  float g = a.g && t >= 0 ? a.g[row] : 0.0f;
+  if (t >= static_cast<int64_t>(a.vocab)) g = NAN;
+  const float h = ENT && a.h ? a.h[row] : 0.0f;
+  const bool empty = r.L == -INFINITY;
+  RowGradient o;
+  o.f.cl = a.c * LOG2E; o.f.m = r.m;
+  o.f.l2 = empty ? 0.0f : r.L * LOG2E;
+  o.f.A = empty ? 0.0f : -a.c * (g + h * (r.H - r.L));
+  o.f.B = -a.c * h * LN2;
+  o.t = t >= 0 && t < static_cast<int64_t>(a.vocab) ? static_cast<uint32_t>(t) : 0xFFFFFFFFu;
+  o.add = empty ? 0.0f : a.c * g;
+  return o;
+}
+// what a row hands out besides its gradient; the log probability of a given class comes from the thread that holds it
+__device__ __forceinline__ void gradient_outputs(const GradArgs& a, uint32_t row, const RowStat& r, const RowGradient& o) {
+  if (a.entropy) a.entropy[row] = r.H;
+  if (a.logprob && o.t == 0xFFFFFFFFu) a.logprob[row] = a.target[row] < 0 ? 0.0f : NAN;
+}
+
+// A block per row, held in its registers: one read, one write.
+template <class E, int TH, int NV, bool ENT>
+__global__ __launch_bounds__(TH) void k_gradient_held(GradArgs a) {
   __shared__ Stat box[16];
   const float cl = a.c * LOG2E;
-  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const E* z = static_cast<const E*>(a.z) + row * a.stride;
-    E* dz = static_cast<E*>(a.dz) + row * a.dstride;
-    const int64_t t = a.target ? a.target[row] : -1;
-    const bool given = t >= 0 && t < static_cast<int64_t>(a.vocab);
-    const float zt = given ? static_cast<float>(z[t]) : 0.0f;         // before anything is written: dz may be z
-    RowStat r;
-    if (a.stats) {
-      const float* s = a.stats + 4ull * row;
-      r.m = s[0]; r.L = s[1]; r.H = s[2];
-      __syncthreads();
-    } else {
-      r = row_stat<ENT>(block_stat<ENT, TH>(pass_stat<E, TH, ENT>(z, a.vocab, cl), cl, box));
-      if (threadIdx.x == 0) {
-        if (a.logprob) a.logprob[row] = t < 0 ? 0.0f : given ? log_prob(r, zt, a.c) : NAN;
-        if (ENT && a.entropy) a.entropy[row] = r.H;
-      }
-      __syncthreads();
-    }
-    float g = a.g && t >= 0 ? a.g[row] : 0.0f;
-    if (t >= static_cast<int64_t>(a.vocab)) g = NAN;
-    const float h = ENT && a.h ? a.h[row] : 0.0f;
-    const bool empty = r.L == -INFINITY;
-    const float l2 = empty ? 0.0f : r.L * LOG2E;
-    const float A = empty ? 0.0f : -a.c * (g + h * (r.H - r.L)), B = -a.c * h * LN2;
-    pass_gradient<E, TH, ENT>(z, dz, a.vocab, cl, r.m, l2, A, B);
-    __syncthreads();
-    if (threadIdx.x == 0 && given && !empty) {
-      const float y = (zt - r.m) * cl, p = exp2_(y - l2);
-      dz[t] = static_cast<E>(a.c * g + p * __builtin_fmaf(B, fmaxf(y, Y_MIN), A));
-    }
-  }
+  const uint64_t row = block_number();
+  if (row >= a.rows) return;
+  Held<E, TH, NV> h;
+  h.load(static_cast<const E*>(a.z) + row * a.stride, a.vocab);
+  const RowStat r = row_stat<ENT>(block_stat<ENT, TH>(h.template stat<ENT>(cl, NoneOut()), cl, box));
+  const RowGradient o = row_gradient<ENT>(a, row, r);
+  h.template gradient<ENT>(static_cast<E*>(a.dz) + row * a.dstride, o.f, o.t, o.add,
+                           [&](float x) { if (a.logprob) a.logprob[row] = log_prob(r, x, a.c); });
+  if (threadIdx.x == 0) gradient_outputs(a, row, r, o);
+}
+
+// A piece of a row per block, the statistics known: the caller's, or (a.stats = NULL) joined from the slices'.
+template <class E, bool ENT>
+__global__ __launch_bounds__(256) void k_gradient_apply(GradArgs a, Slices sl) {
+  constexpr int NV = 4;
+  typedef Held<E, 256, NV> H;
+  const uint32_t per = (a.vocab + H::SIZE - 1) / H::SIZE;
+  const uint64_t pieces = static_cast<uint64_t>(a.rows) * per;
+  const uint64_t p = block_number();
+  if (p >= pieces) return;
+  const uint32_t row = static_cast<uint32_t>(p / per), i0 = static_cast<uint32_t>(p % per) * H::SIZE, n = min(a.vocab - i0, H::SIZE);
+  H h;
+  h.load(static_cast<const E*>(a.z) + row * a.stride + i0, n);
+  RowStat r;
+  if (a.stats) { const float* s = a.stats + 4ull * row; r.m = s[0]; r.L = s[1]; r.H = s[2]; }
+  else r = row_stat<ENT>(joined<ENT>(sl, row, a.c * LOG2E));
+  const RowGradient o = row_gradient<ENT>(a, row, r);
+  h.template gradient<ENT>(static_cast<E*>(a.dz) + row * a.dstride + i0, o.f, o.t - i0, o.add,
+                           [&](float x) { if (a.logprob) a.logprob[row] = log_prob(r, x, a.c); });
+  if (threadIdx.x == 0 && i0 == 0) gradient_outputs(a, row, r, o);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -469,217 +782,345 @@ struct TeacherBox {
   uint32_t first[HASH_SIZE];       // where a class stands first
   int32_t index[TEACHER_MAX];      // -1: no entry
   float z[TEACHER_MAX];            // the student's logits there
-  float q[TEACHER_MAX];            // the teacher's probabilities
-  uint32_t bad;
-  float m, L, F, m_all, L_all;
+  float q[TEACHER_MAX], p[TEACHER_MAX];      // the teacher's and the student's probabilities
+  uint32_t bad, some;              // an index outside; whether the row teaches anything
+  double lse, sum_q;
+  float m, L, F, m_all;
+  double t_all;                    // sum of exp(c (z_i - m_all)) over the whole row
 };
+template <int TH> constexpr int entries_of() { return (TEACHER_MAX + TH - 1) / TH; }
 
-// The teacher's entries of a row: their classes, the student's logits there; entries that are none, and classes that stood earlier
-// in the row, have index -1.  Ends behind a barrier.
+// The teacher's entries of a row: their classes in the box; entries that are none, and classes that stood earlier in the row, have
+// index -1.  The student's logits there are on their way to x: teacher_logits() puts them into the box.  Ends behind a barrier.
+template <int TH>
+__device__ __forceinline__ void load_entries(const DistillArgs& a, uint32_t row, int32_t (&idx)[entries_of<TH>()]) {
+#pragma unroll
+  for (int j = 0; j < entries_of<TH>(); ++j) idx[j] = a.index[static_cast<uint64_t>(row) * a.K + min(threadIdx.x + j * TH, a.K - 1)];
+}
 template <class E, int TH>
-__device__ __forceinline__ void teacher_entries(const DistillArgs& a, uint32_t row, const E* z, TeacherBox& b) {
-  for (uint32_t i = threadIdx.x; i < HASH_SIZE; i += TH) { b.key[i] = -1; b.first[i] = 0xFFFFFFFFu; }
+__device__ __forceinline__ void teacher_entries(const DistillArgs& a, const E* z, TeacherBox& b, int32_t (&idx)[entries_of<TH>()],
+                                                E (&x)[entries_of<TH>()]) {
+  constexpr int M = entries_of<TH>();
+  uint32_t shift = 26;                                                // 4 slots per entry, 64 at least
+  while (1u << (32 - shift) < 4 * a.K) --shift;
+  const uint32_t slots = 1u << (32 - shift);
+  for (uint32_t i = threadIdx.x; i < slots; i += TH) { b.key[i] = -1; b.first[i] = 0xFFFFFFFFu; }
   if (threadIdx.x == 0) b.bad = 0;
-  __syncthreads();
-  constexpr uint32_t M = (TEACHER_MAX + TH - 1) / TH;
-  int32_t idx[M];
+  lds_barrier();
   uint32_t slot[M];
 #pragma unroll
-  for (uint32_t j = 0; j < M; ++j) {
+  for (int j = 0; j < M; ++j) {
     const uint32_t k = threadIdx.x + j * TH;
-    idx[j] = -1; slot[j] = 0;
-    if (k < a.K) {
-      const int32_t i = a.index[static_cast<uint64_t>(row) * a.K + k];
-      if (i >= 0 && static_cast<uint32_t>(i) >= a.vocab) b.bad = 1;
-      else if (i >= 0) {
-        idx[j] = i;
-        uint32_t s = (static_cast<uint32_t>(i) * 2654435761u) >> 22;
-        for (;;) {                                                    // at most TEACHER_MAX of the HASH_SIZE slots are taken
-          const int32_t old = atomicCAS(&b.key[s], -1, i);
-          if (old == -1 || old == i) break;
-          s = (s + 1) % HASH_SIZE;
-        }
-        slot[j] = s;
-        atomicMin(&b.first[s], k);
+    slot[j] = 0;
+    if (k >= a.K) idx[j] = -1;
+    if (idx[j] >= 0 && static_cast<uint32_t>(idx[j]) >= a.vocab) { b.bad = 1; idx[j] = -1; }
+    x[j] = z[max(idx[j], 0)];
+    if (idx[j] >= 0) {
+      uint32_t s = (static_cast<uint32_t>(idx[j]) * 2654435761u) >> shift;
+      for (;;) {                                                      // at most a quarter of the slots is taken
+        const int32_t old = atomicCAS(&b.key[s], -1, idx[j]);
+        if (old == -1 || old == idx[j]) break;
+        s = (s + 1) & (slots - 1);
       }
+      slot[j] = s;
+      atomicMin(&b.first[s], k);
     }
   }
-  __syncthreads();
+  lds_barrier();
 #pragma unroll
-  for (uint32_t j = 0; j < M; ++j) {
+  for (int j = 0; j < M; ++j) {
     const uint32_t k = threadIdx.x + j * TH;
-    if (k < a.K) {
-      const int32_t i = idx[j] >= 0 && b.first[slot[j]] == k ? idx[j] : -1;
-      b.index[k] = i;
-      b.z[k] = i >= 0 ? static_cast<float>(z[i]) : 0.0f;
-    }
+    if (k < a.K) b.index[k] = idx[j] >= 0 && b.first[slot[j]] == k ? idx[j] : -1;
   }
-  __syncthreads();
+  lds_barrier();
+}
+template <class E, int TH>
+__device__ __forceinline__ void teacher_logits(const DistillArgs& a, TeacherBox& b, const E (&x)[entries_of<TH>()]) {
+#pragma unroll
+  for (int j = 0; j < entries_of<TH>(); ++j) {
+    const uint32_t k = threadIdx.x + j * TH;
+    if (k < a.K) b.z[k] = static_cast<float>(x[j]);
+  }
 }
 
-// The statistics of the row without the teacher's classes: their places are marked in LDS, a span of the row at a time.
-template <class E, int TH>
-__device__ __forceinline__ Stat pass_rest(const E* z, uint32_t n, uint32_t K, float cl, const TeacherBox& b, uint32_t* mask) {
+// marks the classes of [i0, i0 + len) that are entries; index(k): entry k
+template <int TH, class F>
+__device__ __forceinline__ void mark(uint32_t* mask, uint32_t i0, uint32_t len, uint32_t K, F&& index) {
+  for (uint32_t i = threadIdx.x; i < len / 32 + 1; i += TH) mask[i] = 0;
+  lds_barrier();
+  for (uint32_t k = threadIdx.x; k < K; k += TH) {
+    const int32_t e = index(k);
+    const uint32_t i = static_cast<uint32_t>(e) - i0;                 // classes before the span are huge
+    if (e >= 0 && i < len) atomicOr(&mask[i / 32], 1u << i % 32);
+  }
+  lds_barrier();
+}
+template <int N>
+__device__ __forceinline__ uint32_t marks(const uint32_t* mask, uint32_t i) { return mask[i / 32] >> i % 32 & ((1u << N) - 1); }
+
+// The statistics of a row's slice without the teacher's classes, whose places are marked in LDS, a span of the slice at a time.
+template <class E, int TH, class F>
+__device__ __forceinline__ Stat pass_rest(const E* z, uint32_t i0, uint32_t n, uint32_t K, float cl, uint32_t* mask, F&& index) {
   constexpr int N = Elem<E>::N, U = 4;
   Stat o = stat_none();
   for (uint32_t s0 = 0; s0 < n; s0 += MASK_SPAN) {
     const uint32_t len = min(n - s0, MASK_SPAN);
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < (len + 31) / 32; i += TH) mask[i] = 0;
-    __syncthreads();
-    for (uint32_t k = threadIdx.x; k < K; k += TH) {
-      const uint32_t i = static_cast<uint32_t>(b.index[k]) - s0;      // -1 and classes before the span are huge
-      if (b.index[k] >= 0 && i < len) atomicOr(&mask[i / 32], 1u << i % 32);
-    }
-    __syncthreads();
+    if (s0) __syncthreads();
+    mark<TH>(mask, i0 + s0, len, K, index);
     walk<E, TH, U>(z + s0, len,
       [&](uint32_t v0, const raw4* r) {
         float v[U * N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          Elem<E>::unpack(r[u], v + u * N);
-          const uint32_t i = (v0 + u * TH) * N;
-          const uint32_t bits = i < len ? mask[i / 32] >> i % 32 & ((1u << N) - 1) : 0;
-          if (bits) {
-#pragma unroll
-            for (int q = 0; q < N; ++q) if (bits >> q & 1) v[u * N + q] = -INFINITY;
-          }
+          const uint32_t i = (v0 + u * TH) * N, bits = i < len ? marks<N>(mask, i) : 0;
+          raw4 x = r[u];
+          if (bits) Elem<E>::erase(x, bits);
+          Elem<E>::unpack(x, v + u * N);
         }
         take<false, U * N>(o, v, cl);
       },
-      [&](uint32_t i, float x) { if (!(mask[i / 32] >> i % 32 & 1)) take<false, 1>(o, &x, cl); });
+      [&](uint32_t i, float x) { if (!marks<1>(mask, i)) take<false, 1>(o, &x, cl); });
   }
   return o;
 }
 
-// By one wave: what the teacher's entries and the row's statistics `o` (of the whole row, or with `rest` of the classes outside)
-// make of the row.  In 64 bits: the loss is a difference of logarithms that nearly agree when the student is good, and there are
-// only K of them.  Leaves q, m, L, F (dz_i = c g F softmax_i over what `o` covers), m_all, L_all in the box; returns the loss.
-__device__ __forceinline__ float teach(const DistillArgs& a, uint32_t row, Stat o, bool from_stats, TeacherBox& b) {
-  constexpr int M = TEACHER_MAX / 64;
-  const bool rest = a.tlse != nullptr;
-  const double c = a.c;
-  double u[M], x[M];
-  bool has[M];
-  double umax = -INFINITY, zmax = -INFINITY;
-  bool some = false, nan = false;
-#pragma unroll
-  for (int j = 0; j < M; ++j) {
-    const uint32_t k = lane_id() + 64 * j;
-    has[j] = k < a.K && b.index[k] >= 0;
-    u[j] = has[j] ? static_cast<double>(a.value[static_cast<uint64_t>(row) * a.K + k]) * a.ct : -INFINITY;
-    x[j] = has[j] ? static_cast<double>(b.z[k]) : -INFINITY;
-    umax = fmax(umax, u[j]);
-    zmax = fmax(zmax, x[j]);
-    some |= has[j];
-    nan |= u[j] != u[j];
-  }
-  some = __any(some);
-  // the teacher's probabilities; without any mass (no entries, or all of them -inf) the row teaches nothing
-  double lse_t = 0.0;
-  if (rest) lse_t = a.tlse[row];
+// what lanes of a wave have written to LDS is there for its other lanes
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// What follows is one wave's, K entries at most four times its lanes, in 64 bits: the loss is a difference of logarithms that nearly agree
+// when the student is good.  The loops stay loops, to leave the registers to the row.
+
+// the teacher's probabilities; without any mass (no entries, or all of them -inf) and without the rest as a class the row teaches nothing
+template <bool REST>
+__device__ __forceinline__ void teacher_probabilities(const DistillArgs& a, uint32_t row, TeacherBox& b) {
+  const float* value = a.value + static_cast<uint64_t>(row) * a.K;
+  double lse = 0.0;
+  bool some = true;
+  if (REST) lse = a.tlse[row];
   else {
-    umax = wave_max_d(umax);
-    some = some && (umax > -INFINITY || __any(nan));
+    float most = -INFINITY;
+    bool any = false;
+#pragma unroll 1
+    for (uint32_t k = lane_id(); k < a.K; k += 64)
+      if (b.index[k] >= 0) { most = fmaxf(most, value[k]); any |= !(value[k] == -INFINITY); }
+    some = __any(any);                                                // (a NaN is not -inf)
+    const double top = static_cast<double>(wave_max_f(most)) * a.ct;
     double t = 0.0;
-#pragma unroll
-    for (int j = 0; j < M; ++j) if (has[j] && some) t += exp(u[j] - umax);
-    t = wave_sum_d(t);
-    lse_t = some ? umax + log(t) : 0.0;
+#pragma unroll 1
+    for (uint32_t k = lane_id(); k < a.K; k += 64)
+      if (b.index[k] >= 0 && some) t += exp(static_cast<double>(value[k]) * a.ct - top);
+    lse = top + log(wave_sum_d(t));
   }
-  double m_all, L_all, m_o = o.m, L_o = log(static_cast<double>(o.s));
-  if (from_stats) {
+  double sum_q = 0.0;
+#pragma unroll 1
+  for (uint32_t k = lane_id(); k < a.K; k += 64)
+    if (b.index[k] >= 0) {
+      const double q = some ? exp(static_cast<double>(value[k]) * a.ct - lse) : 0.0;
+      b.q[k] = static_cast<float>(q);
+      sum_q += q;
+    }
+  sum_q = wave_sum_d(sum_q);
+  if (lane_id() == 0) { b.lse = lse; b.sum_q = sum_q; b.some = some; }
+  wave_lds_fence();
+}
+
+// What the row's statistics `o` (of the whole row, or with REST of the classes outside) make of it: p, m, L, F (dz_i = c g F softmax_i
+// over what `o` covers), m_all, t_all.  Statistics that the caller kept (a.stats_in) take the place of `o`.
+template <bool REST>
+__device__ __forceinline__ void student_probabilities(const DistillArgs& a, uint32_t row, Stat o, TeacherBox& b) {
+  const double c = a.c;
+  double F = b.some ? 1.0 : 0.0, t = o.s;
+  float m_all = o.m, L = logf(o.s);
+  if (a.stats_in) {
     const float* s = a.stats_in + 8ull * row;
-    m_o = s[0]; L_o = s[1]; m_all = s[3]; L_all = s[4];
-  } else if (!rest) {
-    m_all = m_o; L_all = L_o;
-  } else {
-    zmax = wave_max_d(zmax);
-    m_all = fmax(zmax, m_o);
-    double t = 0.0;
-#pragma unroll
-    for (int j = 0; j < M; ++j) if (has[j]) t += exp((x[j] - m_all) * c);
-    t = wave_sum_d(t) + (o.s == 0.0f ? 0.0 : o.s * exp((m_o - m_all) * c));
-    L_all = log(t);
+    o.m = s[0]; L = s[1]; F = s[2]; m_all = s[3];
+    t = exp(static_cast<double>(s[4]));
+  } else if (REST) {
+    float most = -INFINITY;
+#pragma unroll 1
+    for (uint32_t k = lane_id(); k < a.K; k += 64) if (b.index[k] >= 0) most = fmaxf(most, b.z[k]);
+    m_all = fmaxf(wave_max_f(most), o.m);
+    double inside = 0.0;
+#pragma unroll 1
+    for (uint32_t k = lane_id(); k < a.K; k += 64) if (b.index[k] >= 0) inside += exp((static_cast<double>(b.z[k]) - m_all) * c);
+    inside = wave_sum_d(inside);
+    const double outside = o.s == 0.0f ? 0.0 : o.s * exp((static_cast<double>(o.m) - m_all) * c);
+    t = inside + outside;
+    F = outside / t - fmax(1.0 - b.sum_q, 0.0);
+    if (o.s == 0.0f) F = 0.0;                                         // nothing outside: the rest is left out
+    if (b.sum_q != b.sum_q) F = NAN;
   }
-  const bool empty = L_all == -INFINITY;
-  double loss = 0.0, sum_q = 0.0, sum_p = 0.0;
-#pragma unroll
-  for (int j = 0; j < M; ++j) {
-    if (!has[j]) continue;
-    const double lq = u[j] - lse_t, q = some ? exp(lq) : 0.0;
-    const double lp = empty || x[j] == -INFINITY ? (L_all == L_all ? -INFINITY : NAN) : (x[j] - m_all) * c - L_all;
-    if (!(q == 0.0)) loss += q * (lq - lp);
-    sum_q += q;
-    sum_p += exp(lp);
-    b.q[lane_id() + 64 * j] = static_cast<float>(q);
-  }
-  double F = some ? 1.0 : 0.0;
-  if (rest && !from_stats) {
-    sum_q = wave_sum_d(sum_q); sum_p = wave_sum_d(sum_p);
-    const double left = fmax(1.0 - sum_q, 0.0);
-    F = 0.0;
-    if (L_o != -INFINITY) {                                           // nothing outside: the rest is left out
-      // the student's rest: from what is inside where that is the smaller part
-      const double lp = sum_p < 0.5 ? log1p(-sum_p) : (m_o - m_all) * c + L_o - L_all;
-      if (!(left == 0.0) && lane_id() == 0) loss += left * (log1p(-sum_q) - lp);
-      F = exp(lp) - left;
-      if (sum_q != sum_q) F = NAN;
+#pragma unroll 1
+  for (uint32_t k = lane_id(); k < a.K; k += 64)
+    if (b.index[k] >= 0) b.p[k] = t == 0.0 ? 0.0f : static_cast<float>(exp((static_cast<double>(b.z[k]) - m_all) * c) / t);
+  if (t == 0.0) F = 0.0;                                              // a row that leaves nothing
+  if (b.bad) F = NAN;
+  if (lane_id() == 0) { b.m = o.m; b.L = L; b.F = static_cast<float>(F); b.m_all = m_all; b.t_all = t; }
+  wave_lds_fence();
+}
+
+template <bool REST>
+__device__ __forceinline__ float distill_loss(const DistillArgs& a, uint32_t row, Stat o, const TeacherBox& b) {
+  const float* value = a.value + static_cast<uint64_t>(row) * a.K;
+  const double c = a.c, m_all = b.m_all, t = b.t_all, L = log(t);
+  double loss = 0.0;
+  if (REST || b.some) {
+#pragma unroll 1
+    for (uint32_t k = lane_id(); k < a.K; k += 64) {
+      if (b.index[k] < 0 || b.q[k] == 0.0f) continue;
+      const double x = b.z[k], lp = t == t && x == -INFINITY ? -INFINITY : (x - m_all) * c - L;
+      loss += b.q[k] * (static_cast<double>(value[k]) * a.ct - b.lse - lp);
     }
   }
   loss = wave_sum_d(loss);
-  if (!from_stats && !rest && !some) loss = 0.0;
-  if (b.bad) { loss = NAN; F = NAN; }
-  if (lane_id() == 0) {
-    b.m = static_cast<float>(m_o); b.L = static_cast<float>(L_o);
-    b.m_all = static_cast<float>(m_all); b.L_all = static_cast<float>(L_all);
-    b.F = from_stats ? a.stats_in[8ull * row + 2] : static_cast<float>(F);
-    if (empty) { b.F = b.bad ? NAN : 0.0f; }
+  const double left = fmax(1.0 - b.sum_q, 0.0);
+  if (REST && o.s != 0.0f && left != 0.0) {
+    // what the student leaves over: from what is inside where that is the smaller part
+    const double outside = o.s * exp((o.m - m_all) * c) / t;
+    const double lp = outside > 0.5 ? log(outside) : (o.m - m_all) * c + log(o.s / t);
+    loss += left * (log1p(-b.sum_q) - lp);
   }
-  return static_cast<float>(loss);
+  return b.bad ? NAN : static_cast<float>(loss);
 }
 
-// GRAD: the gradient too.  REST: what the teacher's entries leave over is one more class.
-template <class E, int TH, bool REST, bool GRAD>
-__global__ __launch_bounds__(TH) void k_distill(DistillArgs a) {
+// the gradient in an entry's class
+template <bool REST>
+__device__ __forceinline__ float taught(const TeacherBox& b, uint32_t k, float g) {
+  if (b.bad) return NAN;
+  if (b.t_all == 0.0 || (!REST && !b.some)) return 0.0f;               // a row that leaves nothing, or teaches nothing
+  return g * (b.p[k] - b.q[k]);
+}
+
+__device__ __forceinline__ void distill_outputs(const DistillArgs& a, uint32_t row, const TeacherBox& b, float loss) {
+  if (a.loss) a.loss[row] = loss;
+  if (a.stats) {
+    float* s = a.stats + 8ull * row;
+    s[0] = b.m; s[1] = b.L; s[2] = b.F; s[3] = b.m_all; s[4] = static_cast<float>(log(b.t_all)); s[5] = s[6] = s[7] = 0.0f;
+  }
+}
+
+// A block per row, held in its registers.  REST: what the teacher's entries leave over is one more class.
+template <class E, int TH, int NV, bool REST>
+__global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
+  typedef Held<E, TH, NV> H;
   __shared__ Stat box[16];
   __shared__ TeacherBox b;
+  __shared__ uint32_t mask[REST ? H::SIZE / 32 + 1 : 1];
+  const float cl = a.c * LOG2E;
+  const uint64_t row = block_number();
+  if (row >= a.rows) return;
+  const E* z = static_cast<const E*>(a.z) + row * a.stride;
+  int32_t idx[entries_of<TH>()];
+  load_entries<TH>(a, row, idx);                                      // first: they come back first
+  H h;
+  h.load(z, a.vocab);
+  E x[entries_of<TH>()];
+  teacher_entries<E, TH>(a, z, b, idx, x);
+  if (threadIdx.x < 64) teacher_probabilities<REST>(a, row, b);     // while the row is on its way
+  Stat o = stat_none();
+  if (!a.stats_in) {
+    if (REST) mark<TH>(mask, 0, a.vocab, a.K, [&](uint32_t k) { return b.index[k]; });
+    o = h.template stat<false>(cl, [&](uint32_t i) { return REST ? marks<H::N>(mask, i) : 0u; });
+  }
+  teacher_logits<E, TH>(a, b, x);
+  o = block_stat<false, TH>(o, cl, box);
+  if (TH == 64) __syncthreads();
+  if (threadIdx.x < 64) student_probabilities<REST>(a, row, o, b);
+  __syncthreads();
+  if (threadIdx.x < 64 && !a.stats_in) {
+    const float loss = distill_loss<REST>(a, row, o, b);
+    if (threadIdx.x == 0) distill_outputs(a, row, b, loss);
+  }
+  if (a.dz) {
+    E* dz = static_cast<E*>(a.dz) + row * a.dstride;
+    const float g = a.c * (a.g ? a.g[row] : 1.0f), L = b.L;
+    h.template gradient<false>(dz, Gradient{cl, b.m, L == -INFINITY ? 0.0f : L * LOG2E, g * b.F, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
+    __syncthreads();                                                // the entries' classes are written again
+    for (uint32_t k = threadIdx.x; k < a.K; k += TH)
+      if (b.index[k] >= 0) dz[b.index[k]] = static_cast<E>(taught<REST>(b, k, g));
+  }
+}
+
+// Rows split into slices: their statistics; what the teacher makes of a row; the gradient, a piece of a row per block.
+template <class E, bool REST>
+__global__ __launch_bounds__(256) void k_distill_slices(DistillArgs a, Slices sl) {
+  __shared__ Stat box[4];
   extern __shared__ uint32_t mask[];
   const float cl = a.c * LOG2E;
-  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const E* z = static_cast<const E*>(a.z) + row * a.stride;
-    teacher_entries<E, TH>(a, row, z, b);
-    Stat o = stat_none();
-    const bool from_stats = GRAD && a.stats_in;
-    if (!from_stats) {
-      o = REST ? pass_rest<E, TH>(z, a.vocab, a.K, cl, b, mask) : pass_stat<E, TH, false>(z, a.vocab, cl);
-      o = block_stat<false, TH>(o, cl, box);
+  const uint64_t pieces = static_cast<uint64_t>(a.rows) * sl.S;
+  const uint64_t p = block_number();
+  if (p >= pieces) return;
+  const uint32_t row = static_cast<uint32_t>(p / sl.S), i0 = static_cast<uint32_t>(p % sl.S) * sl.len, n = min(a.vocab - i0, sl.len);
+  const E* z = static_cast<const E*>(a.z) + row * a.stride + i0;
+  const int32_t* index = a.index + static_cast<uint64_t>(row) * a.K;
+  Stat o = REST ? pass_rest<E, 256>(z, i0, n, a.K, cl, mask, [&](uint32_t k) { return index[k]; }) : pass_stat<E, 256, false>(z, n, cl);
+  o = block_stat<false, 256>(o, cl, box);
+  if (threadIdx.x == 0) sl.part[p] = Stat4{o.m, o.s, o.w, 0.0f};
+}
+
+struct Taught {                            // what k_distill_join leaves for k_distill_apply
+  Stat4* row;                              // [rows] m, L log2(e), A of Gradient
+  int32_t* index;                          // [rows, K] classes, -1: none
+  float* value;                            // [rows, K] the gradient there
+};
+
+template <class E, bool REST>
+__global__ __launch_bounds__(256) void k_distill_join(DistillArgs a, Slices sl, Taught w) {
+  __shared__ TeacherBox b;
+  const float cl = a.c * LOG2E;
+  const uint64_t row = block_number();
+  if (row >= a.rows) return;
+  int32_t idx[1];
+  load_entries<256>(a, row, idx);
+  E x[1];
+  teacher_entries<E, 256>(a, static_cast<const E*>(a.z) + row * a.stride, b, idx, x);
+  teacher_logits<E, 256>(a, b, x);
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const Stat o = a.stats_in ? stat_none() : joined<false>(sl, row, cl);
+    teacher_probabilities<REST>(a, row, b);
+    student_probabilities<REST>(a, row, o, b);
+    if (!a.stats_in) {
+      const float loss = distill_loss<REST>(a, row, o, b);
+      if (threadIdx.x == 0) distill_outputs(a, row, b, loss);
     }
-    if (threadIdx.x < 64) {
-      const float loss = teach(a, row, o, from_stats, b);
-      if (threadIdx.x == 0) {
-        if (a.loss) a.loss[row] = loss;
-        if (!GRAD && a.stats) {
-          float* s = a.stats + 8ull * row;
-          s[0] = b.m; s[1] = b.L; s[2] = b.F; s[3] = b.m_all; s[4] = b.L_all; s[5] = s[6] = s[7] = 0.0f;
-        }
-      }
+  }
+  __syncthreads();
+  if (w.row) {
+    const float g = a.c * (a.g ? a.g[row] : 1.0f), L = b.L;
+    if (threadIdx.x == 0) w.row[row] = Stat4{b.m, L == -INFINITY ? 0.0f : L * LOG2E, g * b.F, 0.0f};
+    const uint32_t k = threadIdx.x;
+    if (k < a.K) {
+      w.index[static_cast<uint64_t>(row) * a.K + k] = b.index[k];
+      w.value[static_cast<uint64_t>(row) * a.K + k] = b.index[k] >= 0 ? taught<REST>(b, k, g) : 0.0f;
     }
-    __syncthreads();
-    if (GRAD) {
-      E* dz = static_cast<E*>(a.dz) + row * a.dstride;
-      const float g = a.c * (a.g ? a.g[row] : 1.0f), L = b.L, L_all = b.L_all, m_all = b.m_all, F = b.F;
-      pass_gradient<E, TH, false>(z, dz, a.vocab, cl, b.m, L == -INFINITY ? 0.0f : L * LOG2E, g * F, 0.0f);
-      __syncthreads();
-      for (uint32_t k = threadIdx.x; k < a.K; k += TH) {
-        const int32_t i = b.index[k];
-        if (i < 0) continue;
-        const float p = L_all == -INFINITY ? 0.0f : expf((b.z[k] - m_all) * a.c - L_all), q = b.q[k];
-        const bool none = L_all == -INFINITY || (!REST && F == 0.0f);
-        dz[i] = static_cast<E>(b.bad ? NAN : none ? 0.0f : g * (p - q));
-      }
-    }
-    __syncthreads();
+  }
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void k_distill_apply(DistillArgs a, Taught w) {
+  constexpr int NV = 4;
+  typedef Held<E, 256, NV> H;
+  const uint32_t per = (a.vocab + H::SIZE - 1) / H::SIZE;
+  const uint64_t pieces = static_cast<uint64_t>(a.rows) * per;
+  const uint64_t p = block_number();
+  if (p >= pieces) return;
+  const uint32_t row = static_cast<uint32_t>(p / per), i0 = static_cast<uint32_t>(p % per) * H::SIZE, n = min(a.vocab - i0, H::SIZE);
+  E* dz = static_cast<E*>(a.dz) + row * a.dstride + i0;
+  H h;
+  h.load(static_cast<const E*>(a.z) + row * a.stride + i0, n);
+  const Stat4 r = w.row[row];
+  h.template gradient<false>(dz, Gradient{a.c * LOG2E, r.m, r.s, r.w, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
+  __syncthreads();
+  const uint32_t k = threadIdx.x;
+  if (k < a.K) {
+    const int32_t e = w.index[static_cast<uint64_t>(row) * a.K + k];
+    const uint32_t i = static_cast<uint32_t>(e) - i0;
+    if (e >= 0 && i < n) dz[i] = static_cast<E>(w.value[static_cast<uint64_t>(row) * a.K + k]);
   }
 }
 

@@ -261,7 +261,7 @@ def test_offsets_beyond_32_bits(B):
     torch.cuda.empty_cache()
 
 
-@pytest.mark.parametrize("N,V", [(70000, 3), (3000, 257), (1500, 4096)])
+@pytest.mark.parametrize("N,V", [(1_100_000, 2), (70000, 3), (3000, 257), (1500, 4096)])
 def test_many_rows(B, N, V):
     z, t = logits_of(N, V, torch.bfloat16), targets_of(N, V)
     check_score(z, t, min(V, 4), 1.0, run_score(B, z, t, min(V, 4), 1.0), f"{N} x {V}")
