@@ -245,8 +245,9 @@ qsl_status qsl_timing_read(qsl_ctx *ctx, double *total_ms, uint32_t *launches);
  *     arrays and `workspace`, which belongs to one call at a time (two captured graphs that may run side by side need one each).
  *     They enqueue kernels on `hip_stream` (NULL = the default stream) of the current HIP device, whose memory all device
  *     pointers are, and can be captured into a graph.
- *   - All arithmetic is in 32 bits or more, whatever the type of the logits; a gradient is rounded to that type once.  Results do not
- *     depend on anything but the inputs: no atomics decide an order of additions.
+ *   - All arithmetic is in 32 bits or more, whatever the type of the logits; a gradient is rounded to that type once.  The
+ *     same call on the same layout of memory gives the same bits: no atomics decide an order of additions.  Between layouts (rows that
+ *     begin at odd places, another stride) the sums may be rounded differently; alternatives are the same.
  *   - A logit of -inf is a class left out: its probability and gradient are 0, its log probability -inf.  A row of nothing else has
  *     lse and log probabilities -inf, entropy 0 and gradient 0.  A NaN or +inf makes the row's results NaN (indices: -1).
  *   - rows = 0 does nothing.  What lies between two rows (stride > vocab) is neither read nor written.

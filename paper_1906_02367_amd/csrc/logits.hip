@@ -67,19 +67,29 @@ template <int V> using Int = std::integral_constant<int, V>;
 
 constexpr uint64_t KB = 1024;
 constexpr uint64_t HELD_MAX = 256 * KB;            // bytes of a row that 1024 threads hold in registers, 16 vectors each
-constexpr uint64_t HELD_TOP_MAX = 64 * KB;         // ... that 256 threads hold
+constexpr uint64_t HELD_TOP_MAX = 128 * KB;        // ... from which alternatives are taken
+constexpr uint64_t SLICE_MAX = 64 * KB;            // ... that 256 threads hold
 
 uint64_t row_bytes(const qsl_logits* z) { return static_cast<uint64_t>(z->vocab) * elem_size(z->dtype); }
 
-// f(threads, vectors a thread holds) for rows of at most HELD_MAX bytes (and the values behind their last vector)
+enum HeldFor { FOR_GRADIENT, FOR_TEACHER, FOR_TOP };
+
+// f(threads, vectors a thread holds) for rows of at most HELD_MAX bytes (and the values behind their last vector).  Where a row can be
+// held by few threads with many vectors or by many with few: many have the shorter way from the first load to the last store, few
+// leave room for other rows while a row is being ranked or a teacher's entries are worked out by one wave.  us, 8,192 rows of 64 KB:
+// gradient 256 x 16 200, 512 x 8 195, 1024 x 4 185; a teacher's 64 entries 214 / 201 / 194; 4,096 rows, 20 alternatives 50 / 53 / 70.  Rows of
+// 128 KB: gradient (4,000 rows) 512 x 16 193, 1024 x 8 192; entries (2,000) 121 / 164; alternatives (4,096) 99 / 148.
 template <class F>
-void pick_held(uint64_t nvec, F&& f) {
+void pick_held(uint64_t nvec, uint64_t rows, HeldFor what, F&& f) {
+  const bool few = rows < FEW_ROWS;                                    // nothing to make room for
   if (nvec <= 64) f(Int<64>(), Int<1>());
   else if (nvec <= 64 * 4) f(Int<64>(), Int<4>());
   else if (nvec <= 256 * 4) f(Int<256>(), Int<4>());
-  else if (nvec <= 256 * 8) f(Int<256>(), Int<8>());
+  else if (nvec <= 256 * 8 && !few) f(Int<256>(), Int<8>());
+  else if (nvec <= 1024 * 4 && (few || what != FOR_TOP)) f(Int<1024>(), Int<4>());
   else if (nvec <= 256 * 16) f(Int<256>(), Int<16>());
-  else if (nvec <= 1024 * 8) f(Int<1024>(), Int<8>());
+  else if (nvec <= 1024 * 8 && (few || what == FOR_GRADIENT)) f(Int<1024>(), Int<8>());
+  else if (nvec <= 512 * 16) f(Int<512>(), Int<16>());
   else f(Int<1024>(), Int<16>());
 }
 
@@ -89,32 +99,34 @@ struct Plan {
   uint32_t S, len;
 };
 
-Plan plan_slices(const qsl_logits* z, uint64_t most_bytes) {
+Plan plan_slices(const qsl_logits* z) {
   const uint64_t bytes = row_bytes(z), es = elem_size(z->dtype);
-  uint64_t S = std::max<uint64_t>((bytes + most_bytes - 1) / most_bytes, WANTED_BLOCKS / std::max(z->rows, 1u));
+  uint64_t S = std::max<uint64_t>((bytes + SLICE_MAX - 1) / SLICE_MAX, WANTED_BLOCKS / std::max(z->rows, 1u));
   S = std::min<uint64_t>({S, SLICES_MAX, (bytes + MIN_SLICE - 1) / MIN_SLICE});
   Plan p;
-  p.split = S > 1;
+  p.split = true;
   // whole 4 KB: slices start where vectors do, and their threads are busy alike
   p.len = static_cast<uint32_t>(align_up((z->vocab + S - 1) / S, 4 * KB / es));
   p.S = (z->vocab + p.len - 1) / p.len;
   return p;
 }
 
-// Alternatives: in a block's registers, or a slice of the row in each; rows of more than 64 slices are walked along.
+constexpr Plan WHOLE = {false, 0, 0};
+
+// Alternatives: rows of up to 128 KB by one block each, longer ones in slices (rows of more than 64 slices are walked along).  us, a block of
+// 1024 x 16 / slices: 2,048 rows of 200 KB, 64 alternatives 111 / 95; 2,048 of 256 KB, 20 alternatives 122 / 96; 64 of 256 KB 16 / 15.
 Plan plan_top(const qsl_logits* z) {
   const uint64_t bytes = row_bytes(z);
-  if (bytes > SLICES_MAX * HELD_TOP_MAX || (bytes <= HELD_TOP_MAX && (z->rows >= FEW_ROWS || bytes <= 4 * MIN_SLICE))) return Plan{false, 0, 0};
-  return plan_slices(z, HELD_TOP_MAX);
+  return bytes <= HELD_TOP_MAX || bytes > SLICES_MAX * SLICE_MAX ? WHOLE : plan_slices(z);
 }
-// Statistics alone (no alternatives), and the gradients: split where there are few rows.
-Plan plan_few(const qsl_logits* z) {
-  const uint64_t bytes = row_bytes(z);
-  if (z->rows >= FEW_ROWS || bytes <= 4 * MIN_SLICE) return Plan{false, 0, 0};
-  return plan_slices(z, bytes);
-}
+// Statistics alone: a row need not be held.  Split where long rows are fewer than the blocks that are resident at once (300 rows of 800 KB: 54 us
+// by a block each, 45 split).
+Plan plan_stats(const qsl_logits* z) { return z->rows < 2 * FEW_ROWS && row_bytes(z) > HELD_MAX ? plan_slices(z) : WHOLE; }
+// Gradients: rows that a block does not hold, and long rows that are few, read twice but by all compute units (64 rows of 256 KB: 18 us
+// by a block each, 13 split; 200 rows: 26 and 32; 16 rows of 128 KB: 9 and 13).
 Plan plan_gradient(const qsl_logits* z) {
-  return row_bytes(z) > HELD_MAX ? plan_slices(z, HELD_MAX) : plan_few(z);
+  const uint64_t bytes = row_bytes(z);
+  return bytes > HELD_MAX || (bytes > HELD_MAX / 2 && z->rows < FEW_ROWS / 2) ? plan_slices(z) : WHOLE;
 }
 
 struct Workspace {
@@ -159,7 +171,7 @@ qsl_status launched() { return hipGetLastError() == hipSuccess ? QSL_OK : QSL_ER
 
 extern "C" size_t qsl_logits_workspace_bytes(const qsl_logits* z, uint32_t top) {
   if (!logits_ok(z) || z->rows == 0 || top > std::max(QSL_TOP_MAX, QSL_TEACHER_MAX)) return 0;
-  uint64_t need = std::max(lay_out(z, plan_few(z), 0, 0, nullptr).need, lay_out(z, plan_gradient(z), 0, top, nullptr).need);
+  uint64_t need = std::max(lay_out(z, plan_stats(z), 0, 0, nullptr).need, lay_out(z, plan_gradient(z), 0, top, nullptr).need);
   if (top) need = std::max(need, lay_out(z, plan_top(z), top, 0, nullptr).need);
   return need;
 }
@@ -179,7 +191,7 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
   if (st != QSL_OK) return st;
   const ScoreArgs a = {z->data, z->stride, z->rows, z->vocab, top, z->scale, target, logprob, entropy, lse, top_index, top_logprob, stats};
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const Plan plan = top ? plan_top(z) : plan_few(z);
+  const Plan plan = top ? plan_top(z) : plan_stats(z);
   const Slices sl = lay_out(z, plan, top, 0, workspace).sl;
   const dim3 rows = grid_of(z->rows);
   pick_type(z, [&](auto e) {
@@ -191,11 +203,12 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
         const uint32_t held = (plan.len / Elem<E>::N + 255) / 256;
         if (!top) k_slice_stats<E, 0, ent()><<<grid, 256, 0, stream>>>(a, sl);
         else if (held <= 4) k_slice_stats<E, 4, ent()><<<grid, 256, 0, stream>>>(a, sl);
+        else if (held <= 8) k_slice_stats<E, 8, ent()><<<grid, 256, 0, stream>>>(a, sl);
         else k_slice_stats<E, 16, ent()><<<grid, 256, 0, stream>>>(a, sl);
         k_score_join<E, ent()><<<rows, 256, 0, stream>>>(a, sl);
       } else if (top && row_bytes(z) <= HELD_TOP_MAX) {
-        pick_held(top > 64 ? std::max(nvec, 64 * 4 + 1u) : nvec, [&](auto th, auto nv) {
-          if constexpr (th() <= 256) k_score_held<E, th(), nv(), ent()><<<rows, th(), 0, stream>>>(a);
+        pick_held(top > 64 ? std::max(nvec, 64 * 4 + 1u) : nvec, z->rows, FOR_TOP, [&](auto th, auto nv) {
+          if constexpr (th() * nv() <= 8192) k_score_held<E, th(), nv(), ent()><<<rows, th(), 0, stream>>>(a);
         });
       } else if (top) {
         k_score<E, 1024, ent(), true><<<rows, 1024, 0, stream>>>(a);
@@ -231,7 +244,7 @@ extern "C" qsl_status qsl_token_logprobs_backward(const qsl_logits* z, const int
     typedef decltype(e) E;
     pick_bool(grad_entropy || entropy, [&](auto ent) {
       if (!stats && !plan.split) {
-        pick_held(z->vocab / Elem<E>::N, [&](auto th, auto nv) { k_gradient_held<E, th(), nv(), ent()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
+        pick_held(z->vocab / Elem<E>::N, z->rows, FOR_GRADIENT, [&](auto th, auto nv) { k_gradient_held<E, th(), nv(), ent()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
         return;
       }
       if (!stats) {
@@ -257,11 +270,11 @@ static qsl_status launch_distill(const qsl_logits* z, const qsl_teacher* t, cons
     typedef decltype(e) E;
     pick_bool(t->lse != nullptr, [&](auto rest) {
       if (!plan.split) {
-        pick_held(z->vocab / Elem<E>::N, [&](auto th, auto nv) { k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
+        pick_held(z->vocab / Elem<E>::N, z->rows, FOR_TEACHER, [&](auto th, auto nv) { k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
         return;
       }
       if (!a.stats_in) {
-        const uint32_t lds = rest() ? 4 * (std::min(plan.len, MASK_SPAN) / 32 + 1) : 0;
+        const uint32_t lds = rest() ? 4 * mask_words(std::min(plan.len, MASK_SPAN)) : 0;
         k_distill_slices<E, rest()><<<grid_of(static_cast<uint64_t>(z->rows) * plan.S), 256, lds, stream>>>(a, ws.sl);
       }
       k_distill_join<E, rest()><<<grid_of(z->rows), 256, 0, stream>>>(a, ws.sl, w);

@@ -35,7 +35,8 @@ constexpr uint32_t HASH_SIZE = 4 * TEACHER_MAX;   // slots in which a teacher's 
 constexpr uint32_t MASK_SPAN = 1u << 18;   // classes whose membership in the teacher's entries is held in LDS at once (32 KB)
 
 // ---------------------------------------------------------------------------------------------
-// elements: 16 bytes at a time, aligned to the element only (rows of an odd length start anywhere)
+// elements: 16 bytes at a time, aligned to 4 bytes where reading (a row of 16-bit values may start between two words: its first value
+// is then taken by itself; read at odd places, 4,096 rows of 128,001 take 211 us instead of 171), to the element where writing
 // ---------------------------------------------------------------------------------------------
 typedef uint32_t raw_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t raw_a2 __attribute__((ext_vector_type(4), aligned(2)));
@@ -44,17 +45,15 @@ typedef uint32_t raw4 __attribute__((ext_vector_type(4)));
 template <class E> struct Elem;
 template <> struct Elem<float> {
   static constexpr int N = 4;
+  typedef uint32_t bits;
+  static __device__ __forceinline__ float from_bits(uint32_t b) { return __uint_as_float(b); }
   static constexpr uint32_t MINUS_INF = 0xFF800000u;
   typedef raw_a4 mem;
   static __device__ __forceinline__ void unpack(raw4 r, float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
   }
-  static __device__ __forceinline__ float value(raw4 r, uint32_t q) {
-    const uint32_t w = q;
-    const uint32_t lo = w & 1 ? r[1] : r[0], hi = w & 1 ? r[3] : r[2], x = w & 2 ? hi : lo;
-    return __uint_as_float(x);
-  }
+  static __device__ __forceinline__ float of_word(uint32_t x, uint32_t q) { (void)q; return __uint_as_float(x); }      // value q from its word
   static __device__ __forceinline__ void erase(raw4& r, uint32_t bits) {      // -inf where a bit is set
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = bits >> i & 1 ? MINUS_INF : r[i];
@@ -68,17 +67,15 @@ template <> struct Elem<float> {
 };
 template <> struct Elem<__bf16> {
   static constexpr int N = 8;
+  typedef uint16_t bits;
+  static __device__ __forceinline__ float from_bits(uint32_t b) { return __uint_as_float(b << 16); }
   static constexpr uint32_t MINUS_INF = 0xFF80FF80u;
   typedef raw_a2 mem;
   static __device__ __forceinline__ void unpack(raw4 r, float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(r[i] << 16); v[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u); }
   }
-  static __device__ __forceinline__ float value(raw4 r, uint32_t q) {
-    const uint32_t w = q >> 1;
-    const uint32_t lo = w & 1 ? r[1] : r[0], hi = w & 1 ? r[3] : r[2], x = w & 2 ? hi : lo;
-    return __uint_as_float(q & 1 ? x & 0xFFFF0000u : x << 16);
-  }
+  static __device__ __forceinline__ float of_word(uint32_t x, uint32_t q) { (void)q; return __uint_as_float(q & 1 ? x & 0xFFFF0000u : x << 16); }      // value q from its word
   static __device__ __forceinline__ void erase(raw4& r, uint32_t bits) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -96,6 +93,8 @@ template <> struct Elem<__bf16> {
 };
 template <> struct Elem<_Float16> {
   static constexpr int N = 8;
+  typedef uint16_t bits;
+  static __device__ __forceinline__ float from_bits(uint32_t b) { return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(b))); }
   static constexpr uint32_t MINUS_INF = 0xFC00FC00u;
   typedef raw_a2 mem;
   static __device__ __forceinline__ void unpack(raw4 r, float* v) {
@@ -103,11 +102,7 @@ template <> struct Elem<_Float16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { const h2 x = __builtin_bit_cast(h2, static_cast<uint32_t>(r[i])); v[2 * i] = static_cast<float>(x[0]); v[2 * i + 1] = static_cast<float>(x[1]); }
   }
-  static __device__ __forceinline__ float value(raw4 r, uint32_t q) {
-    const uint32_t w = q >> 1;
-    const uint32_t lo = w & 1 ? r[1] : r[0], hi = w & 1 ? r[3] : r[2], x = w & 2 ? hi : lo;
-    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(q & 1 ? x >> 16 : x)));
-  }
+  static __device__ __forceinline__ float of_word(uint32_t x, uint32_t q) { (void)q; return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(q & 1 ? x >> 16 : x))); }      // value q from its word
   static __device__ __forceinline__ void erase(raw4& r, uint32_t bits) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -124,6 +119,8 @@ template <> struct Elem<_Float16> {
   }
 };
 
+// values before the first whole word
+template <class E> __device__ __forceinline__ uint32_t odd_ones(const E* z) { return sizeof(E) == 2 && (reinterpret_cast<uintptr_t>(z) & 2) ? 1 : 0; }
 template <class E> __device__ __forceinline__ raw4 load16(const E* p) { return *reinterpret_cast<const typename Elem<E>::mem*>(p); }
 template <class E> __device__ __forceinline__ void store16(E* p, raw4 r) { *reinterpret_cast<typename Elem<E>::mem*>(p) = r; }
 
@@ -136,9 +133,9 @@ struct __align__(16) Stat4 { float m, s, w, pad; };
 __device__ __forceinline__ Stat stat_none() { return Stat{LOWEST, 0.0f, 0.0f}; }
 __device__ __forceinline__ float exp2_(float y) { return __builtin_amdgcn_exp2f(y); }
 
-// takes n values in; -inf adds nothing, NaN and +inf make s NaN
+// takes n values in and returns the largest; -inf adds nothing, NaN and +inf make s NaN
 template <bool ENT, int N>
-__device__ __forceinline__ void take(Stat& o, const float* v, float cl) {
+__device__ __forceinline__ float take(Stat& o, const float* v, float cl) {
   float vm = v[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) vm = fmaxf(vm, v[i]);
@@ -152,6 +149,7 @@ __device__ __forceinline__ void take(Stat& o, const float* v, float cl) {
     o.s += e;
     if (ENT) o.w = __builtin_fmaf(e, fmaxf(y, Y_MIN), o.w);
   }
+  return vm;
 }
 
 template <int CTRL, int ROWS>
@@ -234,22 +232,23 @@ __device__ __forceinline__ RowStat row_stat(Stat o) {
 // ---------------------------------------------------------------------------------------------
 // walking along a row: U loads of 16 bytes of a thread are under way at a time
 // ---------------------------------------------------------------------------------------------
-// f(first index, N values): vectors that lie wholly in the row; then at most one call for the thread's single value behind them
+// whole(v, r): the thread's vectors v, v + TH, ...; vector v begins at value first + v N, those from nvec on hold -inf.  Then at most one call
+// single(index, value) for the thread's value before or behind the vectors.
 template <class E, int TH, int U, class F, class G>
-__device__ __forceinline__ void walk(const E* z, uint32_t n, F&& whole, G&& single) {
+__device__ __forceinline__ void walk(const E* z, uint32_t n, uint32_t first, F&& whole, G&& single) {
   constexpr int N = Elem<E>::N;
-  const uint32_t nvec = n / N;
+  const uint32_t nvec = (n - first) / N;
   for (uint32_t v0 = threadIdx.x; v0 < nvec; v0 += TH * U) {
     raw4 r[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       r[u] = raw4{Elem<E>::MINUS_INF, Elem<E>::MINUS_INF, Elem<E>::MINUS_INF, Elem<E>::MINUS_INF};
       const uint32_t v = v0 + u * TH;
-      if (v < nvec) r[u] = load16(z + static_cast<uint64_t>(v) * N);
+      if (v < nvec) r[u] = load16(z + first + static_cast<uint64_t>(v) * N);
     }
     whole(v0, r);
   }
-  const uint32_t i = nvec * N + threadIdx.x;
+  const uint32_t i = threadIdx.x < first ? threadIdx.x : nvec * N + threadIdx.x;
   if (i < n) single(i, static_cast<float>(z[i]));
 }
 
@@ -257,7 +256,7 @@ template <class E, int TH, bool ENT>
 __device__ __forceinline__ Stat pass_stat(const E* z, uint32_t n, float cl) {
   constexpr int N = Elem<E>::N, U = 4;
   Stat o = stat_none();
-  walk<E, TH, U>(z, n,
+  walk<E, TH, U>(z, n, odd_ones(z),
     [&](uint32_t, const raw4* r) {
       float v[U * N];
 #pragma unroll
@@ -276,6 +275,8 @@ __device__ __forceinline__ float gradient_value(const Gradient& f, float x) {
   return ENT ? p * __builtin_fmaf(f.B, fmaxf(y, Y_MIN), f.A) : p * f.A;
 }
 
+struct NoneOut { __device__ __forceinline__ uint32_t operator()(uint32_t) const { return 0; } };
+
 // A piece of a row that the block holds in registers, NV vectors a thread and the values behind the last whole vector one a thread: it
 // is read from memory once, whatever is made of it.  load() only starts the loads; loads past the end go to the last vector, and
 // settle() makes -inf of them.
@@ -284,30 +285,36 @@ struct Held {
   static constexpr int N = Elem<E>::N;
   static constexpr uint32_t SIZE = TH * NV * N;                        // values in whole vectors
   raw4 r[NV];
-  E last;
-  uint32_t nvec, n;
+  uint32_t last;                                                       // its bits
+  uint32_t first, nvec, n;                                             // vector v begins at value first + v N
   __device__ __forceinline__ uint32_t vec(int u) const { return threadIdx.x + u * TH; }
-  __device__ __forceinline__ uint32_t last_index() const { return nvec * N + threadIdx.x; }
+  __device__ __forceinline__ uint32_t last_index() const { return threadIdx.x < first ? threadIdx.x : nvec * N + threadIdx.x; }
   __device__ __forceinline__ void load(const E* z, uint32_t n_) {
-    n = n_; nvec = n / N;
+    n = n_; first = odd_ones(z); nvec = (n - first) / N;
     if (nvec) {
 #pragma unroll
-      for (int u = 0; u < NV; ++u) r[u] = load16(z + static_cast<uint64_t>(min(vec(u), nvec - 1)) * N);
+      for (int u = 0; u < NV; ++u) r[u] = load16(z + first + static_cast<uint64_t>(min(vec(u), nvec - 1)) * N);
     }
-    last = z[min(last_index(), n - 1)];
+    last = *reinterpret_cast<const typename Elem<E>::bits*>(z + min(last_index(), n - 1));
   }
   // What is made of vector u comes after `y` is known: keeps the compiler from waiting for all loads before the first sum, and from
   // holding all values unpacked from one use to the next (16 vectors of bf16: 152 VGPRs without this, 101 with it).
   __device__ __forceinline__ void in_order(int u, float& y) { asm volatile("" : "+v"(r[u]), "+v"(y)); }
+  __device__ __forceinline__ float last_value(float& y) {              // (the last load: waiting for it is waiting for all)
+    asm volatile("" : "+v"(last), "+v"(y));
+    return Elem<E>::from_bits(last);
+  }
   __device__ __forceinline__ void settle(int u) {
+    if ((u + 1) * TH <= nvec) return;                                  // the same for all threads
+    asm volatile("");                                                  // ... and a branch: the four selections below are not for every vector
     const bool out = vec(u) >= nvec;
 #pragma unroll
     for (int q = 0; q < 4; ++q) r[u][q] = out ? Elem<E>::MINUS_INF : r[u][q];
   }
-  // out(first index of vector u): the bits of the values that are left out
+  static constexpr int U = NV < 16 / N ? NV : 16 / N;                  // vectors that are taken in together: 16 values
+  // out(v): the bits of the values of vector v - 1 that are left out (v = 0: of the values before vector 0).  most[i]: the largest of vectors i U .. i U + U - 1
   template <bool ENT, class F>
-  __device__ __forceinline__ Stat stat(float cl, F&& out) {
-    constexpr int U = NV < 16 / N ? NV : 16 / N;
+  __device__ __forceinline__ Stat stat(float cl, F&& out, float (&most)[NV / U]) {
     Stat o = stat_none();
 #pragma unroll
     for (int u0 = 0; u0 < NV; u0 += U) {
@@ -317,35 +324,65 @@ struct Held {
         in_order(u0 + u, o.s);
         if (ENT) in_order(u0 + u, o.w);
         settle(u0 + u);
-        const uint32_t bits = out(min(vec(u0 + u), nvec) * N);
+        const uint32_t bits = out(min(vec(u0 + u), nvec) + 1);
         if (bits) Elem<E>::erase(r[u0 + u], bits);
         Elem<E>::unpack(r[u0 + u], v + u * N);
       }
-      take<ENT, U * N>(o, v, cl);
+      most[u0 / U] = take<ENT, U * N>(o, v, cl);
     }
-    const float x = last_index() < n && !(out(nvec * N) >> threadIdx.x % 32 & 1 && threadIdx.x < N) ? static_cast<float>(last) : -INFINITY;
+    const float xl = last_value(o.s);
+    const bool left_out = threadIdx.x < N && out(threadIdx.x < first ? 0 : nvec + 1) >> (threadIdx.x < first ? N - first : threadIdx.x - first) & 1;
+    const float x = last_index() < n && !left_out ? xl : -INFINITY;
     take<ENT, 1>(o, &x, cl);
     return o;
   }
-  // f(index, value) for the values that are at least `tau`: few, so the code for one of them stands once per vector
+  template <bool ENT>
+  __device__ __forceinline__ Stat stat(float cl) {
+    float most[NV / U];
+    return stat<ENT>(cl, NoneOut(), most);
+  }
+  // f(index, value) for the values that are at least `tau`, found by their chunk's largest.  A thread has few such chunks, and goes
+  // through them one by one while the others go through theirs (chunk by chunk for all threads, almost every chunk has one
+  // somewhere in the wave).  Where tau is -inf, the values of -inf only from the vectors that begin before `keep`.
   template <class F>
-  __device__ __forceinline__ void at_least(float tau, F&& f) {
+  __device__ __forceinline__ void at_least(float tau, uint32_t keep, const float (&most)[NV / U], F&& f) {
+    constexpr int C = NV / U, W = 4 * U;                               // chunks, words of one
+    uint32_t chunks = 0;
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      in_order(u, tau);
-      float v[N];
-      Elem<E>::unpack(r[u], v);
+    for (int i = 0; i < C; ++i) chunks |= most[i] >= (first + vec(i * U) * N < keep ? tau : fmaxf(tau, LOWEST)) ? 1u << i : 0u;
+    while (chunks) {
+      const uint32_t i = __builtin_ctz(chunks);
+      chunks &= chunks - 1;
+      uint32_t w[W];
+#pragma unroll
+      for (int x = 0; x < W; ++x) {
+        w[x] = r[x / 4][x % 4];
+#pragma unroll
+        for (int j = 1; j < C; ++j) w[x] = i == static_cast<uint32_t>(j) ? r[j * U + x / 4][x % 4] : w[x];
+      }
       uint32_t hits = 0;
 #pragma unroll
-      for (int q = 0; q < N; ++q) hits |= v[q] >= tau ? 1u << q : 0u;
-      if (vec(u) >= nvec) hits = 0;
+      for (int u = 0; u < U; ++u) {
+        const uint32_t v = threadIdx.x + (i * U + u) * TH;
+        const float least = first + v * N < keep ? tau : fmaxf(tau, LOWEST);
+        float x[N];
+        Elem<E>::unpack(raw4{w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]}, x);
+        uint32_t h = 0;
+#pragma unroll
+        for (int q = 0; q < N; ++q) h |= x[q] >= least ? 1u << q : 0u;
+        if (v < nvec) hits |= h << u * N;
+      }
       while (hits) {
         const uint32_t q = __builtin_ctz(hits);
         hits &= hits - 1;
-        f(vec(u) * N + q, Elem<E>::value(r[u], q));
+        uint32_t x = w[0];
+#pragma unroll
+        for (int j = 1; j < W; ++j) x = q / (N / 4) == static_cast<uint32_t>(j) ? w[j] : x;
+        f(first + (threadIdx.x + (i * U + q / N) * TH) * N + q % N, Elem<E>::of_word(x, q));
       }
     }
-    if (last_index() < n && static_cast<float>(last) >= tau) f(last_index(), static_cast<float>(last));
+    const float x = Elem<E>::from_bits(last);
+    if (last_index() < n && x >= (last_index() < keep ? tau : fmaxf(tau, LOWEST))) f(last_index(), x);
   }
   // the gradient of the piece; where class t is in it, `add` comes on top and given(its logit) is called
   template <bool ENT, class F>
@@ -355,7 +392,7 @@ struct Held {
       in_order(u, f.A);
       float v[N];
       Elem<E>::unpack(r[u], v);
-      const uint32_t q0 = t - vec(u) * N;
+      const uint32_t q0 = t - first - vec(u) * N;
       if (q0 < static_cast<uint32_t>(N) && vec(u) < nvec) {
         float x = v[0];
 #pragma unroll
@@ -367,17 +404,15 @@ struct Held {
 #pragma unroll
         for (int q = 0; q < N; ++q) v[q] = gradient_value<ENT>(f, v[q]);
       }
-      if (vec(u) < nvec) store16(dz + static_cast<uint64_t>(vec(u)) * N, Elem<E>::pack(v));
+      if (vec(u) < nvec) store16((dz + first + u * TH * N) + threadIdx.x * N, Elem<E>::pack(v));      // one offset for all u
     }
     if (last_index() < n) {
-      const float x = static_cast<float>(last);
+      const float x = last_value(f.A);
       if (t == last_index()) given(x);
       dz[last_index()] = static_cast<E>(gradient_value<ENT>(f, x) + (t == last_index() ? add : 0.0f));
     }
   }
 };
-struct NoneOut { __device__ __forceinline__ uint32_t operator()(uint32_t) const { return 0; } };
-
 // a barrier for what is in LDS: loads from memory stay under way
 __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -401,25 +436,54 @@ __device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xFFFFFFFFu -
 template <uint32_t CAP>
 struct TopBox {
   __align__(16) uint64_t list[CAP + 8];    // zeros behind the last one up to a multiple of 8
+  uint16_t above[CAP], place[CAP];
+  uint32_t equal[CAP];
   __align__(16) float group[GROUPS];
+  float tau;
   uint32_t n;
   uint64_t kth;
 };
 
-// for i < held: f(i, list[i], how many of list[0 .. among) are larger); zeros stand behind list[held - 1] up to a multiple of 8
-template <int TH, class F>
-__device__ __forceinline__ void ranked(const uint64_t* list, uint32_t held, uint32_t among, F&& f) {
+// f(key, rank) for list[0 .. held), all of them different.  Upper halves are compared with all others (64 bits at a time cost twice as
+// much), whole keys with the few that have the same upper half (or with all, where they are many).
+template <int TH, uint32_t CAP, class F>
+__device__ __forceinline__ void ranked(TopBox<CAP>& b, uint32_t held, F&& f) {
+  if (threadIdx.x < 8) b.list[held + threadIdx.x] = 0;
+  for (uint32_t i = threadIdx.x; i < held; i += TH) b.equal[i] = 0;
+  __syncthreads();
 #pragma unroll 1
   for (uint32_t i = threadIdx.x; i < held; i += TH) {
-    const uint64_t k = list[i];
-    uint32_t rank = 0;
+    const uint32_t k = static_cast<uint32_t>(b.list[i] >> 32);
+    uint32_t above = 0;
 #pragma unroll 1
-    for (uint32_t j = 0; j < among; j += 8) {                         // 8 at a time: one at a time every comparison waits for its own read
+    for (uint32_t j = 0; j < held; j += 8) {                          // 8 at a time: one at a time every comparison waits for its own read
 #pragma unroll
       for (uint32_t q = 0; q < 8; q += 2) {
-        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(list + j + q);
-        rank += (o.x > k) + (o.y > k);
+        const uint4 o = *reinterpret_cast<const uint4*>(b.list + j + q);
+        above += (o.y > k) + (o.w > k);
       }
+    }
+    b.above[i] = above;
+    b.place[above + atomicAdd(&b.equal[above], 1u)] = i;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x; i < held; i += TH) {
+    const uint64_t k = b.list[i];
+    const uint32_t above = b.above[i], equal = b.equal[above];
+    uint32_t rank = above;
+    if (equal > 16) {
+      rank = 0;
+#pragma unroll 1
+      for (uint32_t j = 0; j < held; j += 8) {
+#pragma unroll
+        for (uint32_t q = 0; q < 8; q += 2) {
+          const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(b.list + j + q);
+          rank += (o.x > k) + (o.y > k);
+        }
+      }
+    } else if (equal > 1) {
+      for (uint32_t j = above; j < above + equal; ++j) rank += b.list[b.place[j]] > k;
     }
     f(k, rank);
   }
@@ -428,36 +492,39 @@ __device__ __forceinline__ void ranked(const uint64_t* list, uint32_t held, uint
 // The K largest of n entries that the threads of a block hold, through out(rank, key); `most`: the thread's largest value (-inf:
 // none); scan(tau, f): f(key) for each of the thread's entries whose value is at least tau.
 // Groups of threads hold distinct entries, so the K-th largest of the groups' maxima is at most the K-th largest value: only what
-// reaches it is a candidate (for values in no particular order a few more than K, in the few threads whose maximum reaches it).  Every
-// wave finds it for itself, 20 bits of it from the top, by counting the maxima that reach a trial value; less than it will do as
-// well.  If more than CAP entries are candidates (many equal or ordered values), the K-th largest of the first REFINE that found room
+// reaches it is a candidate (for values in no particular order a few more than K, in the few threads whose maximum reaches it).  One
+// wave finds its upper 16 bits, by counting the maxima that reach a trial value; less than it will do as well.  Values of -inf count only where fewer than K others are left; of those the lowest indices are wanted, and they are among the first
+// K entries: a mask that leaves less than K classes does not make all others candidates.  If more than CAP entries are candidates (many equal or ordered values), the K-th largest of the first REFINE that found room
 // is the next bound: a larger one, since keys differ, and for entries in no particular order it leaves K / REFINE of them.
 template <int TH, uint32_t CAP, class S, class F>
 __device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, TopBox<CAP>& b, S&& scan, F&& out) {
   constexpr uint32_t PER = TH > GROUPS ? TH / GROUPS : 1, G = TH / PER, M = G / 64;
-  static_assert(PER == 1 || PER == 4, "a group is a thread or the four lanes of a quad");
+  static_assert(PER == 1 || PER == 2 || PER == 4, "a group is a thread, or two or four lanes of a quad");
   float gm = most;
-  if (PER == 4) {
-    gm = fmaxf(gm, dpp_keep<0xB1, 0xF>(gm, gm));                      // the lanes of a quad: 1 0 3 2, then 2 3 0 1
-    gm = fmaxf(gm, dpp_keep<0x4E, 0xF>(gm, gm));
-  }
+  if (PER >= 2) gm = fmaxf(gm, dpp_keep<0xB1, 0xF>(gm, gm));          // the lanes of a quad: 1 0 3 2, then 2 3 0 1
+  if (PER == 4) gm = fmaxf(gm, dpp_keep<0x4E, 0xF>(gm, gm));
   if (TH > 64 && threadIdx.x % PER == 0) b.group[threadIdx.x / PER] = gm;
   if (threadIdx.x == 0) b.n = 0;
   __syncthreads();
-  float tau = -INFINITY;
-  if (K <= G && n > 2 * K) {
-    uint32_t o[M], T = 0;
+  if (threadIdx.x < 64) {
+    float tau = -INFINITY;
+    if (K <= G && n > 2 * K) {
+      uint32_t o[M], T = 0;
 #pragma unroll
-    for (uint32_t j = 0; j < M; ++j) o[j] = ordered(TH > 64 ? b.group[lane_id() + 64 * j] : gm);
+      for (uint32_t j = 0; j < M; ++j) o[j] = ordered(TH > 64 ? b.group[lane_id() + 64 * j] : gm);
 #pragma unroll 1
-    for (uint32_t bit = 1u << 31; bit >= 1u << 12; bit >>= 1) {
-      uint32_t reach = 0;
+      for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
+        uint32_t reach = 0;
 #pragma unroll
-      for (uint32_t j = 0; j < M; ++j) reach += __popcll(__ballot(o[j] >= (T | bit)));
-      if (reach >= K) T |= bit;
+        for (uint32_t j = 0; j < M; ++j) reach += __popcll(__ballot(o[j] >= (T | bit)));
+        if (reach >= K) T |= bit;
+      }
+      if (T > ordered(-INFINITY)) tau = from_ordered(T);
     }
-    if (T > ordered(-INFINITY)) tau = from_ordered(T);
+    if (threadIdx.x == 0) b.tau = tau;
   }
+  __syncthreads();
+  const float tau = b.tau;
   uint64_t bound = 0;
   for (;;) {
     if (most >= tau)
@@ -467,14 +534,13 @@ __device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, To
         if (at < CAP) b.list[at] = k;
       });
     __syncthreads();
-    const uint32_t found = b.n, held = min(found, CAP);
-    if (threadIdx.x < 8) b.list[held + threadIdx.x] = 0;
-    __syncthreads();
+    const uint32_t found = b.n;
     if (found <= CAP) {
-      ranked<TH>(b.list, held, held, [&](uint64_t k, uint32_t rank) { if (rank < K) out(rank, k); });
+      ranked<TH>(b, found, [&](uint64_t k, uint32_t rank) { if (rank < K) out(rank, k); });
       return;
     }
-    ranked<TH>(b.list, REFINE, REFINE, [&](uint64_t k, uint32_t rank) { if (rank == K - 1) b.kth = k; });
+    __syncthreads();                                                  // (list[REFINE] is about to be cleared)
+    ranked<TH>(b, REFINE, [&](uint64_t k, uint32_t rank) { if (rank == K - 1) b.kth = k; });
     __syncthreads();
     bound = b.kth;
     if (threadIdx.x == 0) b.n = 0;
@@ -486,19 +552,22 @@ __device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, To
 template <class E, int TH, uint32_t CAP, class F>
 __device__ __forceinline__ void row_top(const E* z, uint32_t n, uint32_t K, float most, TopBox<CAP>& b, F&& out) {
   constexpr int N = Elem<E>::N, U = 4;
+  const uint32_t first = odd_ones(z), nvec = (n - first) / N;
   block_top<TH, CAP>(n, K, most, b, [&](float tau, auto&& f) {
-    walk<E, TH, U>(z, n,
+    walk<E, TH, U>(z, n, first,
       [&](uint32_t v0, const raw4* r) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          if (v0 + u * TH >= n / N) continue;
+          if (v0 + u * TH >= nvec) continue;
           float v[N];
           Elem<E>::unpack(r[u], v);
+          const uint32_t i = first + (v0 + u * TH) * N;
+          const float least = i < K ? tau : fmaxf(tau, LOWEST);
 #pragma unroll
-          for (int q = 0; q < N; ++q) if (v[q] >= tau) f(top_key(v[q], (v0 + u * TH) * N + q));
+          for (int q = 0; q < N; ++q) if (v[q] >= least) f(top_key(v[q], i + q));
         }
       },
-      [&](uint32_t i, float x) { if (x >= tau) f(top_key(x, i)); });
+      [&](uint32_t i, float x) { if (x >= (i < K ? tau : fmaxf(tau, LOWEST))) f(top_key(x, i)); });
   }, out);
 }
 
@@ -552,6 +621,10 @@ __device__ __forceinline__ void alternatives(const ScoreArgs& a, uint32_t row, c
     for (uint32_t k = threadIdx.x; k < a.K; k += TH) { if (ti) ti[k] = -1; if (tl) tl[k] = NAN; }
     return;
   }
+  if (r.L == -INFINITY) {                                             // nothing but -inf
+    for (uint32_t k = threadIdx.x; k < a.K; k += TH) { if (ti) ti[k] = static_cast<int32_t>(k); if (tl) tl[k] = -INFINITY; }
+    return;
+  }
   f([&](uint32_t rank, uint64_t k) {
     if (ti) ti[rank] = static_cast<int32_t>(key_index(k));
     if (tl) tl[rank] = log_prob(r, key_value(k), a.c);
@@ -582,7 +655,7 @@ __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
 // Alternatives of a row that fits the block's registers.
 template <class E, int TH, int NV, bool ENT>
 __global__ __launch_bounds__(TH) void k_score_held(ScoreArgs a) {
-  constexpr uint32_t CAP = CAND_CAP;
+  constexpr uint32_t CAP = TH == 64 ? REFINE : CAND_CAP;               // (one wave: LDS would limit how many are resident)
   __shared__ Stat box[16];
   __shared__ TopBox<CAP> tb;
   const float cl = a.c * LOG2E;
@@ -593,13 +666,14 @@ __global__ __launch_bounds__(TH) void k_score_held(ScoreArgs a) {
   Held<E, TH, NV> h;
   h.load(z, a.vocab);
   given.load(a, row, z);
-  const Stat mine = h.template stat<ENT>(cl, NoneOut());
+  float most[NV / Held<E, TH, NV>::U];
+  const Stat mine = h.template stat<ENT>(cl, NoneOut(), most);
   const Stat o = block_stat<ENT, TH>(mine, cl, box);
   const RowStat r = row_stat<ENT>(o);
   if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
   alternatives<TH>(a, row, r, [&](auto&& out) {
     block_top<TH, CAP>(a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb,
-                       [&](float tau, auto&& f) { h.at_least(tau, [&](uint32_t i, float x) { f(top_key(x, i)); }); }, out);
+                       [&](float tau, auto&& f) { h.at_least(tau, a.K, most, [&](uint32_t i, float x) { f(top_key(x, i)); }); }, out);
   });
 }
 
@@ -633,12 +707,13 @@ __global__ __launch_bounds__(256) void k_slice_stats(ScoreArgs a, Slices sl) {
   else {
     Held<E, 256, NV> h;
     h.load(z, n);
-    const Stat mine = h.template stat<ENT>(cl, NoneOut());
+    float most[NV / Held<E, 256, NV>::U];
+    const Stat mine = h.template stat<ENT>(cl, NoneOut(), most);
     hand_over(mine);
     uint64_t* key = sl.key + p * a.K;
     for (uint32_t k = threadIdx.x; k < a.K; k += 256) if (k >= n) key[k] = 0;      // (of a slice with a NaN nobody looks at the keys)
     block_top<256, CAND_CAP>(n, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb,
-                             [&](float tau, auto&& f) { h.at_least(tau, [&](uint32_t i, float x) { f(top_key(x, i0 + i)); }); },
+                             [&](float tau, auto&& f) { h.at_least(tau, a.K, most, [&](uint32_t i, float x) { f(top_key(x, i0 + i)); }); },
                              [&](uint32_t rank, uint64_t k) { key[rank] = k; });
   }
 }
@@ -659,7 +734,10 @@ __global__ __launch_bounds__(256) void k_score_join(ScoreArgs a, Slices sl) {
   if (row >= a.rows) return;
   const uint32_t n = sl.S * a.K;
   const uint64_t* key = sl.key + row * n;
-  const uint64_t mine = threadIdx.x < n ? key[threadIdx.x] : 0;
+  constexpr uint32_t M = 4;
+  uint64_t mine[M];
+#pragma unroll
+  for (uint32_t j = 0; j < M; ++j) mine[j] = threadIdx.x + 256 * j < n ? key[threadIdx.x + 256 * j] : 0;
   Given<E> given;
   given.load(a, row, static_cast<const E*>(a.z) + row * a.stride);
   const Stat o = joined<ENT>(sl, row, cl);
@@ -668,16 +746,20 @@ __global__ __launch_bounds__(256) void k_score_join(ScoreArgs a, Slices sl) {
   if (a.K == 0) return;
   alternatives<256>(a, row, r, [&](auto&& out) {
     if (n <= 256) {                                                   // no bound needed: rank them all
-      tb.list[threadIdx.x] = mine;
-      if (threadIdx.x < 8) tb.list[256 + threadIdx.x] = 0;
+      if (threadIdx.x < n) tb.list[threadIdx.x] = mine[0];
       __syncthreads();
-      ranked<256>(tb.list, n, n, [&](uint64_t k, uint32_t rank) { if (k && rank < a.K) out(rank, k); });
+      ranked<256>(tb, n, [&](uint64_t k, uint32_t rank) { if (k && rank < a.K) out(rank, k); });
       return;
     }
-    uint64_t most = mine;
-    for (uint32_t i = threadIdx.x + 256; i < n; i += 256) most = max(most, key[i]);
+    auto each = [&](auto&& f) {
+#pragma unroll
+      for (uint32_t j = 0; j < M; ++j) if (mine[j]) f(mine[j]);
+      for (uint32_t i = threadIdx.x + 256 * M; i < n; i += 256) { const uint64_t k = key[i]; if (k) f(k); }
+    };
+    uint64_t most = 0;
+    each([&](uint64_t k) { most = max(most, k); });
     block_top<256, CAND_CAP>(n, a.K, most ? key_value(most) : -INFINITY, tb,
-      [&](float tau, auto&& f) { for (uint32_t i = threadIdx.x; i < n; i += 256) { const uint64_t k = key[i]; if (k && key_value(k) >= tau) f(k); } }, out);
+                             [&](float tau, auto&& f) { each([&](uint64_t k) { if (key_value(k) >= tau) f(k); }); }, out);
   });
 }
 
@@ -702,12 +784,22 @@ struct RowGradient {
   float add;                               // what it gets on top
 };
 
+// what is given for a row, read ahead of it
+struct RowWeights { int64_t t; float g, h; };
 template <bool ENT>
-__device__ __forceinline__ RowGradient row_gradient(const GradArgs& a, uint32_t row, const RowStat& r) {
-  const int64_t t = a.target ? a.target[row] : -1;
-  float g = a.g && t >= 0 ? a.g[row] : 0.0f;
-  if (t >= static_cast<int64_t>(a.vocab)) g = NAN;
-  const float h = ENT && a.h ? a.h[row] : 0.0f;
+__device__ __forceinline__ RowWeights row_weights(const GradArgs& a, uint32_t row) {
+  RowWeights w;
+  w.t = a.target ? a.target[row] : -1;
+  w.g = a.g ? a.g[row] : 0.0f;
+  w.h = ENT && a.h ? a.h[row] : 0.0f;
+  if (w.t < 0) w.g = 0.0f;
+  if (w.t >= static_cast<int64_t>(a.vocab)) w.g = NAN;
+  return w;
+}
+template <bool ENT>
+__device__ __forceinline__ RowGradient row_gradient(const GradArgs& a, const RowWeights& w, const RowStat& r) {
+  const int64_t t = w.t;
+  const float g = w.g, h = w.h;
   const bool empty = r.L == -INFINITY;
   RowGradient o;
   o.f.cl = a.c * LOG2E; o.f.m = r.m;
@@ -719,25 +811,26 @@ __device__ __forceinline__ RowGradient row_gradient(const GradArgs& a, uint32_t 
   return o;
 }
 // what a row hands out besides its gradient; the log probability of a given class comes from the thread that holds it
-__device__ __forceinline__ void gradient_outputs(const GradArgs& a, uint32_t row, const RowStat& r, const RowGradient& o) {
+__device__ __forceinline__ void gradient_outputs(const GradArgs& a, uint32_t row, const RowStat& r, const RowGradient& o, int64_t given) {
   if (a.entropy) a.entropy[row] = r.H;
-  if (a.logprob && o.t == 0xFFFFFFFFu) a.logprob[row] = a.target[row] < 0 ? 0.0f : NAN;
+  if (a.logprob && o.t == 0xFFFFFFFFu) a.logprob[row] = given < 0 ? 0.0f : NAN;
 }
 
-// A block per row, held in its registers: one read, one write.
+// A block per row, held in its registers: one read, one write.  (8 vectors: 64 VGPRs, so that two blocks of 1024 are resident.)
 template <class E, int TH, int NV, bool ENT>
-__global__ __launch_bounds__(TH) void k_gradient_held(GradArgs a) {
+__global__ __launch_bounds__(TH, NV <= 8 ? 8 : 4) void k_gradient_held(GradArgs a) {
   __shared__ Stat box[16];
   const float cl = a.c * LOG2E;
   const uint64_t row = block_number();
   if (row >= a.rows) return;
+  const RowWeights w = row_weights<ENT>(a, row);
   Held<E, TH, NV> h;
   h.load(static_cast<const E*>(a.z) + row * a.stride, a.vocab);
-  const RowStat r = row_stat<ENT>(block_stat<ENT, TH>(h.template stat<ENT>(cl, NoneOut()), cl, box));
-  const RowGradient o = row_gradient<ENT>(a, row, r);
+  const RowStat r = row_stat<ENT>(block_stat<ENT, TH>(h.template stat<ENT>(cl), cl, box));
+  const RowGradient o = row_gradient<ENT>(a, w, r);
   h.template gradient<ENT>(static_cast<E*>(a.dz) + row * a.dstride, o.f, o.t, o.add,
                            [&](float x) { if (a.logprob) a.logprob[row] = log_prob(r, x, a.c); });
-  if (threadIdx.x == 0) gradient_outputs(a, row, r, o);
+  if (threadIdx.x == 0) gradient_outputs(a, row, r, o, w.t);
 }
 
 // A piece of a row per block, the statistics known: the caller's, or (a.stats = NULL) joined from the slices'.
@@ -750,15 +843,16 @@ __global__ __launch_bounds__(256) void k_gradient_apply(GradArgs a, Slices sl) {
   const uint64_t p = block_number();
   if (p >= pieces) return;
   const uint32_t row = static_cast<uint32_t>(p / per), i0 = static_cast<uint32_t>(p % per) * H::SIZE, n = min(a.vocab - i0, H::SIZE);
+  const RowWeights w = row_weights<ENT>(a, row);
   H h;
   h.load(static_cast<const E*>(a.z) + row * a.stride + i0, n);
   RowStat r;
   if (a.stats) { const float* s = a.stats + 4ull * row; r.m = s[0]; r.L = s[1]; r.H = s[2]; }
   else r = row_stat<ENT>(joined<ENT>(sl, row, a.c * LOG2E));
-  const RowGradient o = row_gradient<ENT>(a, row, r);
+  const RowGradient o = row_gradient<ENT>(a, w, r);
   h.template gradient<ENT>(static_cast<E*>(a.dz) + row * a.dstride + i0, o.f, o.t - i0, o.add,
                            [&](float x) { if (a.logprob) a.logprob[row] = log_prob(r, x, a.c); });
-  if (threadIdx.x == 0 && i0 == 0) gradient_outputs(a, row, r, o);
+  if (threadIdx.x == 0 && i0 == 0) gradient_outputs(a, row, r, o, w.t);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -843,20 +937,22 @@ __device__ __forceinline__ void teacher_logits(const DistillArgs& a, TeacherBox&
   }
 }
 
-// marks the classes of [i0, i0 + len) that are entries; index(k): entry k
-template <int TH, class F>
-__device__ __forceinline__ void mark(uint32_t* mask, uint32_t i0, uint32_t len, uint32_t K, F&& index) {
-  for (uint32_t i = threadIdx.x; i < len / 32 + 1; i += TH) mask[i] = 0;
+// Marks the classes of [i0, i0 + len) that are entries: bits v N .. v N + N - 1 of the mask are vector v - 1's, those before `first` stand
+// right before vector 0's.  index(k): entry k.
+constexpr uint32_t mask_words(uint32_t len) { return (len + 8) / 32 + 1; }
+template <int TH, int N, class F>
+__device__ __forceinline__ void mark(uint32_t* mask, uint32_t i0, uint32_t len, uint32_t first, uint32_t K, F&& index) {
+  for (uint32_t i = threadIdx.x; i < mask_words(len); i += TH) mask[i] = 0;
   lds_barrier();
   for (uint32_t k = threadIdx.x; k < K; k += TH) {
     const int32_t e = index(k);
-    const uint32_t i = static_cast<uint32_t>(e) - i0;                 // classes before the span are huge
-    if (e >= 0 && i < len) atomicOr(&mask[i / 32], 1u << i % 32);
+    const uint32_t i = static_cast<uint32_t>(e) - i0, at = i + N - first;      // classes before the span are huge
+    if (e >= 0 && i < len) atomicOr(&mask[at / 32], 1u << at % 32);
   }
   lds_barrier();
 }
 template <int N>
-__device__ __forceinline__ uint32_t marks(const uint32_t* mask, uint32_t i) { return mask[i / 32] >> i % 32 & ((1u << N) - 1); }
+__device__ __forceinline__ uint32_t marks(const uint32_t* mask, uint32_t v) { return mask[v * N / 32] >> v * N % 32 & ((1u << N) - 1); }
 
 // The statistics of a row's slice without the teacher's classes, whose places are marked in LDS, a span of the slice at a time.
 template <class E, int TH, class F>
@@ -864,22 +960,25 @@ __device__ __forceinline__ Stat pass_rest(const E* z, uint32_t i0, uint32_t n, u
   constexpr int N = Elem<E>::N, U = 4;
   Stat o = stat_none();
   for (uint32_t s0 = 0; s0 < n; s0 += MASK_SPAN) {
-    const uint32_t len = min(n - s0, MASK_SPAN);
+    const uint32_t len = min(n - s0, MASK_SPAN), first = odd_ones(z + s0), nvec = (len - first) / N;
     if (s0) __syncthreads();
-    mark<TH>(mask, i0 + s0, len, K, index);
-    walk<E, TH, U>(z + s0, len,
+    mark<TH, N>(mask, i0 + s0, len, first, K, index);
+    walk<E, TH, U>(z + s0, len, first,
       [&](uint32_t v0, const raw4* r) {
         float v[U * N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const uint32_t i = (v0 + u * TH) * N, bits = i < len ? marks<N>(mask, i) : 0;
+          const uint32_t bits = v0 + u * TH < nvec ? marks<N>(mask, v0 + u * TH + 1) : 0;
           raw4 x = r[u];
           if (bits) Elem<E>::erase(x, bits);
           Elem<E>::unpack(x, v + u * N);
         }
         take<false, U * N>(o, v, cl);
       },
-      [&](uint32_t i, float x) { if (!marks<1>(mask, i)) take<false, 1>(o, &x, cl); });
+      [&](uint32_t i, float x) {
+        const uint32_t at = i + N - first;
+        if (!(mask[at / 32] >> at % 32 & 1)) take<false, 1>(o, &x, cl);
+      });
   }
   return o;
 }
@@ -1009,7 +1108,7 @@ __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
   typedef Held<E, TH, NV> H;
   __shared__ Stat box[16];
   __shared__ TeacherBox b;
-  __shared__ uint32_t mask[REST ? H::SIZE / 32 + 1 : 1];
+  __shared__ uint32_t mask[REST ? mask_words(H::SIZE + 8) : 1];
   const float cl = a.c * LOG2E;
   const uint64_t row = block_number();
   if (row >= a.rows) return;
@@ -1023,8 +1122,9 @@ __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
   if (threadIdx.x < 64) teacher_probabilities<REST>(a, row, b);     // while the row is on its way
   Stat o = stat_none();
   if (!a.stats_in) {
-    if (REST) mark<TH>(mask, 0, a.vocab, a.K, [&](uint32_t k) { return b.index[k]; });
-    o = h.template stat<false>(cl, [&](uint32_t i) { return REST ? marks<H::N>(mask, i) : 0u; });
+    if (REST) mark<TH, H::N>(mask, 0, a.vocab, h.first, a.K, [&](uint32_t k) { return b.index[k]; });
+    float most[NV / H::U];
+    o = h.template stat<false>(cl, [&](uint32_t v) { return REST ? marks<H::N>(mask, v) : 0u; }, most);
   }
   teacher_logits<E, TH>(a, b, x);
   o = block_stat<false, TH>(o, cl, box);
