@@ -13,6 +13,10 @@ that report, still scaled by 1/R, and sends the model back to those workers only
 the virtual sequence of Section 3.4, so that the memory identity  xhat_t - xtilde_t = (1/R) sum_r m_t
 can be checked along the run.
 
+`SoftmaxProblem.error` is the other axis of the plots of Section 5 (top-1 and top-5 error), `DistilledProblem` the same model
+trained on the labels and on a trained model's top log probabilities; both, and the gradients of the latter's local steps, come from the
+library's operators on logits.
+
     python -m paper_1906_02367_amd.algorithm1        # loss against bits for a few operators
 """
 from __future__ import annotations
@@ -61,6 +65,66 @@ class SoftmaxProblem:
         p = torch.softmax(logits, dim=2)
         p.scatter_add_(2, yb.unsqueeze(-1), -torch.ones(R, b, 1, device=self.device))
         g = torch.bmm(p.transpose(1, 2), xb) / b                                             # [R, C, F+1]
+        return g.reshape(R, D) + self.lam * w_local
+
+
+    def logits(self, w):
+        return self.x.reshape(self.n, -1) @ w.view(N_CLASSES, -1).t()
+
+    def error(self, w, tops=(1, 5)):
+        """Share of the samples whose class is not among the `k` likeliest, for each k (ties to the lower class)."""
+        index = torch.empty(self.n, max(tops), dtype=torch.int32, device=self.device)
+        B.token_logprobs(self.logits(w), top_index=index)
+        hit = index == self.y.reshape(-1, 1)
+        return tuple(1.0 - float(hit[:, :k].any(1).float().mean()) for k in tops)
+
+    def top_logprobs(self, w, top, temperature=1.0):
+        """What a model of parameters `w` has to teach: the `top` likeliest classes of every sample and their log probabilities,
+        [R, samples of a worker, top]."""
+        index = torch.empty(self.n, top, dtype=torch.int32, device=self.device)
+        value = torch.empty(self.n, top, device=self.device)
+        B.token_logprobs(self.logits(w), scale=1.0 / temperature, top_index=index, top_logprob=value)
+        return index.view(self.R, -1, top), value.view(self.R, -1, top)
+
+
+class DistilledProblem(SoftmaxProblem):
+    """The same data and model, taught by the labels and by a teacher: a cross entropy + (1 - a) T^2 KL(teacher || student), both at
+    temperature T, the teacher known by its `top` likeliest classes of every sample and what they leave over."""
+
+    def __init__(self, problem, teacher, top=3, a=0.5, temperature=2.0, seed=0):
+        self.device, self.R, self.n, self.lam = problem.device, problem.R, problem.n, problem.lam
+        self.x, self.y = problem.x, problem.y
+        self.gen = torch.Generator(device=self.device).manual_seed(7 + seed)
+        self.a, self.T, self.top = a, temperature, top
+        self.index, self.value = problem.top_logprobs(teacher, top, temperature)
+
+    def _teacher(self, index, value):
+        # log probabilities: they carry the temperature already, and the logarithm of all their sum is 0
+        rows = index.numel() // self.top
+        return dict(teacher_index=index.reshape(rows, self.top), teacher_value=value.reshape(rows, self.top), scale=1.0 / self.T,
+                    teacher_scale=1.0, teacher_lse=torch.zeros(rows, device=self.device))
+
+    def loss(self, w):
+        z = self.logits(w)
+        logprob, kl = torch.empty(self.n, device=self.device), torch.empty(self.n, device=self.device)
+        B.token_logprobs(z, self.y.reshape(-1), logprob=logprob)
+        B.distill(z, loss=kl, **self._teacher(self.index, self.value))
+        ce = -self.a * logprob.double().mean() + (1.0 - self.a) * self.T ** 2 * kl.double().mean()
+        return float(ce + 0.5 * self.lam * (w.double() ** 2).sum())
+
+    def minibatch_grads(self, w_local, b):
+        R, F = self.R, N_FEATURES + 1
+        idx = torch.randint(0, self.x.shape[1], (R, b), generator=self.gen, device=self.device)
+        xb = torch.gather(self.x, 1, idx.unsqueeze(-1).expand(R, b, F))
+        yb = torch.gather(self.y, 1, idx).reshape(-1)
+        index, value = (torch.gather(t, 1, idx.unsqueeze(-1).expand(R, b, self.top)) for t in (self.index, self.value))
+        z = torch.bmm(xb, w_local.view(R, N_CLASSES, F).transpose(1, 2).contiguous()).view(R * b, N_CLASSES)
+        d_ce, d_kl = torch.empty_like(z), torch.empty_like(z)
+        share = torch.full((R * b,), 1.0 / b, device=self.device)
+        B.token_logprobs_backward(z, yb, d_ce, grad_logprob=-self.a * share)
+        B.distill_backward(z, dlogits=d_kl, grad_loss=(1.0 - self.a) * self.T ** 2 * share, **self._teacher(index, value))
+        dz = (d_ce + d_kl).view(R, b, N_CLASSES)
+        g = torch.bmm(dz.transpose(1, 2).contiguous(), xb)
         return g.reshape(R, D) + self.lam * w_local
 
 
@@ -162,12 +226,21 @@ def main():
             ("scaled 2-bit QTop_k, H=4", Operator(quantizer=B.QSGD_SCALED, s=3), 4),
             ("SignTop_k, H=4", Operator(quantizer=B.SIGN_L1), 4),
             ("SignTop_k, H=8", Operator(quantizer=B.SIGN_L1), 8)]
-    print(f"{'scheme':34s} {'final loss':>10s} {'log2(bits)':>11s} {'identity err':>13s}")
+    print(f"{'scheme':34s} {'final loss':>10s} {'top-1 error':>11s} {'top-5':>7s} {'log2(bits)':>11s} {'identity err':>13s}")
+
+    def line(name, res, ident):
+        top1, top5 = prob.error(res["x"])
+        print(f"{name:34s} {res['loss'][-1]:10.4f} {top1:11.4f} {top5:7.4f} {math.log2(res['bits'][-1]):11.2f} {ident:>13s}")
+
+    teacher = None
     for name, op, H in rows:
         res = run_sync(prob, op, H=H, T=800)
-        print(f"{name:34s} {res['loss'][-1]:10.4f} {math.log2(res['bits'][-1]):11.2f} {res['identity_err']:13.2e}")
-    res = run_async(prob, Operator(quantizer=B.SIGN_L1), H=4, T=800)
-    print(f"{'SignTop_k, asynchronous, H<=4':34s} {res['loss'][-1]:10.4f} {math.log2(res['bits'][-1]):11.2f} {'':>13s}")
+        line(name, res, f"{res['identity_err']:.2e}")
+        if op.quantizer == B.SIGN_L1 and H == 4:
+            teacher = res["x"]
+    line("SignTop_k, asynchronous, H<=4", run_async(prob, Operator(quantizer=B.SIGN_L1), H=4, T=800), "")
+    res = run_sync(DistilledProblem(prob, teacher), Operator(quantizer=B.SIGN_L1), H=4, T=800)
+    line("SignTop_k, H=4, taught by that one", res, f"{res['identity_err']:.2e}")
 
 
 if __name__ == "__main__":
