@@ -159,13 +159,13 @@ def _rows_of(t, what):
     return t.data_ptr(), stride if rows > 1 else vocab
 
 
-def _beside(t, what, z, dtype, shape):
-    """Address of an argument that goes with the logits `z`: on their device, contiguous, of that type and shape; None for None."""
+def _beside(t, what, device, dtype, shape):
+    """Address of an argument that goes with logits on `device` (its index): there, contiguous, of that type and shape; None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or t.device != z.device or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous {dtype} tensor {list(shape)} on {z.device}, got {t.dtype} {list(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{what}: expected a contiguous {dtype} tensor {list(shape)} on cuda:{device}, got {t.dtype} {list(t.shape)} on {t.device}")
 
 
 _current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
@@ -180,8 +180,8 @@ def _on_logits(where, fn, logits, scale, top, workspace, *args):
         need = _lib.qsl_logits_workspace_bytes(z, top)
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
-    at, size = (None, 0) if workspace is None else (_beside(workspace, "workspace", logits, torch.uint8, (workspace.numel(),)), workspace.numel())
     device = logits.get_device()
+    at, size = (None, 0) if workspace is None else (_beside(workspace, "workspace", device, torch.uint8, (workspace.numel(),)), workspace.numel())
     if device == _current_device():
         st = fn(z, *args, at, size, _raw_stream(device))
     else:
@@ -201,18 +201,18 @@ def token_logprobs(logits, target=None, scale=1.0, logprob=None, entropy=None, l
                    stats=None, workspace=None):
     """`qsl_token_logprobs`: log probabilities of the given classes, entropy and best alternatives of every row of
     logits [rows, vocab], into those of the output tensors that are given."""
-    N = logits.shape[0]
+    N, dev = logits.shape[0], logits.get_device()
     some = top_index if top_index is not None else top_logprob
     top = 0 if some is None else some.shape[-1]
     f32 = torch.float32
-    _on_logits("qsl_token_logprobs", _lib.qsl_token_logprobs, logits, scale, top, workspace, _beside(target, "target", logits, torch.int64, (N,)), top,
-               _beside(logprob, "logprob", logits, f32, (N,)), _beside(entropy, "entropy", logits, f32, (N,)), _beside(lse, "lse", logits, f32, (N,)),
-               _beside(top_index, "top_index", logits, torch.int32, (N, top)), _beside(top_logprob, "top_logprob", logits, f32, (N, top)),
-               _beside(stats, "stats", logits, f32, (N, 4)))
+    _on_logits("qsl_token_logprobs", _lib.qsl_token_logprobs, logits, scale, top, workspace, _beside(target, "target", dev, torch.int64, (N,)), top,
+               _beside(logprob, "logprob", dev, f32, (N,)), _beside(entropy, "entropy", dev, f32, (N,)), _beside(lse, "lse", dev, f32, (N,)),
+               _beside(top_index, "top_index", dev, torch.int32, (N, top)), _beside(top_logprob, "top_logprob", dev, f32, (N, top)),
+               _beside(stats, "stats", dev, f32, (N, 4)))
 
 
 def _gradient_rows(dlogits, logits):
-    if dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.device != logits.device:
+    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape or dlogits.get_device() != logits.get_device():
         raise ValueError("dlogits: expected the logits' type, shape and device")
     return _rows_of(dlogits, "dlogits")
 
@@ -220,39 +220,39 @@ def _gradient_rows(dlogits, logits):
 def token_logprobs_backward(logits, target, dlogits, scale=1.0, grad_logprob=None, grad_entropy=None, stats=None, logprob=None,
                             entropy=None, workspace=None):
     """`qsl_token_logprobs_backward`: the gradient of sum(grad_logprob * logprob) + sum(grad_entropy * entropy) in the logits."""
-    N = logits.shape[0]
+    N, dev = logits.shape[0], logits.get_device()
     f32 = torch.float32
     out, dstride = _gradient_rows(dlogits, logits)
     _on_logits("qsl_token_logprobs_backward", _lib.qsl_token_logprobs_backward, logits, scale, 0, workspace,
-               _beside(target, "target", logits, torch.int64, (N,)), _beside(grad_logprob, "grad_logprob", logits, f32, (N,)),
-               _beside(grad_entropy, "grad_entropy", logits, f32, (N,)), _beside(stats, "stats", logits, f32, (N, 4)),
-               _beside(logprob, "logprob", logits, f32, (N,)), _beside(entropy, "entropy", logits, f32, (N,)), out, dstride)
+               _beside(target, "target", dev, torch.int64, (N,)), _beside(grad_logprob, "grad_logprob", dev, f32, (N,)),
+               _beside(grad_entropy, "grad_entropy", dev, f32, (N,)), _beside(stats, "stats", dev, f32, (N, 4)),
+               _beside(logprob, "logprob", dev, f32, (N,)), _beside(entropy, "entropy", dev, f32, (N,)), out, dstride)
 
 
 def _teacher(logits, index, value, lse, scale):
-    N, top = logits.shape[0], index.shape[-1]
-    return C.byref(_Teacher(_beside(index, "teacher_index", logits, torch.int32, (N, top)),
-                            _beside(value, "teacher_value", logits, torch.float32, (N, top)),
-                            _beside(lse, "teacher_lse", logits, torch.float32, (N,)), top, scale))
+    N, dev, top = logits.shape[0], logits.get_device(), index.shape[-1]
+    return C.byref(_Teacher(_beside(index, "teacher_index", dev, torch.int32, (N, top)),
+                            _beside(value, "teacher_value", dev, torch.float32, (N, top)),
+                            _beside(lse, "teacher_lse", dev, torch.float32, (N,)), top, scale))
 
 
 def distill(logits, teacher_index, teacher_value, scale=1.0, teacher_scale=1.0, teacher_lse=None, loss=None, stats=None, workspace=None):
     """`qsl_distill`: the Kullback-Leibler divergence of every row from a teacher's top logits [rows, top]."""
-    N = logits.shape[0]
+    N, dev = logits.shape[0], logits.get_device()
     _on_logits("qsl_distill", _lib.qsl_distill, logits, scale, teacher_index.shape[-1], workspace,
-               _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(loss, "loss", logits, torch.float32, (N,)),
-               _beside(stats, "stats", logits, torch.float32, (N, 8)))
+               _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(loss, "loss", dev, torch.float32, (N,)),
+               _beside(stats, "stats", dev, torch.float32, (N, 8)))
 
 
 def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, teacher_scale=1.0, teacher_lse=None, grad_loss=None,
                      stats=None, loss=None, workspace=None):
     """`qsl_distill_backward`: the gradient of sum(grad_loss * loss) in the logits."""
-    N = logits.shape[0]
+    N, dev = logits.shape[0], logits.get_device()
     f32 = torch.float32
     out, dstride = _gradient_rows(dlogits, logits)
     _on_logits("qsl_distill_backward", _lib.qsl_distill_backward, logits, scale, teacher_index.shape[-1], workspace,
-               _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(grad_loss, "grad_loss", logits, f32, (N,)),
-               _beside(stats, "stats", logits, f32, (N, 8)), _beside(loss, "loss", logits, f32, (N,)), out, dstride)
+               _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(grad_loss, "grad_loss", dev, f32, (N,)),
+               _beside(stats, "stats", dev, f32, (N, 8)), _beside(loss, "loss", dev, f32, (N,)), out, dstride)
 
 
 class Qsl:

@@ -489,6 +489,30 @@ __device__ __forceinline__ void ranked(TopBox<CAP>& b, uint32_t held, F&& f) {
   }
 }
 
+// The last part of block_top: the K largest of the entries that scan() offers from `bound` on; at least K are.
+template <int TH, uint32_t CAP, class S, class F>
+__device__ __forceinline__ void block_top_from(uint64_t bound, uint32_t K, TopBox<CAP>& b, S&& scan, F&& out) {
+  for (;;) {
+    scan([&](uint64_t k) {
+      if (k < bound) return;
+      const uint32_t at = atomicAdd(&b.n, 1u);
+      if (at < CAP) b.list[at] = k;
+    });
+    __syncthreads();
+    const uint32_t found = b.n;
+    if (found <= CAP) {
+      ranked<TH>(b, found, [&](uint64_t k, uint32_t rank) { if (rank < K) out(rank, k); });
+      return;
+    }
+    __syncthreads();                                                  // (list[REFINE] is about to be cleared)
+    ranked<TH>(b, REFINE, [&](uint64_t k, uint32_t rank) { if (rank == K - 1) b.kth = k; });
+    __syncthreads();
+    bound = b.kth;
+    if (threadIdx.x == 0) b.n = 0;
+    __syncthreads();
+  }
+}
+
 // The K largest of n entries that the threads of a block hold, through out(rank, key); `most`: the thread's largest value (-inf:
 // none); scan(tau, f): f(key) for each of the thread's entries whose value is at least tau.
 // Groups of threads hold distinct entries, so the K-th largest of the groups' maxima is at most the K-th largest value: only what
@@ -525,27 +549,7 @@ __device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, To
   }
   __syncthreads();
   const float tau = b.tau;
-  uint64_t bound = 0;
-  for (;;) {
-    if (most >= tau)
-      scan(tau, [&](uint64_t k) {
-        if (k < bound) return;
-        const uint32_t at = atomicAdd(&b.n, 1u);
-        if (at < CAP) b.list[at] = k;
-      });
-    __syncthreads();
-    const uint32_t found = b.n;
-    if (found <= CAP) {
-      ranked<TH>(b, found, [&](uint64_t k, uint32_t rank) { if (rank < K) out(rank, k); });
-      return;
-    }
-    __syncthreads();                                                  // (list[REFINE] is about to be cleared)
-    ranked<TH>(b, REFINE, [&](uint64_t k, uint32_t rank) { if (rank == K - 1) b.kth = k; });
-    __syncthreads();
-    bound = b.kth;
-    if (threadIdx.x == 0) b.n = 0;
-    __syncthreads();
-  }
+  block_top_from<TH>(0, K, b, [&](auto&& f) { if (most >= tau) scan(tau, f); }, out);
 }
 
 // the same for a row in memory
@@ -738,28 +742,27 @@ __global__ __launch_bounds__(256) void k_score_join(ScoreArgs a, Slices sl) {
   uint64_t mine[M];
 #pragma unroll
   for (uint32_t j = 0; j < M; ++j) mine[j] = threadIdx.x + 256 * j < n ? key[threadIdx.x + 256 * j] : 0;
+  // The first ceil(K / S) of every slice are K entries or more, so the least of them is a bound (0 where a slice is shorter).
+  uint32_t lo = 0xFFFFFFFFu, hi = 0xFFFFFFFFu;
+  if (a.K && lane_id() < sl.S) {
+    const uint64_t k = key[lane_id() * a.K + (a.K + sl.S - 1) / sl.S - 1];
+    lo = static_cast<uint32_t>(k); hi = static_cast<uint32_t>(k >> 32);
+  }
   Given<E> given;
   given.load(a, row, static_cast<const E*>(a.z) + row * a.stride);
   const Stat o = joined<ENT>(sl, row, cl);
   const RowStat r = row_stat<ENT>(o);
-  if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
+  if (threadIdx.x == 0) { score_outputs(a, row, given, o, r); tb.n = 0; }
   if (a.K == 0) return;
+  const uint32_t least = ~wave_max(~hi);                               // of the upper halves, then of the lower ones beside it
+  const uint64_t bound = static_cast<uint64_t>(least) << 32 | ~wave_max(hi == least ? ~lo : 0u);
+  __syncthreads();
   alternatives<256>(a, row, r, [&](auto&& out) {
-    if (n <= 256) {                                                   // no bound needed: rank them all
-      if (threadIdx.x < n) tb.list[threadIdx.x] = mine[0];
-      __syncthreads();
-      ranked<256>(tb, n, [&](uint64_t k, uint32_t rank) { if (k && rank < a.K) out(rank, k); });
-      return;
-    }
-    auto each = [&](auto&& f) {
+    block_top_from<256>(bound, a.K, tb, [&](auto&& f) {
 #pragma unroll
       for (uint32_t j = 0; j < M; ++j) if (mine[j]) f(mine[j]);
       for (uint32_t i = threadIdx.x + 256 * M; i < n; i += 256) { const uint64_t k = key[i]; if (k) f(k); }
-    };
-    uint64_t most = 0;
-    each([&](uint64_t k) { most = max(most, k); });
-    block_top<256, CAND_CAP>(n, a.K, most ? key_value(most) : -INFINITY, tb,
-                             [&](float tau, auto&& f) { each([&](uint64_t k) { if (key_value(k) >= tau) f(k); }); }, out);
+    }, out);
   });
 }
 
@@ -816,9 +819,9 @@ __device__ __forceinline__ void gradient_outputs(const GradArgs& a, uint32_t row
   if (a.logprob && o.t == 0xFFFFFFFFu) a.logprob[row] = given < 0 ? 0.0f : NAN;
 }
 
-// A block per row, held in its registers: one read, one write.  (8 vectors: 64 VGPRs, so that two blocks of 1024 are resident.)
+// A block per row, held in its registers: one read, one write.
 template <class E, int TH, int NV, bool ENT>
-__global__ __launch_bounds__(TH, NV <= 8 ? 8 : 4) void k_gradient_held(GradArgs a) {
+__global__ __launch_bounds__(TH) void k_gradient_held(GradArgs a) {
   __shared__ Stat box[16];
   const float cl = a.c * LOG2E;
   const uint64_t row = block_number();
@@ -875,10 +878,11 @@ struct TeacherBox {
   int32_t key[HASH_SIZE];          // the classes, each in the first free slot from its own on
   uint32_t first[HASH_SIZE];       // where a class stands first
   int32_t index[TEACHER_MAX];      // -1: no entry
+  float value[TEACHER_MAX];        // the teacher's logits
   float z[TEACHER_MAX];            // the student's logits there
-  float q[TEACHER_MAX], p[TEACHER_MAX];      // the teacher's and the student's probabilities
+  float q[TEACHER_MAX];            // the teacher's probabilities
   uint32_t bad, some;              // an index outside; whether the row teaches anything
-  double lse, sum_q;
+  double lse, sum_q;               // of the teacher's logits
   float m, L, F, m_all;
   double t_all;                    // sum of exp(c (z_i - m_all)) over the whole row
 };
@@ -887,13 +891,21 @@ template <int TH> constexpr int entries_of() { return (TEACHER_MAX + TH - 1) / T
 // The teacher's entries of a row: their classes in the box; entries that are none, and classes that stood earlier in the row, have
 // index -1.  The student's logits there are on their way to x: teacher_logits() puts them into the box.  Ends behind a barrier.
 template <int TH>
-__device__ __forceinline__ void load_entries(const DistillArgs& a, uint32_t row, int32_t (&idx)[entries_of<TH>()]) {
+struct Entries {
+  int32_t index[entries_of<TH>()];
+  float value[entries_of<TH>()];
+  __device__ __forceinline__ void load(const DistillArgs& a, uint64_t row) {
 #pragma unroll
-  for (int j = 0; j < entries_of<TH>(); ++j) idx[j] = a.index[static_cast<uint64_t>(row) * a.K + min(threadIdx.x + j * TH, a.K - 1)];
-}
+    for (int j = 0; j < entries_of<TH>(); ++j) {
+      const uint64_t at = row * a.K + min(threadIdx.x + j * TH, a.K - 1);
+      index[j] = a.index[at];
+      value[j] = a.value[at];
+    }
+  }
+};
 template <class E, int TH>
-__device__ __forceinline__ void teacher_entries(const DistillArgs& a, const E* z, TeacherBox& b, int32_t (&idx)[entries_of<TH>()],
-                                                E (&x)[entries_of<TH>()]) {
+__device__ __forceinline__ void teacher_entries(const DistillArgs& a, const E* z, TeacherBox& b, Entries<TH>& e, E (&x)[entries_of<TH>()]) {
+  int32_t (&idx)[entries_of<TH>()] = e.index;
   constexpr int M = entries_of<TH>();
   uint32_t shift = 26;                                                // 4 slots per entry, 64 at least
   while (1u << (32 - shift) < 4 * a.K) --shift;
@@ -924,7 +936,7 @@ __device__ __forceinline__ void teacher_entries(const DistillArgs& a, const E* z
 #pragma unroll
   for (int j = 0; j < M; ++j) {
     const uint32_t k = threadIdx.x + j * TH;
-    if (k < a.K) b.index[k] = idx[j] >= 0 && b.first[slot[j]] == k ? idx[j] : -1;
+    if (k < a.K) { b.index[k] = idx[j] >= 0 && b.first[slot[j]] == k ? idx[j] : -1; b.value[k] = e.value[j]; }
   }
   lds_barrier();
 }
@@ -995,42 +1007,44 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 // the teacher's probabilities; without any mass (no entries, or all of them -inf) and without the rest as a class the row teaches nothing
 template <bool REST>
-__device__ __forceinline__ void teacher_probabilities(const DistillArgs& a, uint32_t row, TeacherBox& b) {
-  const float* value = a.value + static_cast<uint64_t>(row) * a.K;
-  double lse = 0.0;
+__device__ __forceinline__ void teacher_probabilities(const DistillArgs& a, uint64_t row, TeacherBox& b) {
+  double lse = 0.0, top = 0.0;
   bool some = true;
-  if (REST) lse = a.tlse[row];
+  if (REST) top = lse = a.tlse[row];
   else {
     float most = -INFINITY;
     bool any = false;
 #pragma unroll 1
     for (uint32_t k = lane_id(); k < a.K; k += 64)
-      if (b.index[k] >= 0) { most = fmaxf(most, value[k]); any |= !(value[k] == -INFINITY); }
+      if (b.index[k] >= 0) { most = fmaxf(most, b.value[k]); any |= !(b.value[k] == -INFINITY); }
     some = __any(any);                                                // (a NaN is not -inf)
-    const double top = static_cast<double>(wave_max_f(most)) * a.ct;
-    double t = 0.0;
-#pragma unroll 1
-    for (uint32_t k = lane_id(); k < a.K; k += 64)
-      if (b.index[k] >= 0 && some) t += exp(static_cast<double>(value[k]) * a.ct - top);
-    lse = top + log(wave_sum_d(t));
+    top = static_cast<double>(wave_max_f(most)) * a.ct;
   }
-  double sum_q = 0.0;
+  double* e = reinterpret_cast<double*>(b.key);                       // (the slots have done their work)
+  static_assert(sizeof b.key >= TEACHER_MAX * sizeof(double), "room for an exponential per entry");
+  double sum = 0.0;
 #pragma unroll 1
   for (uint32_t k = lane_id(); k < a.K; k += 64)
     if (b.index[k] >= 0) {
-      const double q = some ? exp(static_cast<double>(value[k]) * a.ct - lse) : 0.0;
-      b.q[k] = static_cast<float>(q);
-      sum_q += q;
+      const double x = some ? exp(static_cast<double>(b.value[k]) * a.ct - top) : 0.0;
+      if (REST) b.q[k] = static_cast<float>(x);
+      else e[k] = x;
+      sum += x;
     }
-  sum_q = wave_sum_d(sum_q);
-  if (lane_id() == 0) { b.lse = lse; b.sum_q = sum_q; b.some = some; }
+  sum = wave_sum_d(sum);
+  if (!REST) {
+#pragma unroll 1
+    for (uint32_t k = lane_id(); k < a.K; k += 64) if (b.index[k] >= 0) b.q[k] = some ? static_cast<float>(e[k] / sum) : 0.0f;
+    lse = top + log(sum);
+  }
+  if (lane_id() == 0) { b.lse = lse; b.sum_q = sum; b.some = some; }
   wave_lds_fence();
 }
 
-// What the row's statistics `o` (of the whole row, or with REST of the classes outside) make of it: p, m, L, F (dz_i = c g F softmax_i
-// over what `o` covers), m_all, t_all.  Statistics that the caller kept (a.stats_in) take the place of `o`.
+// What the row's statistics `o` (of the whole row, or with REST of the classes outside) make of it: m, L, F (dz_i = c g F softmax_i over
+// what `o` covers), m_all, t_all.  Statistics that the caller kept (a.stats_in) take the place of `o`.
 template <bool REST>
-__device__ __forceinline__ void student_probabilities(const DistillArgs& a, uint32_t row, Stat o, TeacherBox& b) {
+__device__ __forceinline__ void student_sums(const DistillArgs& a, uint64_t row, Stat o, TeacherBox& b) {
   const double c = a.c;
   double F = b.some ? 1.0 : 0.0, t = o.s;
   float m_all = o.m, L = logf(o.s);
@@ -1053,9 +1067,6 @@ __device__ __forceinline__ void student_probabilities(const DistillArgs& a, uint
     if (o.s == 0.0f) F = 0.0;                                         // nothing outside: the rest is left out
     if (b.sum_q != b.sum_q) F = NAN;
   }
-#pragma unroll 1
-  for (uint32_t k = lane_id(); k < a.K; k += 64)
-    if (b.index[k] >= 0) b.p[k] = t == 0.0 ? 0.0f : static_cast<float>(exp((static_cast<double>(b.z[k]) - m_all) * c) / t);
   if (t == 0.0) F = 0.0;                                              // a row that leaves nothing
   if (b.bad) F = NAN;
   if (lane_id() == 0) { b.m = o.m; b.L = L; b.F = static_cast<float>(F); b.m_all = m_all; b.t_all = t; }
@@ -1063,8 +1074,7 @@ __device__ __forceinline__ void student_probabilities(const DistillArgs& a, uint
 }
 
 template <bool REST>
-__device__ __forceinline__ float distill_loss(const DistillArgs& a, uint32_t row, Stat o, const TeacherBox& b) {
-  const float* value = a.value + static_cast<uint64_t>(row) * a.K;
+__device__ __forceinline__ float distill_loss(const DistillArgs& a, Stat o, const TeacherBox& b) {
   const double c = a.c, m_all = b.m_all, t = b.t_all, L = log(t);
   double loss = 0.0;
   if (REST || b.some) {
@@ -1072,7 +1082,7 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, uint32_t row
     for (uint32_t k = lane_id(); k < a.K; k += 64) {
       if (b.index[k] < 0 || b.q[k] == 0.0f) continue;
       const double x = b.z[k], lp = t == t && x == -INFINITY ? -INFINITY : (x - m_all) * c - L;
-      loss += b.q[k] * (static_cast<double>(value[k]) * a.ct - b.lse - lp);
+      loss += b.q[k] * (static_cast<double>(b.value[k]) * a.ct - b.lse - lp);
     }
   }
   loss = wave_sum_d(loss);
@@ -1088,10 +1098,11 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, uint32_t row
 
 // the gradient in an entry's class
 template <bool REST>
-__device__ __forceinline__ float taught(const TeacherBox& b, uint32_t k, float g) {
+__device__ __forceinline__ float taught(const TeacherBox& b, uint32_t k, float g, float cl) {
   if (b.bad) return NAN;
   if (b.t_all == 0.0 || (!REST && !b.some)) return 0.0f;               // a row that leaves nothing, or teaches nothing
-  return g * (b.p[k] - b.q[k]);
+  const float p = exp2_((b.z[k] - b.m_all) * cl) / static_cast<float>(b.t_all);
+  return g * (p - b.q[k]);
 }
 
 __device__ __forceinline__ void distill_outputs(const DistillArgs& a, uint32_t row, const TeacherBox& b, float loss) {
@@ -1113,35 +1124,36 @@ __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
   const uint64_t row = block_number();
   if (row >= a.rows) return;
   const E* z = static_cast<const E*>(a.z) + row * a.stride;
-  int32_t idx[entries_of<TH>()];
-  load_entries<TH>(a, row, idx);                                      // first: they come back first
+  const float g = a.c * (a.g ? a.g[row] : 1.0f);
+  Entries<TH> e;
+  e.load(a, row);                                                     // first: they come back first
   H h;
   h.load(z, a.vocab);
   E x[entries_of<TH>()];
-  teacher_entries<E, TH>(a, z, b, idx, x);
-  if (threadIdx.x < 64) teacher_probabilities<REST>(a, row, b);     // while the row is on its way
+  teacher_entries<E, TH>(a, z, b, e, x);
+  if (REST && !a.stats_in) mark<TH, H::N>(mask, 0, a.vocab, h.first, a.K, [&](uint32_t k) { return b.index[k]; });
+  if (threadIdx.x < 64) teacher_probabilities<REST>(a, row, b);       // while the others sum
   Stat o = stat_none();
   if (!a.stats_in) {
-    if (REST) mark<TH, H::N>(mask, 0, a.vocab, h.first, a.K, [&](uint32_t k) { return b.index[k]; });
     float most[NV / H::U];
     o = h.template stat<false>(cl, [&](uint32_t v) { return REST ? marks<H::N>(mask, v) : 0u; }, most);
   }
   teacher_logits<E, TH>(a, b, x);
   o = block_stat<false, TH>(o, cl, box);
   if (TH == 64) __syncthreads();
-  if (threadIdx.x < 64) student_probabilities<REST>(a, row, o, b);
+  if (threadIdx.x < 64) student_sums<REST>(a, row, o, b);
   __syncthreads();
-  if (threadIdx.x < 64 && !a.stats_in) {
-    const float loss = distill_loss<REST>(a, row, o, b);
+  const float L = b.L;
+  E* dz = static_cast<E*>(a.dz) + row * a.dstride;
+  if (a.dz) h.template gradient<false>(dz, Gradient{cl, b.m, L == -INFINITY ? 0.0f : L * LOG2E, g * b.F, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
+  if (threadIdx.x < 64 && !a.stats_in) {                              // while the stores are on their way
+    const float loss = distill_loss<REST>(a, o, b);
     if (threadIdx.x == 0) distill_outputs(a, row, b, loss);
   }
   if (a.dz) {
-    E* dz = static_cast<E*>(a.dz) + row * a.dstride;
-    const float g = a.c * (a.g ? a.g[row] : 1.0f), L = b.L;
-    h.template gradient<false>(dz, Gradient{cl, b.m, L == -INFINITY ? 0.0f : L * LOG2E, g * b.F, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
-    __syncthreads();                                                // the entries' classes are written again
+    __syncthreads();                                                  // the entries' classes are written again
     for (uint32_t k = threadIdx.x; k < a.K; k += TH)
-      if (b.index[k] >= 0) dz[b.index[k]] = static_cast<E>(taught<REST>(b, k, g));
+      if (b.index[k] >= 0) dz[b.index[k]] = static_cast<E>(taught<REST>(b, k, g, cl));
   }
 }
 
@@ -1174,30 +1186,32 @@ __global__ __launch_bounds__(256) void k_distill_join(DistillArgs a, Slices sl, 
   const float cl = a.c * LOG2E;
   const uint64_t row = block_number();
   if (row >= a.rows) return;
-  int32_t idx[1];
-  load_entries<256>(a, row, idx);
+  const float g = a.c * (a.g ? a.g[row] : 1.0f);
+  Entries<256> e;
+  e.load(a, row);
   E x[1];
-  teacher_entries<E, 256>(a, static_cast<const E*>(a.z) + row * a.stride, b, idx, x);
+  teacher_entries<E, 256>(a, static_cast<const E*>(a.z) + row * a.stride, b, e, x);
+  Stat o = stat_none();
+  if (threadIdx.x < 64) {
+    if (!a.stats_in) o = joined<false>(sl, row, cl);
+    teacher_probabilities<REST>(a, row, b);
+  }
   teacher_logits<E, 256>(a, b, x);
   __syncthreads();
-  if (threadIdx.x < 64) {
-    const Stat o = a.stats_in ? stat_none() : joined<false>(sl, row, cl);
-    teacher_probabilities<REST>(a, row, b);
-    student_probabilities<REST>(a, row, o, b);
-    if (!a.stats_in) {
-      const float loss = distill_loss<REST>(a, row, o, b);
-      if (threadIdx.x == 0) distill_outputs(a, row, b, loss);
-    }
-  }
+  if (threadIdx.x < 64) student_sums<REST>(a, row, o, b);
   __syncthreads();
   if (w.row) {
-    const float g = a.c * (a.g ? a.g[row] : 1.0f), L = b.L;
+    const float L = b.L;
     if (threadIdx.x == 0) w.row[row] = Stat4{b.m, L == -INFINITY ? 0.0f : L * LOG2E, g * b.F, 0.0f};
     const uint32_t k = threadIdx.x;
     if (k < a.K) {
       w.index[static_cast<uint64_t>(row) * a.K + k] = b.index[k];
-      w.value[static_cast<uint64_t>(row) * a.K + k] = b.index[k] >= 0 ? taught<REST>(b, k, g) : 0.0f;
+      w.value[static_cast<uint64_t>(row) * a.K + k] = b.index[k] >= 0 ? taught<REST>(b, k, g, cl) : 0.0f;
     }
+  }
+  if (threadIdx.x < 64 && !a.stats_in) {
+    const float loss = distill_loss<REST>(a, o, b);
+    if (threadIdx.x == 0) distill_outputs(a, row, b, loss);
   }
 }
 
