@@ -20,6 +20,7 @@ namespace {
 constexpr uint64_t GRID_X = 1u << 20;              // blocks in a row of the grid (a launch counts its threads in 32 bits)
 constexpr uint32_t FEW_ROWS = 256;                 // fewer rows than this leave compute units without a block
 constexpr uint32_t WANTED_BLOCKS = 1024;           // blocks of 256 threads that keep the chip busy
+constexpr uint64_t CACHE_BYTES = 256ull << 20;     // the last cache before the memory
 constexpr uint64_t MIN_SLICE = 4096;               // bytes: 16 a thread
 
 bool scale_ok(float c) { return c >= 0x1p-100f && c <= 0x1p100f; }
@@ -201,6 +202,7 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
   const Plan plan = top ? plan_top(z) : plan_stats(z);
   const Slices sl = lay_out(z, plan, top, 0, workspace).sl;
   const dim3 rows = grid_of(z->rows);
+  const bool last = !stats || z->rows * row_bytes(z) > CACHE_BYTES;      // with `stats` the gradient is to follow, which finds the rows in the cache
   pick_type(z, [&](auto e) {
     typedef decltype(e) E;
     const uint32_t nvec = z->vocab / Elem<E>::N;
@@ -218,13 +220,13 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
           if constexpr (th() * nv() <= 8192) k_score_held<E, th(), nv(), ent()><<<rows, th(), 0, stream>>>(a);
         });
       } else if (top) {
-        k_score<E, 1024, ent(), true><<<rows, 1024, 0, stream>>>(a);
-      } else if (nvec <= 256) {
-        k_score<E, 64, ent(), false><<<rows, 64, 0, stream>>>(a);
-      } else if (nvec <= 2048) {
-        k_score<E, 256, ent(), false><<<rows, 256, 0, stream>>>(a);
+        k_score<false, E, 1024, ent(), true><<<rows, 1024, 0, stream>>>(a);
       } else {
-        k_score<E, 1024, ent(), false><<<rows, 1024, 0, stream>>>(a);
+        pick_bool(last, [&](auto once) {
+          if (nvec <= 256) k_score<once(), E, 64, ent(), false><<<rows, 64, 0, stream>>>(a);
+          else if (nvec <= 2048) k_score<once(), E, 256, ent(), false><<<rows, 256, 0, stream>>>(a);
+          else k_score<once(), E, 1024, ent(), false><<<rows, 1024, 0, stream>>>(a);
+        });
       }
     });
   });

@@ -121,8 +121,17 @@ template <> struct Elem<_Float16> {
 
 // values before the first whole word
 template <class E> __device__ __forceinline__ uint32_t odd_ones(const E* z) { return sizeof(E) == 2 && (reinterpret_cast<uintptr_t>(z) & 2) ? 1 : 0; }
-template <class E> __device__ __forceinline__ raw4 load16(const E* p) { return *reinterpret_cast<const typename Elem<E>::mem*>(p); }
-template <class E> __device__ __forceinline__ void store16(E* p, raw4 r) { *reinterpret_cast<typename Elem<E>::mem*>(p) = r; }
+// LAST: the value is not read again, so it need not be kept in the caches (k_score, 4,096 rows of 256 KB 191 / 181 us; k_gradient_apply
+// behind k_score 584 / 555 together).  Not where a second kernel reads the row (slices and pieces of 300 rows of 600 KB 106 / 98).
+template <bool LAST, class E> __device__ __forceinline__ raw4 load16(const E* p) {
+  const typename Elem<E>::mem* m = reinterpret_cast<const typename Elem<E>::mem*>(p);
+  if constexpr (LAST) return __builtin_nontemporal_load(m);
+  else return *m;
+}
+// gradients are not read here again (8,192 rows of 64 KB 177 / 171 us, 300 of 400 KB in pieces 73 / 61)
+template <class E> __device__ __forceinline__ void store16(E* p, raw4 r) {
+  __builtin_nontemporal_store(static_cast<typename Elem<E>::mem>(r), reinterpret_cast<typename Elem<E>::mem*>(p));
+}
 
 // ---------------------------------------------------------------------------------------------
 // statistics
@@ -234,7 +243,7 @@ __device__ __forceinline__ RowStat row_stat(Stat o) {
 // ---------------------------------------------------------------------------------------------
 // whole(v, r): the thread's vectors v, v + TH, ...; vector v begins at value first + v N, those from nvec on hold -inf.  Then at most one call
 // single(index, value) for the thread's value before or behind the vectors.
-template <class E, int TH, int U, class F, class G>
+template <bool LAST, class E, int TH, int U, class F, class G>
 __device__ __forceinline__ void walk(const E* z, uint32_t n, uint32_t first, F&& whole, G&& single) {
   constexpr int N = Elem<E>::N;
   const uint32_t nvec = (n - first) / N;
@@ -244,7 +253,7 @@ __device__ __forceinline__ void walk(const E* z, uint32_t n, uint32_t first, F&&
     for (int u = 0; u < U; ++u) {
       r[u] = raw4{Elem<E>::MINUS_INF, Elem<E>::MINUS_INF, Elem<E>::MINUS_INF, Elem<E>::MINUS_INF};
       const uint32_t v = v0 + u * TH;
-      if (v < nvec) r[u] = load16(z + first + static_cast<uint64_t>(v) * N);
+      if (v < nvec) r[u] = load16<LAST>(z + first + static_cast<uint64_t>(v) * N);
     }
     whole(v0, r);
   }
@@ -252,11 +261,11 @@ __device__ __forceinline__ void walk(const E* z, uint32_t n, uint32_t first, F&&
   if (i < n) single(i, static_cast<float>(z[i]));
 }
 
-template <class E, int TH, bool ENT>
+template <bool LAST, class E, int TH, bool ENT>
 __device__ __forceinline__ Stat pass_stat(const E* z, uint32_t n, float cl) {
   constexpr int N = Elem<E>::N, U = 4;
   Stat o = stat_none();
-  walk<E, TH, U>(z, n, odd_ones(z),
+  walk<LAST, E, TH, U>(z, n, odd_ones(z),
     [&](uint32_t, const raw4* r) {
       float v[U * N];
 #pragma unroll
@@ -280,7 +289,7 @@ struct NoneOut { __device__ __forceinline__ uint32_t operator()(uint32_t) const 
 // A piece of a row that the block holds in registers, NV vectors a thread and the values behind the last whole vector one a thread: it
 // is read from memory once, whatever is made of it.  load() only starts the loads; loads past the end go to the last vector, and
 // settle() makes -inf of them.
-template <class E, int TH, int NV>
+template <bool LAST, class E, int TH, int NV>
 struct Held {
   static constexpr int N = Elem<E>::N;
   static constexpr uint32_t SIZE = TH * NV * N;                        // values in whole vectors
@@ -293,7 +302,7 @@ struct Held {
     n = n_; first = odd_ones(z); nvec = (n - first) / N;
     if (nvec) {
 #pragma unroll
-      for (int u = 0; u < NV; ++u) r[u] = load16(z + first + static_cast<uint64_t>(min(vec(u), nvec - 1)) * N);
+      for (int u = 0; u < NV; ++u) r[u] = load16<LAST>(z + first + static_cast<uint64_t>(min(vec(u), nvec - 1)) * N);
     }
     last = *reinterpret_cast<const typename Elem<E>::bits*>(z + min(last_index(), n - 1));
   }
@@ -558,7 +567,7 @@ __device__ __forceinline__ void row_top(const E* z, uint32_t n, uint32_t K, floa
   constexpr int N = Elem<E>::N, U = 4;
   const uint32_t first = odd_ones(z), nvec = (n - first) / N;
   block_top<TH, CAP>(n, K, most, b, [&](float tau, auto&& f) {
-    walk<E, TH, U>(z, n, first,
+    walk<true, E, TH, U>(z, n, first,
       [&](uint32_t v0, const raw4* r) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -636,7 +645,7 @@ __device__ __forceinline__ void alternatives(const ScoreArgs& a, uint32_t row, c
 }
 
 // A block per row, which it walks along (with alternatives it reads the threads' shares that hold candidates again).
-template <class E, int TH, bool ENT, bool TOP>
+template <bool LAST, class E, int TH, bool ENT, bool TOP>
 __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
   __shared__ Stat box[16];
   __shared__ TopBox<TOP ? CAND_CAP : 1> tb;
@@ -646,7 +655,7 @@ __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
   const E* z = static_cast<const E*>(a.z) + row * a.stride;
   Given<E> given;
   given.load(a, row, z);
-  const Stat mine = pass_stat<E, TH, ENT>(z, a.vocab, cl);
+  const Stat mine = pass_stat<LAST && !TOP, E, TH, ENT>(z, a.vocab, cl);
   const Stat o = block_stat<ENT, TH>(mine, cl, box);
   const RowStat r = row_stat<ENT>(o);
   if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
@@ -667,10 +676,10 @@ __global__ __launch_bounds__(TH) void k_score_held(ScoreArgs a) {
   if (row >= a.rows) return;
   const E* z = static_cast<const E*>(a.z) + row * a.stride;
   Given<E> given;
-  Held<E, TH, NV> h;
+  Held<true, E, TH, NV> h;
   h.load(z, a.vocab);
   given.load(a, row, z);
-  float most[NV / Held<E, TH, NV>::U];
+  float most[NV / Held<true, E, TH, NV>::U];
   const Stat mine = h.template stat<ENT>(cl, NoneOut(), most);
   const Stat o = block_stat<ENT, TH>(mine, cl, box);
   const RowStat r = row_stat<ENT>(o);
@@ -707,11 +716,11 @@ __global__ __launch_bounds__(256) void k_slice_stats(ScoreArgs a, Slices sl) {
     const Stat o = block_stat<ENT, 256>(mine, cl, box);
     if (threadIdx.x == 0) sl.part[p] = Stat4{o.m, o.s, o.w, 0.0f};
   };
-  if constexpr (NV == 0) hand_over(pass_stat<E, 256, ENT>(z, n, cl));
+  if constexpr (NV == 0) hand_over(pass_stat<false, E, 256, ENT>(z, n, cl));
   else {
-    Held<E, 256, NV> h;
+    Held<true, E, 256, NV> h;
     h.load(z, n);
-    float most[NV / Held<E, 256, NV>::U];
+    float most[NV / Held<true, E, 256, NV>::U];
     const Stat mine = h.template stat<ENT>(cl, NoneOut(), most);
     hand_over(mine);
     uint64_t* key = sl.key + p * a.K;
@@ -827,7 +836,7 @@ __global__ __launch_bounds__(TH) void k_gradient_held(GradArgs a) {
   const uint64_t row = block_number();
   if (row >= a.rows) return;
   const RowWeights w = row_weights<ENT>(a, row);
-  Held<E, TH, NV> h;
+  Held<false, E, TH, NV> h;
   h.load(static_cast<const E*>(a.z) + row * a.stride, a.vocab);
   const RowStat r = row_stat<ENT>(block_stat<ENT, TH>(h.template stat<ENT>(cl), cl, box));
   const RowGradient o = row_gradient<ENT>(a, w, r);
@@ -840,7 +849,7 @@ __global__ __launch_bounds__(TH) void k_gradient_held(GradArgs a) {
 template <class E, bool ENT>
 __global__ __launch_bounds__(256) void k_gradient_apply(GradArgs a, Slices sl) {
   constexpr int NV = 4;
-  typedef Held<E, 256, NV> H;
+  typedef Held<true, E, 256, NV> H;
   const uint32_t per = (a.vocab + H::SIZE - 1) / H::SIZE;
   const uint64_t pieces = static_cast<uint64_t>(a.rows) * per;
   const uint64_t p = block_number();
@@ -975,7 +984,7 @@ __device__ __forceinline__ Stat pass_rest(const E* z, uint32_t i0, uint32_t n, u
     const uint32_t len = min(n - s0, MASK_SPAN), first = odd_ones(z + s0), nvec = (len - first) / N;
     if (s0) __syncthreads();
     mark<TH, N>(mask, i0 + s0, len, first, K, index);
-    walk<E, TH, U>(z + s0, len, first,
+    walk<false, E, TH, U>(z + s0, len, first,
       [&](uint32_t v0, const raw4* r) {
         float v[U * N];
 #pragma unroll
@@ -1116,7 +1125,7 @@ __device__ __forceinline__ void distill_outputs(const DistillArgs& a, uint32_t r
 // A block per row, held in its registers.  REST: what the teacher's entries leave over is one more class.
 template <class E, int TH, int NV, bool REST>
 __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
-  typedef Held<E, TH, NV> H;
+  typedef Held<false, E, TH, NV> H;
   __shared__ Stat box[16];
   __shared__ TeacherBox b;
   __shared__ uint32_t mask[REST ? mask_words(H::SIZE + 8) : 1];
@@ -1169,7 +1178,7 @@ __global__ __launch_bounds__(256) void k_distill_slices(DistillArgs a, Slices sl
   const uint32_t row = static_cast<uint32_t>(p / sl.S), i0 = static_cast<uint32_t>(p % sl.S) * sl.len, n = min(a.vocab - i0, sl.len);
   const E* z = static_cast<const E*>(a.z) + row * a.stride + i0;
   const int32_t* index = a.index + static_cast<uint64_t>(row) * a.K;
-  Stat o = REST ? pass_rest<E, 256>(z, i0, n, a.K, cl, mask, [&](uint32_t k) { return index[k]; }) : pass_stat<E, 256, false>(z, n, cl);
+  Stat o = REST ? pass_rest<E, 256>(z, i0, n, a.K, cl, mask, [&](uint32_t k) { return index[k]; }) : pass_stat<false, E, 256, false>(z, n, cl);
   o = block_stat<false, 256>(o, cl, box);
   if (threadIdx.x == 0) sl.part[p] = Stat4{o.m, o.s, o.w, 0.0f};
 }
@@ -1218,7 +1227,7 @@ __global__ __launch_bounds__(256) void k_distill_join(DistillArgs a, Slices sl, 
 template <class E>
 __global__ __launch_bounds__(256) void k_distill_apply(DistillArgs a, Taught w) {
   constexpr int NV = 4;
-  typedef Held<E, 256, NV> H;
+  typedef Held<true, E, 256, NV> H;
   const uint32_t per = (a.vocab + H::SIZE - 1) / H::SIZE;
   const uint64_t pieces = static_cast<uint64_t>(a.rows) * per;
   const uint64_t p = block_number();
