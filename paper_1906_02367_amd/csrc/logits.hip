@@ -28,16 +28,21 @@ uint64_t align_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 uint32_t elem_size(uint32_t dtype) { return dtype == QSL_F32 ? 4 : 2; }
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// rows that do not overlap and whose offsets, in elements, stay below 2^48
+bool stride_ok(const qsl_logits* z, uint64_t stride) {
+  return stride >= z->vocab && stride < 1ull << 48 && (z->rows <= 1 || stride <= (1ull << 48) / z->rows);
+}
+
 bool logits_ok(const qsl_logits* z) {
   if (!z || z->dtype > QSL_F16 || z->vocab == 0 || z->vocab >= 1u << 31 || z->rows >= 1u << 31) return false;
-  if (z->stride < z->vocab || z->stride >= 1ull << 40 || !scale_ok(z->scale)) return false;
+  if (!stride_ok(z, z->stride) || !scale_ok(z->scale)) return false;
   return z->rows == 0 || (z->data && aligned(z->data, elem_size(z->dtype)));
 }
 
 // dlogits are the logits, or lie apart from them
 bool gradient_ok(const qsl_logits* z, const void* dz, uint64_t dstride) {
   const uint64_t es = elem_size(z->dtype);
-  if (dstride < z->vocab || dstride >= 1ull << 40 || !aligned(dz, es)) return false;
+  if (!stride_ok(z, dstride) || !aligned(dz, es)) return false;
   if (z->rows == 0) return true;
   if (!dz) return false;
   if (dz == z->data && (dstride == z->stride || z->rows == 1)) return true;

@@ -266,6 +266,54 @@ def test_offsets_beyond_32_bits(B):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("N,V,dtype", [(2, 1_100_003, "fp32"), (1, 17_000_003, "bf16")])
+def test_very_long_rows(B, N, V, dtype):
+    """More than 64 slices of what a block holds: rows that are walked along; slices of several spans of marked classes."""
+    dt = TYPES[dtype]
+    z, t = logits_of(N, V, dt), targets_of(N, V)
+    for K in (0, 100):
+        check_score(z, t, K, 1.0, run_score(B, z, t, K, 1.0), f"{N} x {V}, K = {K}")
+    g = torch.linspace(0.5, 1, N, device=dev)
+    r = X.rows_of(z, 1.0)
+    dz = torch.empty_like(z)
+    B.token_logprobs_backward(z, t, dz, grad_logprob=g)
+    X.check(dz, *X.logprob_gradient(r, t, g, None, dt), "gradient")
+    gen = torch.Generator().manual_seed(1)
+    index = torch.randint(0, V, (N, 200), generator=gen).to(torch.int32)
+    value = 20.0 + torch.rand(N, 200, generator=gen)
+    lse = torch.full((N,), 26.0)
+    loss, tol_loss, want, tol = X.distill(r, index, value, 1.0, lse, g.cpu(), dt)
+    got = new(N)
+    B.distill_backward(z, index.to(dev), value.to(dev), dz, teacher_lse=lse.to(dev), grad_loss=g, loss=got)
+    X.check(got, loss, tol_loss, "loss")
+    X.check(dz, want, tol, "gradient of the loss")
+
+
+def test_own_workspace(B):
+    """One workspace for calls that follow one another; a longer one than needed; the refusals of the binding."""
+    N, V, K = 3, 150001, 30
+    z, t = logits_of(N, V, torch.float32), targets_of(N, V)
+    index, value, lse = teacher_of(N, V, K)
+    need = B.logits_workspace_bytes(z, K)
+    assert need > 0
+    ws = torch.empty(need + 512, dtype=torch.uint8, device=dev)
+    a, b = run_score(B, z, t, K, 1.0), run_score(B, z, t, K, 1.0, workspace=ws)
+    for n in a:
+        assert torch.equal(a[n], b[n]), n
+    d1, d2 = torch.empty_like(z), torch.empty_like(z)
+    B.distill_backward(z, index, value, d1, teacher_lse=lse)
+    B.distill_backward(z, index, value, d2, teacher_lse=lse, workspace=ws)
+    assert torch.equal(d1, d2)
+    B.token_logprobs_backward(z, t, d1, grad_logprob=torch.ones(N, device=dev))
+    B.token_logprobs_backward(z, t, d2, grad_logprob=torch.ones(N, device=dev), workspace=ws)
+    assert torch.equal(d1, d2)
+    for bad in (ws[:need - 256], ws[8:]):
+        with pytest.raises(B.QslError):
+            B.distill_backward(z, index, value, d1, teacher_lse=lse, workspace=bad)
+    with pytest.raises(ValueError):
+        B.distill_backward(z, index, value, d1, teacher_lse=lse, workspace=ws.cpu())
+
+
 @pytest.mark.parametrize("N,V", [(1_100_000, 2), (70000, 3), (3000, 257), (1500, 4096)])
 def test_many_rows(B, N, V):
     z, t = logits_of(N, V, torch.bfloat16), targets_of(N, V)

@@ -47,7 +47,7 @@ def rows(**kw):
     return Logits(**d)
 
 
-BAD_ROWS = [dict(data=None), dict(data=A + 2), dict(data=A + 1, dtype=1), dict(stride=999), dict(stride=1 << 40), dict(vocab=0), dict(vocab=1 << 31, stride=1 << 32),
+BAD_ROWS = [dict(data=None), dict(data=A + 2), dict(data=A + 1, dtype=1), dict(stride=999), dict(stride=1 << 48), dict(stride=1 << 40, rows=1 << 30), dict(vocab=0), dict(vocab=1 << 31, stride=1 << 32),
             dict(rows=1 << 31), dict(dtype=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=1e-38)]
 
 
@@ -87,6 +87,38 @@ def test_gradient_arguments_that_are_refused(lib):
     assert call(dz=A, ds=1001) == INVALID                                 # the logits with another stride
     assert call(dz=A + 4) == INVALID and call(dz=A + 4 * 3999) == INVALID and call(dz=A - 4 * 3999) == INVALID     # overlapping them
     assert call(stats=A + 8) == INVALID and call(g=A + 2) == INVALID and call(h=A + 2) == INVALID
+
+
+def test_workspaces_that_are_refused(lib):
+    """Long rows are split, and the parts' results meet in the caller's workspace."""
+    z = C.byref(rows(vocab=200_000, stride=200_000, rows=2))
+    need = [lib.qsl_logits_workspace_bytes(z, top) for top in (0, 5, 128, 256)]
+    assert 0 < need[0] < need[1] < need[2] and all(n % 256 == 0 for n in need)
+    assert lib.qsl_logits_workspace_bytes(z, 257) == 0
+    t = C.byref(Teacher(A, A, None, 5, 1.0))
+    calls = [lambda top, ws, n: lib.qsl_token_logprobs(z, A, top, A, None, None, A if top else None, None, None, ws, n, None),
+             lambda top, ws, n: lib.qsl_token_logprobs_backward(z, A, A, None, None, None, None, 1 << 36, 200_000, ws, n, None),
+             lambda top, ws, n: lib.qsl_distill(z, t, A, None, ws, n, None),
+             lambda top, ws, n: lib.qsl_distill_backward(z, t, None, None, None, 1 << 36, 200_000, ws, n, None)]
+    for k, call in enumerate(calls):
+        top = 5 if k != 1 else 0
+        n = need[1] if k != 1 else need[0]
+        assert call(top, None, n) == INVALID and call(top, A + 128, n) == INVALID and call(top, A, n - 1) == TOO_SMALL, k
+    assert lib.qsl_logits_workspace_bytes(C.byref(rows(vocab=10, stride=10, rows=6000)), 5) == 0        # short rows need none
+    assert lib.qsl_logits_workspace_bytes(None, 0) == 0
+
+
+def test_no_rows_is_no_work(lib):
+    """Pointers that nothing is read from may be null; what says how rows look is checked all the same."""
+    z = C.byref(rows(rows=0, data=None))
+    assert lib.qsl_token_logprobs(z, None, 0, None, None, None, None, None, None, None, 0, None) == 0
+    assert lib.qsl_token_logprobs_backward(z, None, None, None, None, None, None, None, 1000, None, 0, None) == 0
+    t = C.byref(Teacher(None, None, None, 4, 1.0))
+    assert lib.qsl_distill(z, t, None, None, None, 0, None) == 0
+    assert lib.qsl_distill_backward(z, t, None, None, None, None, 1000, None, 0, None) == 0
+    assert lib.qsl_token_logprobs(z, None, 129, None, None, None, None, None, None, None, 0, None) == INVALID
+    assert lib.qsl_distill(z, C.byref(Teacher(None, None, None, 0, 1.0)), None, None, None, 0, None) == INVALID
+    assert lib.qsl_token_logprobs_backward(z, None, None, None, None, None, None, None, 999, None, 0, None) == INVALID
 
 
 def test_teachers_that_are_refused(lib):
