@@ -112,10 +112,10 @@ struct Plan {
   uint32_t S, len;
 };
 
-Plan plan_slices(const qsl_logits* z) {
+Plan plan_slices(const qsl_logits* z, uint64_t least = MIN_SLICE) {
   const uint64_t bytes = row_bytes(z), es = elem_size(z->dtype);
   uint64_t S = std::max<uint64_t>((bytes + SLICE_MAX - 1) / SLICE_MAX, WANTED_BLOCKS / std::max(z->rows, 1u));
-  S = std::min<uint64_t>({S, SLICES_MAX, (bytes + MIN_SLICE - 1) / MIN_SLICE});
+  S = std::min<uint64_t>({S, SLICES_MAX, (bytes + least - 1) / least});
   Plan p;
   p.split = true;
   // whole 4 KB: slices start where vectors do, and their threads are busy alike
@@ -130,7 +130,7 @@ constexpr Plan WHOLE = {false, 0, 0};
 // 1024 x 16 / slices: 2,048 rows of 200 KB, 64 alternatives 111 / 95; 2,048 of 256 KB, 20 alternatives 122 / 96; 64 of 256 KB 16 / 15.
 Plan plan_top(const qsl_logits* z) {
   const uint64_t bytes = row_bytes(z);
-  return bytes <= HELD_TOP_MAX || bytes > SLICES_MAX * SLICE_MAX ? WHOLE : plan_slices(z);
+  return bytes <= HELD_TOP_MAX || bytes > SLICES_MAX * SLICE_MAX ? WHOLE : plan_slices(z, 4 * MIN_SLICE);      // every slice's K have to be joined
 }
 // Statistics alone: a row need not be held.  Split where long rows are fewer than the blocks that are resident at once (300 rows of 800 KB: 54 us
 // by a block each, 45 split).

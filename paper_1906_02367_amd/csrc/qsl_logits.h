@@ -14,6 +14,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "qsl_device.h"
 
 using namespace qsl;
@@ -529,8 +531,9 @@ __device__ __forceinline__ void block_top_from(uint64_t bound, uint32_t K, TopBo
 // wave finds its upper 16 bits, by counting the maxima that reach a trial value; less than it will do as well.  Values of -inf count only where fewer than K others are left; of those the lowest indices are wanted, and they are among the first
 // K entries: a mask that leaves less than K classes does not make all others candidates.  If more than CAP entries are candidates (many equal or ordered values), the K-th largest of the first REFINE that found room
 // is the next bound: a larger one, since keys differ, and for entries in no particular order it leaves K / REFINE of them.
-template <int TH, uint32_t CAP, class S, class F>
-__device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, TopBox<CAP>& b, S&& scan, F&& out) {
+// OWN: `most` is the largest of what the thread's scan() goes through (else of any entries, no two threads' the same).
+template <int TH, uint32_t CAP, class OWN, class S, class F>
+__device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, TopBox<CAP>& b, OWN, S&& scan, F&& out) {
   constexpr uint32_t PER = TH > GROUPS ? TH / GROUPS : 1, G = TH / PER, M = G / 64;
   static_assert(PER == 1 || PER == 2 || PER == 4, "a group is a thread, or two or four lanes of a quad");
   float gm = most;
@@ -558,7 +561,7 @@ __device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, To
   }
   __syncthreads();
   const float tau = b.tau;
-  block_top_from<TH>(0, K, b, [&](auto&& f) { if (most >= tau) scan(tau, f); }, out);
+  block_top_from<TH>(0, K, b, [&](auto&& f) { if (!OWN::value || most >= tau) scan(tau, f); }, out);
 }
 
 // the same for a row in memory
@@ -566,7 +569,7 @@ template <class E, int TH, uint32_t CAP, class F>
 __device__ __forceinline__ void row_top(const E* z, uint32_t n, uint32_t K, float most, TopBox<CAP>& b, F&& out) {
   constexpr int N = Elem<E>::N, U = 4;
   const uint32_t first = odd_ones(z), nvec = (n - first) / N;
-  block_top<TH, CAP>(n, K, most, b, [&](float tau, auto&& f) {
+  block_top<TH, CAP>(n, K, most, b, std::true_type(), [&](float tau, auto&& f) {
     walk<true, E, TH, U>(z, n, first,
       [&](uint32_t v0, const raw4* r) {
 #pragma unroll
@@ -685,7 +688,7 @@ __global__ __launch_bounds__(TH) void k_score_held(ScoreArgs a) {
   const RowStat r = row_stat<ENT>(o);
   if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
   alternatives<TH>(a, row, r, [&](auto&& out) {
-    block_top<TH, CAP>(a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb,
+    block_top<TH, CAP>(a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb, std::true_type(),
                        [&](float tau, auto&& f) { h.at_least(tau, a.K, most, [&](uint32_t i, float x) { f(top_key(x, i)); }); }, out);
   });
 }
@@ -725,7 +728,7 @@ __global__ __launch_bounds__(256) void k_slice_stats(ScoreArgs a, Slices sl) {
     hand_over(mine);
     uint64_t* key = sl.key + p * a.K;
     for (uint32_t k = threadIdx.x; k < a.K; k += 256) if (k >= n) key[k] = 0;      // (of a slice with a NaN nobody looks at the keys)
-    block_top<256, CAND_CAP>(n, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb,
+    block_top<256, CAND_CAP>(n, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb, std::true_type(),
                              [&](float tau, auto&& f) { h.at_least(tau, a.K, most, [&](uint32_t i, float x) { f(top_key(x, i0 + i)); }); },
                              [&](uint32_t rank, uint64_t k) { key[rank] = k; });
   }
@@ -747,30 +750,25 @@ __global__ __launch_bounds__(256) void k_score_join(ScoreArgs a, Slices sl) {
   if (row >= a.rows) return;
   const uint32_t n = sl.S * a.K;
   const uint64_t* key = sl.key + row * n;
-  constexpr uint32_t M = 4;
+  constexpr uint32_t M = 8;
   uint64_t mine[M];
 #pragma unroll
   for (uint32_t j = 0; j < M; ++j) mine[j] = threadIdx.x + 256 * j < n ? key[threadIdx.x + 256 * j] : 0;
-  // The first ceil(K / S) of every slice are K entries or more, so the least of them is a bound (0 where a slice is shorter).
-  uint32_t lo = 0xFFFFFFFFu, hi = 0xFFFFFFFFu;
-  if (a.K && lane_id() < sl.S) {
-    const uint64_t k = key[lane_id() * a.K + (a.K + sl.S - 1) / sl.S - 1];
-    lo = static_cast<uint32_t>(k); hi = static_cast<uint32_t>(k >> 32);
-  }
+  // The bound comes from the first 256 / S of every slice, 193 of them or more: hardly ever are more of a slice's among the K.
+  const uint32_t place = threadIdx.x / sl.S;
+  const uint64_t sample = place < a.K && place < 256 / sl.S ? key[threadIdx.x % sl.S * a.K + place] : 0;
   Given<E> given;
   given.load(a, row, static_cast<const E*>(a.z) + row * a.stride);
   const Stat o = joined<ENT>(sl, row, cl);
   const RowStat r = row_stat<ENT>(o);
-  if (threadIdx.x == 0) { score_outputs(a, row, given, o, r); tb.n = 0; }
+  if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
   if (a.K == 0) return;
-  const uint32_t least = ~wave_max(~hi);                               // of the upper halves, then of the lower ones beside it
-  const uint64_t bound = static_cast<uint64_t>(least) << 32 | ~wave_max(hi == least ? ~lo : 0u);
-  __syncthreads();
   alternatives<256>(a, row, r, [&](auto&& out) {
-    block_top_from<256>(bound, a.K, tb, [&](auto&& f) {
+    block_top<256, CAND_CAP>(n, a.K, sample ? key_value(sample) : -INFINITY, tb, std::false_type(), [&](float tau, auto&& f) {
+      auto offer = [&](uint64_t k) { if (k && key_value(k) >= tau) f(k); };
 #pragma unroll
-      for (uint32_t j = 0; j < M; ++j) if (mine[j]) f(mine[j]);
-      for (uint32_t i = threadIdx.x + 256 * M; i < n; i += 256) { const uint64_t k = key[i]; if (k) f(k); }
+      for (uint32_t j = 0; j < M; ++j) offer(mine[j]);
+      for (uint32_t i = threadIdx.x + 256 * M; i < n; i += 256) offer(key[i]);
     }, out);
   });
 }
