@@ -7,7 +7,7 @@
 // A thread keeps (m, s, w) of the values that it has met, w = sum e_i y_i with y_i = c log2(e) (z_i - m), e_i = exp2(y_i): when m
 // grows by a step, y falls by delta = c log2(e) (m_old - m_new), hence s <- s 2^delta, w <- (w + s delta) 2^delta; H = L - ln 2 w / s.
 // All of it is held in 32 bits.  m starts at the lowest finite float, so a value of -inf has e = 0 and a row of them s = 0.
-// Part of the translation unit logits.hip; not a public header.
+// Part of the translation unit logits.hip; not a public header.  (It stands in a folder of its own beside the compression kernels'.)
 #pragma once
 
 #include <float.h>
@@ -647,7 +647,10 @@ __device__ __forceinline__ void alternatives(const ScoreArgs& a, uint32_t row, c
   });
 }
 
-// A block per row, which it walks along (with alternatives it reads the threads' shares that hold candidates again).
+// A block per row, which it walks along once: bound by memory (4,096 rows of 128,000 bf16 with the entropy 154 - 170 us, 6.2 - 6.8 TB/s; four
+// fifths of the vector issue slots, most of them for the exponentials).  Eight loads a thread under way instead of four cost
+// registers, hence waves: 214 us.  With alternatives (rows of more than 64 slices only) the threads that hold candidates read their
+// shares again.
 template <bool LAST, class E, int TH, bool ENT, bool TOP>
 __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
   __shared__ Stat box[16];
@@ -668,7 +671,9 @@ __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
     });
 }
 
-// Alternatives of a row that fits the block's registers.
+// Alternatives of a row that fits the block's registers: read once, ranked from there.  What ranking costs comes on top of the memory's time, as
+// far as other rows of the compute unit do not fill the gap: 4,096 rows of 32,000 bf16, 20 alternatives 48 us (their bytes 43), 128
+// alternatives 67; short rows are bound by the ranking's issue slots (16,384 rows of 2,000: 25 us, their bytes 11).
 template <class E, int TH, int NV, bool ENT>
 __global__ __launch_bounds__(TH) void k_score_held(ScoreArgs a) {
   constexpr uint32_t CAP = TH == 64 ? REFINE : CAND_CAP;               // (one wave: LDS would limit how many are resident)
@@ -704,7 +709,8 @@ struct Slices {
   uint64_t* key;                           // [rows, S, K] the slice's largest, largest first; 0: none
 };
 
-// NV = 0: the slice is walked along, without alternatives
+// NV = 0: the slice is walked along, without alternatives.  2,048 rows of 50,001 fp32 in four slices each, 64 alternatives: 78 us (5.2
+// TB/s), by one block of 1024 x 16 a row 110, since nothing fills the time in which that block ranks.
 template <class E, int NV, bool ENT>
 __global__ __launch_bounds__(256) void k_slice_stats(ScoreArgs a, Slices sl) {
   __shared__ Stat box[4];
@@ -742,6 +748,7 @@ __device__ __forceinline__ Stat joined(const Slices& sl, uint32_t row, float cl)
   return wave_stat<ENT>(o, cl);
 }
 
+// A block per row: a chain of reads and barriers, 5 us for 64 rows, 8 for 2,048.
 template <class E, bool ENT>
 __global__ __launch_bounds__(256) void k_score_join(ScoreArgs a, Slices sl) {
   __shared__ TopBox<CAND_CAP> tb;
@@ -826,7 +833,8 @@ __device__ __forceinline__ void gradient_outputs(const GradArgs& a, uint32_t row
   if (a.logprob && o.t == 0xFFFFFFFFu) a.logprob[row] = given < 0 ? 0.0f : NAN;
 }
 
-// A block per row, held in its registers: one read, one write.
+// A block per row, held in its registers: one read, one write, and bound by them (8,192 rows of 32,000 bf16 170 us, 6.2 TB/s, where a copy
+// reaches 5.2; walking along the row twice, the second time mostly in the caches, 214).
 template <class E, int TH, int NV, bool ENT>
 __global__ __launch_bounds__(TH) void k_gradient_held(GradArgs a) {
   __shared__ Stat box[16];
@@ -843,7 +851,9 @@ __global__ __launch_bounds__(TH) void k_gradient_held(GradArgs a) {
   if (threadIdx.x == 0) gradient_outputs(a, row, r, o, w.t);
 }
 
-// A piece of a row per block, the statistics known: the caller's, or (a.stats = NULL) joined from the slices'.
+// A piece of a row per block, the statistics known: the caller's, or (a.stats = NULL) joined from the slices'.  4,096 rows of 131,072 bf16
+// with the entropy 348 us, 6.2 TB/s.  (Rows from the last to the first, so that what the forward call read last is still in a cache:
+// 350.)
 template <class E, bool ENT>
 __global__ __launch_bounds__(256) void k_gradient_apply(GradArgs a, Slices sl) {
   constexpr int NV = 4;
@@ -1120,7 +1130,10 @@ __device__ __forceinline__ void distill_outputs(const DistillArgs& a, uint32_t r
   }
 }
 
-// A block per row, held in its registers.  REST: what the teacher's entries leave over is one more class.
+// A block per row, held in its registers.  REST: what the teacher's entries leave over is one more class.  8,192 rows of 32,000 bf16, 64 entries
+// and the rest 197 us, without the rest 194, against 170 of the gradient alone: between the sums and the gradient one wave works on the
+// entries, and two rows a compute unit do not hide all of it.  (Loss and entries' gradient before the stores, values read where
+// they are needed: 212.)
 template <class E, int TH, int NV, bool REST>
 __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
   typedef Held<false, E, TH, NV> H;
@@ -1164,7 +1177,8 @@ __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
   }
 }
 
-// Rows split into slices: their statistics; what the teacher makes of a row; the gradient, a piece of a row per block.
+// Rows split into slices: their statistics; what the teacher makes of a row; the gradient, a piece of a row per block.  300 rows of 151,001 fp32,
+// 200 entries: 32 + 8 + 57 us; a row of 604 KB fits no block's registers, so it is read twice, the second time in part from the last cache.
 template <class E, bool REST>
 __global__ __launch_bounds__(256) void k_distill_slices(DistillArgs a, Slices sl) {
   __shared__ Stat box[4];
