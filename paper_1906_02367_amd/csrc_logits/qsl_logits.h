@@ -163,6 +163,8 @@ __device__ __forceinline__ float take(Stat& o, const float* v, float cl) {
   return vm;
 }
 
+// lanes of a quad 1 0 3 2 and 2 3 0 1, lanes of 8 and of 16 backwards
+constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp_keep(float x, float old) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false));
@@ -219,6 +221,28 @@ __device__ __forceinline__ Stat wave_stat(Stat o, float cl) {
   return o;
 }
 
+// the statistics of N = 2 .. 16 waves, lane i % N holding wave i's: sums over N neighbours by moves within the rows of 16 lanes
+template <bool ENT, int N>
+__device__ __forceinline__ Stat row16_stat(Stat o, float cl) {
+  float m = o.m;
+  if (N >= 2) m = fmaxf(m, dpp_keep<DPP_XOR1, 0xF>(m, m));
+  if (N >= 4) m = fmaxf(m, dpp_keep<DPP_XOR2, 0xF>(m, m));
+  if (N >= 8) m = fmaxf(m, dpp_keep<DPP_HALF_MIRROR, 0xF>(m, m));
+  if (N >= 16) m = fmaxf(m, dpp_keep<DPP_MIRROR, 0xF>(m, m));
+  o = raised<ENT>(o, m, cl);
+  auto sum = [](float x) {
+    if (N >= 2) x += dpp_keep<DPP_XOR1, 0xF>(x, 0.0f);
+    if (N >= 4) x += dpp_keep<DPP_XOR2, 0xF>(x, 0.0f);
+    if (N >= 8) x += dpp_keep<DPP_HALF_MIRROR, 0xF>(x, 0.0f);
+    if (N >= 16) x += dpp_keep<DPP_MIRROR, 0xF>(x, 0.0f);
+    return lane_float(x, 0);
+  };
+  o.m = lane_float(m, 0);
+  o.s = sum(o.s);
+  if (ENT) o.w = sum(o.w);
+  return o;
+}
+
 // the statistics of all threads of a block of TH, in every thread; `box` holds TH / 64 of them
 template <bool ENT, int TH>
 __device__ __forceinline__ Stat block_stat(Stat o, float cl, Stat* box) {
@@ -226,18 +250,16 @@ __device__ __forceinline__ Stat block_stat(Stat o, float cl, Stat* box) {
   if (TH == 64) return o;
   if (lane_id() == 0) box[threadIdx.x >> 6] = o;
   __syncthreads();
-  o = lane_id() < TH / 64 ? box[lane_id()] : stat_none();
-  return wave_stat<ENT>(o, cl);
+  o = box[lane_id() % (TH / 64)];                                     // every row of 16 lanes holds all of them, once each or more
+  return row16_stat<ENT, TH / 64>(o, cl);
 }
 
-// what the outputs need of a finished row
-struct RowStat { float m, L, H; };
-template <bool ENT>
-__device__ __forceinline__ RowStat row_stat(Stat o) {
-  RowStat r;
-  r.m = o.m; r.L = logf(o.s);
-  r.H = !ENT ? 0.0f : o.s == 0.0f ? 0.0f : r.L - LN2 * (o.w / o.s);
-  return r;
+// Of a finished row's sums: the logarithm is taken where an output needs it (the gradient does not, unless the entropy's).
+__device__ __forceinline__ float row_entropy(const Stat& o) { return o.s == 0.0f ? 0.0f : logf(o.s) - LN2 * (o.w / o.s); }
+__device__ __forceinline__ float row_lse(const Stat& o, float c) { return o.s == 0.0f ? -INFINITY : o.m * c + logf(o.s); }
+// also where the row holds nothing else (s = 0)
+__device__ __forceinline__ float log_prob(const Stat& o, float z, float c) {
+  return z == -INFINITY && o.s == o.s ? -INFINITY : (z - o.m) * c - logf(o.s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -278,12 +300,12 @@ __device__ __forceinline__ Stat pass_stat(const E* z, uint32_t n, float cl) {
   return o;
 }
 
-// dz = p (A + B y) with y = (x - m) cl, p = exp2(y - l2): the gradient in a class that nothing is given for
-struct Gradient { float cl, m, l2, A, B; };
+// dz = e (A + B y) with y = (x - m) cl, e = exp2(y): the gradient in a class that nothing is given for, A and B divided by s
+struct Gradient { float cl, m, A, B; };
 template <bool ENT>
 __device__ __forceinline__ float gradient_value(const Gradient& f, float x) {
-  const float y = (x - f.m) * f.cl, p = exp2_(y - f.l2);
-  return ENT ? p * __builtin_fmaf(f.B, fmaxf(y, Y_MIN), f.A) : p * f.A;
+  const float y = (x - f.m) * f.cl, e = exp2_(y);
+  return ENT ? e * __builtin_fmaf(f.B, fmaxf(y, Y_MIN), f.A) : e * f.A;
 }
 
 struct NoneOut { __device__ __forceinline__ uint32_t operator()(uint32_t) const { return 0; } };
@@ -537,8 +559,8 @@ __device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, To
   constexpr uint32_t PER = TH > GROUPS ? TH / GROUPS : 1, G = TH / PER, M = G / 64;
   static_assert(PER == 1 || PER == 2 || PER == 4, "a group is a thread, or two or four lanes of a quad");
   float gm = most;
-  if (PER >= 2) gm = fmaxf(gm, dpp_keep<0xB1, 0xF>(gm, gm));          // the lanes of a quad: 1 0 3 2, then 2 3 0 1
-  if (PER == 4) gm = fmaxf(gm, dpp_keep<0x4E, 0xF>(gm, gm));
+  if (PER >= 2) gm = fmaxf(gm, dpp_keep<DPP_XOR1, 0xF>(gm, gm));          // the lanes of a quad: 1 0 3 2, then 2 3 0 1
+  if (PER == 4) gm = fmaxf(gm, dpp_keep<DPP_XOR2, 0xF>(gm, gm));
   if (TH > 64 && threadIdx.x % PER == 0) b.group[threadIdx.x / PER] = gm;
   if (threadIdx.x == 0) b.n = 0;
   __syncthreads();
@@ -602,10 +624,6 @@ struct ScoreArgs {
   float* stats;
 };
 
-__device__ __forceinline__ float log_prob(const RowStat& r, float z, float c) {
-  return z == -INFINITY && r.L == r.L ? -INFINITY : (z - r.m) * c - r.L;       // also where the row holds nothing else (L = -inf)
-}
-
 // the given class and its logit, read by one thread ahead of the row: two reads, one behind the other
 template <class E>
 struct Given {
@@ -616,34 +634,34 @@ struct Given {
     t = a.target[row];
     x = z[t >= 0 && t < static_cast<int64_t>(a.vocab) ? t : 0];
   }
-  __device__ __forceinline__ float logprob(const ScoreArgs& a, const RowStat& r) const {
-    return t < 0 ? 0.0f : t >= static_cast<int64_t>(a.vocab) ? NAN : log_prob(r, static_cast<float>(x), a.c);
+  __device__ __forceinline__ float logprob(const ScoreArgs& a, const Stat& o) const {
+    return t < 0 ? 0.0f : t >= static_cast<int64_t>(a.vocab) ? NAN : log_prob(o, static_cast<float>(x), a.c);
   }
 };
 
 template <class E>
-__device__ __forceinline__ void score_outputs(const ScoreArgs& a, uint32_t row, const Given<E>& g, const Stat& o, const RowStat& r) {
-  if (a.logprob) a.logprob[row] = g.logprob(a, r);
-  if (a.entropy) a.entropy[row] = r.H;
-  if (a.lse) a.lse[row] = o.s == 0.0f ? -INFINITY : r.m * a.c + r.L;
-  if (a.stats) { float* s = a.stats + 4ull * row; s[0] = r.m; s[1] = r.L; s[2] = r.H; s[3] = 0.0f; }
+__device__ __forceinline__ void score_outputs(const ScoreArgs& a, uint32_t row, const Given<E>& g, const Stat& o) {
+  if (a.logprob) a.logprob[row] = g.logprob(a, o);
+  if (a.entropy) a.entropy[row] = row_entropy(o);
+  if (a.lse) a.lse[row] = row_lse(o, a.c);
+  if (a.stats) { float* s = a.stats + 4ull * row; s[0] = o.m; s[1] = o.s; s[2] = row_entropy(o); s[3] = 0.0f; }
 }
 // f(out) with out(rank, key) writing an alternative; where the row has no order (a NaN or +inf in it) the outputs say so instead
 template <int TH, class F>
-__device__ __forceinline__ void alternatives(const ScoreArgs& a, uint32_t row, const RowStat& r, F&& f) {
+__device__ __forceinline__ void alternatives(const ScoreArgs& a, uint32_t row, const Stat& o, F&& f) {
   int32_t* ti = a.top_index ? a.top_index + static_cast<uint64_t>(row) * a.K : nullptr;
   float* tl = a.top_logprob ? a.top_logprob + static_cast<uint64_t>(row) * a.K : nullptr;
-  if (r.L != r.L) {
+  if (o.s != o.s) {
     for (uint32_t k = threadIdx.x; k < a.K; k += TH) { if (ti) ti[k] = -1; if (tl) tl[k] = NAN; }
     return;
   }
-  if (r.L == -INFINITY) {                                             // nothing but -inf
+  if (o.s == 0.0f) {                                                  // nothing but -inf
     for (uint32_t k = threadIdx.x; k < a.K; k += TH) { if (ti) ti[k] = static_cast<int32_t>(k); if (tl) tl[k] = -INFINITY; }
     return;
   }
   f([&](uint32_t rank, uint64_t k) {
     if (ti) ti[rank] = static_cast<int32_t>(key_index(k));
-    if (tl) tl[rank] = log_prob(r, key_value(k), a.c);
+    if (tl) tl[rank] = log_prob(o, key_value(k), a.c);
   });
 }
 
@@ -663,10 +681,9 @@ __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
   given.load(a, row, z);
   const Stat mine = pass_stat<LAST && !TOP, E, TH, ENT>(z, a.vocab, cl);
   const Stat o = block_stat<ENT, TH>(mine, cl, box);
-  const RowStat r = row_stat<ENT>(o);
-  if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
+  if (threadIdx.x == 0) score_outputs(a, row, given, o);
   if (TOP)
-    alternatives<TH>(a, row, r, [&](auto&& out) {
+    alternatives<TH>(a, row, o, [&](auto&& out) {
       row_top<E, TH, TOP ? CAND_CAP : 1>(z, a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb, out);
     });
 }
@@ -690,9 +707,8 @@ __global__ __launch_bounds__(TH) void k_score_held(ScoreArgs a) {
   float most[NV / Held<true, E, TH, NV>::U];
   const Stat mine = h.template stat<ENT>(cl, NoneOut(), most);
   const Stat o = block_stat<ENT, TH>(mine, cl, box);
-  const RowStat r = row_stat<ENT>(o);
-  if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
-  alternatives<TH>(a, row, r, [&](auto&& out) {
+  if (threadIdx.x == 0) score_outputs(a, row, given, o);
+  alternatives<TH>(a, row, o, [&](auto&& out) {
     block_top<TH, CAP>(a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb, std::true_type(),
                        [&](float tau, auto&& f) { h.at_least(tau, a.K, most, [&](uint32_t i, float x) { f(top_key(x, i)); }); }, out);
   });
@@ -767,10 +783,9 @@ __global__ __launch_bounds__(256) void k_score_join(ScoreArgs a, Slices sl) {
   Given<E> given;
   given.load(a, row, static_cast<const E*>(a.z) + row * a.stride);
   const Stat o = joined<ENT>(sl, row, cl);
-  const RowStat r = row_stat<ENT>(o);
-  if (threadIdx.x == 0) score_outputs(a, row, given, o, r);
+  if (threadIdx.x == 0) score_outputs(a, row, given, o);
   if (a.K == 0) return;
-  alternatives<256>(a, row, r, [&](auto&& out) {
+  alternatives<256>(a, row, o, [&](auto&& out) {
     block_top<256, CAND_CAP>(n, a.K, sample ? key_value(sample) : -INFINITY, tb, std::false_type(), [&](float tau, auto&& f) {
       auto offer = [&](uint64_t k) { if (k && key_value(k) >= tau) f(k); };
 #pragma unroll
@@ -814,23 +829,20 @@ __device__ __forceinline__ RowWeights row_weights(const GradArgs& a, uint32_t ro
   return w;
 }
 template <bool ENT>
-__device__ __forceinline__ RowGradient row_gradient(const GradArgs& a, const RowWeights& w, const RowStat& r) {
-  const int64_t t = w.t;
-  const float g = w.g, h = w.h;
-  const bool empty = r.L == -INFINITY;
-  RowGradient o;
-  o.f.cl = a.c * LOG2E; o.f.m = r.m;
-  o.f.l2 = empty ? 0.0f : r.L * LOG2E;
-  o.f.A = empty ? 0.0f : -a.c * (g + h * (r.H - r.L));
-  o.f.B = -a.c * h * LN2;
-  o.t = t >= 0 && t < static_cast<int64_t>(a.vocab) ? static_cast<uint32_t>(t) : 0xFFFFFFFFu;
-  o.add = empty ? 0.0f : a.c * g;
-  return o;
+__device__ __forceinline__ RowGradient row_gradient(const GradArgs& a, const RowWeights& w, const Stat& o, float H) {
+  const bool empty = o.s == 0.0f;
+  RowGradient r;
+  r.f.cl = a.c * LOG2E; r.f.m = o.m;
+  r.f.A = empty ? 0.0f * w.g : -a.c * (ENT ? w.g + w.h * (H - logf(o.s)) : w.g) / o.s;
+  r.f.B = ENT && !empty ? -a.c * w.h * LN2 / o.s : 0.0f;
+  r.t = w.t >= 0 && w.t < static_cast<int64_t>(a.vocab) ? static_cast<uint32_t>(w.t) : 0xFFFFFFFFu;
+  r.add = empty ? 0.0f : a.c * w.g;
+  return r;
 }
 // what a row hands out besides its gradient; the log probability of a given class comes from the thread that holds it
-__device__ __forceinline__ void gradient_outputs(const GradArgs& a, uint32_t row, const RowStat& r, const RowGradient& o, int64_t given) {
-  if (a.entropy) a.entropy[row] = r.H;
-  if (a.logprob && o.t == 0xFFFFFFFFu) a.logprob[row] = given < 0 ? 0.0f : NAN;
+__device__ __forceinline__ void gradient_outputs(const GradArgs& a, uint32_t row, float H, const RowGradient& r, int64_t given) {
+  if (a.entropy) a.entropy[row] = H;
+  if (a.logprob && r.t == 0xFFFFFFFFu) a.logprob[row] = given < 0 ? 0.0f : NAN;
 }
 
 // A block per row, held in its registers: one read, one write, and bound by them (8,192 rows of 32,000 bf16 170 us, 6.2 TB/s, where a copy
@@ -844,11 +856,12 @@ __global__ __launch_bounds__(TH) void k_gradient_held(GradArgs a) {
   const RowWeights w = row_weights<ENT>(a, row);
   Held<false, E, TH, NV> h;
   h.load(static_cast<const E*>(a.z) + row * a.stride, a.vocab);
-  const RowStat r = row_stat<ENT>(block_stat<ENT, TH>(h.template stat<ENT>(cl), cl, box));
-  const RowGradient o = row_gradient<ENT>(a, w, r);
-  h.template gradient<ENT>(static_cast<E*>(a.dz) + row * a.dstride, o.f, o.t, o.add,
-                           [&](float x) { if (a.logprob) a.logprob[row] = log_prob(r, x, a.c); });
-  if (threadIdx.x == 0) gradient_outputs(a, row, r, o, w.t);
+  const Stat o = block_stat<ENT, TH>(h.template stat<ENT>(cl), cl, box);
+  const float H = ENT ? row_entropy(o) : 0.0f;
+  const RowGradient r = row_gradient<ENT>(a, w, o, H);
+  h.template gradient<ENT>(static_cast<E*>(a.dz) + row * a.dstride, r.f, r.t, r.add,
+                           [&](float x) { if (a.logprob) a.logprob[row] = log_prob(o, x, a.c); });
+  if (threadIdx.x == 0) gradient_outputs(a, row, H, r, w.t);
 }
 
 // A piece of a row per block, the statistics known: the caller's, or (a.stats = NULL) joined from the slices'.  4,096 rows of 131,072 bf16
@@ -866,13 +879,14 @@ __global__ __launch_bounds__(256) void k_gradient_apply(GradArgs a, Slices sl) {
   const RowWeights w = row_weights<ENT>(a, row);
   H h;
   h.load(static_cast<const E*>(a.z) + row * a.stride + i0, n);
-  RowStat r;
-  if (a.stats) { const float* s = a.stats + 4ull * row; r.m = s[0]; r.L = s[1]; r.H = s[2]; }
-  else r = row_stat<ENT>(joined<ENT>(sl, row, a.c * LOG2E));
-  const RowGradient o = row_gradient<ENT>(a, w, r);
-  h.template gradient<ENT>(static_cast<E*>(a.dz) + row * a.dstride + i0, o.f, o.t - i0, o.add,
-                           [&](float x) { if (a.logprob) a.logprob[row] = log_prob(r, x, a.c); });
-  if (threadIdx.x == 0 && i0 == 0) gradient_outputs(a, row, r, o, w.t);
+  Stat o;
+  float entropy;
+  if (a.stats) { const float* s = a.stats + 4ull * row; o.m = s[0]; o.s = s[1]; entropy = s[2]; }
+  else { o = joined<ENT>(sl, row, a.c * LOG2E); entropy = ENT ? row_entropy(o) : 0.0f; }
+  const RowGradient r = row_gradient<ENT>(a, w, o, entropy);
+  h.template gradient<ENT>(static_cast<E*>(a.dz) + row * a.dstride + i0, r.f, r.t - i0, r.add,
+                           [&](float x) { if (a.logprob) a.logprob[row] = log_prob(o, x, a.c); });
+  if (threadIdx.x == 0 && i0 == 0) gradient_outputs(a, row, entropy, r, w.t);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -900,7 +914,7 @@ struct TeacherBox {
   float q[TEACHER_MAX];            // the teacher's probabilities
   uint32_t bad, some;              // an index outside; whether the row teaches anything
   double lse, sum_q;               // of the teacher's logits
-  float m, L, F, m_all;
+  float m, s, F, m_all;
   double t_all;                    // sum of exp(c (z_i - m_all)) over the whole row
 };
 template <int TH> constexpr int entries_of() { return (TEACHER_MAX + TH - 1) / TH; }
@@ -1058,16 +1072,16 @@ __device__ __forceinline__ void teacher_probabilities(const DistillArgs& a, uint
   wave_lds_fence();
 }
 
-// What the row's statistics `o` (of the whole row, or with REST of the classes outside) make of it: m, L, F (dz_i = c g F softmax_i over
+// What the row's statistics `o` (of the whole row, or with REST of the classes outside) make of it: m, s, F (dz_i = c g F softmax_i over
 // what `o` covers), m_all, t_all.  Statistics that the caller kept (a.stats_in) take the place of `o`.
 template <bool REST>
 __device__ __forceinline__ void student_sums(const DistillArgs& a, uint64_t row, Stat o, TeacherBox& b) {
   const double c = a.c;
   double F = b.some ? 1.0 : 0.0, t = o.s;
-  float m_all = o.m, L = logf(o.s);
+  float m_all = o.m;
   if (a.stats_in) {
     const float* s = a.stats_in + 8ull * row;
-    o.m = s[0]; L = s[1]; F = s[2]; m_all = s[3];
+    o.m = s[0]; o.s = s[1]; F = s[2]; m_all = s[3];
     t = exp(static_cast<double>(s[4]));
   } else if (REST) {
     float most = -INFINITY;
@@ -1086,7 +1100,7 @@ __device__ __forceinline__ void student_sums(const DistillArgs& a, uint64_t row,
   }
   if (t == 0.0) F = 0.0;                                              // a row that leaves nothing
   if (b.bad) F = NAN;
-  if (lane_id() == 0) { b.m = o.m; b.L = L; b.F = static_cast<float>(F); b.m_all = m_all; b.t_all = t; }
+  if (lane_id() == 0) { b.m = o.m; b.s = o.s; b.F = static_cast<float>(F); b.m_all = m_all; b.t_all = t; }
   wave_lds_fence();
 }
 
@@ -1126,7 +1140,7 @@ __device__ __forceinline__ void distill_outputs(const DistillArgs& a, uint32_t r
   if (a.loss) a.loss[row] = loss;
   if (a.stats) {
     float* s = a.stats + 8ull * row;
-    s[0] = b.m; s[1] = b.L; s[2] = b.F; s[3] = b.m_all; s[4] = static_cast<float>(log(b.t_all)); s[5] = s[6] = s[7] = 0.0f;
+    s[0] = b.m; s[1] = b.s; s[2] = b.F; s[3] = b.m_all; s[4] = static_cast<float>(log(b.t_all)); s[5] = s[6] = s[7] = 0.0f;
   }
 }
 
@@ -1163,9 +1177,8 @@ __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
   if (TH == 64) __syncthreads();
   if (threadIdx.x < 64) student_sums<REST>(a, row, o, b);
   __syncthreads();
-  const float L = b.L;
   E* dz = static_cast<E*>(a.dz) + row * a.dstride;
-  if (a.dz) h.template gradient<false>(dz, Gradient{cl, b.m, L == -INFINITY ? 0.0f : L * LOG2E, g * b.F, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
+  if (a.dz) h.template gradient<false>(dz, Gradient{cl, b.m, b.s == 0.0f ? 0.0f * b.F : g * b.F / b.s, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
   if (threadIdx.x < 64 && !a.stats_in) {                              // while the stores are on their way
     const float loss = distill_loss<REST>(a, o, b);
     if (threadIdx.x == 0) distill_outputs(a, row, b, loss);
@@ -1196,7 +1209,7 @@ __global__ __launch_bounds__(256) void k_distill_slices(DistillArgs a, Slices sl
 }
 
 struct Taught {                            // what k_distill_join leaves for k_distill_apply
-  Stat4* row;                              // [rows] m, L log2(e), A of Gradient
+  Stat4* row;                              // [rows] m, A of Gradient
   int32_t* index;                          // [rows, K] classes, -1: none
   float* value;                            // [rows, K] the gradient there
 };
@@ -1222,8 +1235,7 @@ __global__ __launch_bounds__(256) void k_distill_join(DistillArgs a, Slices sl, 
   if (threadIdx.x < 64) student_sums<REST>(a, row, o, b);
   __syncthreads();
   if (w.row) {
-    const float L = b.L;
-    if (threadIdx.x == 0) w.row[row] = Stat4{b.m, L == -INFINITY ? 0.0f : L * LOG2E, g * b.F, 0.0f};
+    if (threadIdx.x == 0) w.row[row] = Stat4{b.m, b.s == 0.0f ? 0.0f * b.F : g * b.F / b.s, 0.0f, 0.0f};
     const uint32_t k = threadIdx.x;
     if (k < a.K) {
       w.index[static_cast<uint64_t>(row) * a.K + k] = b.index[k];
@@ -1249,7 +1261,7 @@ __global__ __launch_bounds__(256) void k_distill_apply(DistillArgs a, Taught w) 
   H h;
   h.load(static_cast<const E*>(a.z) + row * a.stride + i0, n);
   const Stat4 r = w.row[row];
-  h.template gradient<false>(dz, Gradient{a.c * LOG2E, r.m, r.s, r.w, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
+  h.template gradient<false>(dz, Gradient{a.c * LOG2E, r.m, r.s, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
   __syncthreads();
   const uint32_t k = threadIdx.x;
   if (k < a.K) {
