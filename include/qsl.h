@@ -265,8 +265,8 @@ typedef struct {
   float scale;               /* c, 2^-100 <= c <= 2^100 (1: the logits as they are; 1 / temperature)    */
 } qsl_logits;
 
-/* Bytes of device memory that a call on such rows needs as `workspace`, a multiple of 256 (0 for short rows, and where there are
- * many of them); `top` is the call's: its alternatives, its teacher's entries, 0 for none.  0 for invalid arguments too. */
+/* Bytes of device memory that a call on such rows needs as `workspace`, a multiple of 256 (0 where a block takes a row by itself: for
+ * shorter rows, unless there are few of them); `top` is the call's: its alternatives, its teacher's entries, 0 for none.  0 for invalid arguments too. */
 size_t qsl_logits_workspace_bytes(const qsl_logits *z, uint32_t top);
 
 /* Log probabilities of given classes, with the entropy and the best alternatives of every row.

@@ -78,32 +78,39 @@ constexpr uint64_t SLICE_MAX = 64 * KB;            // ... that 256 threads hold
 
 uint64_t row_bytes(const qsl_logits* z) { return static_cast<uint64_t>(z->vocab) * elem_size(z->dtype); }
 
-enum HeldFor { FOR_GRADIENT, FOR_TEACHER, FOR_TOP, FOR_MANY_TOP };      // FOR_MANY_TOP: more than 64 alternatives
-
-// f(threads, vectors a thread holds) for rows of at most HELD_MAX bytes (and the values behind their last vector).  Where a row can be
+// f(threads, vectors a thread holds) for rows that a block holds (and the values before and behind their vectors).  Where a row can be
 // held by few threads with many vectors or by many with few: many have the shorter way from the first load to the last store, few
-// leave room for other rows while a row is being ranked.  us:
+// leave room for other rows while a row is being ranked; few rows have nothing to make room for.  us:
 //   8,192 rows of 64 KB   gradient 256 x 16 198, 512 x 8 193, 1024 x 4 178; a teacher's 64 entries 217 / 204 / 197
 //   4,096 rows of 64 KB   20 alternatives 256 x 16 50, 512 x 8 53, 1024 x 4 70
 //   8,192 rows of 32 KB   gradient 256 x 8 100, 512 x 4 95; entries 111 / 107; 20 alternatives 128 x 16 53, 256 x 8 54, 512 x 4 67
 //   16 KB                 gradient (16,384 rows) 256 x 4 97, 128 x 8 100; 20 alternatives (8,192) 36 / 31
 //   128 KB                gradient (4,000) 512 x 16 188, 1024 x 8 190, with the entropy 193 / 197; entries (2,000) 113 / 149; 20 alternatives
 //                         (4,096) 99 / 148
-// Groups of threads give the alternatives' bound, so more than 64 of them take 256 threads at least.
 template <class F>
-void pick_held(uint64_t nvec, uint64_t rows, HeldFor what, F&& f) {
-  const bool few = rows < FEW_ROWS, top = what == FOR_TOP || what == FOR_MANY_TOP;      // few: nothing to make room for
-  if (nvec <= 64 && what != FOR_MANY_TOP) f(Int<64>(), Int<1>());
-  else if (nvec <= 64 * 4 && what != FOR_MANY_TOP) f(Int<64>(), Int<4>());
-  else if (nvec <= 128 * 8 && what == FOR_TOP && !few) f(Int<128>(), Int<8>());
+void pick_for_gradient(uint64_t nvec, uint64_t rows, F&& f) {
+  if (nvec <= 64) f(Int<64>(), Int<1>());
+  else if (nvec <= 64 * 4) f(Int<64>(), Int<4>());
   else if (nvec <= 256 * 4) f(Int<256>(), Int<4>());
-  else if (nvec <= 512 * 4 && !top) f(Int<512>(), Int<4>());
-  else if (nvec <= 256 * 8 && top && !few) f(Int<256>(), Int<8>());
-  else if (nvec <= 1024 * 4 && (few || !top)) f(Int<1024>(), Int<4>());
-  else if (nvec <= 256 * 16) f(Int<256>(), Int<16>());
-  else if (nvec <= 1024 * 8 && few) f(Int<1024>(), Int<8>());
-  else if (nvec <= 512 * 16) f(Int<512>(), Int<16>());
+  else if (nvec <= 512 * 4) f(Int<512>(), Int<4>());
+  else if (nvec <= 1024 * 4) f(Int<1024>(), Int<4>());
+  else if (nvec <= 512 * 16 && rows >= FEW_ROWS) f(Int<512>(), Int<16>());
+  else if (nvec <= 1024 * 8) f(Int<1024>(), Int<8>());
   else f(Int<1024>(), Int<16>());
+}
+// for alternatives, whose bound comes from groups of threads: more than 64 of them take 256 threads at least
+template <class F>
+void pick_for_top(uint64_t nvec, uint64_t rows, uint32_t top, F&& f) {
+  const bool few = rows < FEW_ROWS;
+  if (nvec <= 64 && top <= 64) f(Int<64>(), Int<1>());
+  else if (nvec <= 64 * 4 && top <= 64) f(Int<64>(), Int<4>());
+  else if (nvec <= 128 * 8 && top <= 64 && !few) f(Int<128>(), Int<8>());
+  else if (nvec <= 256 * 4) f(Int<256>(), Int<4>());
+  else if (nvec <= 256 * 8 && !few) f(Int<256>(), Int<8>());
+  else if (nvec <= 256 * 16 && !few) f(Int<256>(), Int<16>());
+  else if (nvec <= 1024 * 4) f(Int<1024>(), Int<4>());
+  else if (!few) f(Int<512>(), Int<16>());
+  else f(Int<1024>(), Int<8>());
 }
 
 // How a call splits its rows.
@@ -221,9 +228,7 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
         else k_slice_stats<E, 16, ent()><<<grid, 256, 0, stream>>>(a, sl);
         k_score_join<E, ent()><<<rows, 256, 0, stream>>>(a, sl);
       } else if (top && row_bytes(z) <= HELD_TOP_MAX) {
-        pick_held(nvec, z->rows, top > 64 ? FOR_MANY_TOP : FOR_TOP, [&](auto th, auto nv) {
-          if constexpr (th() * nv() <= 8192) k_score_held<E, th(), nv(), ent()><<<rows, th(), 0, stream>>>(a);
-        });
+        pick_for_top(nvec, z->rows, top, [&](auto th, auto nv) { k_score_held<E, th(), nv(), ent()><<<rows, th(), 0, stream>>>(a); });
       } else if (top) {
         k_score<false, E, 1024, ent(), true><<<rows, 1024, 0, stream>>>(a);
       } else {
@@ -258,7 +263,7 @@ extern "C" qsl_status qsl_token_logprobs_backward(const qsl_logits* z, const int
     typedef decltype(e) E;
     pick_bool(grad_entropy || entropy, [&](auto ent) {
       if (!stats && !plan.split) {
-        pick_held(z->vocab / Elem<E>::N, z->rows, FOR_GRADIENT, [&](auto th, auto nv) { k_gradient_held<E, th(), nv(), ent()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
+        pick_for_gradient(z->vocab / Elem<E>::N, z->rows, [&](auto th, auto nv) { k_gradient_held<E, th(), nv(), ent()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
         return;
       }
       if (!stats) {
@@ -284,7 +289,7 @@ static qsl_status launch_distill(const qsl_logits* z, const qsl_teacher* t, cons
     typedef decltype(e) E;
     pick_bool(t->lse != nullptr, [&](auto rest) {
       if (!plan.split) {
-        pick_held(z->vocab / Elem<E>::N, z->rows, FOR_TEACHER, [&](auto th, auto nv) { k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
+        pick_for_gradient(z->vocab / Elem<E>::N, z->rows, [&](auto th, auto nv) { k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
         return;
       }
       if (!a.stats_in) {

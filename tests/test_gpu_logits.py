@@ -266,6 +266,28 @@ def test_offsets_beyond_32_bits(B):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("V,dtype", [(1500, "fp16"), (6001, "bf16"), (13000, "fp16"), (20001, "bf16"), (25003, "fp32"), (50003, "bf16"), (100001, "bf16")])
+def test_long_rows_that_are_many(B, V, dtype):
+    """So many rows that every one has a block of its own: the forms that hold the longest rows."""
+    N, dt = 260, TYPES[dtype]
+    z, t = logits_of(N, V, dt, pad=1), targets_of(N, V)
+    for K in (10, 100):
+        check_score(z, t, K, 1.0, run_score(B, z, t, K, 1.0), f"{dtype} {N} x {V}, K = {K}")
+    g = torch.linspace(-1, 1, N, device=dev)
+    r = X.rows_of(z, 1.0)
+    dz = torch.empty_like(z)
+    for h in (None, 0.5 * g):
+        B.token_logprobs_backward(z, t, dz, grad_logprob=g, grad_entropy=h)
+        X.check(dz, *X.logprob_gradient(r, t, g, h, dt), f"{dtype} {N} x {V}: gradient")
+    index, value, lse = teacher_of(N, V, 33, ragged=True)
+    for l in (None, lse):
+        loss, tol_loss, want, tol = X.distill(r, index.cpu(), value.cpu(), 1.0, None if l is None else l.cpu(), g.cpu(), dt)
+        got = new(N)
+        B.distill_backward(z, index, value, dz, teacher_lse=l, grad_loss=g, loss=got)
+        X.check(got, loss, tol_loss, f"{dtype} {N} x {V}, rest {l is not None}: loss")
+        X.check(dz, want, tol, f"{dtype} {N} x {V}, rest {l is not None}: gradient of the loss")
+
+
 @pytest.mark.parametrize("N,V,dtype", [(2, 1_100_003, "fp32"), (1, 17_000_003, "bf16")])
 def test_very_long_rows(B, N, V, dtype):
     """More than 64 slices of what a block holds: rows that are walked along; slices of several spans of marked classes."""
