@@ -665,9 +665,9 @@ __device__ __forceinline__ void alternatives(const ScoreArgs& a, uint32_t row, c
   });
 }
 
-// A block per row, which it walks along once: bound by memory (4,096 rows of 128,000 bf16 with the entropy 154 - 170 us, 6.2 - 6.8 TB/s; four
-// fifths of the vector issue slots, most of them for the exponentials).  Eight loads a thread under way instead of four cost
-// registers, hence waves: 214 us.  With alternatives (rows of more than 64 slices only) the threads that hold candidates read their
+// A block per row, which it walks along once: bound by memory, and as near by its instructions (4,096 rows of 128,000 bf16 with the entropy
+// 153 - 170 us, 6.2 - 6.8 TB/s; 9.7 vector instructions per 64 values, one of them an exponential at a quarter of the rate, are 150 us
+// of issue at 2.4 GHz).  Eight loads a thread under way instead of four cost registers, hence waves: 214 us.  With alternatives (rows of more than 64 slices only) the threads that hold candidates read their
 // shares again.
 template <bool LAST, class E, int TH, bool ENT, bool TOP>
 __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
