@@ -351,6 +351,8 @@ struct Held {
     Stat o = stat_none();
 #pragma unroll
     for (int u0 = 0; u0 < NV; u0 += U) {
+      most[u0 / U] = -INFINITY;
+      if (u0 * TH >= nvec) continue;                                   // the same for all threads: nothing of the piece is left
       float v[U * N];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -422,6 +424,7 @@ struct Held {
   __device__ __forceinline__ void gradient(E* dz, Gradient f, uint32_t t, float add, F&& given) {
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
+      if (u * TH >= nvec) continue;
       in_order(u, f.A);
       float v[N];
       Elem<E>::unpack(r[u], v);
