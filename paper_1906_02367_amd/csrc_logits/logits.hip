@@ -81,7 +81,7 @@ uint64_t row_bytes(const qsl_logits* z) { return static_cast<uint64_t>(z->vocab)
 // f(threads, vectors a thread holds) for rows that a block holds (and the values before and behind their vectors).  Where a row can be
 // held by few threads with many vectors or by many with few: many have the shorter way from the first load to the last store, few
 // leave room for other rows while a row is being ranked; few rows have nothing to make room for.  us:
-//   8,192 rows of 64 KB   gradient 256 x 16 198, 512 x 8 193, 1024 x 4 178; a teacher's 64 entries 217 / 204 / 197
+//   8,192 rows of 64 KB   gradient 256 x 16 198, 512 x 8 193, 1024 x 4 178
 //   4,096 rows of 64 KB   20 alternatives 256 x 16 50, 512 x 8 53, 1024 x 4 70
 //   8,192 rows of 32 KB   gradient 256 x 8 100, 512 x 4 95; entries 111 / 107; 20 alternatives 128 x 16 53, 256 x 8 54, 512 x 4 67
 //   16 KB                 gradient (16,384 rows) 256 x 4 97, 128 x 8 100; 20 alternatives (8,192) 36 / 31
@@ -97,6 +97,15 @@ void pick_for_gradient(uint64_t nvec, uint64_t rows, F&& f) {
   else if (nvec <= 512 * 16 && rows >= FEW_ROWS) f(Int<512>(), Int<16>());
   else if (nvec <= 1024 * 8) f(Int<1024>(), Int<8>());
   else f(Int<1024>(), Int<16>());
+}
+// for a teacher's entries, whose block also has one wave's work to wait for: rows that leave much of 1024 x 4 empty go to 512 x 8, of which more
+// are resident, and so do all rows of 16-bit values whose sum goes without the entries, which takes more operations a vector.  us, 8,192 rows,
+// 1024 x 4 / 512 x 8: bf16 of 20,000, 24,000 and 28,000, the entries alone 146 / 135, 156 / 160, 178 / 191, the rest as one class 172 / 146,
+// 187 / 161, 195 / 186 (32,000: 207 / 203); fp32 of 10,000 and 12,000, the rest as one class 144 / 132, 157 / 162
+template <class F>
+void pick_for_teacher(uint64_t nvec, uint64_t rows, bool rest16, F&& f) {
+  if (nvec > 512 * 4 && nvec <= 512 * (rest16 ? 8 : 5)) f(Int<512>(), Int<8>());
+  else pick_for_gradient(nvec, rows, f);
 }
 // for alternatives, whose bound comes from groups of threads: more than 64 of them take 256 threads at least
 template <class F>
@@ -289,7 +298,8 @@ static qsl_status launch_distill(const qsl_logits* z, const qsl_teacher* t, cons
     typedef decltype(e) E;
     pick_bool(t->lse != nullptr, [&](auto rest) {
       if (!plan.split) {
-        pick_for_gradient(z->vocab / Elem<E>::N, z->rows, [&](auto th, auto nv) { k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
+        pick_for_teacher(z->vocab / Elem<E>::N, z->rows, rest() && sizeof(E) == 2,
+                         [&](auto th, auto nv) { k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
         return;
       }
       if (!a.stats_in) {

@@ -288,6 +288,28 @@ def test_long_rows_that_are_many(B, V, dtype):
         X.check(dz, want, tol, f"{dtype} {N} x {V}, rest {l is not None}: gradient of the loss")
 
 
+@pytest.mark.parametrize("V", [2047, 2048, 2049, 6144, 6145, 16385, 20479, 20480, 20489, 24576, 24577, 28672, 32768])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_that_end_where_a_piece_does(B, dtype, V):
+    """Rows that end at, before or behind a multiple of what the block's threads take at once, with nothing in the pieces that follow."""
+    N, dt = 5, TYPES[dtype]
+    z, t = logits_of(N, V, dt, pad=V % 2), targets_of(N, V)
+    t[0], t[2] = V - 1, 0
+    check_score(z, t, 12, 0.9, run_score(B, z, t, 12, 0.9), f"{dtype} {N} x {V}")
+    g = torch.linspace(-1, 1, N, device=dev)
+    r = X.rows_of(z, 0.9)
+    dz = torch.empty_like(z)
+    B.token_logprobs_backward(z, t, dz, scale=0.9, grad_logprob=g)
+    X.check(dz, *X.logprob_gradient(r, t, g, None, dt), f"{dtype} {N} x {V}: gradient")
+    index, value, lse = teacher_of(N, V, 33, ragged=True)
+    for l in (None, lse):
+        loss, tol_loss, want, tol = X.distill(r, index.cpu(), value.cpu(), 1.0, None if l is None else l.cpu(), g.cpu(), dt)
+        got = new(N)
+        B.distill_backward(z, index, value, dz, scale=0.9, teacher_lse=l, grad_loss=g, loss=got)
+        X.check(got, loss, tol_loss, f"{dtype} {N} x {V}, rest {l is not None}: loss")
+        X.check(dz, want, tol, f"{dtype} {N} x {V}, rest {l is not None}: gradient of the loss")
+
+
 @pytest.mark.parametrize("N,V,dtype", [(2, 1_100_003, "fp32"), (1, 17_000_003, "bf16")])
 def test_very_long_rows(B, N, V, dtype):
     """More than 64 slices of what a block holds: rows that are walked along; slices of several spans of marked classes."""
