@@ -98,14 +98,15 @@ void pick_for_gradient(uint64_t nvec, uint64_t rows, F&& f) {
   else if (nvec <= 1024 * 8) f(Int<1024>(), Int<8>());
   else f(Int<1024>(), Int<16>());
 }
-// for a teacher's entries, whose block also has one wave's work to wait for: rows that leave much of 1024 x 4 empty go to 512 x 8, of which more
-// are resident, and so do all rows of 16-bit values whose sum goes without the entries, which takes more operations a vector.  us, 8,192 rows,
-// 1024 x 4 / 512 x 8: bf16 of 20,000, 24,000 and 28,000, the entries alone 146 / 135, 156 / 160, 178 / 191, the rest as one class 172 / 146,
-// 187 / 161, 195 / 186 (32,000: 207 / 203); fp32 of 10,000 and 12,000, the rest as one class 144 / 132, 157 / 162
-template <class F>
-void pick_for_teacher(uint64_t nvec, uint64_t rows, bool rest16, F&& f) {
-  if (nvec > 512 * 4 && nvec <= 512 * (rest16 ? 8 : 5)) f(Int<512>(), Int<8>());
-  else pick_for_gradient(nvec, rows, f);
+// for a teacher's entries.  Summing 16-bit values without the entries' takes the most operations a vector: rows that leave a quarter of 1024 x 4
+// empty go to 512 x 8, of which more are resident.  us, 8,192 rows of bf16, 1024 x 4 / 512 x 8: the rest as one class 17,000 155 / 124, 20,000
+// 159 / 136, 24,000 167 / 153, 28,000 181 / 186, 32,000 198 / 210; the entries alone 20,000 133 / 138; fp32 of 10,000 125 / 138
+template <bool REST16, class F>
+void pick_for_teacher(uint64_t nvec, uint64_t rows, F&& f) {
+  if constexpr (REST16) {
+    if (nvec > 512 * 4 && nvec * 16 <= 48 * KB) { f(Int<512>(), Int<8>()); return; }
+  }
+  pick_for_gradient(nvec, rows, f);
 }
 // for alternatives, whose bound comes from groups of threads: more than 64 of them take 256 threads at least
 template <class F>
@@ -298,8 +299,9 @@ static qsl_status launch_distill(const qsl_logits* z, const qsl_teacher* t, cons
     typedef decltype(e) E;
     pick_bool(t->lse != nullptr, [&](auto rest) {
       if (!plan.split) {
-        pick_for_teacher(z->vocab / Elem<E>::N, z->rows, rest() && sizeof(E) == 2,
-                         [&](auto th, auto nv) { k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a); });
+        pick_for_teacher<rest() && sizeof(E) == 2>(z->vocab / Elem<E>::N, z->rows, [&](auto th, auto nv) {
+          k_distill_held<E, th(), nv(), rest()><<<grid_of(z->rows), th(), 0, stream>>>(a);
+        });
         return;
       }
       if (!a.stats_in) {
