@@ -108,12 +108,13 @@ void pick_for_teacher(uint64_t nvec, uint64_t rows, F&& f) {
   }
   pick_for_gradient(nvec, rows, f);
 }
-// for alternatives, whose bound comes from groups of threads: more than 64 of them take 256 threads at least
+// for alternatives, whose bound comes from the maxima of groups of threads, of which there have to be more than alternatives (a wave of 64 and
+// 64 alternatives: 12,000 rows of 1,500 103 us, 128 x 8 37), or from all values of a wave
 template <class F>
 void pick_for_top(uint64_t nvec, uint64_t rows, uint32_t top, F&& f) {
   const bool few = rows < FEW_ROWS;
-  if (nvec <= 64 && top <= 64) f(Int<64>(), Int<1>());
-  else if (nvec <= 64 * 4 && top <= 64) f(Int<64>(), Int<4>());
+  if (nvec <= 64) f(Int<64>(), Int<1>());
+  else if (nvec <= 64 * 4 && (top <= 32 || maxima_say_little(top, nvec))) f(Int<64>(), Int<4>());
   else if (nvec <= 128 * 8 && top <= 64 && !few) f(Int<128>(), Int<8>());
   else if (nvec <= 256 * 4) f(Int<256>(), Int<4>());
   else if (nvec <= 256 * 8 && !few) f(Int<256>(), Int<8>());

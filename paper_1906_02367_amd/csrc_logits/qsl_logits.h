@@ -32,6 +32,8 @@ constexpr uint32_t TOP_MAX = 128;          // alternatives of a row at most
 constexpr uint32_t TEACHER_MAX = 256;      // entries of a teacher's row at most
 constexpr uint32_t CAND_CAP = 512;         // candidates for the alternatives that are ranked at once
 constexpr uint32_t REFINE = 256;           // ... of which so many give the next bound when there are more
+// K alternatives of a row of few vectors: almost every vector's largest value is above the K-th largest of them, if there are K
+constexpr __host__ __device__ bool maxima_say_little(uint64_t K, uint64_t nvec) { return K > nvec - nvec / 8; }
 constexpr uint32_t GROUPS = 256;           // maxima of groups of threads that the threshold is taken from, at most
 constexpr uint32_t HASH_SIZE = 4 * TEACHER_MAX;   // slots in which a teacher's entries are looked up, at most
 constexpr uint32_t MASK_SPAN = 1u << 18;   // classes whose membership in the teacher's entries is held in LDS at once (32 KB)
@@ -310,6 +312,12 @@ __device__ __forceinline__ float gradient_value(const Gradient& f, float x) {
 
 struct NoneOut { __device__ __forceinline__ uint32_t operator()(uint32_t) const { return 0; } };
 
+// an integer that orders like the value (not for NaN; -0 counts as +0)
+__device__ __forceinline__ uint32_t ordered(float z) {
+  const uint32_t u = __float_as_uint(z + 0.0f);
+  return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+
 // A piece of a row that the block holds in registers, NV vectors a thread and the values behind the last whole vector one a thread: it
 // is read from memory once, whatever is made of it.  load() only starts the loads; loads past the end go to the last vector, and
 // settle() makes -inf of them.
@@ -419,6 +427,20 @@ struct Held {
     const float x = Elem<E>::from_bits(last);
     if (last_index() < n && x >= (last_index() < keep ? tau : fmaxf(tau, LOWEST))) f(last_index(), x);
   }
+  // how many values reach `least` (above -inf), of a wave that holds the piece; after stat()
+  __device__ __forceinline__ uint32_t count(float least) {
+    uint32_t c = __popcll(__ballot(last_index() < n && Elem<E>::from_bits(last) >= least));
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      if (u / U * U * TH >= nvec) continue;                            // (what stat() has passed over)
+      asm volatile("" : "+v"(r[u]));                                   // unpacked anew for every count: the values would not leave room for other waves
+      float v[N];
+      Elem<E>::unpack(r[u], v);
+#pragma unroll
+      for (int q = 0; q < N; ++q) c += __popcll(__ballot(v[q] >= least));
+    }
+    return c;
+  }
   // the gradient of the piece; where class t is in it, `add` comes on top and given(its logit) is called
   template <bool ENT, class F>
   __device__ __forceinline__ void gradient(E* dz, Gradient f, uint32_t t, float add, F&& given) {
@@ -460,10 +482,6 @@ __device__ __forceinline__ void lds_barrier() {
 // the K largest values of a row, ties to the lower index
 // ---------------------------------------------------------------------------------------------
 // orders like (value, lower index first); no two entries of a row have the same key, and 0 is none's
-__device__ __forceinline__ uint32_t ordered(float z) {                // (not for NaN)
-  const uint32_t u = __float_as_uint(z + 0.0f);                       // -0 counts as +0
-  return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
-}
 __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o >> 31 ? o ^ 0x80000000u : ~o); }
 __device__ __forceinline__ uint64_t top_key(float z, uint32_t i) { return static_cast<uint64_t>(ordered(z)) << 32 | (0xFFFFFFFFu - i); }
 __device__ __forceinline__ float key_value(uint64_t k) { return from_ordered(static_cast<uint32_t>(k >> 32)); }
@@ -525,6 +543,17 @@ __device__ __forceinline__ void ranked(TopBox<CAP>& b, uint32_t held, F&& f) {
   }
 }
 
+// The K-th largest of a wave's values but for the lower 16 bits of its ordered(), which are 0: less than it, found bit by bit, with
+// reach(trial) values of the wave reaching a trial.  -inf where fewer than K are above -inf.
+template <class F>
+__device__ __forceinline__ float wave_kth(uint32_t K, F&& reach) {
+  uint32_t T = 0;
+#pragma unroll 1
+  for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+    if (reach(T | bit) >= K) T |= bit;
+  return T > ordered(-INFINITY) ? from_ordered(T) : -INFINITY;
+}
+
 // The last part of block_top: the K largest of the entries that scan() offers from `bound` on; at least K are.
 template <int TH, uint32_t CAP, class S, class F>
 __device__ __forceinline__ void block_top_from(uint64_t bound, uint32_t K, TopBox<CAP>& b, S&& scan, F&& out) {
@@ -553,7 +582,7 @@ __device__ __forceinline__ void block_top_from(uint64_t bound, uint32_t K, TopBo
 // none); scan(tau, f): f(key) for each of the thread's entries whose value is at least tau.
 // Groups of threads hold distinct entries, so the K-th largest of the groups' maxima is at most the K-th largest value: only what
 // reaches it is a candidate (for values in no particular order a few more than K, in the few threads whose maximum reaches it).  One
-// wave finds its upper 16 bits, by counting the maxima that reach a trial value; less than it will do as well.  Values of -inf count only where fewer than K others are left; of those the lowest indices are wanted, and they are among the first
+// wave finds its upper 16 bits; less than it will do as well.  Values of -inf count only where fewer than K others are left; of those the lowest indices are wanted, and they are among the first
 // K entries: a mask that leaves less than K classes does not make all others candidates.  If more than CAP entries are candidates (many equal or ordered values), the K-th largest of the first REFINE that found room
 // is the next bound: a larger one, since keys differ, and for entries in no particular order it leaves K / REFINE of them.
 // OWN: `most` is the largest of what the thread's scan() goes through (else of any entries, no two threads' the same).
@@ -570,17 +599,15 @@ __device__ __forceinline__ void block_top(uint32_t n, uint32_t K, float most, To
   if (threadIdx.x < 64) {
     float tau = -INFINITY;
     if (K <= G && n > 2 * K) {
-      uint32_t o[M], T = 0;
+      uint32_t o[M];
 #pragma unroll
       for (uint32_t j = 0; j < M; ++j) o[j] = ordered(TH > 64 ? b.group[lane_id() + 64 * j] : gm);
-#pragma unroll 1
-      for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
-        uint32_t reach = 0;
+      tau = wave_kth(K, [&](uint32_t trial) {
+        uint32_t c = 0;
 #pragma unroll
-        for (uint32_t j = 0; j < M; ++j) reach += __popcll(__ballot(o[j] >= (T | bit)));
-        if (reach >= K) T |= bit;
-      }
-      if (T > ordered(-INFINITY)) tau = from_ordered(T);
+        for (uint32_t j = 0; j < M; ++j) c += __popcll(__ballot(o[j] >= trial));
+        return c;
+      });
     }
     if (threadIdx.x == 0) b.tau = tau;
   }
@@ -712,8 +739,20 @@ __global__ __launch_bounds__(TH) void k_score_held(ScoreArgs a) {
   const Stat o = block_stat<ENT, TH>(mine, cl, box);
   if (threadIdx.x == 0) score_outputs(a, row, given, o);
   alternatives<TH>(a, row, o, [&](auto&& out) {
-    block_top<TH, CAP>(a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb, std::true_type(),
-                       [&](float tau, auto&& f) { h.at_least(tau, a.K, most, [&](uint32_t i, float x) { f(top_key(x, i)); }); }, out);
+    auto scan = [&](float tau, auto&& f) { h.at_least(tau, a.K, most, [&](uint32_t i, float x) { f(top_key(x, i)); }); };
+    if constexpr (TH == 64) {
+      // All values counted instead of the vectors' maxima (16 times), unless ranking all is little.  us, 12,000 rows of bf16, with maxima /
+      // this: 210 values, 32 and 128 alternatives 65 / 23, 70 / 43; 500, 128 208 / 42; 800, 128 236 / 54.  Where there are more vectors:
+      // 500, 32 16 / 21; 210, 20 15 / 20.  Ranking all: 64, 20 19 / 23; 70, 64 23 / 27.
+      if (maxima_say_little(a.K, h.nvec) && a.vocab > min(max(2 * a.K, 64u), 128u)) {
+        const float tau = wave_kth(a.K, [&](uint32_t trial) { return h.count(from_ordered(trial)); });
+        if (threadIdx.x == 0) tb.n = 0;
+        __syncthreads();
+        block_top_from<TH>(0, a.K, tb, [&](auto&& f) { scan(tau, f); }, out);
+        return;
+      }
+    }
+    block_top<TH, CAP>(a.vocab, a.K, mine.s > 0.0f ? mine.m : -INFINITY, tb, std::true_type(), scan, out);
   });
 }
 

@@ -288,6 +288,25 @@ def test_long_rows_that_are_many(B, V, dtype):
         X.check(dz, want, tol, f"{dtype} {N} x {V}, rest {l is not None}: gradient of the loss")
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("V", [63, 65, 96, 129, 200, 257, 500, 601, 897, 1021, 1500, 2049])
+def test_many_alternatives_of_short_rows(B, V, dtype):
+    """As many alternatives as there are vectors in a row, half and twice as many; some rows with fewer classes than that, equal values."""
+    N, dt = 21, TYPES[dtype]
+    for n_rows, pad in ((N, 1), (700, 0)):
+        z, t = logits_of(n_rows, V, dt, pad=pad), targets_of(n_rows, V)
+        z[3] = torch.randint(-2, 3, (V,), generator=torch.Generator().manual_seed(V)).to(dt).to(dev)         # ties
+        z[4, : V - V // 5] = -INF                                      # fewer classes than alternatives
+        z[5, 1:] = -INF
+        z[6] = -INF
+        z[7] = torch.finfo(dt).min
+        z[8, V // 2 :] = torch.finfo(dt).min
+        z[9] = z[9].abs() * -0.0                                       # both zeros
+        z[10] = z[10] * 1e-3 + 1.0                                     # few different values in 16 bits
+        for K in sorted({min(V, 128), min(V, 64), min(V, 65), min(V, 33), 20, max(1, min(128, V // 8)), max(1, min(128, V // 4))}):
+            check_score(z, t, K, 0.8, run_score(B, z, t, K, 0.8), f"{dtype} {n_rows} x {V}, K = {K}")
+
+
 @pytest.mark.parametrize("V", [2047, 2048, 2049, 6144, 6145, 16385, 20479, 20480, 20489, 24576, 24577, 28672, 32768])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_rows_that_end_where_a_piece_does(B, dtype, V):
