@@ -25,6 +25,7 @@ FLAG_DENSE_FORMAT = 16
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # QSL_F32, QSL_BF16, QSL_F16
 TOP_MAX = 128
 TEACHER_MAX = 256
+SIZE_END = 1 << 31                                                    # rows and classes stay below
 
 OK, ERR_INVALID_ARG, ERR_BUFFER_TOO_SMALL, ERR_NONFINITE_INPUT, ERR_DEVICE, ERR_UNSUPPORTED = range(6)
 
@@ -153,6 +154,8 @@ def _rows_of(t, what):
     if t.dim() != 2 or not t.is_cuda or t.dtype not in DTYPES:
         raise ValueError(f"{what}: expected a device tensor [rows, vocab] of float32, bfloat16 or float16")
     rows, vocab = t.shape
+    if rows >= SIZE_END or vocab >= SIZE_END:                             # (ctypes would keep the lower 32 bits)
+        raise ValueError(f"{what}: expected less than 2^31 rows and classes, got {list(t.shape)}")
     stride, step = t.stride()
     if (step != 1 and vocab != 1) or (rows > 1 and stride < vocab):
         raise ValueError(f"{what}: expected contiguous rows that do not overlap, got strides {t.stride()}")
@@ -174,6 +177,8 @@ _current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurre
 def _on_logits(where, fn, logits, scale, top, workspace, *args):
     """Calls fn(rows, *args, workspace, its size, stream) on the logits' device and its current stream."""
     data, stride = _rows_of(logits, "logits")
+    if top >= SIZE_END:
+        raise ValueError(f"{where}: {top} alternatives or entries a row")
     rows, vocab = logits.shape
     z = C.byref(_Logits(data, stride, rows, vocab, DTYPES[logits.dtype], scale))
     if workspace is None:
@@ -194,6 +199,8 @@ def _on_logits(where, fn, logits, scale, top, workspace, *args):
 def logits_workspace_bytes(logits, top=0):
     """`qsl_logits_workspace_bytes` of these rows: what `workspace=` of the calls below has to hold (they allocate it if it is not given)."""
     data, stride = _rows_of(logits, "logits")
+    if not 0 <= top < SIZE_END:
+        return 0
     return int(_lib.qsl_logits_workspace_bytes(C.byref(_Logits(data, stride, logits.shape[0], logits.shape[1], DTYPES[logits.dtype], 1.0)), top))
 
 
