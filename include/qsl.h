@@ -313,7 +313,8 @@ typedef struct {
  *   lse != NULL:  q_k = exp(scale value_k - lse); what the entries leave over, q_r = max(0, 1 - sum_k q_k), is one more class, which the
  *                 student gives p_r = 1 - sum_k p_{index_k}:                     loss as above + q_r (ln q_r - ln p_r)
  *                 (without that term where no class is left outside the entries, or all of them have logit -inf)
- * Terms with q = 0 are 0; a class with q > 0 and logit -inf makes the loss +inf.  A row without entries has loss 0 and gradient 0.
+ * Terms with q = 0 are 0; a class with q > 0 and logit -inf makes the loss +inf.  A row without entries, or (lse == NULL) with none but of
+ * value -inf, has loss 0 and gradient 0.  A NaN or +inf among the logits comes first: it makes the loss and the whole gradient NaN there too.
  *   loss   device, float [rows] or NULL
  *   stats  device, float [rows, 8] or NULL: for qsl_distill_backward on the same arguments; one of the two has to be there */
 qsl_status qsl_distill(const qsl_logits *z, const qsl_teacher *teacher, float *loss, float *stats, void *workspace,

@@ -1141,7 +1141,7 @@ __device__ __forceinline__ void student_sums(const DistillArgs& a, uint64_t row,
     if (b.sum_q != b.sum_q) F = NAN;
   }
   if (t == 0.0) F = 0.0;                                              // a row that leaves nothing
-  if (b.bad) F = NAN;
+  if (b.bad || t != t) F = NAN;                                       // (t has met every logit: also the entries', where nothing else is left)
   if (lane_id() == 0) { b.m = o.m; b.s = o.s; b.F = static_cast<float>(F); b.m_all = m_all; b.t_all = t; }
   wave_lds_fence();
 }
@@ -1166,13 +1166,13 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, Stat o, cons
     const double lp = outside > 0.5 ? log(outside) : (o.m - m_all) * c + log(o.s / t);
     loss += left * (log1p(-b.sum_q) - lp);
   }
-  return b.bad ? NAN : static_cast<float>(loss);
+  return b.bad || t != t ? NAN : static_cast<float>(loss);
 }
 
 // the gradient in an entry's class
 template <bool REST>
 __device__ __forceinline__ float taught(const TeacherBox& b, uint32_t k, float g, float cl) {
-  if (b.bad) return NAN;
+  if (b.bad || b.t_all != b.t_all) return NAN;
   if (b.t_all == 0.0 || (!REST && !b.some)) return 0.0f;               // a row that leaves nothing, or teaches nothing
   const float p = exp2_((b.z[k] - b.m_all) * cl) / static_cast<float>(b.t_all);
   return g * (p - b.q[k]);
