@@ -303,7 +303,8 @@ typedef struct {
   const int32_t *index;      /* device, [rows, top]: classes; < 0: no entry; >= vocab: the row's results are NaN; a class that stands in a row
                                 more than once counts where it stands first                              */
   const float *value;        /* device, [rows, top]: the teacher's logits (or log probabilities) there   */
-  const float *lse;          /* device, [rows]: ln of the sum of exp(scale * logit) over all the teacher's classes, or NULL */
+  const float *lse;          /* device, [rows]: ln of the sum of exp(scale * logit) over all the teacher's classes, or NULL.  (Of log
+                                probabilities with scale 1: 0, or -inf where qsl_token_logprobs gave an lse of -inf)         */
   uint32_t top;              /* entries per row, 1 .. QSL_TEACHER_MAX                                    */
   float scale;               /* the factor of `value`, in the range of qsl_logits' scale                 */
 } qsl_teacher;
@@ -313,8 +314,12 @@ typedef struct {
  *   lse != NULL:  q_k = exp(scale value_k - lse); what the entries leave over, q_r = max(0, 1 - sum_k q_k), is one more class, which the
  *                 student gives p_r = 1 - sum_k p_{index_k}:                     loss as above + q_r (ln q_r - ln p_r)
  *                 (without that term where no class is left outside the entries, or all of them have logit -inf)
- * Terms with q = 0 are 0; a class with q > 0 and logit -inf makes the loss +inf.  A row without entries, or (lse == NULL) with none but of
- * value -inf, has loss 0 and gradient 0.  A NaN or +inf among the logits comes first: it makes the loss and the whole gradient NaN there too.
+ * Terms with q = 0 are 0; a class with q > 0 and logit -inf makes the loss +inf.  A row teaches nothing, loss 0 and gradient 0,
+ *   - with lse == NULL if it has no entries, or none but of value -inf;
+ *   - with an lse of -inf, a teacher's row that held nothing but -inf, whatever the entries.  (Entries of value -inf with a finite lse say that
+ *     the teacher's mass lies elsewhere, q_r = 1; no entries with a finite lse: q_r = p_r = 1, loss 0.)
+ * A NaN or +inf among the logits comes first: it makes the loss and the whole gradient NaN there too; so does a NaN among the entries' values
+ * unless the logits are all -inf (gradient 0).
  *   loss   device, float [rows] or NULL
  *   stats  device, float [rows, 8] or NULL: for qsl_distill_backward on the same arguments; one of the two has to be there */
 qsl_status qsl_distill(const qsl_logits *z, const qsl_teacher *teacher, float *loss, float *stats, void *workspace,

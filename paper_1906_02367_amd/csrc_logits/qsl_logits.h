@@ -954,7 +954,7 @@ struct TeacherBox {
   float value[TEACHER_MAX];        // the teacher's logits
   float z[TEACHER_MAX];            // the student's logits there
   float q[TEACHER_MAX];            // the teacher's probabilities
-  uint32_t bad, some;              // an index outside; whether the row teaches anything
+  uint32_t bad, some;              // an index outside; whether the row teaches anything (a NaN counts)
   double lse, sum_q;               // of the teacher's logits
   float m, s, F, m_all;
   double t_all;                    // sum of exp(c (z_i - m_all)) over the whole row
@@ -1078,13 +1078,16 @@ __device__ __forceinline__ void wave_lds_fence() {
 // What follows is one wave's, K entries at most four times its lanes, in 64 bits: the loss is a difference of logarithms that nearly agree
 // when the student is good.  The loops stay loops, to leave the registers to the row.
 
-// the teacher's probabilities; without any mass (no entries, or all of them -inf) and without the rest as a class the row teaches nothing
+// the teacher's probabilities.  A row teaches nothing whose entries have no mass (none, or all of them -inf) and that leaves nothing over:
+// without the rest as a class, or where its normaliser says that the teacher's row held nothing but -inf.
 template <bool REST>
 __device__ __forceinline__ void teacher_probabilities(const DistillArgs& a, uint64_t row, TeacherBox& b) {
   double lse = 0.0, top = 0.0;
   bool some = true;
-  if (REST) top = lse = a.tlse[row];
-  else {
+  if (REST) {
+    top = lse = a.tlse[row];
+    some = lse != -INFINITY;
+  } else {
     float most = -INFINITY;
     bool any = false;
 #pragma unroll 1
@@ -1099,12 +1102,13 @@ __device__ __forceinline__ void teacher_probabilities(const DistillArgs& a, uint
 #pragma unroll 1
   for (uint32_t k = lane_id(); k < a.K; k += 64)
     if (b.index[k] >= 0) {
-      const double x = some ? exp(static_cast<double>(b.value[k]) * a.ct - top) : 0.0;
+      const double x = some ? exp(static_cast<double>(b.value[k]) * a.ct - top) : REST && b.value[k] != b.value[k] ? NAN : 0.0;
       if (REST) b.q[k] = static_cast<float>(x);
       else e[k] = x;
       sum += x;
     }
   sum = wave_sum_d(sum);
+  if (sum != sum) some = true;
   if (!REST) {
 #pragma unroll 1
     for (uint32_t k = lane_id(); k < a.K; k += 64) if (b.index[k] >= 0) b.q[k] = some ? static_cast<float>(e[k] / sum) : 0.0f;
@@ -1138,9 +1142,9 @@ __device__ __forceinline__ void student_sums(const DistillArgs& a, uint64_t row,
     t = inside + outside;
     F = outside / t - fmax(1.0 - b.sum_q, 0.0);
     if (o.s == 0.0f) F = 0.0;                                         // nothing outside: the rest is left out
-    if (b.sum_q != b.sum_q) F = NAN;
   }
-  if (t == 0.0) F = 0.0;                                              // a row that leaves nothing
+  if (b.sum_q != b.sum_q) F = NAN;                                    // a NaN among the teacher's entries
+  if (t == 0.0 || !b.some) F = 0.0;                                   // a row that leaves nothing, or teaches nothing
   if (b.bad || t != t) F = NAN;                                       // (t has met every logit: also the entries', where nothing else is left)
   if (lane_id() == 0) { b.m = o.m; b.s = o.s; b.F = static_cast<float>(F); b.m_all = m_all; b.t_all = t; }
   wave_lds_fence();
@@ -1150,7 +1154,7 @@ template <bool REST>
 __device__ __forceinline__ float distill_loss(const DistillArgs& a, Stat o, const TeacherBox& b) {
   const double c = a.c, m_all = b.m_all, t = b.t_all, L = log(t);
   double loss = 0.0;
-  if (REST || b.some) {
+  if (b.some) {
 #pragma unroll 1
     for (uint32_t k = lane_id(); k < a.K; k += 64) {
       if (b.index[k] < 0 || b.q[k] == 0.0f) continue;
@@ -1160,7 +1164,7 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, Stat o, cons
   }
   loss = wave_sum_d(loss);
   const double left = fmax(1.0 - b.sum_q, 0.0);
-  if (REST && o.s != 0.0f && left != 0.0) {
+  if (REST && b.some && o.s != 0.0f && left != 0.0) {
     // what the student leaves over: from what is inside where that is the smaller part
     const double outside = o.s * exp((o.m - m_all) * c) / t;
     const double lp = outside > 0.5 ? log(outside) : (o.m - m_all) * c + log(o.s / t);
@@ -1170,10 +1174,10 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, Stat o, cons
 }
 
 // the gradient in an entry's class
-template <bool REST>
 __device__ __forceinline__ float taught(const TeacherBox& b, uint32_t k, float g, float cl) {
   if (b.bad || b.t_all != b.t_all) return NAN;
-  if (b.t_all == 0.0 || (!REST && !b.some)) return 0.0f;               // a row that leaves nothing, or teaches nothing
+  if (b.t_all == 0.0 || !b.some) return 0.0f;                          // a row that leaves nothing, or teaches nothing
+  if (b.sum_q != b.sum_q) return NAN;
   const float p = exp2_((b.z[k] - b.m_all) * cl) / static_cast<float>(b.t_all);
   return g * (p - b.q[k]);
 }
@@ -1228,7 +1232,7 @@ __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
   if (a.dz) {
     __syncthreads();                                                  // the entries' classes are written again
     for (uint32_t k = threadIdx.x; k < a.K; k += TH)
-      if (b.index[k] >= 0) dz[b.index[k]] = static_cast<E>(taught<REST>(b, k, g, cl));
+      if (b.index[k] >= 0) dz[b.index[k]] = static_cast<E>(taught(b, k, g, cl));
   }
 }
 
@@ -1281,7 +1285,7 @@ __global__ __launch_bounds__(256) void k_distill_join(DistillArgs a, Slices sl, 
     const uint32_t k = threadIdx.x;
     if (k < a.K) {
       w.index[static_cast<uint64_t>(row) * a.K + k] = b.index[k];
-      w.value[static_cast<uint64_t>(row) * a.K + k] = b.index[k] >= 0 ? taught<REST>(b, k, g, cl) : 0.0f;
+      w.value[static_cast<uint64_t>(row) * a.K + k] = b.index[k] >= 0 ? taught(b, k, g, cl) : 0.0f;
     }
   }
   if (threadIdx.x < 64 && !a.stats_in) {

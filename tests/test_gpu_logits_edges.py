@@ -48,6 +48,40 @@ def three_ways(B, z, index, value, **kw):
 
 
 @pytest.mark.parametrize("N,V,dtype", HELD_AND_SPLIT)
+def test_a_teacher_whose_row_has_no_class(B, N, V, dtype):
+    """What token_logprobs hands out for a row of -inf, handed on: it teaches nothing, with the rest as a class and without."""
+    K = 6
+    teacher = logits_of(N, V, dtype, seed=1)
+    teacher[0] = -INF
+    teacher[3] = -INF
+    z = logits_of(N, V, dtype)
+    z[3] = -INF                                                        # nor has the student's
+    index, value, lse = taught_by(B, teacher, K)
+    assert lse[0] == -INF and (value[0] == -INF).all()
+    kept = torch.where(lse == -INF, lse, 0.0)                          # of log probabilities the sum is 1
+    r = X.rows_of(z, 1.0)
+    for l in (None, kept):
+        g, loss, loss2, dz, dz2 = three_ways(B, z, index, value, teacher_lse=l)
+        some = torch.tensor([n for n in range(N) if n not in (0, 3)])
+        rows = {k: v[some] if torch.is_tensor(v) and v.dim() else v for k, v in r.items()}
+        want, tol_loss, want_dz, tol = X.distill(rows, index.cpu()[some], value.cpu()[some], 1.0, None if l is None else l.cpu()[some], g.cpu()[some], TYPES[dtype])
+        for a, b in ((loss, dz), (loss2, dz2)):
+            assert a[[0, 3]].tolist() == [0.0, 0.0] and not b[[0, 3]].any(), (V, l is None)
+            X.check(a[some], want, tol_loss, f"{V}: loss")
+            X.check(b[some], want_dz, tol, f"{V}: gradient")
+    # the teacher's logits instead of their logarithms, and its lse as it is
+    raw = teacher.float().gather(1, index.long())
+    g, loss, loss2, dz, dz2 = three_ways(B, z, index, raw, teacher_lse=lse)
+    assert loss[[0, 3]].tolist() == [0.0, 0.0] and not dz[[0, 3]].any() and not dz2[[0, 3]].any() and torch.equal(loss, loss2)
+    # a NaN in the table or among the student's logits is one in the results, whatever the teacher has
+    raw[0, 2] = NAN
+    z[3, V // 2] = NAN
+    g, loss, loss2, dz, dz2 = three_ways(B, z, index, raw, teacher_lse=lse)
+    assert torch.isnan(loss[[0, 3]]).all() and torch.isnan(loss2[[0, 3]]).all() and torch.isnan(dz[[0, 3]]).all() and torch.isnan(dz2[[0, 3]]).all()
+    assert torch.isfinite(dz[1]).all() and torch.isfinite(loss[1])
+
+
+@pytest.mark.parametrize("N,V,dtype", HELD_AND_SPLIT)
 def test_nan_among_the_entries_with_nothing_outside(B, N, V, dtype):
     """Only the entries' classes are left, one of them NaN or +inf: the row's results are NaN, at the classes outside too."""
     K = 5
@@ -68,3 +102,16 @@ def test_nan_among_the_entries_with_nothing_outside(B, N, V, dtype):
             assert torch.isnan(loss[n]) and torch.isnan(loss2[n]), (n, l is None)
             assert torch.isnan(dz[n]).all() and torch.isnan(dz2[n]).all(), (n, l is None)
         assert torch.isfinite(loss[2]) and torch.isfinite(dz[2]).all() and torch.isfinite(dz2[2]).all()
+
+
+@pytest.mark.parametrize("N,V,dtype", HELD_AND_SPLIT)
+def test_nan_in_a_teachers_table(B, N, V, dtype):
+    """One NaN among a row's values: loss and gradient of the row are NaN at every class, other rows are as without it."""
+    index, value, lse = taught_by(B, logits_of(N, V, dtype, seed=2), 5)
+    z = logits_of(N, V, dtype)
+    for l in (None, torch.full((N,), 0.125, device=dev)):
+        clean = three_ways(B, z, index, value, teacher_lse=l)[1:]
+        broken = value.clone()
+        broken[1, 3] = NAN
+        for a, b in zip(three_ways(B, z, index, broken, teacher_lse=l)[1:], clean):
+            assert torch.isnan(a[1]).all() and torch.equal(a[[0, 2, 3, 4]], b[[0, 2, 3, 4]]), (V, l is None)
