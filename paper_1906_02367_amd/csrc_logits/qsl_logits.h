@@ -1128,7 +1128,7 @@ __device__ __forceinline__ void student_sums(const DistillArgs& a, uint64_t row,
   if (a.stats_in) {
     const float* s = a.stats_in + 8ull * row;
     o.m = s[0]; o.s = s[1]; F = s[2]; m_all = s[3];
-    t = exp(static_cast<double>(s[4]));
+    t = s[4];                                                         // as taught() rounds it: nothing is lost
   } else if (REST) {
     float most = -INFINITY;
 #pragma unroll 1
@@ -1186,7 +1186,7 @@ __device__ __forceinline__ void distill_outputs(const DistillArgs& a, uint32_t r
   if (a.loss) a.loss[row] = loss;
   if (a.stats) {
     float* s = a.stats + 8ull * row;
-    s[0] = b.m; s[1] = b.s; s[2] = b.F; s[3] = b.m_all; s[4] = static_cast<float>(log(b.t_all)); s[5] = s[6] = s[7] = 0.0f;
+    s[0] = b.m; s[1] = b.s; s[2] = b.F; s[3] = b.m_all; s[4] = static_cast<float>(b.t_all); s[5] = s[6] = s[7] = 0.0f;
   }
 }
 

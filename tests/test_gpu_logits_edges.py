@@ -115,3 +115,15 @@ def test_nan_in_a_teachers_table(B, N, V, dtype):
         broken[1, 3] = NAN
         for a, b in zip(three_ways(B, z, index, broken, teacher_lse=l)[1:], clean):
             assert torch.isnan(a[1]).all() and torch.equal(a[[0, 2, 3, 4]], b[[0, 2, 3, 4]]), (V, l is None)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("N,V,dtype", HELD_AND_SPLIT)
+def test_kept_statistics_of_a_distillation_lose_nothing(B, N, V, dtype, rest):
+    """The row's sums are kept in the precision that the gradient takes them in: from them it comes out with the same bits."""
+    index, value, lse = taught_by(B, logits_of(N, V, dtype, seed=3), min(V, 64))
+    z = logits_of(N, V, dtype, seed=4)
+    if rest:
+        value -= 0.25                                                  # something is left over
+    g, loss, loss2, dz, dz2 = three_ways(B, z, index, value, teacher_lse=torch.zeros(N, device=dev) if rest else None)
+    assert torch.equal(loss, loss2) and torch.equal(dz, dz2)
