@@ -250,6 +250,8 @@ qsl_status qsl_timing_read(qsl_ctx *ctx, double *total_ms, uint32_t *launches);
  *     begin at odd places, another stride) the sums may be rounded differently; alternatives are the same.
  *   - A logit of -inf is a class left out: its probability and gradient are 0, its log probability -inf.  A row of nothing else has
  *     lse and log probabilities -inf, entropy 0 and gradient 0.  A NaN or +inf makes the row's results NaN (indices: -1).
+ *   - Arrays that a call writes, `workspace` among them, share no memory with one another or with what it reads, or the call is refused. Two
+ *     exceptions: dlogits may be the logits (below), and the loss of qsl_distill_backward may stand where grad_loss does.
  *   - rows = 0 does nothing.  What lies between two rows (stride > vocab) is neither read nor written.
  */
 enum { QSL_F32 = 0, QSL_BF16 = 1, QSL_F16 = 2 };

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "qsl.h"
@@ -37,6 +38,32 @@ bool logits_ok(const qsl_logits* z) {
   if (!z || z->dtype > QSL_F16 || z->vocab == 0 || z->vocab >= 1u << 31 || z->rows >= 1u << 31) return false;
   if (!stride_ok(z, z->stride) || !scale_ok(z->scale)) return false;
   return z->rows == 0 || (z->data && aligned(z->data, elem_size(z->dtype)));
+}
+
+// `rows` pieces of `bytes` each, `step` from one to the next
+struct Memory { uintptr_t at; uint64_t bytes, step, rows; };
+Memory array(const void* p, uint64_t bytes) { return Memory{reinterpret_cast<uintptr_t>(p), bytes, bytes, p && bytes ? 1u : 0u}; }
+Memory rows_at(const qsl_logits* z, const void* p, uint64_t stride) {
+  const uint64_t es = elem_size(z->dtype);
+  return Memory{reinterpret_cast<uintptr_t>(p), z->vocab * es, stride * es, p ? z->rows : 0};
+}
+bool meet(const Memory& a, const Memory& b) {
+  if (a.rows == 0 || b.rows == 0) return false;
+  const uintptr_t a_end = a.at + (a.rows - 1) * a.step + a.bytes, b_end = b.at + (b.rows - 1) * b.step + b.bytes;
+  if (a_end <= b.at || b_end <= a.at) return false;
+  if (a.rows > 1 && b.rows == 1) return meet(b, a);
+  if (b.rows == 1 || a.rows > 1) return true;
+  // one piece among many: where it begins, or the next piece behind that
+  const uint64_t x = a.at > b.at ? a.at - b.at : 0, k = x / b.step;
+  return x < k * b.step + b.bytes || (k + 1 < b.rows && a_end - b.at > (k + 1) * b.step);
+}
+// no output shares memory with another or with an input
+bool apart(std::initializer_list<Memory> out, std::initializer_list<Memory> in) {
+  for (const Memory* o = out.begin(); o != out.end(); ++o) {
+    for (const Memory* p = out.begin(); p != o; ++p) if (meet(*o, *p)) return false;
+    for (const Memory& i : in) if (meet(*o, i)) return false;
+  }
+  return true;
 }
 
 // dlogits are the logits, or lie apart from them
@@ -220,10 +247,15 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
       !aligned(top_logprob, 4) || !aligned(stats, 16)) return QSL_ERR_INVALID_ARG;
   const qsl_status st = check_workspace(z, top, workspace, workspace_bytes);
   if (st != QSL_OK) return st;
+  const Plan plan = top ? plan_top(z) : plan_stats(z);
+  const Workspace ws = lay_out(z, plan, top, 0, workspace);
+  const uint64_t n = z->rows;
+  if (!apart({array(logprob, 4 * n), array(entropy, 4 * n), array(lse, 4 * n), array(top_index, 4 * n * top), array(top_logprob, 4 * n * top),
+              array(stats, 16 * n), array(workspace, ws.need)},
+             {array(logprob ? target : nullptr, 8 * n), rows_at(z, z->data, z->stride)})) return QSL_ERR_INVALID_ARG;
   const ScoreArgs a = {z->data, z->stride, z->rows, z->vocab, top, z->scale, target, logprob, entropy, lse, top_index, top_logprob, stats};
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const Plan plan = top ? plan_top(z) : plan_stats(z);
-  const Slices sl = lay_out(z, plan, top, 0, workspace).sl;
+  const Slices sl = ws.sl;
   const dim3 rows = grid_of(z->rows);
   const bool last = !stats || z->rows * row_bytes(z) > CACHE_BYTES;      // with `stats` the gradient is to follow, which finds the rows in the cache
   pick_type(z, [&](auto e) {
@@ -266,10 +298,15 @@ extern "C" qsl_status qsl_token_logprobs_backward(const qsl_logits* z, const int
       !aligned(entropy, 4)) return QSL_ERR_INVALID_ARG;
   const qsl_status st = check_workspace(z, 0, workspace, workspace_bytes);
   if (st != QSL_OK) return st;
+  const Plan plan = plan_gradient(z);
+  const Workspace ws = lay_out(z, plan, 0, 0, workspace);
+  const uint64_t n = z->rows;
+  const Memory lp = array(logprob, 4 * n), H = array(entropy, 4 * n), parts = array(workspace, stats ? 0 : ws.need);
+  if (!apart({lp, H, parts, rows_at(z, dlogits, dstride)}, {array(target, 8 * n), array(grad_logprob, 4 * n), array(grad_entropy, 4 * n), array(stats, 16 * n)}) ||
+      !apart({lp, H, parts}, {rows_at(z, z->data, z->stride)})) return QSL_ERR_INVALID_ARG;
   const GradArgs a = {z->data, dlogits, z->stride, dstride, z->rows, z->vocab, z->scale, target, grad_logprob, grad_entropy, stats, logprob, entropy};
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const Plan plan = plan_gradient(z);
-  const Slices sl = lay_out(z, plan, 0, 0, workspace).sl;
+  const Slices sl = ws.sl;
   pick_type(z, [&](auto e) {
     typedef decltype(e) E;
     pick_bool(grad_entropy || entropy, [&](auto ent) {
@@ -292,9 +329,14 @@ static qsl_status launch_distill(const qsl_logits* z, const qsl_teacher* t, cons
                                  void* hip_stream) {
   const qsl_status st = check_workspace(z, t->top, workspace, workspace_bytes);
   if (st != QSL_OK) return st;
-  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const Plan plan = plan_gradient(z);
   const Workspace ws = lay_out(z, plan, 0, t->top, workspace);
+  const uint64_t n = z->rows, entries = 4 * n * t->top;
+  const Memory loss = array(a.loss, 4 * n), stats = array(a.stats, 32 * n), parts = array(workspace, ws.need), dz = rows_at(z, a.dz, a.dstride), g = array(a.g, 4 * n);
+  // a row's weight is read before its loss is written, by the threads of one block: one array may hold both
+  if (!apart({loss, stats, parts, dz}, {array(t->index, entries), array(t->value, entries), array(t->lse, 4 * n), array(a.stats_in, 32 * n)}) ||
+      !apart({loss, stats, parts}, {rows_at(z, z->data, z->stride)}) || !apart({stats, parts, dz}, {g}) || (a.loss != a.g && meet(loss, g))) return QSL_ERR_INVALID_ARG;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const Taught w = a.dz ? ws.w : Taught{nullptr, nullptr, nullptr};
   pick_type(z, [&](auto e) {
     typedef decltype(e) E;

@@ -127,3 +127,47 @@ def test_kept_statistics_of_a_distillation_lose_nothing(B, N, V, dtype, rest):
         value -= 0.25                                                  # something is left over
     g, loss, loss2, dz, dz2 = three_ways(B, z, index, value, teacher_lse=torch.zeros(N, device=dev) if rest else None)
     assert torch.equal(loss, loss2) and torch.equal(dz, dz2)
+
+
+@pytest.mark.parametrize("N,V,dtype", HELD_AND_SPLIT + [(700, 90, "fp32"), (300, 100001, "fp32")])
+def test_the_loss_where_its_weights_stood(B, N, V, dtype):
+    """The one array of qsl_distill_backward that may hold an input and an output."""
+    index, value, lse = taught_by(B, logits_of(N, V, dtype, seed=3), 5)
+    z = logits_of(N, V, dtype)
+    for l in (None, torch.full((N,), 0.125, device=dev)):
+        g, loss, loss2, dz, dz2 = three_ways(B, z, index, value, teacher_lse=l)
+        both, dz3 = g.clone(), torch.empty_like(z)
+        B.distill_backward(z, index, value, dz3, grad_loss=both, loss=both, teacher_lse=l)
+        assert torch.equal(both, loss) and torch.equal(dz3, dz), (V, l is None)
+
+
+@pytest.mark.parametrize("V", [40, 150001])
+def test_arrays_between_rows_and_beside_the_workspace(B, V):
+    """What lies in the gaps between rows, or right behind what it could be taken to overlap, is apart."""
+    N, K = 6, 5
+    held = torch.full((N, V + 60), 77.0, device=dev)
+    z = held[:, :V]
+    z.copy_(logits_of(N, V, "fp32"))
+    t = torch.randint(0, V, (N,), generator=torch.Generator().manual_seed(1)).to(dev)
+    gap = [held[n, V + (-V) % 4:][: 4 * N] for n in range(N)]             # 16-byte aligned if the row is
+    need = B.logits_workspace_bytes(z, K)
+    arena = torch.empty(need + 4096, dtype=torch.uint8, device=dev)
+    behind = arena[need:].view(torch.float32)
+    want = dict(logprob=new(N), entropy=new(N), lse=new(N), top_index=new(N, K, dtype=torch.int32), top_logprob=new(N, K), stats=new(N, 4))
+    B.token_logprobs(z, t, **want)
+    got = dict(logprob=gap[0][:N], entropy=gap[0][N:2 * N], lse=gap[1][:N], stats=behind[: 4 * N].view(N, 4), top_index=new(N, K, dtype=torch.int32),
+               top_logprob=behind[4 * N:4 * N + N * K].view(N, K))
+    B.token_logprobs(z, t, workspace=arena, **got)                        # larger than needed: only its first part is used
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    g = gap[2][:N].copy_(torch.linspace(-1, 1, N, device=dev))
+    dz, dz2 = torch.empty(N, V, device=dev), torch.empty(N, V, device=dev)
+    lp = gap[4][:N]
+    B.token_logprobs_backward(z, t, dz, grad_logprob=g, logprob=lp)
+    B.token_logprobs_backward(z, t, dz2, grad_logprob=g.clone(), logprob=want["logprob"])
+    assert torch.equal(dz, dz2) and torch.equal(lp, want["logprob"])
+    bad = [lambda: B.token_logprobs(z, t, logprob=z[1, :N]), lambda: B.token_logprobs_backward(z, t, dz, grad_logprob=g, logprob=g),
+           lambda: B.token_logprobs_backward(z, t, dz, grad_logprob=dz[3, :N]), lambda: B.token_logprobs(z, t, logprob=lp, entropy=lp)]
+    for f in bad:
+        with pytest.raises(B.QslError):
+            f()
