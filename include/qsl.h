@@ -250,6 +250,7 @@ qsl_status qsl_timing_read(qsl_ctx *ctx, double *total_ms, uint32_t *launches);
  *     begin at odd places, another stride) the sums may be rounded differently; alternatives are the same.
  *   - A logit of -inf is a class left out: its probability and gradient are 0, its log probability -inf.  A row of nothing else has
  *     lse and log probabilities -inf, entropy 0 and gradient 0.  A NaN or +inf makes the row's results NaN (indices: -1).
+ *   - Every array is aligned to its type's size, and where it is said to more than that.
  *   - Arrays that a call writes, `workspace` among them, share no memory with one another or with what it reads, or the call is refused. Two
  *     exceptions: dlogits may be the logits (below), and the loss of qsl_distill_backward may stand where grad_loss does.
  *   - rows = 0 does nothing.  What lies between two rows (stride > vocab) is neither read nor written.
@@ -279,7 +280,7 @@ size_t qsl_logits_workspace_bytes(const qsl_logits *z, uint32_t top);
  *   lse          device, float [rows] or NULL: ln sum_i exp(c z_i)
  *   top_index    device, int32 [rows, top] or NULL: the classes of the largest logits, largest first, ties to the lower index
  *   top_logprob  device, float [rows, top] or NULL: their logp
- *   stats        device, float [rows, 4] or NULL: for qsl_token_logprobs_backward on the same logits and scale
+ *   stats        device, float [rows, 4], 16-byte aligned, or NULL: for qsl_token_logprobs_backward on the same logits and scale
  *   workspace    device, at least qsl_logits_workspace_bytes() bytes, 256-byte aligned; may be NULL if that is 0 */
 qsl_status qsl_token_logprobs(const qsl_logits *z, const int64_t *target, uint32_t top, float *logprob, float *entropy,
                               float *lse, int32_t *top_index, float *top_logprob, float *stats, void *workspace,
@@ -294,7 +295,8 @@ qsl_status qsl_token_logprobs(const qsl_logits *z, const int64_t *target, uint32
  *                 weights are known beforehand needs this call alone: it can also hand out
  *   logprob, entropy  device, float [rows] or NULL, only with stats = NULL; logprob needs target
  *   dlogits       device, [rows] rows of vocab values of the logits' type, row n at element n * dstride; every value is written.  May be
- *                 the logits themselves (same pointer and stride); may not overlap them otherwise */
+ *                 the logits themselves (same pointer and stride); else the two share no element: they lie apart as a whole, or their rows, of
+ *                 the same stride, stand in turn */
 qsl_status qsl_token_logprobs_backward(const qsl_logits *z, const int64_t *target, const float *grad_logprob,
                                        const float *grad_entropy, const float *stats, float *logprob, float *entropy,
                                        void *dlogits, uint64_t dstride, void *workspace, size_t workspace_bytes,
@@ -323,7 +325,7 @@ typedef struct {
  * A NaN or +inf among the logits comes first: it makes the loss and the whole gradient NaN there too; so does a NaN among the entries' values
  * unless the logits are all -inf (gradient 0).
  *   loss   device, float [rows] or NULL
- *   stats  device, float [rows, 8] or NULL: for qsl_distill_backward on the same arguments; one of the two has to be there */
+ *   stats  device, float [rows, 8], 16-byte aligned, or NULL: for qsl_distill_backward on the same arguments; one of the two has to be there */
 qsl_status qsl_distill(const qsl_logits *z, const qsl_teacher *teacher, float *loss, float *stats, void *workspace,
                        size_t workspace_bytes, void *hip_stream);
 

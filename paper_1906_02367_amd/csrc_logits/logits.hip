@@ -52,7 +52,12 @@ bool meet(const Memory& a, const Memory& b) {
   const uintptr_t a_end = a.at + (a.rows - 1) * a.step + a.bytes, b_end = b.at + (b.rows - 1) * b.step + b.bytes;
   if (a_end <= b.at || b_end <= a.at) return false;
   if (a.rows > 1 && b.rows == 1) return meet(b, a);
-  if (b.rows == 1 || a.rows > 1) return true;
+  if (b.rows == 1) return true;
+  if (a.rows > 1) {      // of the same step: pieces in turn, the later ones in the gaps of the others; of another they are taken to meet
+    const Memory& f = a.at <= b.at ? a : b;
+    const uint64_t x = (b.at + a.at - 2 * f.at) % f.step;
+    return a.step != b.step || x < f.bytes || x + (&f == &a ? b : a).bytes > f.step;
+  }
   // one piece among many: where it begins, or the next piece behind that
   const uint64_t x = a.at > b.at ? a.at - b.at : 0, k = x / b.step;
   return x < k * b.step + b.bytes || (k + 1 < b.rows && a_end - b.at > (k + 1) * b.step);
@@ -66,16 +71,14 @@ bool apart(std::initializer_list<Memory> out, std::initializer_list<Memory> in) 
   return true;
 }
 
-// dlogits are the logits, or lie apart from them
+// dlogits are the logits, or share no element with them
 bool gradient_ok(const qsl_logits* z, const void* dz, uint64_t dstride) {
   const uint64_t es = elem_size(z->dtype);
   if (!stride_ok(z, dstride) || !aligned(dz, es)) return false;
   if (z->rows == 0) return true;
   if (!dz) return false;
   if (dz == z->data && (dstride == z->stride || z->rows == 1)) return true;
-  const uintptr_t a = reinterpret_cast<uintptr_t>(z->data), b = reinterpret_cast<uintptr_t>(dz);
-  const uint64_t la = ((z->rows - 1) * z->stride + z->vocab) * es, lb = ((z->rows - 1) * dstride + z->vocab) * es;
-  return a + la <= b || b + lb <= a;
+  return !meet(rows_at(z, z->data, z->stride), rows_at(z, dz, dstride));
 }
 
 bool teacher_ok(const qsl_logits* z, const qsl_teacher* t) {

@@ -171,3 +171,34 @@ def test_arrays_between_rows_and_beside_the_workspace(B, V):
     for f in bad:
         with pytest.raises(B.QslError):
             f()
+
+
+@pytest.mark.parametrize("first", [True, False])
+@pytest.mark.parametrize("gap", [0, 1])
+@pytest.mark.parametrize("N,V,dtype", HELD_AND_SPLIT + [(200, 33, "fp16"), (130, 100003, "bf16")])
+def test_gradient_rows_between_the_logits_rows(B, N, V, dtype, gap, first):
+    """Two halves of one array: rows in turn, none of which shares an element with another."""
+    held = torch.full((N, 2 * V + 2 * gap), 77.0, dtype=TYPES[dtype], device=dev)
+    a, b = held[:, :V], held[:, V + gap:2 * V + gap]
+    z, dz = (a, b) if first else (b, a)
+    z.copy_(logits_of(N, V, dtype))
+    before = z.clone()
+    t, g = torch.randint(0, V, (N,), generator=torch.Generator().manual_seed(1)).to(dev), torch.linspace(-1, 1, N, device=dev)
+    r = X.rows_of(z, 1.0)
+    lp, stats = new(N), new(N, 4)
+    B.token_logprobs(z, t, logprob=lp, stats=stats)
+    for kw in ({}, dict(stats=stats)):
+        dz.fill_(55.0)
+        B.token_logprobs_backward(z, t, dz, grad_logprob=g, **kw)
+        X.check(dz, *X.logprob_gradient(r, t, g, None, TYPES[dtype]), f"{N} x {V}")
+        assert torch.equal(z, before)
+    if N < 100:
+        index, value, lse = taught_by(B, logits_of(N, V, dtype, seed=3), 5)
+        apart = torch.empty_like(before)
+        B.distill_backward(before, index, value, apart, grad_loss=g)
+        B.distill_backward(z, index, value, dz, grad_loss=g)
+        want, tol_loss, want_dz, tol = X.distill(r, index.cpu(), value.cpu(), 1.0, None, g.cpu(), TYPES[dtype])
+        X.check(dz, want_dz, tol, f"{N} x {V}: distillation")
+        assert torch.equal(z, before)
+    if gap:
+        assert (held[:, V] == 77).all() and (held[:, 2 * V + 1] == 77).all()

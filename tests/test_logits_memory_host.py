@@ -83,3 +83,17 @@ def test_the_workspace_over_others(calls):
     }.items():
         for kw in clashes:
             assert calls[name](**kw) == INVALID, (name, kw)
+
+
+@pytest.mark.parametrize("dtype,es", [(0, 4), (1, 2), (2, 2)])
+def test_gradient_rows_that_share_elements_with_the_logits_rows(lib, dtype, es):  # noqa: F811
+    """Rows of 1,000 with 2,000 from one to the next: the second array's may begin 1,000 elements behind or before the first's, nowhere else."""
+    N, V, stride = 5, 1000, 2000
+    t = C.byref(Teacher(at(1), at(2), None, 5, 1.0))
+    for d in (1, 999, 1001, 1999, 2000, 2001, 2999, 3001, 4 * stride, 4 * stride + 999):
+        for dz, ds in ((Z + es * d, stride), (Z - es * d, stride)):
+            z = C.byref(Logits(Z, stride, N, V, dtype, 1.0))
+            assert lib.qsl_token_logprobs_backward(z, at(3), at(4), None, None, None, None, dz, ds, None, 0, None) == INVALID, (d, dz < Z)
+            assert lib.qsl_distill_backward(z, t, None, None, None, dz, ds, None, 0, None) == INVALID, (d, dz < Z)
+    for dz, ds in ((Z + es * 1000, 2001), (Z + es * 1000, 1999), (Z, 2001)):                    # of another stride: not looked at so closely
+        assert lib.qsl_token_logprobs_backward(C.byref(Logits(Z, stride, N, V, dtype, 1.0)), at(3), at(4), None, None, None, None, dz, ds, None, 0, None) == INVALID
