@@ -268,8 +268,10 @@ typedef struct {
   float scale;               /* c, 2^-100 <= c <= 2^100 (1: the logits as they are; 1 / temperature)    */
 } qsl_logits;
 
-/* Bytes of device memory that a call on such rows needs as `workspace`, a multiple of 256 (0 where a block takes a row by itself: for
- * shorter rows, unless there are few of them); `top` is the call's: its alternatives, its teacher's entries, 0 for none.  0 for invalid arguments too. */
+/* Bytes of device memory that are enough as `workspace` of any call on such rows, a multiple of 256; `top` is the call's: its alternatives, its
+ * teacher's entries, 0 for none.  0 for invalid arguments too.  A call that splits rows (long ones, and fairly long ones that are few) is
+ * refused with less; one that does not looks at no workspace.  Without alternatives no call does where this is 0 for top = 0, whatever a
+ * teacher's entries; qsl_token_logprobs_backward with kept statistics never does. */
 size_t qsl_logits_workspace_bytes(const qsl_logits *z, uint32_t top);
 
 /* Log probabilities of given classes, with the entropy and the best alternatives of every row.
@@ -281,7 +283,7 @@ size_t qsl_logits_workspace_bytes(const qsl_logits *z, uint32_t top);
  *   top_index    device, int32 [rows, top] or NULL: the classes of the largest logits, largest first, ties to the lower index
  *   top_logprob  device, float [rows, top] or NULL: their logp
  *   stats        device, float [rows, 4], 16-byte aligned, or NULL: for qsl_token_logprobs_backward on the same logits and scale
- *   workspace    device, at least qsl_logits_workspace_bytes() bytes, 256-byte aligned; may be NULL if that is 0 */
+ *   workspace    device, at least qsl_logits_workspace_bytes() bytes, 256-byte aligned; may be NULL where the call needs none */
 qsl_status qsl_token_logprobs(const qsl_logits *z, const int64_t *target, uint32_t top, float *logprob, float *entropy,
                               float *lse, int32_t *top_index, float *top_logprob, float *stats, void *workspace,
                               size_t workspace_bytes, void *hip_stream);

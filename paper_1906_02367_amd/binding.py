@@ -174,16 +174,19 @@ def _beside(t, what, device, dtype, shape):
 _current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _on_logits(where, fn, logits, scale, top, workspace, *args):
-    """Calls fn(rows, *args, workspace, its size, stream) on the logits' device and its current stream."""
+def _on_logits(where, fn, logits, scale, top, workspace, *args, entries=False, kept=False):
+    """Calls fn(rows, *args, workspace, its size, stream) on the logits' device and its current stream.  entries: `top` counts a teacher's
+    entries, not alternatives; kept: the call has its statistics."""
     data, stride = _rows_of(logits, "logits")
     if top >= SIZE_END:
         raise ValueError(f"{where}: {top} alternatives or entries a row")
     rows, vocab = logits.shape
     z = C.byref(_Logits(data, stride, rows, vocab, DTYPES[logits.dtype], scale))
-    if workspace is None:
-        need = _lib.qsl_logits_workspace_bytes(z, top)
+    if workspace is None and not kept:
+        need = _lib.qsl_logits_workspace_bytes(z, 0 if entries else top)
         if need:
+            if entries:
+                need = _lib.qsl_logits_workspace_bytes(z, top)
             workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
     device = logits.get_device()
     at, size = (None, 0) if workspace is None else (_beside(workspace, "workspace", device, torch.uint8, (workspace.numel(),)), workspace.numel())
@@ -233,7 +236,8 @@ def token_logprobs_backward(logits, target, dlogits, scale=1.0, grad_logprob=Non
     _on_logits("qsl_token_logprobs_backward", _lib.qsl_token_logprobs_backward, logits, scale, 0, workspace,
                _beside(target, "target", dev, torch.int64, (N,)), _beside(grad_logprob, "grad_logprob", dev, f32, (N,)),
                _beside(grad_entropy, "grad_entropy", dev, f32, (N,)), _beside(stats, "stats", dev, f32, (N, 4)),
-               _beside(logprob, "logprob", dev, f32, (N,)), _beside(entropy, "entropy", dev, f32, (N,)), out, dstride)
+               _beside(logprob, "logprob", dev, f32, (N,)), _beside(entropy, "entropy", dev, f32, (N,)), out, dstride,
+               kept=stats is not None)
 
 
 def _teacher(logits, index, value, lse, scale):
@@ -248,7 +252,7 @@ def distill(logits, teacher_index, teacher_value, scale=1.0, teacher_scale=1.0, 
     N, dev = logits.shape[0], logits.get_device()
     _on_logits("qsl_distill", _lib.qsl_distill, logits, scale, teacher_index.shape[-1], workspace,
                _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(loss, "loss", dev, torch.float32, (N,)),
-               _beside(stats, "stats", dev, torch.float32, (N, 8)))
+               _beside(stats, "stats", dev, torch.float32, (N, 8)), entries=True)
 
 
 def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, teacher_scale=1.0, teacher_lse=None, grad_loss=None,
@@ -259,7 +263,8 @@ def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, t
     out, dstride = _gradient_rows(dlogits, logits)
     _on_logits("qsl_distill_backward", _lib.qsl_distill_backward, logits, scale, teacher_index.shape[-1], workspace,
                _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(grad_loss, "grad_loss", dev, f32, (N,)),
-               _beside(stats, "stats", dev, f32, (N, 8)), _beside(loss, "loss", dev, f32, (N,)), out, dstride)
+               _beside(stats, "stats", dev, f32, (N, 8)), _beside(loss, "loss", dev, f32, (N,)), out, dstride,
+               entries=True)
 
 
 class Qsl:

@@ -213,9 +213,10 @@ Workspace lay_out(const qsl_logits* z, const Plan& p, uint32_t keys, uint32_t en
   return w;
 }
 
-qsl_status check_workspace(const qsl_logits* z, uint32_t top, const void* workspace, size_t bytes) {
+// `used`: what the call's own plan lays out; a call that uses none is not asked for any, the others for what the query says
+qsl_status check_workspace(const qsl_logits* z, uint32_t top, uint64_t used, const void* workspace, size_t bytes) {
+  if (used == 0) return QSL_OK;
   const size_t need = qsl_logits_workspace_bytes(z, top);
-  if (need == 0) return QSL_OK;
   if (!workspace || !aligned(workspace, 256)) return QSL_ERR_INVALID_ARG;
   return bytes < need ? QSL_ERR_BUFFER_TOO_SMALL : QSL_OK;
 }
@@ -233,7 +234,7 @@ qsl_status launched() { return hipGetLastError() == hipSuccess ? QSL_OK : QSL_ER
 extern "C" size_t qsl_logits_workspace_bytes(const qsl_logits* z, uint32_t top) {
   if (!logits_ok(z) || z->rows == 0 || top > std::max(QSL_TOP_MAX, QSL_TEACHER_MAX)) return 0;
   uint64_t need = std::max(lay_out(z, plan_stats(z), 0, 0, nullptr).need, lay_out(z, plan_gradient(z), 0, top, nullptr).need);
-  if (top) need = std::max(need, lay_out(z, plan_top(z), top, 0, nullptr).need);
+  if (top && top <= QSL_TOP_MAX) need = std::max(need, lay_out(z, plan_top(z), top, 0, nullptr).need);      // (more than that only a teacher has)
   return need;
 }
 
@@ -248,10 +249,10 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
   if (logprob && !target) return QSL_ERR_INVALID_ARG;
   if (!aligned(target, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4) || !aligned(top_index, 4) ||
       !aligned(top_logprob, 4) || !aligned(stats, 16)) return QSL_ERR_INVALID_ARG;
-  const qsl_status st = check_workspace(z, top, workspace, workspace_bytes);
-  if (st != QSL_OK) return st;
   const Plan plan = top ? plan_top(z) : plan_stats(z);
   const Workspace ws = lay_out(z, plan, top, 0, workspace);
+  const qsl_status st = check_workspace(z, top, ws.need, workspace, workspace_bytes);
+  if (st != QSL_OK) return st;
   const uint64_t n = z->rows;
   if (!apart({array(logprob, 4 * n), array(entropy, 4 * n), array(lse, 4 * n), array(top_index, 4 * n * top), array(top_logprob, 4 * n * top),
               array(stats, 16 * n), array(workspace, ws.need)},
@@ -299,12 +300,12 @@ extern "C" qsl_status qsl_token_logprobs_backward(const qsl_logits* z, const int
   if (stats && (logprob || entropy)) return QSL_ERR_INVALID_ARG;
   if (!aligned(target, 8) || !aligned(grad_logprob, 4) || !aligned(grad_entropy, 4) || !aligned(stats, 16) || !aligned(logprob, 4) ||
       !aligned(entropy, 4)) return QSL_ERR_INVALID_ARG;
-  const qsl_status st = check_workspace(z, 0, workspace, workspace_bytes);
-  if (st != QSL_OK) return st;
-  const Plan plan = plan_gradient(z);
+  const Plan plan = stats ? WHOLE : plan_gradient(z);
   const Workspace ws = lay_out(z, plan, 0, 0, workspace);
+  const qsl_status st = check_workspace(z, 0, ws.need, workspace, workspace_bytes);
+  if (st != QSL_OK) return st;
   const uint64_t n = z->rows;
-  const Memory lp = array(logprob, 4 * n), H = array(entropy, 4 * n), parts = array(workspace, stats ? 0 : ws.need);
+  const Memory lp = array(logprob, 4 * n), H = array(entropy, 4 * n), parts = array(workspace, ws.need);
   if (!apart({lp, H, parts, rows_at(z, dlogits, dstride)}, {array(target, 8 * n), array(grad_logprob, 4 * n), array(grad_entropy, 4 * n), array(stats, 16 * n)}) ||
       !apart({lp, H, parts}, {rows_at(z, z->data, z->stride)})) return QSL_ERR_INVALID_ARG;
   const GradArgs a = {z->data, dlogits, z->stride, dstride, z->rows, z->vocab, z->scale, target, grad_logprob, grad_entropy, stats, logprob, entropy};
@@ -330,10 +331,10 @@ extern "C" qsl_status qsl_token_logprobs_backward(const qsl_logits* z, const int
 
 static qsl_status launch_distill(const qsl_logits* z, const qsl_teacher* t, const DistillArgs& a, void* workspace, size_t workspace_bytes,
                                  void* hip_stream) {
-  const qsl_status st = check_workspace(z, t->top, workspace, workspace_bytes);
-  if (st != QSL_OK) return st;
   const Plan plan = plan_gradient(z);
   const Workspace ws = lay_out(z, plan, 0, t->top, workspace);
+  const qsl_status st = check_workspace(z, t->top, ws.need, workspace, workspace_bytes);
+  if (st != QSL_OK) return st;
   const uint64_t n = z->rows, entries = 4 * n * t->top;
   const Memory loss = array(a.loss, 4 * n), stats = array(a.stats, 32 * n), parts = array(workspace, ws.need), dz = rows_at(z, a.dz, a.dstride), g = array(a.g, 4 * n);
   // a row's weight is read before its loss is written, by the threads of one block: one array may hold both

@@ -202,3 +202,30 @@ def test_gradient_rows_between_the_logits_rows(B, N, V, dtype, gap, first):
         assert torch.equal(z, before)
     if gap:
         assert (held[:, V] == 77).all() and (held[:, 2 * V + 1] == 77).all()
+
+
+@pytest.mark.parametrize("N,V", [(140, 100003), (600, 140001), (3, 140001)])
+def test_calls_that_need_no_workspace_take_none(B, N, V):
+    """Straight through the C entry points, without the binding's allocation."""
+    z, t = logits_of(N, V, "bf16"), torch.randint(0, V, (N,), generator=torch.Generator().manual_seed(1)).to(dev)
+    index, value, lse = taught_by(B, z, 5)
+    stats, want, dz = new(N, 4), torch.empty_like(z), torch.empty_like(z)
+    lp, g, loss, want_loss = new(N), torch.linspace(-1, 1, N, device=dev), new(N), new(N)
+    B.token_logprobs(z, t, logprob=lp, stats=stats)
+    B.token_logprobs_backward(z, t, want, grad_logprob=g, stats=stats, workspace=torch.empty(B.logits_workspace_bytes(z), dtype=torch.uint8, device=dev))
+    rows = B.C.byref(B._Logits(z.data_ptr(), V, N, V, 1, 1.0))
+    stream = torch.cuda.current_stream().cuda_stream
+    st = B._lib.qsl_token_logprobs_backward(rows, t.data_ptr(), g.data_ptr(), None, stats.data_ptr(), None, None, dz.data_ptr(), V, None, 0, stream)
+    assert st == B.OK and torch.equal(dz, want)
+    teacher = B.C.byref(B._Teacher(index.data_ptr(), value.data_ptr(), None, 5, 1.0))
+    B.distill(z, index, value, loss=want_loss)
+    st = B._lib.qsl_distill(rows, teacher, loss.data_ptr(), None, None, 0, stream)
+    if B.logits_workspace_bytes(z) == 0:
+        assert st == B.OK and torch.equal(loss, want_loss)
+    else:
+        assert st == B.ERR_INVALID_ARG
+    st = B._lib.qsl_token_logprobs(rows, t.data_ptr(), 0, loss.data_ptr(), None, None, None, None, None, None, 0, stream)
+    if N >= 512 or B.logits_workspace_bytes(z) == 0:                   # many rows: a block walks along each
+        assert st == B.OK and torch.equal(loss, lp)
+    else:
+        assert st == B.ERR_INVALID_ARG

@@ -97,3 +97,13 @@ def test_gradient_rows_that_share_elements_with_the_logits_rows(lib, dtype, es):
             assert lib.qsl_distill_backward(z, t, None, None, None, dz, ds, None, 0, None) == INVALID, (d, dz < Z)
     for dz, ds in ((Z + es * 1000, 2001), (Z + es * 1000, 1999), (Z, 2001)):                    # of another stride: not looked at so closely
         assert lib.qsl_token_logprobs_backward(C.byref(Logits(Z, stride, N, V, dtype, 1.0)), at(3), at(4), None, None, None, None, dz, ds, None, 0, None) == INVALID
+
+
+def test_workspaces_that_no_call_needs(lib):  # noqa: F811
+    """Rows of 128 to 256 KB, not few: only alternatives split them, and of those a call has at most 128."""
+    z = C.byref(Logits(Z, 131072, 4096, 131072, 1, 1.0))
+    need = [lib.qsl_logits_workspace_bytes(z, top) for top in (0, 1, 128, 129, 256)]
+    assert need[0] == 0 and 0 < need[1] < need[2] and need[3:] == [0, 0]
+    few = C.byref(Logits(Z, 131072, 100, 131072, 1, 1.0))               # few: split for gradients too
+    need = [lib.qsl_logits_workspace_bytes(few, top) for top in (0, 1, 256)]
+    assert 0 < need[0] < need[1] and need[0] < need[2]
