@@ -875,7 +875,7 @@ __device__ __forceinline__ RowGradient row_gradient(const GradArgs& a, const Row
   const bool empty = o.s == 0.0f;
   RowGradient r;
   r.f.cl = a.c * LOG2E; r.f.m = o.m;
-  r.f.A = empty ? 0.0f * w.g : -a.c * (ENT ? w.g + w.h * (H - logf(o.s)) : w.g) / o.s;
+  r.f.A = empty ? (w.t >= static_cast<int64_t>(a.vocab) ? NAN : 0.0f) : -a.c * (ENT ? w.g + w.h * (H - logf(o.s)) : w.g) / o.s;
   r.f.B = ENT && !empty ? -a.c * w.h * LN2 / o.s : 0.0f;
   r.t = w.t >= 0 && w.t < static_cast<int64_t>(a.vocab) ? static_cast<uint32_t>(w.t) : 0xFFFFFFFFu;
   r.add = empty ? 0.0f : a.c * w.g;
@@ -1182,6 +1182,9 @@ __device__ __forceinline__ float taught(const TeacherBox& b, uint32_t k, float g
   return g * (p - b.q[k]);
 }
 
+// A of Gradient for what the row's sums cover; 0 where nothing is taught, whatever the row's weight
+__device__ __forceinline__ float untaught(const TeacherBox& b, float g) { return b.F == 0.0f || b.s == 0.0f ? 0.0f * b.F : g * b.F / b.s; }
+
 __device__ __forceinline__ void distill_outputs(const DistillArgs& a, uint32_t row, const TeacherBox& b, float loss) {
   if (a.loss) a.loss[row] = loss;
   if (a.stats) {
@@ -1224,7 +1227,7 @@ __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
   if (threadIdx.x < 64) student_sums<REST>(a, row, o, b);
   __syncthreads();
   E* dz = static_cast<E*>(a.dz) + row * a.dstride;
-  if (a.dz) h.template gradient<false>(dz, Gradient{cl, b.m, b.s == 0.0f ? 0.0f * b.F : g * b.F / b.s, 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
+  if (a.dz) h.template gradient<false>(dz, Gradient{cl, b.m, untaught(b, g), 0.0f}, 0xFFFFFFFFu, 0.0f, [](float) {});
   if (threadIdx.x < 64 && !a.stats_in) {                              // while the stores are on their way
     const float loss = distill_loss<REST>(a, o, b);
     if (threadIdx.x == 0) distill_outputs(a, row, b, loss);
@@ -1281,7 +1284,7 @@ __global__ __launch_bounds__(256) void k_distill_join(DistillArgs a, Slices sl, 
   if (threadIdx.x < 64) student_sums<REST>(a, row, o, b);
   __syncthreads();
   if (w.row) {
-    if (threadIdx.x == 0) w.row[row] = Stat4{b.m, b.s == 0.0f ? 0.0f * b.F : g * b.F / b.s, 0.0f, 0.0f};
+    if (threadIdx.x == 0) w.row[row] = Stat4{b.m, untaught(b, g), 0.0f, 0.0f};
     const uint32_t k = threadIdx.x;
     if (k < a.K) {
       w.index[static_cast<uint64_t>(row) * a.K + k] = b.index[k];

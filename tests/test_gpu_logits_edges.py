@@ -229,3 +229,36 @@ def test_calls_that_need_no_workspace_take_none(B, N, V):
         assert st == B.OK and torch.equal(loss, lp)
     else:
         assert st == B.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("N,V,dtype", HELD_AND_SPLIT)
+def test_weights_that_are_no_numbers_on_rows_without_a_gradient(B, N, V, dtype):
+    """A row of -inf has gradient 0, and so has one that nothing is taught in, whatever weight the caller's arithmetic made of them."""
+    z = logits_of(N, V, dtype)
+    z[0], z[1] = -INF, -INF
+    t = torch.zeros(N, dtype=torch.int64, device=dev)
+    t[1] = V - 1
+    lp, stats = new(N), new(N, 4)
+    B.token_logprobs(z, t, logprob=lp, stats=stats)
+    for g0, g1 in ((NAN, INF), (INF, NAN), (-INF, 1.0)):
+        g = torch.ones(N, device=dev)
+        g[0], g[1] = g0, g1
+        r = X.rows_of(z, 1.0)
+        for h in (None, g):
+            for kw in ({}, dict(stats=stats)):
+                dz = torch.full_like(z, 55.0)
+                B.token_logprobs_backward(z, t, dz, grad_logprob=g, grad_entropy=h, **kw)
+                assert not dz[:2].any(), (V, g0, h is None)
+                clean = torch.where(torch.isfinite(g), g, 0.0)
+                X.check(dz, *X.logprob_gradient(r, t, clean, None if h is None else clean, TYPES[dtype]), f"{V}")
+    index, value, lse = taught_by(B, logits_of(N, V, dtype, seed=3), 5)
+    z = logits_of(N, V, dtype)
+    value[0], lse[0] = -INF, -INF                                      # an empty teacher's row
+    index[1] = -1                                                      # no entries
+    z[2] = -INF                                                        # an empty student's
+    for l in (None, torch.where(lse == -INF, lse, 0.0)):
+        g = torch.ones(N, device=dev)
+        g[0], g[1], g[2] = NAN, INF if l is None else 1.0, INF
+        dz = torch.full_like(z, 55.0)
+        B.distill_backward(z, index, value, dz, grad_loss=g, teacher_lse=l)
+        assert not dz[[0, 2]].any() and (l is not None or not dz[1].any()) and torch.isfinite(dz).all(), (V, l is None)
