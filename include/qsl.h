@@ -253,6 +253,7 @@ qsl_status qsl_timing_read(qsl_ctx *ctx, double *total_ms, uint32_t *launches);
  *   - Every array is aligned to its type's size, and where it is said to more than that.
  *   - Arrays that a call writes, `workspace` among them, share no memory with one another or with what it reads, or the call is refused. Two
  *     exceptions: dlogits may be the logits (below), and the loss of qsl_distill_backward may stand where grad_loss does.
+ *   - QSL_ERR_DEVICE: a launch failed, or an earlier error of this thread was still to be reported (hipGetLastError).
  *   - rows = 0 does nothing.  What lies between two rows (stride > vocab) is neither read nor written.
  */
 enum { QSL_F32 = 0, QSL_BF16 = 1, QSL_F16 = 2 };

@@ -180,8 +180,13 @@ Plan plan_top(const qsl_logits* z) {
   const uint64_t bytes = row_bytes(z);
   return bytes <= HELD_TOP_MAX || bytes > SLICES_MAX * SLICE_MAX ? WHOLE : plan_slices(z, 4 * MIN_SLICE);      // every slice's K have to be joined
 }
-// Statistics alone: a row need not be held.  Split where long rows are fewer than the blocks that are resident at once (300 rows of 800 KB: 54 us
-// by a block each, 45 split).
+// Statistics alone: a row need not be held.  Split where long rows are fewer than the blocks that are resident at once.  us, by a block each /
+// split, bf16 with the entropy:
+//   800 KB    1 row 31 / 6, 64 34 / 16, 200 37 / 32, 300 62 / 44, 400 64 / 61, 500 70 / 79, 1,000 131 / 148
+//   320 KB    1 row 13 / 5, 64 15 / 10, 200 17 / 16, 300 25 / 22, 400 27 / 27, 500 29 / 32, 1,000 54 / 60
+//   250 KB    1 row 11 / 6, 64 13 / 8, 100 13 / 10, 200 14 / 16; 128 KB 1 row 7 / 6, 100 8 / 8, 200 9 / 10: what splitting saves there for
+//             up to 100 rows is mostly less than the second launch costs the host (4 us)
+// (From about 400 rows on splitting does not pay; the border is where every row's block is resident.)
 Plan plan_stats(const qsl_logits* z) { return z->rows < 2 * FEW_ROWS && row_bytes(z) > HELD_MAX ? plan_slices(z) : WHOLE; }
 // Gradients: rows that a block does not hold, and long rows that are few, read twice but by all compute units (64 rows of 256 KB: 18 us
 // by a block each, 13 split; 200 rows: 26 and 32; 16 rows of 128 KB: 9 and 13).
@@ -279,6 +284,10 @@ extern "C" qsl_status qsl_token_logprobs(const qsl_logits* z, const int64_t* tar
       } else if (top) {
         k_score<false, E, 1024, ent(), true><<<rows, 1024, 0, stream>>>(a);
       } else {
+        // us, 64 / 256 / 1024 threads, bf16 with the entropy: 16,384 rows of 256 vectors 12 / 36 / 68, of 320 21 / 36 / 81, of 1,024 47 / 41 / 130,
+        // of 2,048 89 / 83 / 142, of 4,096 176 / 163 / 169, of 8,192 343 / 331 / 317; 64 rows of 256 vectors 3.5 / 3.8 / 4.0, of 320
+        // 4.0 / 3.8 / 4.2, of 2,048 7.9 / 4.5 / 5.1, of 2,560 9.2 / 5.2 / 5.1, of 4,096 19 / 7.6 / 5.6.  (The borders are those of few rows;
+        // many rows of 257 to about 900 vectors are faster by a wave each.)
         pick_bool(last, [&](auto once) {
           if (nvec <= 256) k_score<once(), E, 64, ent(), false><<<rows, 64, 0, stream>>>(a);
           else if (nvec <= 2048) k_score<once(), E, 256, ent(), false><<<rows, 256, 0, stream>>>(a);

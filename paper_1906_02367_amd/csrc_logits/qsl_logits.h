@@ -25,7 +25,7 @@ namespace {
 constexpr float LOWEST = -FLT_MAX, LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
 constexpr float Y_MIN = -1e4f;             // exp2 of this is 0; keeps 0 * -inf out of w
 // Blocks are numbered over a grid of two dimensions, whose last row may be short of work.  (A loop over rows in the kernel would have its
-// offsets held in registers from row to row: 189 VGPRs instead of 101 for 16 vectors.)
+// offsets held in registers from row to row: 127 VGPRs instead of 93 to 95 for 16 vectors of 16-bit values.)
 __device__ __forceinline__ uint64_t block_number() { return static_cast<uint64_t>(blockIdx.y) * gridDim.x + blockIdx.x; }
 
 constexpr uint32_t TOP_MAX = 128;          // alternatives of a row at most
@@ -339,7 +339,8 @@ struct Held {
     last = *reinterpret_cast<const typename Elem<E>::bits*>(z + min(last_index(), n - 1));
   }
   // What is made of vector u comes after `y` is known: keeps the compiler from waiting for all loads before the first sum, and from
-  // holding all values unpacked from one use to the next (16 vectors of bf16: 152 VGPRs without this, 101 with it).
+  // holding all values unpacked from one use to the next.  (The branches that pass over empty pieces do so too: with both, 16 vectors of
+  // 16-bit values take 93 to 95 VGPRs, and this alone is one or two of them in the kernels of few vectors.)
   __device__ __forceinline__ void in_order(int u, float& y) { asm volatile("" : "+v"(r[u]), "+v"(y)); }
   __device__ __forceinline__ float last_value(float& y) {              // (the last load: waiting for it is waiting for all)
     asm volatile("" : "+v"(last), "+v"(y));
@@ -696,9 +697,9 @@ __device__ __forceinline__ void alternatives(const ScoreArgs& a, uint32_t row, c
 }
 
 // A block per row, which it walks along once: bound by memory, and as near by its instructions (4,096 rows of 128,000 bf16 with the entropy
-// 153 - 170 us, 6.2 - 6.8 TB/s; 9.7 vector instructions per 64 values, one of them an exponential at a quarter of the rate, are 150 us
-// of issue at 2.4 GHz).  Eight loads a thread under way instead of four cost registers, hence waves: 214 us.  With alternatives (rows of more than 64 slices only) the threads that hold candidates read their
-// shares again.
+// 154 - 160 us, 6.6 - 6.8 TB/s; 9.9 vector instructions per 64 values (SQ_INSTS_VALU), of four cycles each 131 us of issue on 1,024 SIMDs at
+// 2.4 GHz, to which comes what the exponential takes longer).  Eight loads a thread under way instead of four cost registers, hence
+// waves: 214 us.  With alternatives (rows of more than 64 slices only) the threads that hold candidates read their shares again.
 template <bool LAST, class E, int TH, bool ENT, bool TOP>
 __global__ __launch_bounds__(TH) void k_score(ScoreArgs a) {
   __shared__ Stat box[16];
@@ -819,7 +820,8 @@ __global__ __launch_bounds__(256) void k_score_join(ScoreArgs a, Slices sl) {
   uint64_t mine[M];
 #pragma unroll
   for (uint32_t j = 0; j < M; ++j) mine[j] = threadIdx.x + 256 * j < n ? key[threadIdx.x + 256 * j] : 0;
-  // The bound comes from the first 256 / S of every slice, 193 of them or more: hardly ever are more of a slice's among the K.
+  // The bound comes from the first 256 / S of every slice, 208 of them or more (S = 52), or from all S K where K is less: hardly ever are more
+  // of a slice's among the K.
   const uint32_t place = threadIdx.x / sl.S;
   const uint64_t sample = place < a.K && place < 256 / sl.S ? key[threadIdx.x % sl.S * a.K + place] : 0;
   Given<E> given;
@@ -1165,7 +1167,8 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& a, Stat o, cons
   loss = wave_sum_d(loss);
   const double left = fmax(1.0 - b.sum_q, 0.0);
   if (REST && b.some && o.s != 0.0f && left != 0.0) {
-    // what the student leaves over: from what is inside where that is the smaller part
+    // what the student leaves over, t being the sum over all: its share's logarithm, but where the share is small that of its parts, which
+    // does not underflow
     const double outside = o.s * exp((o.m - m_all) * c) / t;
     const double lp = outside > 0.5 ? log(outside) : (o.m - m_all) * c + log(o.s / t);
     loss += left * (log1p(-b.sum_q) - lp);
@@ -1194,8 +1197,8 @@ __device__ __forceinline__ void distill_outputs(const DistillArgs& a, uint32_t r
 }
 
 // A block per row, held in its registers.  REST: what the teacher's entries leave over is one more class.  8,192 rows of 32,000 bf16, 64 entries
-// and the rest 197 us, without the rest 194, against 170 of the gradient alone: between the sums and the gradient one wave works on the
-// entries, and two rows a compute unit do not hide all of it.  (Loss and entries' gradient before the stores, values read where
+// and the rest (1024 x 4) 196 - 199 us, without the rest 194, against 170 of the gradient alone: between the sums and the gradient one wave
+// works on the entries, and two rows a compute unit do not hide all of it.  (Loss and entries' gradient before the stores, values read where
 // they are needed: 212.)
 template <class E, int TH, int NV, bool REST>
 __global__ __launch_bounds__(TH) void k_distill_held(DistillArgs a) {
