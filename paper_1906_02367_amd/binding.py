@@ -163,7 +163,8 @@ def _rows_of(t, what):
 
 
 def _beside(t, what, device, dtype, shape):
-    """Address of an argument that goes with logits on `device` (its index): there, contiguous, of that type and shape; None for None."""
+    """Address of an argument that goes with logits on `device` (its index): there, contiguous, of that type and shape; None for None (which
+    callers pass over for what is mostly not given: the call alone costs 40 ns)."""
     if t is None:
         return None
     if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
@@ -216,9 +217,9 @@ def token_logprobs(logits, target=None, scale=1.0, logprob=None, entropy=None, l
     top = 0 if some is None else some.shape[-1]
     f32 = torch.float32
     _on_logits("qsl_token_logprobs", _lib.qsl_token_logprobs, logits, scale, top, workspace, _beside(target, "target", dev, torch.int64, (N,)), top,
-               _beside(logprob, "logprob", dev, f32, (N,)), _beside(entropy, "entropy", dev, f32, (N,)), _beside(lse, "lse", dev, f32, (N,)),
-               _beside(top_index, "top_index", dev, torch.int32, (N, top)), _beside(top_logprob, "top_logprob", dev, f32, (N, top)),
-               _beside(stats, "stats", dev, f32, (N, 4)))
+               _beside(logprob, "logprob", dev, f32, (N,)), None if entropy is None else _beside(entropy, "entropy", dev, f32, (N,)),
+               None if lse is None else _beside(lse, "lse", dev, f32, (N,)), _beside(top_index, "top_index", dev, torch.int32, (N, top)),
+               _beside(top_logprob, "top_logprob", dev, f32, (N, top)), None if stats is None else _beside(stats, "stats", dev, f32, (N, 4)))
 
 
 def _gradient_rows(dlogits, logits):
@@ -235,8 +236,9 @@ def token_logprobs_backward(logits, target, dlogits, scale=1.0, grad_logprob=Non
     out, dstride = _gradient_rows(dlogits, logits)
     _on_logits("qsl_token_logprobs_backward", _lib.qsl_token_logprobs_backward, logits, scale, 0, workspace,
                _beside(target, "target", dev, torch.int64, (N,)), _beside(grad_logprob, "grad_logprob", dev, f32, (N,)),
-               _beside(grad_entropy, "grad_entropy", dev, f32, (N,)), _beside(stats, "stats", dev, f32, (N, 4)),
-               _beside(logprob, "logprob", dev, f32, (N,)), _beside(entropy, "entropy", dev, f32, (N,)), out, dstride,
+               None if grad_entropy is None else _beside(grad_entropy, "grad_entropy", dev, f32, (N,)),
+               None if stats is None else _beside(stats, "stats", dev, f32, (N, 4)), _beside(logprob, "logprob", dev, f32, (N,)),
+               None if entropy is None else _beside(entropy, "entropy", dev, f32, (N,)), out, dstride,
                kept=stats is not None)
 
 
@@ -244,7 +246,7 @@ def _teacher(logits, index, value, lse, scale):
     N, dev, top = logits.shape[0], logits.get_device(), index.shape[-1]
     return C.byref(_Teacher(_beside(index, "teacher_index", dev, torch.int32, (N, top)),
                             _beside(value, "teacher_value", dev, torch.float32, (N, top)),
-                            _beside(lse, "teacher_lse", dev, torch.float32, (N,)), top, scale))
+                            None if lse is None else _beside(lse, "teacher_lse", dev, torch.float32, (N,)), top, scale))
 
 
 def distill(logits, teacher_index, teacher_value, scale=1.0, teacher_scale=1.0, teacher_lse=None, loss=None, stats=None, workspace=None):
@@ -252,7 +254,7 @@ def distill(logits, teacher_index, teacher_value, scale=1.0, teacher_scale=1.0, 
     N, dev = logits.shape[0], logits.get_device()
     _on_logits("qsl_distill", _lib.qsl_distill, logits, scale, teacher_index.shape[-1], workspace,
                _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(loss, "loss", dev, torch.float32, (N,)),
-               _beside(stats, "stats", dev, torch.float32, (N, 8)), entries=True)
+               None if stats is None else _beside(stats, "stats", dev, torch.float32, (N, 8)), entries=True)
 
 
 def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, teacher_scale=1.0, teacher_lse=None, grad_loss=None,
@@ -263,7 +265,7 @@ def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, t
     out, dstride = _gradient_rows(dlogits, logits)
     _on_logits("qsl_distill_backward", _lib.qsl_distill_backward, logits, scale, teacher_index.shape[-1], workspace,
                _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(grad_loss, "grad_loss", dev, f32, (N,)),
-               _beside(stats, "stats", dev, f32, (N, 8)), _beside(loss, "loss", dev, f32, (N,)), out, dstride,
+               None if stats is None else _beside(stats, "stats", dev, f32, (N, 8)), _beside(loss, "loss", dev, f32, (N,)), out, dstride,
                entries=True)
 
 

@@ -40,17 +40,19 @@ bool logits_ok(const qsl_logits* z) {
   return z->rows == 0 || (z->data && aligned(z->data, elem_size(z->dtype)));
 }
 
-// `rows` pieces of `bytes` each, `step` from one to the next
-struct Memory { uintptr_t at; uint64_t bytes, step, rows; };
-Memory array(const void* p, uint64_t bytes) { return Memory{reinterpret_cast<uintptr_t>(p), bytes, bytes, p && bytes ? 1u : 0u}; }
+// `rows` pieces of `bytes` each, `step` from one to the next, up to `end` (0: none)
+struct Memory { uintptr_t at, end; uint64_t bytes, step, rows; };
+Memory array(const void* p, uint64_t bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return Memory{at, p && bytes ? at + bytes : 0, bytes, bytes, 1};
+}
 Memory rows_at(const qsl_logits* z, const void* p, uint64_t stride) {
   const uint64_t es = elem_size(z->dtype);
-  return Memory{reinterpret_cast<uintptr_t>(p), z->vocab * es, stride * es, p ? z->rows : 0};
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return Memory{at, p ? at + ((z->rows - 1) * stride + z->vocab) * es : 0, z->vocab * es, stride * es, z->rows};
 }
 bool meet(const Memory& a, const Memory& b) {
-  if (a.rows == 0 || b.rows == 0) return false;
-  const uintptr_t a_end = a.at + (a.rows - 1) * a.step + a.bytes, b_end = b.at + (b.rows - 1) * b.step + b.bytes;
-  if (a_end <= b.at || b_end <= a.at) return false;
+  if (a.end <= b.at || b.end <= a.at) return false;
   if (a.rows > 1 && b.rows == 1) return meet(b, a);
   if (b.rows == 1) return true;
   if (a.rows > 1) {      // of the same step: pieces in turn, the later ones in the gaps of the others; of another they are taken to meet
@@ -60,7 +62,7 @@ bool meet(const Memory& a, const Memory& b) {
   }
   // one piece among many: where it begins, or the next piece behind that
   const uint64_t x = a.at > b.at ? a.at - b.at : 0, k = x / b.step;
-  return x < k * b.step + b.bytes || (k + 1 < b.rows && a_end - b.at > (k + 1) * b.step);
+  return x < k * b.step + b.bytes || (k + 1 < b.rows && a.end - b.at > (k + 1) * b.step);
 }
 // no output shares memory with another or with an input
 bool apart(std::initializer_list<Memory> out, std::initializer_list<Memory> in) {
