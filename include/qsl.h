@@ -343,6 +343,87 @@ qsl_status qsl_distill_backward(const qsl_logits *z, const qsl_teacher *teacher,
                                 float *loss, void *dlogits, uint64_t dstride, void *workspace, size_t workspace_bytes,
                                 void *hip_stream);
 
+/* ---- between the data and the logits: a layer's residual stream ---------------------------------------------------------
+ * What joins a layer's output x to the residual stream and hands it to the next layer, forward and backward, on `rows` rows (samples,
+ * tokens, heads) of `cols` columns:
+ *     total = residual + drop(x)          y = weight * total / sqrt(mean_i total_i^2 + eps)
+ * drop(v)_i = v_i / q where column i of the row is kept and 0 where it is not, whatever v_i is there; q = T / 65536 is the share that is kept.
+ *   - As for the calls on logits: no context, nothing kept from call to call, kernels on `hip_stream` of the current HIP device, calls may run at
+ *     the same time (each with a workspace of its own) and be captured; rows = 0 does nothing; what lies between two rows is neither
+ *     read nor written; the same call gives the same bits; QSL_ERR_DEVICE as there.
+ *   - All arithmetic is in 32 bits or more, whatever the arrays' type; every result is rounded once, to its own type, and nothing is computed
+ *     from a rounded one: y belongs to the total before its rounding.
+ *   - Arrays that a call writes share no memory with one another or with what it reads, or the call is refused, except where it is said:
+ *     there one may BE the other, with the same pointer and stride.
+ */
+enum { QSL_E4M3 = 3, QSL_I8 = 4 };      /* 8 bits: e4m3 without infinities (largest value 448); whole numbers -127 .. 127 */
+#define QSL_NORM_COLS_MAX 32768         /* columns of a row that is normed, at most */
+
+/* Which values are kept.  Column i of row n is kept if the 16-bit piece i mod 8 (the words' lower halves first) of the Philox4x32-10 block
+ * with counter (i / 8, row0 + n, r mod 2^32, (r >> 32) | 2 << 30), key (seed mod 2^32, seed >> 32), is below
+ * T = floor((1 - p) 65536 + 1/2).  The mask is stored nowhere: the backward pass forms it again from the same numbers, and a part of a batch has
+ * the masks that it has in the whole (row0).  This is the library's third stream of random words (see qsl_compress for the others). */
+typedef struct {
+  double p;                  /* share that is dropped, 0 <= p <= 1, taken to a multiple of 2^-16 by T            */
+  uint64_t seed;
+  uint64_t round;            /* < 2^62: the step, for instance                                                   */
+  const uint64_t *round_at;  /* device, 8-byte aligned, or NULL: added to round when the kernel runs (a replayed graph then has another mask each
+                                time); r is the sum modulo 2^62                                                  */
+  uint32_t row0;             /* number of the first row; row0 + rows <= 2^32                                     */
+} qsl_drop;
+
+/* Rows of a matrix: row n starts at element n * stride, stride >= cols; aligned to the type's size.  data = NULL: not there. */
+typedef struct { void *data; uint64_t stride; } qsl_rows;
+
+/* y = residual + drop(x).  The gradient in x is the same call on the gradient in y, without the residual; the residual's is that in y.
+ *   rows, cols    < 2^31 each; dtype QSL_F32, QSL_BF16, QSL_F16 of all three
+ *   x, y          there;  y may be x or the residual
+ *   residual      may be absent (zeros), or NULL
+ *   drop          NULL: p = 0 */
+qsl_status qsl_dropout(uint32_t rows, uint32_t cols, uint32_t dtype, const qsl_rows *x, const qsl_rows *residual, const qsl_drop *drop,
+                       const qsl_rows *y, void *hip_stream);
+
+/* What is normed and how. */
+typedef struct {
+  uint32_t rows;             /* < 2^31                                                                           */
+  uint32_t cols;             /* 1 .. QSL_NORM_COLS_MAX                                                           */
+  uint32_t dtype;            /* of x, the residual, the total and the gradients: QSL_F32, QSL_BF16, QSL_F16       */
+  uint32_t weight_dtype;     /* dtype, or QSL_F32                                                                */
+  const void *weight;        /* device, [cols], or NULL (ones)                                                   */
+  float eps;                 /* 2^-100 .. 2^100                                                                  */
+} qsl_norm;
+
+/* The norm.
+ *   x, residual, drop   as above;  x is there
+ *   total    may be absent; receives residual + drop(x); may be x or the residual
+ *   y        there; with out_dtype = norm->dtype it may be x or the residual
+ *   out_dtype  norm->dtype, or QSL_E4M3 or QSL_I8: y then has 8-bit codes, which stand for code * scale, and `scales` is there
+ *   group    8 bits: columns that share a scale, 32, 64 or 128 (a row's last group may be shorter), or 0 for the whole row
+ *   scales   device, float [rows, ceil(cols / group)] ([rows] with group = 0), 4-byte aligned:
+ *              scale = max(a, 2^-100) / Q,  a = max |y| of the group, Q = 448 (QSL_E4M3) or 127 (QSL_I8),  code = y * (Q / max(a, 2^-100))
+ *            rounded to the nearest, ties to even.  A NaN or an infinity among a group's y makes its scale NaN and its codes 0.
+ * A NaN in a total makes its whole row NaN; an infinity makes the row's finite values 0 and itself NaN, as the formula says.  (Finite totals
+ * whose squares do not fit are normed all the same.)  A row of zeros gives zeros. */
+qsl_status qsl_rms_norm(const qsl_norm *norm, const qsl_rows *x, const qsl_rows *residual, const qsl_drop *drop, const qsl_rows *total,
+                        const qsl_rows *y, uint32_t out_dtype, uint32_t group, float *scales, void *hip_stream);
+
+/* Bytes of device memory that qsl_rms_norm_backward needs as `workspace` for dweight, a multiple of 256; 0 for invalid arguments. */
+size_t qsl_rms_norm_workspace_bytes(const qsl_norm *norm);
+
+/* The gradient of qsl_rms_norm (of y before any rounding to 8 bits), from the totals as they were stored: with r = 1 / sqrt(mean total^2 + eps),
+ * u = r total, g = weight dy,
+ *     dresidual = r (g - u mean_j(g_j u_j)) + dtotal,      dx = drop(dresidual),      dweight = sum over the rows of dy u
+ *   total      there (x itself where nothing was added and nothing dropped)
+ *   dy         there; the gradient in y, of norm->dtype
+ *   dtotal     may be absent; what arrives at the total from elsewhere (the layers that the residual stream goes on to)
+ *   dresidual  may be absent; may be total, dy or dtotal
+ *   dx         may be absent; may be total, dy or dtotal, but not dresidual
+ *   dweight    device, float [cols], or NULL: written, not added to; zeros for rows = 0.  One of the three has to be there
+ *   workspace  device, 256-byte aligned; looked at only with dweight */
+qsl_status qsl_rms_norm_backward(const qsl_norm *norm, const qsl_rows *total, const qsl_rows *dy, const qsl_rows *dtotal, const qsl_drop *drop,
+                                 const qsl_rows *dresidual, const qsl_rows *dx, float *dweight, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream);
+
 const char *qsl_status_string(qsl_status st);
 
 #ifdef __cplusplus

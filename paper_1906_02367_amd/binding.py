@@ -23,6 +23,8 @@ FLAG_NO_WARM_START = 8
 FLAG_DENSE_FORMAT = 16
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # QSL_F32, QSL_BF16, QSL_F16
+CODES = {torch.float8_e4m3fn: 3, torch.int8: 4}                       # QSL_E4M3, QSL_I8
+NORM_COLS_MAX = 32768
 TOP_MAX = 128
 TEACHER_MAX = 256
 SIZE_END = 1 << 31                                                    # rows and classes stay below
@@ -49,6 +51,19 @@ class _Logits(C.Structure):
 
 class _Teacher(C.Structure):
     _fields_ = [("index", C.c_void_p), ("value", C.c_void_p), ("lse", C.c_void_p), ("top", C.c_uint32), ("scale", C.c_float)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_uint64)]
+
+
+class _Drop(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("round", C.c_uint64), ("round_at", C.c_void_p), ("row0", C.c_uint32)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("cols", C.c_uint32), ("dtype", C.c_uint32), ("weight_dtype", C.c_uint32), ("weight", C.c_void_p),
+                ("eps", C.c_float)]
 
 
 def _load():
@@ -82,6 +97,11 @@ def _load():
     lib.qsl_token_logprobs_backward.restype = C.c_int
     lib.qsl_distill.argtypes = [zp, tp, vp, vp, vp, sz, vp]; lib.qsl_distill.restype = C.c_int
     lib.qsl_distill_backward.argtypes = [zp, tp, vp, vp, vp, vp, u64, vp, sz, vp]; lib.qsl_distill_backward.restype = C.c_int
+    rp, dp, np_ = C.POINTER(_Rows), C.POINTER(_Drop), C.POINTER(_Norm)
+    lib.qsl_dropout.argtypes = [u32, u32, u32, rp, rp, dp, rp, vp]; lib.qsl_dropout.restype = C.c_int
+    lib.qsl_rms_norm.argtypes = [np_, rp, rp, dp, rp, rp, u32, u32, vp, vp]; lib.qsl_rms_norm.restype = C.c_int
+    lib.qsl_rms_norm_workspace_bytes.argtypes = [np_]; lib.qsl_rms_norm_workspace_bytes.restype = sz
+    lib.qsl_rms_norm_backward.argtypes = [np_, rp, rp, rp, dp, rp, rp, vp, vp, sz, vp]; lib.qsl_rms_norm_backward.restype = C.c_int
     return lib
 
 
@@ -91,7 +111,8 @@ EXPORTED = ["qsl_create", "qsl_destroy", "qsl_set_stream", "qsl_msg_capacity_byt
             "qsl_compress_diff", "qsl_error_update", "qsl_aggregate", "qsl_aggregate_static", "qsl_bits_sent", "qsl_bits_index_free", "qsl_plan_paths",
             "qsl_device_status", "qsl_debug_units",
             "qsl_timing_enable", "qsl_timing_read", "qsl_status_string", "qsl_logits_workspace_bytes", "qsl_token_logprobs",
-            "qsl_token_logprobs_backward", "qsl_distill", "qsl_distill_backward"]
+            "qsl_token_logprobs_backward", "qsl_distill", "qsl_distill_backward", "qsl_dropout", "qsl_rms_norm",
+            "qsl_rms_norm_workspace_bytes", "qsl_rms_norm_backward"]
 
 
 def _check(status, where):
@@ -267,6 +288,103 @@ def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, t
                _teacher(logits, teacher_index, teacher_value, teacher_lse, teacher_scale), _beside(grad_loss, "grad_loss", dev, f32, (N,)),
                None if stats is None else _beside(stats, "stats", dev, f32, (N, 8)), _beside(loss, "loss", dev, f32, (N,)), out, dstride,
                entries=True)
+
+
+def _matrix(t, what, device, dtype, shape):
+    """A `qsl_rows` of a [rows, cols] tensor on `device` (its index) whose rows are contiguous and do not overlap; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{what}: expected a {dtype} tensor {list(shape)} on cuda:{device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    stride, step = t.stride()
+    rows, cols = shape
+    if (step != 1 and cols != 1) or (rows > 1 and stride < cols):
+        raise ValueError(f"{what}: expected contiguous rows that do not overlap, got strides {t.stride()}")
+    return C.byref(_Rows(t.data_ptr(), stride if rows > 1 else cols))
+
+
+def _residual_shape(x, what):
+    """Device, type and shape of the call, by its first array."""
+    if x.dim() != 2 or not x.is_cuda or x.dtype not in DTYPES:
+        raise ValueError(f"{what}: expected a device tensor [rows, cols] of float32, bfloat16 or float16")
+    if x.shape[0] >= SIZE_END or x.shape[1] >= SIZE_END:                  # (ctypes would keep the lower 32 bits)
+        raise ValueError(f"{what}: expected less than 2^31 rows and columns, got {list(x.shape)}")
+    return x.get_device(), x.dtype, x.shape
+
+
+def _drop(p, seed, round, row0, round_at, device):
+    """A `qsl_drop`; None where nothing is dropped."""
+    if p == 0.0:
+        return None
+    if not (0 <= seed < 1 << 64 and 0 <= round < 1 << 62 and 0 <= row0 < 1 << 32):
+        raise ValueError(f"expected a seed below 2^64, a round below 2^62 and a first row below 2^32, got {seed}, {round}, {row0}")
+    return C.byref(_Drop(p, seed, round, None if round_at is None else _beside(round_at.view(-1), "round_at", device, torch.int64, (1,)), row0))
+
+
+def _norm(rows, cols, dtype, weight, eps, device):
+    if weight is None:
+        return C.byref(_Norm(rows, cols, DTYPES[dtype], DTYPES[dtype], None, eps))
+    at = _beside(weight, "weight", device, torch.float32 if weight.dtype is torch.float32 else dtype, (cols,))
+    return C.byref(_Norm(rows, cols, DTYPES[dtype], DTYPES[weight.dtype], at, eps))
+
+
+def _on_device(where, fn, device, *args):
+    """Calls fn(*args, stream) on the device and its current stream."""
+    if device == _current_device():
+        st = fn(*args, _raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, _raw_stream(device))
+    if st != OK:
+        raise QslError(st, where)
+
+
+def dropout(x, y, p, seed=0, round=0, row0=0, residual=None, round_at=None):
+    """`qsl_dropout`: y = residual + drop(x) of x [rows, cols]; y may be x or the residual.  The gradient in x is the same call, with the same
+    numbers, on the gradient in y, without the residual.  round_at: an int64 tensor of one value on the device, added to `round` when the
+    kernel runs."""
+    dev, dtype, shape = _residual_shape(x, "x")
+    _on_device("qsl_dropout", _lib.qsl_dropout, dev, shape[0], shape[1], DTYPES[dtype], _matrix(x, "x", dev, dtype, shape),
+               _matrix(residual, "residual", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev), _matrix(y, "y", dev, dtype, shape))
+
+
+def rms_norm(x, y, weight=None, eps=1e-6, residual=None, total=None, p=0.0, seed=0, round=0, row0=0, round_at=None, scales=None, group=0):
+    """`qsl_rms_norm`: total = residual + drop(x), y = weight * total / sqrt(mean(total^2) + eps).  y has x's type, or is float8_e4m3fn or int8: codes
+    with `scales` [rows, number of groups], a group being `group` (32, 64, 128) columns, or 0 for the whole row."""
+    dev, dtype, shape = _residual_shape(x, "x")
+    rows, cols = shape
+    out = CODES.get(y.dtype, DTYPES[dtype])
+    if not 0 <= group < SIZE_END:
+        raise ValueError(f"group: expected 0, 32, 64 or 128, got {group}")
+    at = None if scales is None else _beside(scales, "scales", dev, torch.float32, (rows, -(-cols // group) if group else 1))
+    _on_device("qsl_rms_norm", _lib.qsl_rms_norm, dev, _norm(rows, cols, dtype, weight, eps, dev), _matrix(x, "x", dev, dtype, shape),
+               _matrix(residual, "residual", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev), _matrix(total, "total", dev, dtype, shape),
+               _matrix(y, "y", dev, y.dtype if y.dtype in CODES else dtype, shape), out, group, at)
+
+
+def rms_norm_workspace_bytes(total):
+    """`qsl_rms_norm_workspace_bytes` of these rows: what `workspace=` of `rms_norm_backward` has to hold for dweight (it is allocated if it
+    is not given)."""
+    dev, dtype, shape = _residual_shape(total, "total")
+    return int(_lib.qsl_rms_norm_workspace_bytes(_norm(shape[0], shape[1], dtype, None, 1.0, dev)))
+
+
+def rms_norm_backward(total, dy, weight=None, eps=1e-6, dtotal=None, dresidual=None, dx=None, dweight=None, p=0.0, seed=0, round=0, row0=0,
+                      round_at=None, workspace=None):
+    """`qsl_rms_norm_backward`: from the totals, the gradient dy in y and what else arrives at the total (`dtotal`), those of the residual, of x
+    and of the weight (float32), into the tensors that are given."""
+    dev, dtype, shape = _residual_shape(total, "total")
+    rows, cols = shape
+    norm = _norm(rows, cols, dtype, weight, eps, dev)
+    dw = None
+    if dweight is not None:
+        dw = _beside(dweight, "dweight", dev, torch.float32, (cols,))
+        if workspace is None:
+            workspace = torch.empty(_lib.qsl_rms_norm_workspace_bytes(norm), dtype=torch.uint8, device=total.device)
+    at, size = (None, 0) if workspace is None else (_beside(workspace, "workspace", dev, torch.uint8, (workspace.numel(),)), workspace.numel())
+    _on_device("qsl_rms_norm_backward", _lib.qsl_rms_norm_backward, dev, norm, _matrix(total, "total", dev, dtype, shape),
+               _matrix(dy, "dy", dev, dtype, shape), _matrix(dtotal, "dtotal", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev),
+               _matrix(dresidual, "dresidual", dev, dtype, shape), _matrix(dx, "dx", dev, dtype, shape), dw, at, size)
 
 
 class Qsl:

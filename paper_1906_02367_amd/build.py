@@ -8,11 +8,13 @@ import tempfile
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 LIB_PATH = os.path.join(_HERE, "libqsl.so")
-# two translation units in folders of their own: the compression path, and the operators on a model's logits
-SOURCES = [os.path.join(_HERE, "csrc", "qsl.hip"), os.path.join(_HERE, "csrc_logits", "logits.hip")]
+# translation units in folders of their own: the compression path, the operators on a model's logits, those on a layer's residual stream
+SOURCES = [os.path.join(_HERE, "csrc", "qsl.hip"), os.path.join(_HERE, "csrc_logits", "logits.hip"), os.path.join(_HERE, "csrc_residual", "residual.hip")]
 HEADERS = [os.path.join(_HERE, "csrc", h) for h in ("qsl_policy.h", "qsl_device.h", "qsl_layout.h", "qsl_stream.h", "qsl_select.h",
                                                     "qsl_encode.h", "qsl_lean.h", "qsl_whole.h", "qsl_window.h", "qsl_dense.h",
                                                     "qsl_decode.h")] + [os.path.join(_HERE, "csrc_logits", "qsl_logits.h"),
+                                                        os.path.join(_HERE, "csrc_residual", "qsl_residual.h"),
+                                                        os.path.join(_HERE, "csrc_common", "qsl_memory.h"),
                                                         os.path.join(ROOT, "include", "qsl.h")]
 
 HIPCC_FLAGS = [
@@ -20,7 +22,7 @@ HIPCC_FLAGS = [
     "-ffp-contract=off",                                        # one rounding per written fp operation
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-fPIC",
-    "-I" + os.path.join(ROOT, "include"), "-I" + os.path.join(_HERE, "csrc"),
+    "-I" + os.path.join(ROOT, "include"), "-I" + os.path.join(_HERE, "csrc"), "-I" + os.path.join(_HERE, "csrc_common"),
 ]
 
 

@@ -7,11 +7,11 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <initializer_list>
 #include <type_traits>
 
 #include "qsl.h"
 #include "qsl_logits.h"
+#include "qsl_memory.h"
 
 static_assert(TOP_MAX == QSL_TOP_MAX && TEACHER_MAX == QSL_TEACHER_MAX, "the header's limits");
 static_assert(REFINE >= 2 * TOP_MAX && CAND_CAP >= REFINE, "a bound from the first candidates must leave some of them out");
@@ -25,14 +25,9 @@ constexpr uint64_t CACHE_BYTES = 256ull << 20;     // the last cache before the 
 constexpr uint64_t MIN_SLICE = 4096;               // bytes: 16 a thread
 
 bool scale_ok(float c) { return c >= 0x1p-100f && c <= 0x1p100f; }
-uint64_t align_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 uint32_t elem_size(uint32_t dtype) { return dtype == QSL_F32 ? 4 : 2; }
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// rows that do not overlap and whose offsets, in elements, stay below 2^48
-bool stride_ok(const qsl_logits* z, uint64_t stride) {
-  return stride >= z->vocab && stride < 1ull << 48 && (z->rows <= 1 || stride <= (1ull << 48) / z->rows);
-}
+bool stride_ok(const qsl_logits* z, uint64_t stride) { return stride_ok(z->rows, z->vocab, stride); }
 
 bool logits_ok(const qsl_logits* z) {
   if (!z || z->dtype > QSL_F16 || z->vocab == 0 || z->vocab >= 1u << 31 || z->rows >= 1u << 31) return false;
@@ -40,38 +35,7 @@ bool logits_ok(const qsl_logits* z) {
   return z->rows == 0 || (z->data && aligned(z->data, elem_size(z->dtype)));
 }
 
-// `rows` pieces of `bytes` each, `step` from one to the next, up to `end` (0: none)
-struct Memory { uintptr_t at, end; uint64_t bytes, step, rows; };
-Memory array(const void* p, uint64_t bytes) {
-  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  return Memory{at, p && bytes ? at + bytes : 0, bytes, bytes, 1};
-}
-Memory rows_at(const qsl_logits* z, const void* p, uint64_t stride) {
-  const uint64_t es = elem_size(z->dtype);
-  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  return Memory{at, p ? at + ((z->rows - 1) * stride + z->vocab) * es : 0, z->vocab * es, stride * es, z->rows};
-}
-bool meet(const Memory& a, const Memory& b) {
-  if (a.end <= b.at || b.end <= a.at) return false;
-  if (a.rows > 1 && b.rows == 1) return meet(b, a);
-  if (b.rows == 1) return true;
-  if (a.rows > 1) {      // of the same step: pieces in turn, the later ones in the gaps of the others; of another they are taken to meet
-    const Memory& f = a.at <= b.at ? a : b;
-    const uint64_t x = (b.at + a.at - 2 * f.at) % f.step;
-    return a.step != b.step || x < f.bytes || x + (&f == &a ? b : a).bytes > f.step;
-  }
-  // one piece among many: where it begins, or the next piece behind that
-  const uint64_t x = a.at > b.at ? a.at - b.at : 0, k = x / b.step;
-  return x < k * b.step + b.bytes || (k + 1 < b.rows && a.end - b.at > (k + 1) * b.step);
-}
-// no output shares memory with another or with an input
-bool apart(std::initializer_list<Memory> out, std::initializer_list<Memory> in) {
-  for (const Memory* o = out.begin(); o != out.end(); ++o) {
-    for (const Memory* p = out.begin(); p != o; ++p) if (meet(*o, *p)) return false;
-    for (const Memory& i : in) if (meet(*o, i)) return false;
-  }
-  return true;
-}
+Memory rows_at(const qsl_logits* z, const void* p, uint64_t stride) { return rows_at(p, z->rows, z->vocab, stride, elem_size(z->dtype)); }
 
 // dlogits are the logits, or share no element with them
 bool gradient_ok(const qsl_logits* z, const void* dz, uint64_t dstride) {

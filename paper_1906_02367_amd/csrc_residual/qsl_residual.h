@@ -1,0 +1,489 @@
+// qsl_residual.h -- kernels on a layer's residual stream: dropout whose mask is formed again wherever it is needed, the root-mean-square norm
+// of residual + dropout(x), whole or in 8 bits with scales, and its gradient.
+//
+// Row n with totals h of C columns, r = (sum h^2 / C + eps)^(-1/2), u = r h:
+//   y = w u                  dh = r (g - u mean_j(g_j u_j)) + what arrives at h from elsewhere, g = w dy           dw = sum over rows of dy u
+//   drop(v)_i = v_i 65536 / T where the row's 16-bit random piece i is below T, else 0
+// A row is read once and held in registers between its sums and its results: every array that a call has to read or write passes the
+// memory once.  All of it is computed in 32 bits.
+// Part of the translation unit residual.hip; not a public header.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "qsl_device.h"
+
+using namespace qsl;
+
+namespace {
+
+__device__ __forceinline__ uint64_t block_number() { return static_cast<uint64_t>(blockIdx.y) * gridDim.x + blockIdx.x; }
+
+// ---------------------------------------------------------------------------------------------
+// units: eight columns of a row, the values that one Philox block decides on, 16 bytes of 16-bit values or 32 of floats.  They begin at
+// every eighth column of the row, wherever that lies: the loads need no more than the elements' alignment.
+// ---------------------------------------------------------------------------------------------
+template <class E> struct Unit { uint32_t w[2 * sizeof(E)]; };
+
+__device__ __forceinline__ void unpack(const Unit<float>& q, float* v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(q.w[i]);
+}
+__device__ __forceinline__ void unpack(const Unit<__bf16>& q, float* v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(q.w[i] << 16); v[2 * i + 1] = __uint_as_float(q.w[i] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void unpack(const Unit<_Float16>& q, float* v) {
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const h2 x = __builtin_bit_cast(h2, q.w[i]); v[2 * i] = static_cast<float>(x[0]); v[2 * i + 1] = static_cast<float>(x[1]); }
+}
+// rounded once, to nearest even
+__device__ __forceinline__ void pack(const float* v, Unit<float>& q) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q.w[i] = __float_as_uint(v[i]);
+}
+template <class E> __device__ __forceinline__ void pack(const float* v, Unit<E>& q) {
+  typedef E e2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const e2 x = {static_cast<E>(v[2 * i]), static_cast<E>(v[2 * i + 1])}; q.w[i] = __builtin_bit_cast(uint32_t, x); }
+}
+
+// 16 bytes with the elements' alignment; an element's bits
+template <class E> struct Raw { typedef uint32_t mem __attribute__((ext_vector_type(4), aligned(2))); typedef uint16_t bits; };
+template <> struct Raw<float> { typedef uint32_t mem __attribute__((ext_vector_type(4), aligned(4))); typedef uint32_t bits; };
+
+// the unit that begins at column c of a row; zeros behind the row's end.  (c + 8 does not pass 32 bits: cols < 2^31.)
+template <class E> __device__ __forceinline__ void load_whole(const E* row, uint32_t c, uint32_t cols, Unit<E>& q) {
+  const bool whole = c + 8 <= cols;
+#pragma unroll
+  for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) {
+    typename Raw<E>::mem m = {0, 0, 0, 0};
+    if (whole) m = reinterpret_cast<const typename Raw<E>::mem*>(row + c)[k];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q.w[4 * k + i] = m[i];
+  }
+}
+// a row's last unit where it is short of columns
+template <class E> __device__ __forceinline__ void load_rest(const E* row, uint32_t c, uint32_t cols, Unit<E>& q) {
+  typedef typename Raw<E>::bits bits;
+  if (c < cols && c + 8 > cols) {
+    const bits* p = reinterpret_cast<const bits*>(row + c);
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t x = c + i < cols ? p[i] : 0;
+      if constexpr (sizeof(E) == 4) q.w[i] = x;
+      else q.w[i / 2] |= x << 16 * (i & 1);
+    }
+  }
+}
+template <class E> __device__ __forceinline__ void store_unit(E* row, uint32_t c, uint32_t cols, const float* v) {
+  Unit<E> q;
+  pack(v, q);
+  if (c + 8 <= cols) {
+#pragma unroll
+    for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) {
+      typename Raw<E>::mem m = {q.w[4 * k], q.w[4 * k + 1], q.w[4 * k + 2], q.w[4 * k + 3]};
+      reinterpret_cast<typename Raw<E>::mem*>(row + c)[k] = m;
+    }
+  } else if (c < cols) {
+    typedef typename Raw<E>::bits bits;
+    bits* p = reinterpret_cast<bits*>(row + c);
+#pragma unroll
+    for (uint32_t i = 0; i < 7; ++i)
+      if (c + i < cols) p[i] = static_cast<bits>(sizeof(E) == 4 ? q.w[i] : q.w[i / 2] >> 16 * (i & 1));
+  }
+}
+
+// U units of a row, `step` columns apart
+template <class E, int U> __device__ __forceinline__ void load_units(const E* row, uint32_t c0, uint32_t step, uint32_t cols, Unit<E>* q) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) load_whole(row, c0 + u * step, cols, q[u]);
+  if (cols & 7) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_rest(row, c0 + u * step, cols, q[u]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// which values are kept
+// ---------------------------------------------------------------------------------------------
+constexpr uint32_t DROP_STREAM = 2, KEEP_ALL = 65536;      // (streams 0 and 1: Rand_k, QSGD)
+struct Drop {
+  uint32_t T;                   // of 65,536; KEEP_ALL: nothing is dropped, nothing formed
+  float factor;                 // 65536 / T
+  uint32_t row0, seed_lo, seed_hi;
+  uint64_t round;
+  const uint64_t* round_at;
+};
+struct Key { uint32_t lo, hi; };
+__device__ __forceinline__ Key key_of(const Drop& d) {
+  uint64_t r = d.round;
+  if (d.T != KEEP_ALL && d.round_at) r += *d.round_at;
+  return Key{static_cast<uint32_t>(r), (static_cast<uint32_t>(r >> 32) & 0x3FFFFFFFu) | DROP_STREAM << 30};
+}
+// v <- drop(v) of a row's unit: one Philox block, eight pieces of 16 bits.  (A word of 32 bits for each would cost as much time as the memory.)
+__device__ __forceinline__ void drop_unit(const Drop& d, const Key& k, uint32_t row, uint32_t unit, float* v) {
+  const Words4 o = philox4x32_10(unit, d.row0 + row, k.lo, k.hi, d.seed_lo, d.seed_hi);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t piece = i & 1 ? o.w[i / 2] >> 16 : o.w[i / 2] & 0xFFFFu;
+    v[i] = piece < d.T ? v[i] * d.factor : 0.0f;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// sums and maxima over the L lanes that hold a row (16, 64, or a block), the same bits in each of them
+// ---------------------------------------------------------------------------------------------
+constexpr int DPP_ROW_ROR = 0x120, DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141;      // quad_perm [1,0,3,2], [2,3,0,1]
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_move(uint32_t x) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, 0xF, 0xF, false));
+}
+template <int CTRL> __device__ __forceinline__ float dpp_move(float x) { return __uint_as_float(dpp_move<CTRL>(__float_as_uint(x))); }
+// Rotations by 8, 4, 2, 1: both lanes of a pair add the same two numbers, so all sixteen end with the same bits.
+__device__ __forceinline__ float sum16(float x) {
+  x += dpp_move<DPP_ROW_ROR + 8>(x);
+  x += dpp_move<DPP_ROW_ROR + 4>(x);
+  x += dpp_move<DPP_ROW_ROR + 2>(x);
+  return x + dpp_move<DPP_ROW_ROR + 1>(x);
+}
+__device__ __forceinline__ float lane_float(float x, int lane) { return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(x)), lane))); }
+// `at`: L / 64 places in LDS that no thread still reads from an earlier call
+template <int L> __device__ __forceinline__ float row_sum(float x, float* at) {
+  x = sum16(x);
+  if constexpr (L == 16) return x;
+  x = (lane_float(x, 0) + lane_float(x, 16)) + (lane_float(x, 32) + lane_float(x, 48));
+  if constexpr (L <= 64) return x;
+  if (lane_id() == 0) at[threadIdx.x / WAVE] = x;
+  __syncthreads();
+  float s = at[0];
+#pragma unroll
+  for (int w = 1; w < L / 64; ++w) s += at[w];
+  return s;
+}
+// over 4, 8 or 16 neighbouring lanes
+__device__ __forceinline__ uint32_t max_of_lanes(uint32_t x, uint32_t lanes) {
+  x = max(x, dpp_move<DPP_XOR1>(x));
+  x = max(x, dpp_move<DPP_XOR2>(x));
+  if (lanes >= 8) x = max(x, dpp_move<DPP_HALF_MIRROR>(x));
+  if (lanes >= 16) x = max(x, dpp_move<DPP_ROW_ROR + 8>(x));
+  return x;
+}
+template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t x, uint32_t* at) {
+  x = max_of_lanes(x, 16);
+  if constexpr (L == 16) return x;
+  x = max(max(lane_value(x, 0), lane_value(x, 16)), max(lane_value(x, 32), lane_value(x, 48)));
+  if constexpr (L <= 64) return x;
+  if (lane_id() == 0) at[threadIdx.x / WAVE] = x;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < L / 64; ++w) x = max(x, at[w]);
+  return x;
+}
+
+// Squares of totals from 2^64 on do not fit into a float: such rows are taken times this.  2^56 squared times QSL_NORM_COLS_MAX does.
+constexpr float SMALLER = 0x1p-72f;
+constexpr float INF = __builtin_inff();
+
+template <int L> constexpr int THREADS = L < 256 ? 256 : L;      // short rows share a block
+// a row's number within the block, for the compiler the same in a wave where it is
+template <int L> __device__ __forceinline__ uint32_t row_in_block() {
+  if constexpr (L >= 256) return 0;
+  else if constexpr (L >= 64) return __builtin_amdgcn_readfirstlane(threadIdx.x / L);
+  else return threadIdx.x / L;
+}
+
+// ---------------------------------------------------------------------------------------------
+// dropout by itself
+// ---------------------------------------------------------------------------------------------
+struct DropArgs {
+  const void *x, *res;
+  void* y;
+  uint64_t x_stride, res_stride, y_stride, rows;
+  uint32_t cols, units;          // units of a row
+  Drop drop;
+};
+constexpr int DROP_EACH = 4;     // units of a thread
+
+template <class E> __global__ __launch_bounds__(256) void k_dropout(DropArgs a) {
+  const uint64_t first = block_number() * (256 * DROP_EACH), row_b = first / a.units;
+  const uint32_t rest = static_cast<uint32_t>(first - row_b * a.units);
+  const Key key = key_of(a.drop);
+  Unit<E> x[DROP_EACH], res[DROP_EACH];
+  uint64_t row[DROP_EACH];
+  uint32_t c[DROP_EACH], cols[DROP_EACH];
+#pragma unroll
+  for (int k = 0; k < DROP_EACH; ++k) {
+    const uint32_t i = rest + k * 256 + threadIdx.x, r = i / a.units;
+    row[k] = row_b + r;
+    c[k] = (i - r * a.units) * 8;
+    cols[k] = row[k] < a.rows ? a.cols : 0;
+    load_units<E, 1>(static_cast<const E*>(a.x) + row[k] * a.x_stride, c[k], 0, cols[k], x + k);
+  }
+  if (a.res) {
+#pragma unroll
+    for (int k = 0; k < DROP_EACH; ++k) load_units<E, 1>(static_cast<const E*>(a.res) + row[k] * a.res_stride, c[k], 0, cols[k], res + k);
+  }
+#pragma unroll
+  for (int k = 0; k < DROP_EACH; ++k) {
+    float v[8];
+    unpack(x[k], v);
+    if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key, static_cast<uint32_t>(row[k]), c[k] / 8, v);
+    if (a.res) {
+      float b[8];
+      unpack(res[k], b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += b[i];
+    }
+    store_unit(static_cast<E*>(a.y) + row[k] * a.y_stride, c[k], cols[k], v);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// the norm
+// ---------------------------------------------------------------------------------------------
+struct NormArgs {
+  const void *x, *res, *weight;
+  void *total, *y;
+  float* scales;
+  uint64_t x_stride, res_stride, total_stride, y_stride, rows;
+  uint32_t cols, weight_is_float, is_e4m3, group;      // group: columns of a scale, 0: the row
+  float eps;
+  Drop drop;
+};
+
+template <class E, int U> __device__ __forceinline__ void load_weight(const void* weight, uint32_t is_float, uint32_t c0, uint32_t step, uint32_t cols, float* w) {
+  if (!weight) {
+#pragma unroll
+    for (int i = 0; i < 8 * U; ++i) w[i] = 1.0f;
+  } else if (sizeof(E) == 4 || is_float) {
+    Unit<float> q[U];
+    load_units<float, U>(static_cast<const float*>(weight), c0, step, cols, q);
+#pragma unroll
+    for (int u = 0; u < U; ++u) unpack(q[u], w + 8 * u);
+  } else {
+    Unit<E> q[U];
+    load_units<E, U>(static_cast<const E*>(weight), c0, step, cols, q);
+#pragma unroll
+    for (int u = 0; u < U; ++u) unpack(q[u], w + 8 * u);
+  }
+}
+
+// 8-bit codes of a unit, eight bytes; `most`: the bits of the group's largest |y|
+__device__ __forceinline__ void store_codes(uint8_t* row, uint32_t c, uint32_t cols, const float* y, uint32_t most, bool is_e4m3, float* scale_at) {
+  const float a = fmaxf(__uint_as_float(most), 0x1p-100f), Q = is_e4m3 ? 448.0f : 127.0f, inv = Q / a;
+  const bool bad = most >= 0x7F800000u;      // an infinity or a NaN
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = bad ? 0.0f : y[i] * inv;
+  uint32_t lo = 0, hi = 0;
+  if (is_e4m3) {
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], lo, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo |= (static_cast<uint32_t>(static_cast<int>(rintf(v[i]))) & 0xFFu) << 8 * i;
+      hi |= (static_cast<uint32_t>(static_cast<int>(rintf(v[4 + i]))) & 0xFFu) << 8 * i;
+    }
+  }
+  if (scale_at) *scale_at = bad ? __builtin_nanf("") : a / Q;
+  typedef uint32_t two __attribute__((ext_vector_type(2), aligned(1)));
+  if (c + 8 <= cols) {
+    const two q = {lo, hi};
+    *reinterpret_cast<two*>(row + c) = q;
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 7; ++i)
+      if (c + i < cols) row[c + i] = static_cast<uint8_t>((i < 4 ? lo : hi) >> 8 * (i & 3));
+  }
+}
+
+template <class E, int L, int U, bool BITS8>
+__global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
+  __shared__ float sums[2][L < 256 ? 1 : L / 64];
+  __shared__ uint32_t maxima[L < 256 ? 1 : L / 64];
+  const uint64_t row = block_number() * (THREADS<L> / L) + row_in_block<L>();
+  const uint32_t lane = threadIdx.x % L, cols = row < a.rows ? a.cols : 0;
+  Unit<E> x[U], res[U];
+  load_units<E, U>(static_cast<const E*>(a.x) + row * a.x_stride, lane * 8, L * 8, cols, x);
+  if (a.res) load_units<E, U>(static_cast<const E*>(a.res) + row * a.res_stride, lane * 8, L * 8, cols, res);
+  float w[8 * U], h[8 * U];
+  load_weight<E, U>(a.weight, a.weight_is_float, lane * 8, L * 8, cols, w);
+  const Key key = key_of(a.drop);
+  float ss = 0.0f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float* v = h + 8 * u;
+    unpack(x[u], v);
+    if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key, static_cast<uint32_t>(row), u * L + lane, v);
+    if (a.res) {
+      float b[8];
+      unpack(res[u], b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += b[i];
+    }
+    if (a.total) store_unit(static_cast<E*>(a.total) + row * a.total_stride, lane * 8 + u * L * 8, cols, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(v[i], v[i], ss);
+  }
+  ss = row_sum<L>(ss, sums[0]);
+  float eps = a.eps;
+  if (__any(ss == INF)) {      // (the same answer in all waves of a row)
+    const float f = ss == INF ? SMALLER : 1.0f;
+    ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8 * U; ++i) { h[i] *= f; ss = __builtin_fmaf(h[i], h[i], ss); }
+    ss = row_sum<L>(ss, sums[1]);
+    eps = f == 1.0f ? eps : 0.0f;
+  }
+  const float r = 1.0f / sqrtf(ss / static_cast<float>(a.cols) + eps);
+#pragma unroll
+  for (int i = 0; i < 8 * U; ++i) h[i] = h[i] * r * w[i];
+  if constexpr (!BITS8) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) store_unit(static_cast<E*>(a.y) + row * a.y_stride, lane * 8 + u * L * 8, cols, h + 8 * u);
+  } else {
+    uint32_t most[U], all = 0;      // of the bits of |y|: a NaN is above the infinities
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      most[u] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (lane * 8 + u * L * 8 + i < cols) most[u] = max(most[u], __float_as_uint(h[8 * u + i]) & 0x7FFFFFFFu);
+      if (a.group) most[u] = max_of_lanes(most[u], a.group / 8);
+      all = max(all, most[u]);
+    }
+    if (!a.group) all = row_max<L>(all, maxima);
+    const uint32_t of_row = a.group ? (a.cols + a.group - 1) / a.group : 1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t c = lane * 8 + u * L * 8, g = a.group ? c / a.group : 0;
+      if (c < cols) store_codes(static_cast<uint8_t*>(a.y) + row * a.y_stride, c, cols, h + 8 * u, a.group ? most[u] : all, a.is_e4m3,
+                                (a.group ? c % a.group == 0 : c == 0) ? a.scales + row * of_row + g : nullptr);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// its gradient
+// ---------------------------------------------------------------------------------------------
+struct BackArgs {
+  const void *total, *dy, *dtotal, *weight;
+  void *dres, *dx;
+  float* part;                   // [blocks, cols]: every block's sum of dy u over its rows; or nullptr
+  uint64_t total_stride, dy_stride, dtotal_stride, dres_stride, dx_stride, rows;
+  uint32_t cols, weight_is_float;
+  float eps;
+  Drop drop;
+};
+
+// A block goes through rows that lie a grid apart and keeps its sum for dw in registers.
+template <class E, int L, int U>
+__global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
+  constexpr int ROWS = THREADS<L> / L;
+  __shared__ float sums[2][4][L < 256 ? 1 : L / 64];
+  __shared__ float joined[ROWS > 1 ? ROWS * 8 * U * L : 1];
+  const uint32_t lane = threadIdx.x % L, c0 = lane * 8;
+  const Key key = key_of(a.drop);
+  float w[8 * U], dw[8 * U];
+  load_weight<E, U>(a.weight, a.weight_is_float, c0, L * 8, a.cols, w);
+#pragma unroll
+  for (int i = 0; i < 8 * U; ++i) dw[i] = 0.0f;
+  uint32_t turn = 0;             // a row's sums go where those before last stood: there is a barrier between reading these and writing them
+  for (uint64_t base = static_cast<uint64_t>(blockIdx.x) * ROWS; base < a.rows; base += static_cast<uint64_t>(gridDim.x) * ROWS) {
+    const uint64_t row = base + row_in_block<L>();
+    const uint32_t cols = row < a.rows ? a.cols : 0;
+    Unit<E> hq[U], dyq[U], dtq[U];
+    load_units<E, U>(static_cast<const E*>(a.total) + row * a.total_stride, c0, L * 8, cols, hq);
+    load_units<E, U>(static_cast<const E*>(a.dy) + row * a.dy_stride, c0, L * 8, cols, dyq);
+    if (a.dtotal) load_units<E, U>(static_cast<const E*>(a.dtotal) + row * a.dtotal_stride, c0, L * 8, cols, dtq);
+    float f = 1.0f, ss = 0.0f, gh = 0.0f;
+    auto sum = [&]() {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float h[8], d[8];
+        unpack(hq[u], h);
+        unpack(dyq[u], d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          h[i] *= f;
+          ss = __builtin_fmaf(h[i], h[i], ss);
+          gh = __builtin_fmaf(d[i] * w[8 * u + i], h[i], gh);
+        }
+      }
+    };
+    sum();
+    ss = row_sum<L>(ss, sums[turn][0]);
+    gh = row_sum<L>(gh, sums[turn][1]);
+    float eps = a.eps;
+    if (__any(ss == INF)) {
+      if (ss == INF) { f = SMALLER; eps = 0.0f; }
+      ss = 0.0f; gh = 0.0f;
+      sum();
+      ss = row_sum<L>(ss, sums[turn][2]);
+      gh = row_sum<L>(gh, sums[turn][3]);
+    }
+    turn ^= 1;
+    const float r = 1.0f / sqrtf(ss / static_cast<float>(a.cols) + eps);      // of the totals times f
+    const float mean = gh * r / static_cast<float>(a.cols), rf = r * f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float h[8], d[8], t[8];
+      unpack(hq[u], h);
+      unpack(dyq[u], d);
+      if (a.dtotal) unpack(dtq[u], t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float un = h[i] * f * r;
+        dw[8 * u + i] = __builtin_fmaf(d[i], un, dw[8 * u + i]);
+        d[i] = rf * (d[i] * w[8 * u + i] - un * mean);
+        if (a.dtotal) d[i] += t[i];
+      }
+      if (a.dres) store_unit(static_cast<E*>(a.dres) + row * a.dres_stride, c0 + u * L * 8, cols, d);
+      if (a.dx) {
+        if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key, static_cast<uint32_t>(row), u * L + lane, d);
+        store_unit(static_cast<E*>(a.dx) + row * a.dx_stride, c0 + u * L * 8, cols, d);
+      }
+    }
+  }
+  if (!a.part) return;
+  float* out = a.part + static_cast<uint64_t>(blockIdx.x) * a.cols;
+  if constexpr (ROWS == 1) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) store_unit(out, c0 + u * L * 8, a.cols, dw + 8 * u);
+  } else {
+    const uint32_t mine = row_in_block<L>();
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) joined[mine * (8 * U * L) + c0 + u * L * 8 + i] = dw[8 * u + i];
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < a.cols; c += THREADS<L>) {
+      float s = joined[c];
+#pragma unroll
+      for (int k = 1; k < ROWS; ++k) s += joined[k * (8 * U * L) + c];
+      out[c] = s;
+    }
+  }
+}
+
+// dw: the blocks' sums, in the blocks' order within each of 16 parts, then the parts.  Blocks of 16 columns x 16 parts.
+__global__ __launch_bounds__(256) void k_sum_parts(const float* part, uint32_t blocks, uint32_t cols, float* dweight) {
+  __shared__ float at[16][17];
+  const uint32_t x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
+  float s = 0.0f;
+  if (c < cols)
+    for (uint32_t b = y; b < blocks; b += 16) s += part[static_cast<uint64_t>(b) * cols + c];
+  at[y][x] = s;
+  __syncthreads();
+  if (y == 0 && c < cols) {
+#pragma unroll
+    for (int k = 1; k < 16; ++k) s += at[k][x];
+    dweight[c] = s;
+  }
+}
+
+}  // namespace

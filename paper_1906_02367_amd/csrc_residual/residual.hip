@@ -1,0 +1,175 @@
+// residual.hip -- host side and C ABI of the operators on a layer's residual stream (include/qsl.h); their kernels are in qsl_residual.h.
+//
+// The calls keep no state: arguments are checked, one rule on the row's length picks the launch, the kernels go to the caller's stream.
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "qsl.h"
+#include "qsl_memory.h"
+#include "qsl_residual.h"
+
+namespace {
+
+constexpr uint64_t GRID_X = 1u << 20;              // blocks in a row of the grid (a launch counts its threads in 32 bits)
+
+uint32_t elem_size(uint32_t dtype) { return dtype == QSL_F32 ? 4 : dtype <= QSL_F16 ? 2 : 1; }
+
+// A matrix of a call: what is there, at which stride.
+struct Matrix { void* data; uint64_t stride; };
+Matrix of(const qsl_rows* r) { return r ? Matrix{r->data, r->stride} : Matrix{nullptr, 0}; }
+bool matrix_ok(const Matrix& m, uint64_t rows, uint64_t cols, uint32_t dtype) {
+  return !m.data || (stride_ok(rows, cols, m.stride) && aligned(m.data, elem_size(dtype)));
+}
+bool same(const Matrix& a, const Matrix& b, uint64_t rows) { return a.data == b.data && (a.stride == b.stride || rows == 1); }
+
+bool drop_ok(const qsl_drop* d, uint64_t rows) {
+  return !d || (d->p >= 0.0 && d->p <= 1.0 && d->round < 1ull << 62 && aligned(d->round_at, 8) && d->row0 + rows <= 1ull << 32);
+}
+Drop drop_of(const qsl_drop* d) {
+  if (!d) return Drop{KEEP_ALL, 1.0f, 0, 0, 0, 0, nullptr};
+  const uint32_t T = static_cast<uint32_t>(floor((1.0 - d->p) * 65536.0 + 0.5));
+  return Drop{T, T ? static_cast<float>(65536.0 / T) : 0.0f, d->row0, static_cast<uint32_t>(d->seed), static_cast<uint32_t>(d->seed >> 32), d->round, d->round_at};
+}
+
+// f(the element type) as a type
+template <class F>
+void pick_type(uint32_t dtype, F&& f) {
+  if (dtype == QSL_F32) f(float());
+  else if (dtype == QSL_BF16) f(__bf16());
+  else f(_Float16());
+}
+template <int V> using Int = std::integral_constant<int, V>;
+
+// f(lanes that hold a row, units each of them holds)
+template <class F>
+void pick_row(uint32_t cols, F&& f) {
+  if (cols <= 16 * 8) f(Int<16>(), Int<1>());
+  else if (cols <= 64 * 8) f(Int<64>(), Int<1>());
+  else if (cols <= 64 * 16) f(Int<64>(), Int<2>());
+  else if (cols <= 256 * 8) f(Int<256>(), Int<1>());
+  else if (cols <= 256 * 16) f(Int<256>(), Int<2>());
+  else if (cols <= 256 * 32) f(Int<256>(), Int<4>());
+  else if (cols <= 512 * 32) f(Int<512>(), Int<4>());
+  else f(Int<1024>(), Int<4>());
+}
+
+dim3 grid_of(uint64_t blocks) {
+  return dim3(static_cast<uint32_t>(std::min(blocks, GRID_X)), static_cast<uint32_t>((blocks + GRID_X - 1) / GRID_X));
+}
+
+bool norm_ok(const qsl_norm* n) {
+  if (!n || n->dtype > QSL_F16 || n->rows >= 1u << 31 || n->cols == 0 || n->cols > QSL_NORM_COLS_MAX) return false;
+  if (n->weight && ((n->weight_dtype != n->dtype && n->weight_dtype != QSL_F32) || !aligned(n->weight, elem_size(n->weight_dtype)))) return false;
+  return n->eps >= 0x1p-100f && n->eps <= 0x1p100f;
+}
+Memory weight_of(const qsl_norm* n) { return array(n->weight, static_cast<uint64_t>(n->cols) * elem_size(n->weight_dtype)); }
+
+// blocks of the backward pass: each goes through many rows, so that their sums for dweight are few
+uint32_t back_blocks(const qsl_norm* n) {
+  uint32_t blocks = 0;
+  pick_row(n->cols, [&](auto l, auto) {
+    const uint64_t per = THREADS<l()> / l(), most = 1024 * 256 / THREADS<l()>;
+    blocks = static_cast<uint32_t>(std::min<uint64_t>((n->rows + per - 1) / per, most));
+  });
+  return blocks;
+}
+
+qsl_status launched() { return hipGetLastError() == hipSuccess ? QSL_OK : QSL_ERR_DEVICE; }
+
+}  // namespace
+
+extern "C" qsl_status qsl_dropout(uint32_t rows, uint32_t cols, uint32_t dtype, const qsl_rows* x, const qsl_rows* residual,
+                                  const qsl_drop* drop, const qsl_rows* y, void* hip_stream) {
+  const Matrix mx = of(x), mr = of(residual), my = of(y);
+  if (dtype > QSL_F16 || rows >= 1u << 31 || cols == 0 || cols >= 1u << 31 || !drop_ok(drop, rows)) return QSL_ERR_INVALID_ARG;
+  if (rows == 0) return QSL_OK;
+  if (!mx.data || !my.data) return QSL_ERR_INVALID_ARG;
+  for (const Matrix& m : {mx, mr, my}) if (!matrix_ok(m, rows, cols, dtype)) return QSL_ERR_INVALID_ARG;
+  const uint64_t es = elem_size(dtype);
+  auto at = [&](const Matrix& m) { return rows_at(m.data, rows, cols, m.stride, es); };
+  for (const Matrix& m : {mx, mr}) if (m.data && !same(m, my, rows) && meet(at(m), at(my))) return QSL_ERR_INVALID_ARG;
+  if (drop && meet(array(drop->round_at, 8), at(my))) return QSL_ERR_INVALID_ARG;
+  const uint32_t units = (cols + 7) / 8;
+  const DropArgs a = {mx.data, mr.data, my.data, mx.stride, mr.stride, my.stride, rows, cols, units, drop_of(drop)};
+  const uint64_t each = 256 * DROP_EACH, blocks = (static_cast<uint64_t>(rows) * units + each - 1) / each;
+  pick_type(dtype, [&](auto e) { k_dropout<decltype(e)><<<grid_of(blocks), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+  return launched();
+}
+
+extern "C" qsl_status qsl_rms_norm(const qsl_norm* norm, const qsl_rows* x, const qsl_rows* residual, const qsl_drop* drop,
+                                   const qsl_rows* total, const qsl_rows* y, uint32_t out_dtype, uint32_t group, float* scales,
+                                   void* hip_stream) {
+  if (!norm_ok(norm)) return QSL_ERR_INVALID_ARG;
+  const uint64_t rows = norm->rows, cols = norm->cols, es = elem_size(norm->dtype);
+  const bool bits8 = out_dtype == QSL_E4M3 || out_dtype == QSL_I8;
+  if (!drop_ok(drop, rows) || (!bits8 && out_dtype != norm->dtype)) return QSL_ERR_INVALID_ARG;
+  if (bits8 ? group != 0 && group != 32 && group != 64 && group != 128 : group != 0 || scales) return QSL_ERR_INVALID_ARG;
+  if (rows == 0) return QSL_OK;
+  const Matrix mx = of(x), mr = of(residual), mt = of(total), my = of(y);
+  if (!mx.data || !my.data || (bits8 && (!scales || !aligned(scales, 4)))) return QSL_ERR_INVALID_ARG;
+  for (const Matrix& m : {mx, mr, mt}) if (!matrix_ok(m, rows, cols, norm->dtype)) return QSL_ERR_INVALID_ARG;
+  if (!matrix_ok(my, rows, cols, out_dtype)) return QSL_ERR_INVALID_ARG;
+  auto at = [&](const Matrix& m, uint64_t size) { return rows_at(m.data, rows, cols, m.stride, size); };
+  const Memory out_t = at(mt, es), out_y = at(my, elem_size(out_dtype)), out_s = array(scales, 4 * rows * (group ? (cols + group - 1) / group : 1));
+  if (!apart({out_t, out_y, out_s}, {weight_of(norm), array(drop ? drop->round_at : nullptr, 8)})) return QSL_ERR_INVALID_ARG;
+  for (const Matrix& m : {mx, mr}) {      // a thread reads x and the residual where it writes the total and y, all of the row before any of it
+    if (!m.data) continue;
+    if (!same(m, mt, rows) && meet(at(m, es), out_t)) return QSL_ERR_INVALID_ARG;
+    if ((bits8 || !same(m, my, rows)) && meet(at(m, es), out_y)) return QSL_ERR_INVALID_ARG;
+    if (meet(at(m, es), out_s)) return QSL_ERR_INVALID_ARG;
+  }
+  const NormArgs a = {mx.data, mr.data, norm->weight, mt.data, my.data, scales, mx.stride, mr.stride, mt.stride, my.stride, rows, norm->cols,
+                      norm->weight_dtype == QSL_F32, out_dtype == QSL_E4M3, group, norm->eps, drop_of(drop)};
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  pick_type(norm->dtype, [&](auto e) {
+    typedef decltype(e) E;
+    pick_row(norm->cols, [&](auto l, auto u) {
+      constexpr int th = THREADS<l()>, per = th / l();
+      const dim3 grid = grid_of((rows + per - 1) / per);
+      if (bits8) k_rms_norm<E, l(), u(), true><<<grid, th, 0, stream>>>(a);
+      else k_rms_norm<E, l(), u(), false><<<grid, th, 0, stream>>>(a);
+    });
+  });
+  return launched();
+}
+
+extern "C" size_t qsl_rms_norm_workspace_bytes(const qsl_norm* norm) {
+  return norm_ok(norm) ? align_up(4ull * back_blocks(norm) * norm->cols, 256) : 0;
+}
+
+extern "C" qsl_status qsl_rms_norm_backward(const qsl_norm* norm, const qsl_rows* total, const qsl_rows* dy, const qsl_rows* dtotal,
+                                            const qsl_drop* drop, const qsl_rows* dresidual, const qsl_rows* dx, float* dweight,
+                                            void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!norm_ok(norm) || !drop_ok(drop, norm->rows) || !aligned(dweight, 4)) return QSL_ERR_INVALID_ARG;
+  const uint64_t rows = norm->rows, cols = norm->cols, es = elem_size(norm->dtype);
+  const Matrix mt = of(total), my = of(dy), md = of(dtotal), mr = of(dresidual), mx = of(dx);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const uint32_t blocks = back_blocks(norm);
+  const uint64_t used = dweight ? 4ull * blocks * cols : 0;
+  if (rows != 0) {
+    if (!mt.data || !my.data || (!mr.data && !mx.data && !dweight)) return QSL_ERR_INVALID_ARG;
+    for (const Matrix& m : {mt, my, md, mr, mx}) if (!matrix_ok(m, rows, cols, norm->dtype)) return QSL_ERR_INVALID_ARG;
+    if (dweight && (!workspace || !aligned(workspace, 256))) return QSL_ERR_INVALID_ARG;
+    if (dweight && workspace_bytes < qsl_rms_norm_workspace_bytes(norm)) return QSL_ERR_BUFFER_TOO_SMALL;
+    auto at = [&](const Matrix& m) { return rows_at(m.data, rows, cols, m.stride, es); };
+    const Memory dw = array(dweight, 4 * cols), parts = array(workspace, used);
+    if (!apart({at(mr), at(mx), dw, parts}, {weight_of(norm), array(drop ? drop->round_at : nullptr, 8)})) return QSL_ERR_INVALID_ARG;
+    for (const Matrix& m : {mt, my, md}) {
+      if (!m.data) continue;
+      for (const Matrix& o : {mr, mx}) if (o.data && !same(m, o, rows) && meet(at(m), at(o))) return QSL_ERR_INVALID_ARG;
+      if (meet(at(m), dw) || meet(at(m), parts)) return QSL_ERR_INVALID_ARG;
+    }
+    const BackArgs a = {mt.data, my.data, md.data, norm->weight, mr.data, mx.data, dweight ? static_cast<float*>(workspace) : nullptr, mt.stride,
+                        my.stride, md.stride, mr.stride, mx.stride, rows, norm->cols, norm->weight_dtype == QSL_F32, norm->eps, drop_of(drop)};
+    pick_type(norm->dtype, [&](auto e) {
+      pick_row(norm->cols, [&](auto l, auto u) { k_rms_norm_backward<decltype(e), l(), u()><<<blocks, THREADS<l()>, 0, stream>>>(a); });
+    });
+  }
+  if (dweight) k_sum_parts<<<(norm->cols + 15) / 16, 256, 0, stream>>>(static_cast<const float*>(workspace), rows ? blocks : 0, norm->cols, dweight);
+  return rows || dweight ? launched() : QSL_OK;
+}
