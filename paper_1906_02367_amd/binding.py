@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -53,17 +54,8 @@ class _Teacher(C.Structure):
     _fields_ = [("index", C.c_void_p), ("value", C.c_void_p), ("lse", C.c_void_p), ("top", C.c_uint32), ("scale", C.c_float)]
 
 
-class _Rows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("stride", C.c_uint64)]
-
-
-class _Drop(C.Structure):
-    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("round", C.c_uint64), ("round_at", C.c_void_p), ("row0", C.c_uint32)]
-
-
-class _Norm(C.Structure):
-    _fields_ = [("rows", C.c_uint32), ("cols", C.c_uint32), ("dtype", C.c_uint32), ("weight_dtype", C.c_uint32), ("weight", C.c_void_p),
-                ("eps", C.c_float)]
+# qsl_rows, qsl_drop, qsl_norm as bytes in the machine's own layout, which are handed over as they are (structures of ctypes cost 0.5 us each)
+_ROWS, _DROP, _NORM = (struct.Struct(f).pack for f in ("@PQ", "@dQQPI4x", "@IIIIPf4x"))
 
 
 def _load():
@@ -97,11 +89,11 @@ def _load():
     lib.qsl_token_logprobs_backward.restype = C.c_int
     lib.qsl_distill.argtypes = [zp, tp, vp, vp, vp, sz, vp]; lib.qsl_distill.restype = C.c_int
     lib.qsl_distill_backward.argtypes = [zp, tp, vp, vp, vp, vp, u64, vp, sz, vp]; lib.qsl_distill_backward.restype = C.c_int
-    rp, dp, np_ = C.POINTER(_Rows), C.POINTER(_Drop), C.POINTER(_Norm)
-    lib.qsl_dropout.argtypes = [u32, u32, u32, rp, rp, dp, rp, vp]; lib.qsl_dropout.restype = C.c_int
-    lib.qsl_rms_norm.argtypes = [np_, rp, rp, dp, rp, rp, u32, u32, vp, vp]; lib.qsl_rms_norm.restype = C.c_int
-    lib.qsl_rms_norm_workspace_bytes.argtypes = [np_]; lib.qsl_rms_norm_workspace_bytes.restype = sz
-    lib.qsl_rms_norm_backward.argtypes = [np_, rp, rp, rp, dp, rp, rp, vp, vp, sz, vp]; lib.qsl_rms_norm_backward.restype = C.c_int
+    st = C.c_char_p                                     # a structure's bytes, or None
+    lib.qsl_dropout.argtypes = [u32, u32, u32, st, st, st, st, vp]; lib.qsl_dropout.restype = C.c_int
+    lib.qsl_rms_norm.argtypes = [st, st, st, st, st, st, u32, u32, vp, vp]; lib.qsl_rms_norm.restype = C.c_int
+    lib.qsl_rms_norm_workspace_bytes.argtypes = [st]; lib.qsl_rms_norm_workspace_bytes.restype = sz
+    lib.qsl_rms_norm_backward.argtypes = [st, st, st, st, st, st, st, vp, vp, sz, vp]; lib.qsl_rms_norm_backward.restype = C.c_int
     return lib
 
 
@@ -291,41 +283,43 @@ def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, t
 
 
 def _matrix(t, what, device, dtype, shape):
-    """A `qsl_rows` of a [rows, cols] tensor on `device` (its index) whose rows are contiguous and do not overlap; None for None."""
-    if t is None:
-        return None
+    """A `qsl_rows` of a [rows, cols] tensor on `device` (its index) whose rows are contiguous and do not overlap."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         raise ValueError(f"{what}: expected a {dtype} tensor {list(shape)} on cuda:{device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.is_contiguous():
+        return _ROWS(t.data_ptr(), shape[1])
     stride, step = t.stride()
     rows, cols = shape
     if (step != 1 and cols != 1) or (rows > 1 and stride < cols):
         raise ValueError(f"{what}: expected contiguous rows that do not overlap, got strides {t.stride()}")
-    return C.byref(_Rows(t.data_ptr(), stride if rows > 1 else cols))
+    return _ROWS(t.data_ptr(), stride if rows > 1 else cols)
 
 
 def _residual_shape(x, what):
     """Device, type and shape of the call, by its first array."""
-    if x.dim() != 2 or not x.is_cuda or x.dtype not in DTYPES:
+    dtype, shape, device = x.dtype, x.shape, x.get_device()
+    if len(shape) != 2 or device < 0 or dtype not in DTYPES:
         raise ValueError(f"{what}: expected a device tensor [rows, cols] of float32, bfloat16 or float16")
-    if x.shape[0] >= SIZE_END or x.shape[1] >= SIZE_END:                  # (ctypes would keep the lower 32 bits)
-        raise ValueError(f"{what}: expected less than 2^31 rows and columns, got {list(x.shape)}")
-    return x.get_device(), x.dtype, x.shape
+    if shape[0] >= SIZE_END or shape[1] >= SIZE_END:                      # (32 bits would keep the lower half)
+        raise ValueError(f"{what}: expected less than 2^31 rows and columns, got {list(shape)}")
+    return device, dtype, shape
 
 
 def _drop(p, seed, round, row0, round_at, device):
-    """A `qsl_drop`; None where nothing is dropped."""
-    if p == 0.0:
-        return None
+    """A `qsl_drop`, for a p that is not 0."""
     if not (0 <= seed < 1 << 64 and 0 <= round < 1 << 62 and 0 <= row0 < 1 << 32):
         raise ValueError(f"expected a seed below 2^64, a round below 2^62 and a first row below 2^32, got {seed}, {round}, {row0}")
-    return C.byref(_Drop(p, seed, round, None if round_at is None else _beside(round_at.view(-1), "round_at", device, torch.int64, (1,)), row0))
+    return _DROP(p, seed, round, 0 if round_at is None else _beside(round_at.view(-1), "round_at", device, torch.int64, (1,)), row0)
 
 
-def _norm(rows, cols, dtype, weight, eps, device):
+def _norm(shape, dtype, weight, eps, device):
+    rows, cols = shape
+    code = DTYPES[dtype]
     if weight is None:
-        return C.byref(_Norm(rows, cols, DTYPES[dtype], DTYPES[dtype], None, eps))
-    at = _beside(weight, "weight", device, torch.float32 if weight.dtype is torch.float32 else dtype, (cols,))
-    return C.byref(_Norm(rows, cols, DTYPES[dtype], DTYPES[weight.dtype], at, eps))
+        return _NORM(rows, cols, code, code, 0, eps)
+    kind = weight.dtype
+    return _NORM(rows, cols, code, 0 if kind is torch.float32 else code,
+                 _beside(weight, "weight", device, kind if kind is torch.float32 else dtype, (cols,)), eps)
 
 
 def _on_device(where, fn, device, *args):
@@ -345,28 +339,31 @@ def dropout(x, y, p, seed=0, round=0, row0=0, residual=None, round_at=None):
     kernel runs."""
     dev, dtype, shape = _residual_shape(x, "x")
     _on_device("qsl_dropout", _lib.qsl_dropout, dev, shape[0], shape[1], DTYPES[dtype], _matrix(x, "x", dev, dtype, shape),
-               _matrix(residual, "residual", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev), _matrix(y, "y", dev, dtype, shape))
+               None if residual is None else _matrix(residual, "residual", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev) if p else None,
+               _matrix(y, "y", dev, dtype, shape))
 
 
 def rms_norm(x, y, weight=None, eps=1e-6, residual=None, total=None, p=0.0, seed=0, round=0, row0=0, round_at=None, scales=None, group=0):
     """`qsl_rms_norm`: total = residual + drop(x), y = weight * total / sqrt(mean(total^2) + eps).  y has x's type, or is float8_e4m3fn or int8: codes
     with `scales` [rows, number of groups], a group being `group` (32, 64, 128) columns, or 0 for the whole row."""
     dev, dtype, shape = _residual_shape(x, "x")
-    rows, cols = shape
-    out = CODES.get(y.dtype, DTYPES[dtype])
-    if not 0 <= group < SIZE_END:
-        raise ValueError(f"group: expected 0, 32, 64 or 128, got {group}")
-    at = None if scales is None else _beside(scales, "scales", dev, torch.float32, (rows, -(-cols // group) if group else 1))
-    _on_device("qsl_rms_norm", _lib.qsl_rms_norm, dev, _norm(rows, cols, dtype, weight, eps, dev), _matrix(x, "x", dev, dtype, shape),
-               _matrix(residual, "residual", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev), _matrix(total, "total", dev, dtype, shape),
-               _matrix(y, "y", dev, y.dtype if y.dtype in CODES else dtype, shape), out, group, at)
+    kind = y.dtype if y.dtype in CODES else dtype
+    at = None
+    if scales is not None or group:
+        if not 0 <= group < SIZE_END:
+            raise ValueError(f"group: expected 0, 32, 64 or 128, got {group}")
+        at = None if scales is None else _beside(scales, "scales", dev, torch.float32, (shape[0], -(-shape[1] // group) if group else 1))
+    _on_device("qsl_rms_norm", _lib.qsl_rms_norm, dev, _norm(shape, dtype, weight, eps, dev), _matrix(x, "x", dev, dtype, shape),
+               None if residual is None else _matrix(residual, "residual", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev) if p else None,
+               None if total is None else _matrix(total, "total", dev, dtype, shape), _matrix(y, "y", dev, kind, shape),
+               CODES[kind] if kind in CODES else DTYPES[kind], group, at)
 
 
 def rms_norm_workspace_bytes(total):
     """`qsl_rms_norm_workspace_bytes` of these rows: what `workspace=` of `rms_norm_backward` has to hold for dweight (it is allocated if it
     is not given)."""
     dev, dtype, shape = _residual_shape(total, "total")
-    return int(_lib.qsl_rms_norm_workspace_bytes(_norm(shape[0], shape[1], dtype, None, 1.0, dev)))
+    return int(_lib.qsl_rms_norm_workspace_bytes(_norm(shape, dtype, None, 1.0, dev)))
 
 
 def rms_norm_backward(total, dy, weight=None, eps=1e-6, dtotal=None, dresidual=None, dx=None, dweight=None, p=0.0, seed=0, round=0, row0=0,
@@ -374,17 +371,21 @@ def rms_norm_backward(total, dy, weight=None, eps=1e-6, dtotal=None, dresidual=N
     """`qsl_rms_norm_backward`: from the totals, the gradient dy in y and what else arrives at the total (`dtotal`), those of the residual, of x
     and of the weight (float32), into the tensors that are given."""
     dev, dtype, shape = _residual_shape(total, "total")
-    rows, cols = shape
-    norm = _norm(rows, cols, dtype, weight, eps, dev)
-    dw = None
+    norm = _norm(shape, dtype, weight, eps, dev)
+    dw, at, size = None, None, 0
     if dweight is not None:
-        dw = _beside(dweight, "dweight", dev, torch.float32, (cols,))
+        dw = _beside(dweight, "dweight", dev, torch.float32, (shape[1],))
         if workspace is None:
-            workspace = torch.empty(_lib.qsl_rms_norm_workspace_bytes(norm), dtype=torch.uint8, device=total.device)
-    at, size = (None, 0) if workspace is None else (_beside(workspace, "workspace", dev, torch.uint8, (workspace.numel(),)), workspace.numel())
+            size = _lib.qsl_rms_norm_workspace_bytes(norm)
+            workspace = torch.empty(size, dtype=torch.uint8, device=total.device)
+            at = workspace.data_ptr()
+    if workspace is not None and at is None:
+        size = workspace.numel()
+        at = _beside(workspace, "workspace", dev, torch.uint8, (size,))
     _on_device("qsl_rms_norm_backward", _lib.qsl_rms_norm_backward, dev, norm, _matrix(total, "total", dev, dtype, shape),
-               _matrix(dy, "dy", dev, dtype, shape), _matrix(dtotal, "dtotal", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev),
-               _matrix(dresidual, "dresidual", dev, dtype, shape), _matrix(dx, "dx", dev, dtype, shape), dw, at, size)
+               _matrix(dy, "dy", dev, dtype, shape), None if dtotal is None else _matrix(dtotal, "dtotal", dev, dtype, shape),
+               _drop(p, seed, round, row0, round_at, dev) if p else None, None if dresidual is None else _matrix(dresidual, "dresidual", dev, dtype, shape),
+               None if dx is None else _matrix(dx, "dx", dev, dtype, shape), dw, at, size)
 
 
 class Qsl:

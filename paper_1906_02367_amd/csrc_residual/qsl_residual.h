@@ -50,58 +50,106 @@ template <class E> __device__ __forceinline__ void pack(const float* v, Unit<E>&
   for (int i = 0; i < 4; ++i) { const e2 x = {static_cast<E>(v[2 * i]), static_cast<E>(v[2 * i + 1])}; q.w[i] = __builtin_bit_cast(uint32_t, x); }
 }
 
-// 16 bytes with the elements' alignment; an element's bits
-template <class E> struct Raw { typedef uint32_t mem __attribute__((ext_vector_type(4), aligned(2))); typedef uint16_t bits; };
-template <> struct Raw<float> { typedef uint32_t mem __attribute__((ext_vector_type(4), aligned(4))); typedef uint32_t bits; };
-
-// the unit that begins at column c of a row; zeros behind the row's end.  (c + 8 does not pass 32 bits: cols < 2^31.)
-template <class E> __device__ __forceinline__ void load_whole(const E* row, uint32_t c, uint32_t cols, Unit<E>& q) {
-  const bool whole = c + 8 <= cols;
+// 16 bytes with the elements' alignment, and the parts of a unit that is short of columns; an element's bits
+template <class E> struct Raw {
+  typedef uint32_t mem __attribute__((ext_vector_type(4), aligned(2)));
+  typedef uint32_t four __attribute__((ext_vector_type(2), aligned(2)));
+  typedef uint32_t two __attribute__((aligned(2)));
+  typedef uint16_t bits;
+};
+template <> struct Raw<float> {
+  typedef uint32_t mem __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t four __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t two __attribute__((ext_vector_type(2), aligned(4)));
+  typedef uint32_t bits;
+};
+// the first n of a unit's elements away, zeros behind the rest
+template <class E> __device__ __forceinline__ void shift_out(Unit<E>& q, uint32_t n) {
+  constexpr int W = 2 * sizeof(E), STEP = W / 8;      // words, words of an element
+  auto away = [&](int words) {
 #pragma unroll
-  for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) {
-    typename Raw<E>::mem m = {0, 0, 0, 0};
-    if (whole) m = reinterpret_cast<const typename Raw<E>::mem*>(row + c)[k];
+    for (int i = 0; i < W; ++i) q.w[i] = i + words < W ? q.w[i + words] : 0;
+  };
+  if (n & 4) away(W / 2);
+  if (n & 2) away(W / 4);
+  if (n & 1) {
+    if constexpr (STEP == 1) away(1);
+    else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q.w[4 * k + i] = m[i];
-  }
-}
-// a row's last unit where it is short of columns
-template <class E> __device__ __forceinline__ void load_rest(const E* row, uint32_t c, uint32_t cols, Unit<E>& q) {
-  typedef typename Raw<E>::bits bits;
-  if (c < cols && c + 8 > cols) {
-    const bits* p = reinterpret_cast<const bits*>(row + c);
-    for (uint32_t i = 0; i < 8; ++i) {
-      const uint32_t x = c + i < cols ? p[i] : 0;
-      if constexpr (sizeof(E) == 4) q.w[i] = x;
-      else q.w[i / 2] |= x << 16 * (i & 1);
+      for (int i = 0; i < W; ++i) q.w[i] = __builtin_amdgcn_alignbit(i + 1 < W ? q.w[i + 1] : 0, q.w[i], 16);
     }
   }
 }
-template <class E> __device__ __forceinline__ void store_unit(E* row, uint32_t c, uint32_t cols, const float* v) {
+// U units of a row of `cols` columns, from column c0 on, `step` columns apart; zeros where there is no row (`live`) or none of it left.  A row's last
+// unit, where it is short, is cut from the row's last eight columns, so that its load is one with the others (by single elements: the gradient
+// of 30,000 rows of 785 bf16 LAST_BY_ELEMENTS instead of LAST_BY_UNITS us).  TINY: rows of less than eight are taken by elements.
+template <class E, int U, bool TINY> __device__ __forceinline__ void load_units(const E* row, uint32_t c0, uint32_t step, uint32_t cols, bool live, Unit<E>* q) {
+  constexpr int W = 2 * sizeof(E);
+  const uint32_t end = live ? cols : 0;
+  if (!TINY || cols >= 8) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t c = c0 + u * step;
+      const E* p = row + min(c, cols - 8);
+#pragma unroll
+      for (int k = 0; k < W / 4; ++k) {
+        typename Raw<E>::mem m = {0, 0, 0, 0};
+        if (c < end) m = reinterpret_cast<const typename Raw<E>::mem*>(p)[k];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[u].w[4 * k + i] = m[i];
+      }
+    }
+    if (cols & 7) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * step + 8 > cols) shift_out(q[u], 8 - (cols & 7));      // (behind the row: zeros stay zeros)
+    }
+  } else {
+    typedef typename Raw<E>::bits bits;
+    const bits* p = reinterpret_cast<const bits*>(row);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) q[u].w[i] = 0;
+    }
+    if (c0 < end) {                                                         // (c0 = 0)
+#pragma unroll
+      for (uint32_t i = 0; i < 7; ++i) {
+        const uint32_t x = i < cols ? static_cast<uint32_t>(p[i]) : 0u;
+        if constexpr (sizeof(E) == 4) q[0].w[i] = x;
+        else q[0].w[i / 2] |= x << 16 * (i & 1);
+      }
+    }
+  }
+}
+// a unit's columns below `end`: cols, or 0 where there is no row
+template <class E> __device__ __forceinline__ void store_unit(E* row, uint32_t c, uint32_t end, const float* v) {
   Unit<E> q;
   pack(v, q);
-  if (c + 8 <= cols) {
+  if (c + 8 <= end) {
 #pragma unroll
     for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) {
       typename Raw<E>::mem m = {q.w[4 * k], q.w[4 * k + 1], q.w[4 * k + 2], q.w[4 * k + 3]};
       reinterpret_cast<typename Raw<E>::mem*>(row + c)[k] = m;
     }
-  } else if (c < cols) {
-    typedef typename Raw<E>::bits bits;
-    bits* p = reinterpret_cast<bits*>(row + c);
-#pragma unroll
-    for (uint32_t i = 0; i < 7; ++i)
-      if (c + i < cols) p[i] = static_cast<bits>(sizeof(E) == 4 ? q.w[i] : q.w[i / 2] >> 16 * (i & 1));
-  }
-}
-
-// U units of a row, `step` columns apart
-template <class E, int U> __device__ __forceinline__ void load_units(const E* row, uint32_t c0, uint32_t step, uint32_t cols, Unit<E>* q) {
-#pragma unroll
-  for (int u = 0; u < U; ++u) load_whole(row, c0 + u * step, cols, q[u]);
-  if (cols & 7) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) load_rest(row, c0 + u * step, cols, q[u]);
+  } else if (c < end) {                                                     // four, two, one
+    uint32_t n = end - c;
+    E* p = row + c;
+    if (n & 4) {
+      typename Raw<E>::four m;
+      __builtin_memcpy(&m, q.w, sizeof(m));
+      *reinterpret_cast<typename Raw<E>::four*>(p) = m;
+      shift_out(q, 4);
+      p += 4;
+    }
+    if (n & 2) {
+      typename Raw<E>::two m;
+      __builtin_memcpy(&m, q.w, sizeof(m));
+      *reinterpret_cast<typename Raw<E>::two*>(p) = m;
+      shift_out(q, 2);
+      p += 2;
+    }
+    if (n & 1) *reinterpret_cast<typename Raw<E>::bits*>(p) = static_cast<typename Raw<E>::bits>(q.w[0]);
   }
 }
 
@@ -122,9 +170,21 @@ __device__ __forceinline__ Key key_of(const Drop& d) {
   if (d.T != KEEP_ALL && d.round_at) r += *d.round_at;
   return Key{static_cast<uint32_t>(r), (static_cast<uint32_t>(r >> 32) & 0x3FFFFFFFu) | DROP_STREAM << 30};
 }
+// philox4x32_10 with its exclusive-ors in one instruction of three operands each
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+__device__ __forceinline__ Words4 random_words(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p0 = static_cast<uint64_t>(0xD2511F53u) * c0, p1 = static_cast<uint64_t>(0xCD9E8D57u) * c2;
+    c0 = xor3(static_cast<uint32_t>(p1 >> 32), c1, k0); c1 = static_cast<uint32_t>(p1);
+    c2 = xor3(static_cast<uint32_t>(p0 >> 32), c3, k1); c3 = static_cast<uint32_t>(p0);
+    k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
+  }
+  return Words4{{c0, c1, c2, c3}};
+}
 // v <- drop(v) of a row's unit: one Philox block, eight pieces of 16 bits.  (A word of 32 bits for each would cost as much time as the memory.)
 __device__ __forceinline__ void drop_unit(const Drop& d, const Key& k, uint32_t row, uint32_t unit, float* v) {
-  const Words4 o = philox4x32_10(unit, d.row0 + row, k.lo, k.hi, d.seed_lo, d.seed_hi);
+  const Words4 o = random_words(unit, d.row0 + row, k.lo, k.hi, d.seed_lo, d.seed_hi);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t piece = i & 1 ? o.w[i / 2] >> 16 : o.w[i / 2] & 0xFFFFu;
@@ -148,17 +208,33 @@ __device__ __forceinline__ float sum16(float x) {
   return x + dpp_move<DPP_ROW_ROR + 1>(x);
 }
 __device__ __forceinline__ float lane_float(float x, int lane) { return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(x)), lane))); }
-// `at`: L / 64 places in LDS that no thread still reads from an earlier call
-template <int L> __device__ __forceinline__ float row_sum(float x, float* at) {
+__device__ __forceinline__ float wave_total(float x) {
   x = sum16(x);
-  if constexpr (L == 16) return x;
-  x = (lane_float(x, 0) + lane_float(x, 16)) + (lane_float(x, 32) + lane_float(x, 48));
+  return (lane_float(x, 0) + lane_float(x, 16)) + (lane_float(x, 32) + lane_float(x, 48));
+}
+// `at`: places in LDS for the row's waves that no thread still reads from an earlier call
+template <int L> __device__ __forceinline__ float row_sum(float x, float* at) {
+  if constexpr (L == 16) return sum16(x);
+  x = wave_total(x);
   if constexpr (L <= 64) return x;
   if (lane_id() == 0) at[threadIdx.x / WAVE] = x;
   __syncthreads();
   float s = at[0];
 #pragma unroll
   for (int w = 1; w < L / 64; ++w) s += at[w];
+  return s;
+}
+// two sums at once
+struct Two { float a, b; };
+template <int L> __device__ __forceinline__ Two row_sums(Two x, Two* at) {
+  if constexpr (L == 16) return Two{sum16(x.a), sum16(x.b)};
+  x = Two{wave_total(x.a), wave_total(x.b)};
+  if constexpr (L <= 64) return x;
+  if (lane_id() == 0) at[threadIdx.x / WAVE] = x;
+  __syncthreads();
+  Two s = at[0];
+#pragma unroll
+  for (int w = 1; w < L / 64; ++w) { s.a += at[w].a; s.b += at[w].b; }
   return s;
 }
 // over 4, 8 or 16 neighbouring lanes
@@ -185,11 +261,13 @@ template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t x, uint32_
 constexpr float SMALLER = 0x1p-72f;
 constexpr float INF = __builtin_inff();
 
-template <int L> constexpr int THREADS = L < 256 ? 256 : L;      // short rows share a block
+template <int L> constexpr int THREADS = L <= 64 ? 256 : L;      // rows of a wave and less share a block
+template <int L> constexpr bool TINY = L == 16;                  // rows of less than eight columns go there
+template <int L> constexpr int WAVES = L <= 64 ? 1 : L / 64;     // of a row
 // a row's number within the block, for the compiler the same in a wave where it is
 template <int L> __device__ __forceinline__ uint32_t row_in_block() {
-  if constexpr (L >= 256) return 0;
-  else if constexpr (L >= 64) return __builtin_amdgcn_readfirstlane(threadIdx.x / L);
+  if constexpr (L > 64) return 0;
+  else if constexpr (L == 64) return __builtin_amdgcn_readfirstlane(threadIdx.x / L);
   else return threadIdx.x / L;
 }
 
@@ -211,18 +289,18 @@ template <class E> __global__ __launch_bounds__(256) void k_dropout(DropArgs a) 
   const Key key = key_of(a.drop);
   Unit<E> x[DROP_EACH], res[DROP_EACH];
   uint64_t row[DROP_EACH];
-  uint32_t c[DROP_EACH], cols[DROP_EACH];
+  uint32_t c[DROP_EACH], end[DROP_EACH];
 #pragma unroll
   for (int k = 0; k < DROP_EACH; ++k) {
     const uint32_t i = rest + k * 256 + threadIdx.x, r = i / a.units;
     row[k] = row_b + r;
     c[k] = (i - r * a.units) * 8;
-    cols[k] = row[k] < a.rows ? a.cols : 0;
-    load_units<E, 1>(static_cast<const E*>(a.x) + row[k] * a.x_stride, c[k], 0, cols[k], x + k);
+    end[k] = row[k] < a.rows ? a.cols : 0;
+    load_units<E, 1, true>(static_cast<const E*>(a.x) + row[k] * a.x_stride, c[k], 0, a.cols, end[k] != 0, x + k);
   }
   if (a.res) {
 #pragma unroll
-    for (int k = 0; k < DROP_EACH; ++k) load_units<E, 1>(static_cast<const E*>(a.res) + row[k] * a.res_stride, c[k], 0, cols[k], res + k);
+    for (int k = 0; k < DROP_EACH; ++k) load_units<E, 1, true>(static_cast<const E*>(a.res) + row[k] * a.res_stride, c[k], 0, a.cols, end[k] != 0, res + k);
   }
 #pragma unroll
   for (int k = 0; k < DROP_EACH; ++k) {
@@ -235,7 +313,7 @@ template <class E> __global__ __launch_bounds__(256) void k_dropout(DropArgs a) 
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += b[i];
     }
-    store_unit(static_cast<E*>(a.y) + row[k] * a.y_stride, c[k], cols[k], v);
+    store_unit(static_cast<E*>(a.y) + row[k] * a.y_stride, c[k], end[k], v);
   }
 }
 
@@ -252,23 +330,22 @@ struct NormArgs {
   Drop drop;
 };
 
-template <class E, int U> __device__ __forceinline__ void load_weight(const void* weight, uint32_t is_float, uint32_t c0, uint32_t step, uint32_t cols, float* w) {
+template <class E, int U, bool TINY> __device__ __forceinline__ void load_weight(const void* weight, uint32_t is_float, uint32_t c0, uint32_t step, uint32_t cols, float* w) {
   if (!weight) {
 #pragma unroll
     for (int i = 0; i < 8 * U; ++i) w[i] = 1.0f;
   } else if (sizeof(E) == 4 || is_float) {
     Unit<float> q[U];
-    load_units<float, U>(static_cast<const float*>(weight), c0, step, cols, q);
+    load_units<float, U, TINY>(static_cast<const float*>(weight), c0, step, cols, true, q);
 #pragma unroll
     for (int u = 0; u < U; ++u) unpack(q[u], w + 8 * u);
   } else {
     Unit<E> q[U];
-    load_units<E, U>(static_cast<const E*>(weight), c0, step, cols, q);
+    load_units<E, U, TINY>(static_cast<const E*>(weight), c0, step, cols, true, q);
 #pragma unroll
     for (int u = 0; u < U; ++u) unpack(q[u], w + 8 * u);
   }
 }
-
 // 8-bit codes of a unit, eight bytes; `most`: the bits of the group's largest |y|
 __device__ __forceinline__ void store_codes(uint8_t* row, uint32_t c, uint32_t cols, const float* y, uint32_t most, bool is_e4m3, float* scale_at) {
   const float a = fmaxf(__uint_as_float(most), 0x1p-100f), Q = is_e4m3 ? 448.0f : 127.0f, inv = Q / a;
@@ -290,28 +367,33 @@ __device__ __forceinline__ void store_codes(uint8_t* row, uint32_t c, uint32_t c
     }
   }
   if (scale_at) *scale_at = bad ? __builtin_nanf("") : a / Q;
-  typedef uint32_t two __attribute__((ext_vector_type(2), aligned(1)));
+  typedef uint32_t eight __attribute__((ext_vector_type(2), aligned(1)));
+  typedef uint32_t four __attribute__((aligned(1)));
+  typedef uint16_t two __attribute__((aligned(1)));
   if (c + 8 <= cols) {
-    const two q = {lo, hi};
-    *reinterpret_cast<two*>(row + c) = q;
+    const eight q = {lo, hi};
+    *reinterpret_cast<eight*>(row + c) = q;
   } else {
-#pragma unroll
-    for (uint32_t i = 0; i < 7; ++i)
-      if (c + i < cols) row[c + i] = static_cast<uint8_t>((i < 4 ? lo : hi) >> 8 * (i & 3));
+    const uint32_t n = cols - c;
+    uint8_t* p = row + c;
+    if (n & 4) { *reinterpret_cast<four*>(p) = lo; lo = hi; p += 4; }
+    if (n & 2) { *reinterpret_cast<two*>(p) = static_cast<uint16_t>(lo); lo >>= 16; p += 2; }
+    if (n & 1) *p = static_cast<uint8_t>(lo);
   }
 }
 
 template <class E, int L, int U, bool BITS8>
 __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
-  __shared__ float sums[2][L < 256 ? 1 : L / 64];
-  __shared__ uint32_t maxima[L < 256 ? 1 : L / 64];
+  __shared__ float sums[2][WAVES<L>];
+  __shared__ uint32_t maxima[WAVES<L>];
   const uint64_t row = block_number() * (THREADS<L> / L) + row_in_block<L>();
   const uint32_t lane = threadIdx.x % L, cols = row < a.rows ? a.cols : 0;
   Unit<E> x[U], res[U];
-  load_units<E, U>(static_cast<const E*>(a.x) + row * a.x_stride, lane * 8, L * 8, cols, x);
-  if (a.res) load_units<E, U>(static_cast<const E*>(a.res) + row * a.res_stride, lane * 8, L * 8, cols, res);
-  float w[8 * U], h[8 * U];
-  load_weight<E, U>(a.weight, a.weight_is_float, lane * 8, L * 8, cols, w);
+  load_units<E, U, TINY<L>>(static_cast<const E*>(a.x) + row * a.x_stride, lane * 8, L * 8, a.cols, cols != 0, x);
+  if (a.res) load_units<E, U, TINY<L>>(static_cast<const E*>(a.res) + row * a.res_stride, lane * 8, L * 8, a.cols, cols != 0, res);
+  float h[8 * U], w[8 * U];
+  // (four units a thread: the registers do not hold them beside the rest)
+  if constexpr (U <= 2) load_weight<E, U, TINY<L>>(a.weight, a.weight_is_float, lane * 8, L * 8, a.cols, w);
   const Key key = key_of(a.drop);
   float ss = 0.0f;
 #pragma unroll
@@ -341,7 +423,11 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
   }
   const float r = 1.0f / sqrtf(ss / static_cast<float>(a.cols) + eps);
 #pragma unroll
-  for (int i = 0; i < 8 * U; ++i) h[i] = h[i] * r * w[i];
+  for (int u = 0; u < U; ++u) {
+    if constexpr (U > 2) load_weight<E, 1, false>(a.weight, a.weight_is_float, lane * 8 + u * L * 8, 0, a.cols, w + 8 * u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[8 * u + i] = h[8 * u + i] * r * w[8 * u + i];
+  }
   if constexpr (!BITS8) {
 #pragma unroll
     for (int u = 0; u < U; ++u) store_unit(static_cast<E*>(a.y) + row * a.y_stride, lane * 8 + u * L * 8, cols, h + 8 * u);
@@ -381,71 +467,100 @@ struct BackArgs {
 };
 
 // A block goes through rows that lie a grid apart and keeps its sum for dw in registers.
+// Where 1024 threads leave a thread 128 registers, the weights are held in LDS, every thread's own; with four units what else arrives at the totals is loaded
+// where it is added.
+template <int L, int U> constexpr bool WEIGHT_IN_LDS = L * U >= 2048;
 template <class E, int L, int U>
 __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   constexpr int ROWS = THREADS<L> / L;
-  __shared__ float sums[2][4][L < 256 ? 1 : L / 64];
+  constexpr bool LDS = WEIGHT_IN_LDS<L, U>, LATE = U > 2;
+  typedef float quad __attribute__((ext_vector_type(4)));
+  __shared__ quad weights[LDS ? 2 * U : 1][LDS ? L : 1];
+  __shared__ Two sums[2][2][WAVES<L>];
   __shared__ float joined[ROWS > 1 ? ROWS * 8 * U * L : 1];
   const uint32_t lane = threadIdx.x % L, c0 = lane * 8;
   const Key key = key_of(a.drop);
-  float w[8 * U], dw[8 * U];
-  load_weight<E, U>(a.weight, a.weight_is_float, c0, L * 8, a.cols, w);
+  float w_all[LDS ? 8 : 8 * U], dw[8 * U];
+  if constexpr (LDS) {
+    for (int u = 0; u < U; ++u) {
+      load_weight<E, 1, false>(a.weight, a.weight_is_float, c0 + u * L * 8, 0, a.cols, w_all);
+      weights[2 * u][lane] = quad{w_all[0], w_all[1], w_all[2], w_all[3]};
+      weights[2 * u + 1][lane] = quad{w_all[4], w_all[5], w_all[6], w_all[7]};
+    }
+  } else {
+    load_weight<E, U, TINY<L>>(a.weight, a.weight_is_float, c0, L * 8, a.cols, w_all);
+  }
+  auto weight_of = [&](int u, float* w) {
+    if constexpr (LDS) {
+      const quad a0 = weights[2 * u][lane], a1 = weights[2 * u + 1][lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { w[i] = a0[i]; w[4 + i] = a1[i]; }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = w_all[8 * u + i];
+    }
+  };
 #pragma unroll
   for (int i = 0; i < 8 * U; ++i) dw[i] = 0.0f;
   uint32_t turn = 0;             // a row's sums go where those before last stood: there is a barrier between reading these and writing them
   for (uint64_t base = static_cast<uint64_t>(blockIdx.x) * ROWS; base < a.rows; base += static_cast<uint64_t>(gridDim.x) * ROWS) {
     const uint64_t row = base + row_in_block<L>();
-    const uint32_t cols = row < a.rows ? a.cols : 0;
-    Unit<E> hq[U], dyq[U], dtq[U];
-    load_units<E, U>(static_cast<const E*>(a.total) + row * a.total_stride, c0, L * 8, cols, hq);
-    load_units<E, U>(static_cast<const E*>(a.dy) + row * a.dy_stride, c0, L * 8, cols, dyq);
-    if (a.dtotal) load_units<E, U>(static_cast<const E*>(a.dtotal) + row * a.dtotal_stride, c0, L * 8, cols, dtq);
-    float f = 1.0f, ss = 0.0f, gh = 0.0f;
+    const bool live = row < a.rows;
+    const uint32_t end = live ? a.cols : 0;
+    const E* dt_row = a.dtotal ? static_cast<const E*>(a.dtotal) + row * a.dtotal_stride : nullptr;
+    Unit<E> hq[U], dyq[U], dtq[LATE ? 1 : U];
+    load_units<E, U, TINY<L>>(static_cast<const E*>(a.total) + row * a.total_stride, c0, L * 8, a.cols, live, hq);
+    load_units<E, U, TINY<L>>(static_cast<const E*>(a.dy) + row * a.dy_stride, c0, L * 8, a.cols, live, dyq);
+    if constexpr (!LATE)
+      if (dt_row) load_units<E, U, TINY<L>>(dt_row, c0, L * 8, a.cols, live, dtq);
+    float f = 1.0f;
     auto sum = [&]() {
+      Two s = {0.0f, 0.0f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        float h[8], d[8];
+        float h[8], d[8], w[8];
         unpack(hq[u], h);
         unpack(dyq[u], d);
+        weight_of(u, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           h[i] *= f;
-          ss = __builtin_fmaf(h[i], h[i], ss);
-          gh = __builtin_fmaf(d[i] * w[8 * u + i], h[i], gh);
+          s.a = __builtin_fmaf(h[i], h[i], s.a);
+          s.b = __builtin_fmaf(d[i] * w[i], h[i], s.b);
         }
       }
+      return s;
     };
-    sum();
-    ss = row_sum<L>(ss, sums[turn][0]);
-    gh = row_sum<L>(gh, sums[turn][1]);
+    Two s = row_sums<L>(sum(), sums[turn][0]);
     float eps = a.eps;
-    if (__any(ss == INF)) {
-      if (ss == INF) { f = SMALLER; eps = 0.0f; }
-      ss = 0.0f; gh = 0.0f;
-      sum();
-      ss = row_sum<L>(ss, sums[turn][2]);
-      gh = row_sum<L>(gh, sums[turn][3]);
+    if (__any(s.a == INF)) {
+      if (s.a == INF) { f = SMALLER; eps = 0.0f; }
+      s = row_sums<L>(sum(), sums[turn][1]);
     }
     turn ^= 1;
-    const float r = 1.0f / sqrtf(ss / static_cast<float>(a.cols) + eps);      // of the totals times f
-    const float mean = gh * r / static_cast<float>(a.cols), rf = r * f;
+    const float r = 1.0f / sqrtf(s.a / static_cast<float>(a.cols) + eps);      // of the totals times f
+    const float mean = s.b * r / static_cast<float>(a.cols), rf = r * f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float h[8], d[8], t[8];
+      float h[8], d[8], t[8], w[8];
       unpack(hq[u], h);
       unpack(dyq[u], d);
-      if (a.dtotal) unpack(dtq[u], t);
+      weight_of(u, w);
+      if (dt_row) {
+        if constexpr (LATE) load_units<E, 1, false>(dt_row, c0 + u * L * 8, 0, a.cols, live, dtq);
+        unpack(dtq[LATE ? 0 : u], t);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float un = h[i] * f * r;
         dw[8 * u + i] = __builtin_fmaf(d[i], un, dw[8 * u + i]);
-        d[i] = rf * (d[i] * w[8 * u + i] - un * mean);
-        if (a.dtotal) d[i] += t[i];
+        d[i] = rf * (d[i] * w[i] - un * mean);
+        if (dt_row) d[i] += t[i];
       }
-      if (a.dres) store_unit(static_cast<E*>(a.dres) + row * a.dres_stride, c0 + u * L * 8, cols, d);
+      if (a.dres) store_unit(static_cast<E*>(a.dres) + row * a.dres_stride, c0 + u * L * 8, end, d);
       if (a.dx) {
         if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key, static_cast<uint32_t>(row), u * L + lane, d);
-        store_unit(static_cast<E*>(a.dx) + row * a.dx_stride, c0 + u * L * 8, cols, d);
+        store_unit(static_cast<E*>(a.dx) + row * a.dx_stride, c0 + u * L * 8, end, d);
       }
     }
   }
@@ -470,19 +585,30 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   }
 }
 
-// dw: the blocks' sums, in the blocks' order within each of 16 parts, then the parts.  Blocks of 16 columns x 16 parts.
-__global__ __launch_bounds__(256) void k_sum_parts(const float* part, uint32_t blocks, uint32_t cols, float* dweight) {
-  __shared__ float at[16][17];
-  const uint32_t x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
+// dw: every 64th of the blocks' sums in turn, then the 64 sums of these, always in the same order.  A block has 16 columns; eight loads of a
+// thread are under way at once.
+constexpr uint32_t SUM_COLS = 16, SUM_PARTS = 64;
+__global__ __launch_bounds__(SUM_COLS * SUM_PARTS) void k_sum_parts(const float* part, uint32_t blocks, uint32_t cols, float* dweight) {
+  __shared__ float at[SUM_PARTS][SUM_COLS + 1];
+  const uint32_t x = threadIdx.x % SUM_COLS, y = threadIdx.x / SUM_COLS, c = blockIdx.x * SUM_COLS + x;
   float s = 0.0f;
-  if (c < cols)
-    for (uint32_t b = y; b < blocks; b += 16) s += part[static_cast<uint64_t>(b) * cols + c];
+  for (uint32_t b = y; b < blocks; b += 8 * SUM_PARTS) {
+    float v[8];
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {
+      const uint32_t n = b + k * SUM_PARTS;
+      v[k] = c < cols && n < blocks ? part[static_cast<uint64_t>(n) * cols + c] : 0.0f;
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) s += v[k];
+  }
   at[y][x] = s;
   __syncthreads();
-  if (y == 0 && c < cols) {
-#pragma unroll
-    for (int k = 1; k < 16; ++k) s += at[k][x];
-    dweight[c] = s;
+  // the 64 sums of a column: by sixteen lanes, four each
+  if (y < 16) {
+    const uint32_t l = threadIdx.x % 16, col = threadIdx.x / 16;
+    s = sum16((at[l][col] + at[l + 16][col]) + (at[l + 32][col] + at[l + 48][col]));
+    if (l == 0 && blockIdx.x * SUM_COLS + col < cols) dweight[blockIdx.x * SUM_COLS + col] = s;
   }
 }
 

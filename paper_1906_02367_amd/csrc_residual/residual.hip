@@ -45,16 +45,49 @@ void pick_type(uint32_t dtype, F&& f) {
 }
 template <int V> using Int = std::integral_constant<int, V>;
 
-// f(lanes that hold a row, units each of them holds)
-template <class F>
+// f(lanes that hold a row, units each of them holds).  us, residual added, total and y written, bf16 / fp32:
+//   131,072 rows of 128    16 x 1 26 / 51, 64 x 1 48 / 64
+//   32,768 rows of 512     64 x 1 25 / 50, 128 x 1 27 / 54, 256 x 1 42 / 57
+//   30,000 rows of 1,024   64 x 2 44.5 / 95, 128 x 1 44 / 90, 256 x 1 47 / 92;  of 785  64 x 2 38 / 77, 128 x 1 46 / 78
+//   16,384 rows of 2,048   128 x 2 46.5 / 103, 256 x 1 49 / 97.5, 512 x 1 51 / 99
+//   16,384 rows of 4,096   256 x 2 91 / 194, 512 x 1 91.5 / 185, 1024 x 1 101 / 201
+//   8,192 rows of 8,192    512 x 2 91.5 / 192, 1024 x 1 92 / 187
+//   4,096 rows of 16,384   512 x 4 98.5 / 207, 1024 x 2 99 / 198
+// 32 bytes of an array in a thread do best, whatever the type, but for rows of a wave (fp32 64 x 2: the form for 16 bits serves both)
+template <class E, class F>
 void pick_row(uint32_t cols, F&& f) {
   if (cols <= 16 * 8) f(Int<16>(), Int<1>());
   else if (cols <= 64 * 8) f(Int<64>(), Int<1>());
   else if (cols <= 64 * 16) f(Int<64>(), Int<2>());
+  else if (cols > 1024 * 16) f(Int<1024>(), Int<4>());
+  else if (cols > 1024 * 8) f(Int<1024>(), Int<2>());
+  else if constexpr (sizeof(E) == 2) {
+    if (cols <= 128 * 16) f(Int<128>(), Int<2>());
+    else if (cols <= 256 * 16) f(Int<256>(), Int<2>());
+    else f(Int<512>(), Int<2>());
+  } else {
+    if (cols <= 256 * 8) f(Int<256>(), Int<1>());
+    else if (cols <= 512 * 8) f(Int<512>(), Int<1>());
+    else f(Int<1024>(), Int<1>());
+  }
+}
+// The gradient's, which holds three arrays and the sum for dweight.  us with all of them, a mask and k_sum_parts, bf16 / fp32, by blocks for a compute unit (of 256
+// threads 2, 3, 4; of 512 1, 2; of 1,024 1):
+//   32,768 rows of 512     64 x 1 38, 37, 39 / 67, 69, 70
+//   30,000 rows of 785     64 x 2 68, 56, 71 / 97, 100, 116
+//   16,384 rows of 2,048   256 x 1 72, 71, 71 / 126, 131, 135;  128 x 2 (bf16) 74, 72, 78
+//   16,384 rows of 4,096   512 x 1 155, 129 / 252, 250;  256 x 2 129, 133, 148 / 251, 256, 258
+//   8,192 rows of 8,192    1024 x 1 132 / 246;  512 x 2 (bf16) 133, 137
+//   2,047 rows of 12,288   1024 x 2 61 / 110;  4,096 of 16,384 138 / 262;  2,048 of 32,768  1024 x 4 259 / 359
+template <class F>
+void pick_row_back(uint32_t cols, F&& f) {
+  if (cols <= 16 * 8) f(Int<16>(), Int<1>());
+  else if (cols <= 64 * 8) f(Int<64>(), Int<1>());
+  else if (cols <= 64 * 16) f(Int<64>(), Int<2>());
   else if (cols <= 256 * 8) f(Int<256>(), Int<1>());
-  else if (cols <= 256 * 16) f(Int<256>(), Int<2>());
-  else if (cols <= 256 * 32) f(Int<256>(), Int<4>());
-  else if (cols <= 512 * 32) f(Int<512>(), Int<4>());
+  else if (cols <= 512 * 8) f(Int<512>(), Int<1>());
+  else if (cols <= 1024 * 8) f(Int<1024>(), Int<1>());
+  else if (cols <= 1024 * 16) f(Int<1024>(), Int<2>());
   else f(Int<1024>(), Int<4>());
 }
 
@@ -69,11 +102,11 @@ bool norm_ok(const qsl_norm* n) {
 }
 Memory weight_of(const qsl_norm* n) { return array(n->weight, static_cast<uint64_t>(n->cols) * elem_size(n->weight_dtype)); }
 
-// blocks of the backward pass: each goes through many rows, so that their sums for dweight are few
+// Blocks of the backward pass: each goes through many rows, so that their sums for dweight are few.
 uint32_t back_blocks(const qsl_norm* n) {
   uint32_t blocks = 0;
-  pick_row(n->cols, [&](auto l, auto) {
-    const uint64_t per = THREADS<l()> / l(), most = 1024 * 256 / THREADS<l()>;
+  pick_row_back(n->cols, [&](auto l, auto) {
+    const uint64_t th = THREADS<l()>, per = th / l(), most = th == 256 ? (n->dtype == QSL_F32 ? 512 : 768) : 256 * 1024 / th;
     blocks = static_cast<uint32_t>(std::min<uint64_t>((n->rows + per - 1) / per, most));
   });
   return blocks;
@@ -128,7 +161,7 @@ extern "C" qsl_status qsl_rms_norm(const qsl_norm* norm, const qsl_rows* x, cons
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   pick_type(norm->dtype, [&](auto e) {
     typedef decltype(e) E;
-    pick_row(norm->cols, [&](auto l, auto u) {
+    pick_row<E>(norm->cols, [&](auto l, auto u) {
       constexpr int th = THREADS<l()>, per = th / l();
       const dim3 grid = grid_of((rows + per - 1) / per);
       if (bits8) k_rms_norm<E, l(), u(), true><<<grid, th, 0, stream>>>(a);
@@ -167,9 +200,9 @@ extern "C" qsl_status qsl_rms_norm_backward(const qsl_norm* norm, const qsl_rows
     const BackArgs a = {mt.data, my.data, md.data, norm->weight, mr.data, mx.data, dweight ? static_cast<float*>(workspace) : nullptr, mt.stride,
                         my.stride, md.stride, mr.stride, mx.stride, rows, norm->cols, norm->weight_dtype == QSL_F32, norm->eps, drop_of(drop)};
     pick_type(norm->dtype, [&](auto e) {
-      pick_row(norm->cols, [&](auto l, auto u) { k_rms_norm_backward<decltype(e), l(), u()><<<blocks, THREADS<l()>, 0, stream>>>(a); });
+      pick_row_back(norm->cols, [&](auto l, auto u) { k_rms_norm_backward<decltype(e), l(), u()><<<blocks, THREADS<l()>, 0, stream>>>(a); });
     });
   }
-  if (dweight) k_sum_parts<<<(norm->cols + 15) / 16, 256, 0, stream>>>(static_cast<const float*>(workspace), rows ? blocks : 0, norm->cols, dweight);
+  if (dweight) k_sum_parts<<<(norm->cols + SUM_COLS - 1) / SUM_COLS, SUM_COLS * SUM_PARTS, 0, stream>>>(static_cast<const float*>(workspace), rows ? blocks : 0, norm->cols, dweight);
   return rows || dweight ? launched() : QSL_OK;
 }
