@@ -407,7 +407,8 @@ typedef struct {
 qsl_status qsl_rms_norm(const qsl_norm *norm, const qsl_rows *x, const qsl_rows *residual, const qsl_drop *drop, const qsl_rows *total,
                         const qsl_rows *y, uint32_t out_dtype, uint32_t group, float *scales, void *hip_stream);
 
-/* Bytes of device memory that qsl_rms_norm_backward needs as `workspace` for dweight, a multiple of 256; 0 for invalid arguments. */
+/* Bytes of device memory that qsl_rms_norm_backward needs as `workspace` for dweight, a multiple of 256; 0 where it needs none (very few rows), and for
+ * invalid arguments. */
 size_t qsl_rms_norm_workspace_bytes(const qsl_norm *norm);
 
 /* The gradient of qsl_rms_norm (of y before any rounding to 8 bits), from the totals as they were stored: with r = 1 / sqrt(mean total^2 + eps),
@@ -419,7 +420,7 @@ size_t qsl_rms_norm_workspace_bytes(const qsl_norm *norm);
  *   dresidual  may be absent; may be total, dy or dtotal
  *   dx         may be absent; may be total, dy or dtotal, but not dresidual
  *   dweight    device, float [cols], or NULL: written, not added to; zeros for rows = 0.  One of the three has to be there
- *   workspace  device, 256-byte aligned; looked at only with dweight */
+ *   workspace  device, at least qsl_rms_norm_workspace_bytes() bytes, 256-byte aligned; looked at only with dweight, and where that is not 0 */
 qsl_status qsl_rms_norm_backward(const qsl_norm *norm, const qsl_rows *total, const qsl_rows *dy, const qsl_rows *dtotal, const qsl_drop *drop,
                                  const qsl_rows *dresidual, const qsl_rows *dx, float *dweight, void *workspace, size_t workspace_bytes,
                                  void *hip_stream);

@@ -377,8 +377,9 @@ def rms_norm_backward(total, dy, weight=None, eps=1e-6, dtotal=None, dresidual=N
         dw = _beside(dweight, "dweight", dev, torch.float32, (shape[1],))
         if workspace is None:
             size = _lib.qsl_rms_norm_workspace_bytes(norm)
-            workspace = torch.empty(size, dtype=torch.uint8, device=total.device)
-            at = workspace.data_ptr()
+            if size:
+                workspace = torch.empty(size, dtype=torch.uint8, device=total.device)
+                at = workspace.data_ptr()
     if workspace is not None and at is None:
         size = workspace.numel()
         at = _beside(workspace, "workspace", dev, torch.uint8, (size,))

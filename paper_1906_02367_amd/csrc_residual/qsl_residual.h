@@ -80,10 +80,22 @@ template <class E> __device__ __forceinline__ void shift_out(Unit<E>& q, uint32_
     }
   }
 }
+// PAST: what is read or written is more than the caches hold, so that nothing of it is found there by what runs next: it need not pass through
+// them.  us for 16,384 rows of 4,096 bf16: the norm 91.5 / 88.1, and with a reader of its results behind it 161 / 158; the gradient 130 / 119.  (Of
+// 8,192 rows 81 / 83 with the reader, and fp32, whose lanes read 32 bytes in two loads, loses in any case: 248 / 278.)
+template <bool PAST, class M> __device__ __forceinline__ M load16(const M* p) {
+  if constexpr (PAST) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <bool PAST, class M> __device__ __forceinline__ void store16(M* p, M m) {
+  if constexpr (PAST) __builtin_nontemporal_store(m, p);
+  else *p = m;
+}
 // U units of a row of `cols` columns, from column c0 on, `step` columns apart; zeros where there is no row (`live`) or none of it left.  A row's last
 // unit, where it is short, is cut from the row's last eight columns, so that its load is one with the others (by single elements: the gradient
-// of 30,000 rows of 785 bf16 LAST_BY_ELEMENTS instead of LAST_BY_UNITS us).  TINY: rows of less than eight are taken by elements.
-template <class E, int U, bool TINY> __device__ __forceinline__ void load_units(const E* row, uint32_t c0, uint32_t step, uint32_t cols, bool live, Unit<E>* q) {
+// of 30,000 rows of 785 bf16 71 instead of 61 us): cut_units has to follow.  It waits for the values, so it follows when all
+// arrays' loads are under way (else 2,047 rows of 12,289 70 instead of 64 us).  TINY: rows of less than eight are taken by elements.
+template <class E, int U, bool TINY, bool PAST> __device__ __forceinline__ void load_units(const E* row, uint32_t c0, uint32_t step, uint32_t cols, bool live, Unit<E>* q) {
   constexpr int W = 2 * sizeof(E);
   const uint32_t end = live ? cols : 0;
   if (!TINY || cols >= 8) {
@@ -94,15 +106,10 @@ template <class E, int U, bool TINY> __device__ __forceinline__ void load_units(
 #pragma unroll
       for (int k = 0; k < W / 4; ++k) {
         typename Raw<E>::mem m = {0, 0, 0, 0};
-        if (c < end) m = reinterpret_cast<const typename Raw<E>::mem*>(p)[k];
+        if (c < end) m = load16<PAST>(reinterpret_cast<const typename Raw<E>::mem*>(p) + k);
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[u].w[4 * k + i] = m[i];
       }
-    }
-    if (cols & 7) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (c0 + u * step + 8 > cols) shift_out(q[u], 8 - (cols & 7));      // (behind the row: zeros stay zeros)
     }
   } else {
     typedef typename Raw<E>::bits bits;
@@ -122,15 +129,21 @@ template <class E, int U, bool TINY> __device__ __forceinline__ void load_units(
     }
   }
 }
+template <class E, int U, bool TINY> __device__ __forceinline__ void cut_units(uint32_t c0, uint32_t step, uint32_t cols, Unit<E>* q) {
+  if ((cols & 7) == 0 || (TINY && cols < 8)) return;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (c0 + u * step < cols && c0 + u * step + 8 > cols) shift_out(q[u], 8 - (cols & 7));      // (no row: zeros stay zeros)
+}
 // a unit's columns below `end`: cols, or 0 where there is no row
-template <class E> __device__ __forceinline__ void store_unit(E* row, uint32_t c, uint32_t end, const float* v) {
+template <bool PAST, class E> __device__ __forceinline__ void store_unit(E* row, uint32_t c, uint32_t end, const float* v) {
   Unit<E> q;
   pack(v, q);
   if (c + 8 <= end) {
 #pragma unroll
     for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) {
       typename Raw<E>::mem m = {q.w[4 * k], q.w[4 * k + 1], q.w[4 * k + 2], q.w[4 * k + 3]};
-      reinterpret_cast<typename Raw<E>::mem*>(row + c)[k] = m;
+      store16<PAST>(reinterpret_cast<typename Raw<E>::mem*>(row + c) + k, m);
     }
   } else if (c < end) {                                                     // four, two, one
     uint32_t n = end - c;
@@ -212,6 +225,15 @@ __device__ __forceinline__ float wave_total(float x) {
   x = sum16(x);
   return (lane_float(x, 0) + lane_float(x, 16)) + (lane_float(x, 32) + lane_float(x, 48));
 }
+// The W waves' values of a row, joined by every W neighbouring lanes: each pair of lanes adds the same two numbers.  (Every thread reading all W:
+// the gradient of 16,384 rows of 4,096 bf16 130.5 us instead of 128.9, of 30,000 of 785 55.9 / 55.4.)
+template <int W> __device__ __forceinline__ float join_sum(float x) {
+  if constexpr (W >= 2) x += dpp_move<DPP_XOR1>(x);
+  if constexpr (W >= 4) x += dpp_move<DPP_XOR2>(x);
+  if constexpr (W >= 8) x += dpp_move<DPP_HALF_MIRROR>(x);
+  if constexpr (W >= 16) x += dpp_move<DPP_ROW_ROR + 8>(x);
+  return x;
+}
 // `at`: places in LDS for the row's waves that no thread still reads from an earlier call
 template <int L> __device__ __forceinline__ float row_sum(float x, float* at) {
   if constexpr (L == 16) return sum16(x);
@@ -219,10 +241,7 @@ template <int L> __device__ __forceinline__ float row_sum(float x, float* at) {
   if constexpr (L <= 64) return x;
   if (lane_id() == 0) at[threadIdx.x / WAVE] = x;
   __syncthreads();
-  float s = at[0];
-#pragma unroll
-  for (int w = 1; w < L / 64; ++w) s += at[w];
-  return s;
+  return join_sum<L / 64>(at[threadIdx.x % (L / 64)]);
 }
 // two sums at once
 struct Two { float a, b; };
@@ -232,10 +251,8 @@ template <int L> __device__ __forceinline__ Two row_sums(Two x, Two* at) {
   if constexpr (L <= 64) return x;
   if (lane_id() == 0) at[threadIdx.x / WAVE] = x;
   __syncthreads();
-  Two s = at[0];
-#pragma unroll
-  for (int w = 1; w < L / 64; ++w) { s.a += at[w].a; s.b += at[w].b; }
-  return s;
+  x = at[threadIdx.x % (L / 64)];
+  return Two{join_sum<L / 64>(x.a), join_sum<L / 64>(x.b)};
 }
 // over 4, 8 or 16 neighbouring lanes
 __device__ __forceinline__ uint32_t max_of_lanes(uint32_t x, uint32_t lanes) {
@@ -252,8 +269,12 @@ template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t x, uint32_
   if constexpr (L <= 64) return x;
   if (lane_id() == 0) at[threadIdx.x / WAVE] = x;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < L / 64; ++w) x = max(x, at[w]);
+  constexpr int W = L / 64;
+  x = at[threadIdx.x % W];
+  if constexpr (W >= 2) x = max(x, dpp_move<DPP_XOR1>(x));
+  if constexpr (W >= 4) x = max(x, dpp_move<DPP_XOR2>(x));
+  if constexpr (W >= 8) x = max(x, dpp_move<DPP_HALF_MIRROR>(x));
+  if constexpr (W >= 16) x = max(x, dpp_move<DPP_ROW_ROR + 8>(x));
   return x;
 }
 
@@ -281,40 +302,31 @@ struct DropArgs {
   uint32_t cols, units;          // units of a row
   Drop drop;
 };
-constexpr int DROP_EACH = 4;     // units of a thread
+constexpr int DROP_THREADS = 256;
 
-template <class E> __global__ __launch_bounds__(256) void k_dropout(DropArgs a) {
-  const uint64_t first = block_number() * (256 * DROP_EACH), row_b = first / a.units;
-  const uint32_t rest = static_cast<uint32_t>(first - row_b * a.units);
-  const Key key = key_of(a.drop);
-  Unit<E> x[DROP_EACH], res[DROP_EACH];
-  uint64_t row[DROP_EACH];
-  uint32_t c[DROP_EACH], end[DROP_EACH];
-#pragma unroll
-  for (int k = 0; k < DROP_EACH; ++k) {
-    const uint32_t i = rest + k * 256 + threadIdx.x, r = i / a.units;
-    row[k] = row_b + r;
-    c[k] = (i - r * a.units) * 8;
-    end[k] = row[k] < a.rows ? a.cols : 0;
-    load_units<E, 1, true>(static_cast<const E*>(a.x) + row[k] * a.x_stride, c[k], 0, a.cols, end[k] != 0, x + k);
-  }
+// A unit a thread.  (Four a thread, whose loads are under way together: 8,192 rows of 4,096 bf16 28.7 us instead of 25.3, 4,095 of 11,009 40.9 / 34.2, fp32
+// 53.4 / 48.9; eight: 30.5.)
+template <class E, bool PAST> __global__ __launch_bounds__(DROP_THREADS) void k_dropout(DropArgs a) {
+  const uint64_t first = block_number() * DROP_THREADS, row_b = first / a.units;
+  const uint32_t i = static_cast<uint32_t>(first - row_b * a.units) + threadIdx.x, r = i / a.units;
+  const uint64_t row = row_b + r;
+  const uint32_t c = (i - r * a.units) * 8;
+  if (row >= a.rows) return;
+  Unit<E> x, res;
+  load_units<E, 1, true, PAST>(static_cast<const E*>(a.x) + row * a.x_stride, c, 0, a.cols, true, &x);
+  if (a.res) load_units<E, 1, true, PAST>(static_cast<const E*>(a.res) + row * a.res_stride, c, 0, a.cols, true, &res);
+  cut_units<E, 1, true>(c, 0, a.cols, &x);
+  float v[8];
+  unpack(x, v);
+  if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key_of(a.drop), static_cast<uint32_t>(row), c / 8, v);
   if (a.res) {
+    float b[8];
+    cut_units<E, 1, true>(c, 0, a.cols, &res);
+    unpack(res, b);
 #pragma unroll
-    for (int k = 0; k < DROP_EACH; ++k) load_units<E, 1, true>(static_cast<const E*>(a.res) + row[k] * a.res_stride, c[k], 0, a.cols, end[k] != 0, res + k);
+    for (int k = 0; k < 8; ++k) v[k] += b[k];
   }
-#pragma unroll
-  for (int k = 0; k < DROP_EACH; ++k) {
-    float v[8];
-    unpack(x[k], v);
-    if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key, static_cast<uint32_t>(row[k]), c[k] / 8, v);
-    if (a.res) {
-      float b[8];
-      unpack(res[k], b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += b[i];
-    }
-    store_unit(static_cast<E*>(a.y) + row[k] * a.y_stride, c[k], end[k], v);
-  }
+  store_unit<PAST>(static_cast<E*>(a.y) + row * a.y_stride, c, a.cols, v);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -336,12 +348,14 @@ template <class E, int U, bool TINY> __device__ __forceinline__ void load_weight
     for (int i = 0; i < 8 * U; ++i) w[i] = 1.0f;
   } else if (sizeof(E) == 4 || is_float) {
     Unit<float> q[U];
-    load_units<float, U, TINY>(static_cast<const float*>(weight), c0, step, cols, true, q);
+    load_units<float, U, TINY, false>(static_cast<const float*>(weight), c0, step, cols, true, q);
+    cut_units<float, U, TINY>(c0, step, cols, q);
 #pragma unroll
     for (int u = 0; u < U; ++u) unpack(q[u], w + 8 * u);
   } else {
     Unit<E> q[U];
-    load_units<E, U, TINY>(static_cast<const E*>(weight), c0, step, cols, true, q);
+    load_units<E, U, TINY, false>(static_cast<const E*>(weight), c0, step, cols, true, q);
+    cut_units<E, U, TINY>(c0, step, cols, q);
 #pragma unroll
     for (int u = 0; u < U; ++u) unpack(q[u], w + 8 * u);
   }
@@ -382,19 +396,21 @@ __device__ __forceinline__ void store_codes(uint8_t* row, uint32_t c, uint32_t c
   }
 }
 
-template <class E, int L, int U, bool BITS8>
+template <class E, int L, int U, bool BITS8, bool PAST>
 __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
   __shared__ float sums[2][WAVES<L>];
   __shared__ uint32_t maxima[WAVES<L>];
   const uint64_t row = block_number() * (THREADS<L> / L) + row_in_block<L>();
   const uint32_t lane = threadIdx.x % L, cols = row < a.rows ? a.cols : 0;
   Unit<E> x[U], res[U];
-  load_units<E, U, TINY<L>>(static_cast<const E*>(a.x) + row * a.x_stride, lane * 8, L * 8, a.cols, cols != 0, x);
-  if (a.res) load_units<E, U, TINY<L>>(static_cast<const E*>(a.res) + row * a.res_stride, lane * 8, L * 8, a.cols, cols != 0, res);
+  load_units<E, U, TINY<L>, PAST>(static_cast<const E*>(a.x) + row * a.x_stride, lane * 8, L * 8, a.cols, cols != 0, x);
+  if (a.res) load_units<E, U, TINY<L>, PAST>(static_cast<const E*>(a.res) + row * a.res_stride, lane * 8, L * 8, a.cols, cols != 0, res);
   float h[8 * U], w[8 * U];
   // (four units a thread: the registers do not hold them beside the rest)
   if constexpr (U <= 2) load_weight<E, U, TINY<L>>(a.weight, a.weight_is_float, lane * 8, L * 8, a.cols, w);
   const Key key = key_of(a.drop);
+  cut_units<E, U, TINY<L>>(lane * 8, L * 8, a.cols, x);
+  if (a.res) cut_units<E, U, TINY<L>>(lane * 8, L * 8, a.cols, res);
   float ss = 0.0f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -407,7 +423,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += b[i];
     }
-    if (a.total) store_unit(static_cast<E*>(a.total) + row * a.total_stride, lane * 8 + u * L * 8, cols, v);
+    if (a.total) store_unit<PAST>(static_cast<E*>(a.total) + row * a.total_stride, lane * 8 + u * L * 8, cols, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(v[i], v[i], ss);
   }
@@ -430,7 +446,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
   }
   if constexpr (!BITS8) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) store_unit(static_cast<E*>(a.y) + row * a.y_stride, lane * 8 + u * L * 8, cols, h + 8 * u);
+    for (int u = 0; u < U; ++u) store_unit<PAST>(static_cast<E*>(a.y) + row * a.y_stride, lane * 8 + u * L * 8, cols, h + 8 * u);
   } else {
     uint32_t most[U], all = 0;      // of the bits of |y|: a NaN is above the infinities
 #pragma unroll
@@ -459,7 +475,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
 struct BackArgs {
   const void *total, *dy, *dtotal, *weight;
   void *dres, *dx;
-  float* part;                   // [blocks, cols]: every block's sum of dy u over its rows; or nullptr
+  float* part;                   // [blocks, cols]: every block's sum of dy u over its rows (dweight itself, if there is one block); or nullptr
   uint64_t total_stride, dy_stride, dtotal_stride, dres_stride, dx_stride, rows;
   uint32_t cols, weight_is_float;
   float eps;
@@ -467,13 +483,14 @@ struct BackArgs {
 };
 
 // A block goes through rows that lie a grid apart and keeps its sum for dw in registers.
-// Where 1024 threads leave a thread 128 registers, the weights are held in LDS, every thread's own; with four units what else arrives at the totals is loaded
-// where it is added.
+// Where 1024 threads leave a thread 128 registers, the weights are held in LDS, every thread's own; where that is not enough, what else arrives at
+// the totals is loaded where it is added.
 template <int L, int U> constexpr bool WEIGHT_IN_LDS = L * U >= 2048;
-template <class E, int L, int U>
+template <class E, int L, int U> constexpr bool LATE_DTOTAL = L * U * sizeof(E) >= 8192;
+template <class E, int L, int U, bool PAST>
 __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   constexpr int ROWS = THREADS<L> / L;
-  constexpr bool LDS = WEIGHT_IN_LDS<L, U>, LATE = U > 2;
+  constexpr bool LDS = WEIGHT_IN_LDS<L, U>, LATE = LATE_DTOTAL<E, L, U>;
   typedef float quad __attribute__((ext_vector_type(4)));
   __shared__ quad weights[LDS ? 2 * U : 1][LDS ? L : 1];
   __shared__ Two sums[2][2][WAVES<L>];
@@ -509,11 +526,14 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
     const uint32_t end = live ? a.cols : 0;
     const E* dt_row = a.dtotal ? static_cast<const E*>(a.dtotal) + row * a.dtotal_stride : nullptr;
     Unit<E> hq[U], dyq[U], dtq[LATE ? 1 : U];
-    load_units<E, U, TINY<L>>(static_cast<const E*>(a.total) + row * a.total_stride, c0, L * 8, a.cols, live, hq);
-    load_units<E, U, TINY<L>>(static_cast<const E*>(a.dy) + row * a.dy_stride, c0, L * 8, a.cols, live, dyq);
+    load_units<E, U, TINY<L>, PAST>(static_cast<const E*>(a.total) + row * a.total_stride, c0, L * 8, a.cols, live, hq);
+    load_units<E, U, TINY<L>, PAST>(static_cast<const E*>(a.dy) + row * a.dy_stride, c0, L * 8, a.cols, live, dyq);
     if constexpr (!LATE)
-      if (dt_row) load_units<E, U, TINY<L>>(dt_row, c0, L * 8, a.cols, live, dtq);
-    float f = 1.0f;
+      if (dt_row) load_units<E, U, TINY<L>, PAST>(dt_row, c0, L * 8, a.cols, live, dtq);
+    cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, hq);
+    cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, dyq);
+    if constexpr (!LATE)
+      if (dt_row) cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, dtq);
     auto sum = [&]() {
       Two s = {0.0f, 0.0f};
 #pragma unroll
@@ -524,7 +544,6 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
         weight_of(u, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          h[i] *= f;
           s.a = __builtin_fmaf(h[i], h[i], s.a);
           s.b = __builtin_fmaf(d[i] * w[i], h[i], s.b);
         }
@@ -532,13 +551,24 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
       return s;
     };
     Two s = row_sums<L>(sum(), sums[turn][0]);
-    float eps = a.eps;
+    float f = 1.0f, eps = a.eps;
     if (__any(s.a == INF)) {
-      if (s.a == INF) { f = SMALLER; eps = 0.0f; }
+      if (s.a == INF) {      // the totals times f, in their type: what that rounds is nothing beside the row's largest
+        f = SMALLER;
+        eps = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float h[8];
+          unpack(hq[u], h);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[i] *= f;
+          pack(h, hq[u]);
+        }
+      }
       s = row_sums<L>(sum(), sums[turn][1]);
     }
     turn ^= 1;
-    const float r = 1.0f / sqrtf(s.a / static_cast<float>(a.cols) + eps);      // of the totals times f
+    const float r = 1.0f / sqrtf(s.a / static_cast<float>(a.cols) + eps);
     const float mean = s.b * r / static_cast<float>(a.cols), rf = r * f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -547,20 +577,23 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
       unpack(dyq[u], d);
       weight_of(u, w);
       if (dt_row) {
-        if constexpr (LATE) load_units<E, 1, false>(dt_row, c0 + u * L * 8, 0, a.cols, live, dtq);
+        if constexpr (LATE) {
+          load_units<E, 1, false, PAST>(dt_row, c0 + u * L * 8, 0, a.cols, live, dtq);
+          cut_units<E, 1, false>(c0 + u * L * 8, 0, a.cols, dtq);
+        }
         unpack(dtq[LATE ? 0 : u], t);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float un = h[i] * f * r;
+        const float un = h[i] * r;
         dw[8 * u + i] = __builtin_fmaf(d[i], un, dw[8 * u + i]);
         d[i] = rf * (d[i] * w[i] - un * mean);
         if (dt_row) d[i] += t[i];
       }
-      if (a.dres) store_unit(static_cast<E*>(a.dres) + row * a.dres_stride, c0 + u * L * 8, end, d);
+      if (a.dres) store_unit<PAST>(static_cast<E*>(a.dres) + row * a.dres_stride, c0 + u * L * 8, end, d);
       if (a.dx) {
         if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key, static_cast<uint32_t>(row), u * L + lane, d);
-        store_unit(static_cast<E*>(a.dx) + row * a.dx_stride, c0 + u * L * 8, end, d);
+        store_unit<PAST>(static_cast<E*>(a.dx) + row * a.dx_stride, c0 + u * L * 8, end, d);
       }
     }
   }
@@ -568,7 +601,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   float* out = a.part + static_cast<uint64_t>(blockIdx.x) * a.cols;
   if constexpr (ROWS == 1) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) store_unit(out, c0 + u * L * 8, a.cols, dw + 8 * u);
+    for (int u = 0; u < U; ++u) store_unit<false>(out, c0 + u * L * 8, a.cols, dw + 8 * u);
   } else {
     const uint32_t mine = row_in_block<L>();
 #pragma unroll

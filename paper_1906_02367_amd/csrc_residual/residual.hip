@@ -15,6 +15,7 @@
 
 namespace {
 
+constexpr uint64_t CACHE_BYTES = 256ull << 20;     // the last cache before the memory
 constexpr uint64_t GRID_X = 1u << 20;              // blocks in a row of the grid (a launch counts its threads in 32 bits)
 
 uint32_t elem_size(uint32_t dtype) { return dtype == QSL_F32 ? 4 : dtype <= QSL_F16 ? 2 : 1; }
@@ -42,6 +43,14 @@ void pick_type(uint32_t dtype, F&& f) {
   if (dtype == QSL_F32) f(float());
   else if (dtype == QSL_BF16) f(__bf16());
   else f(_Float16());
+}
+// f(whether `written` bytes go past the caches): those of 16-bit types, if the caches do not hold them
+template <class E, class F>
+void pick_past(uint64_t written, F&& f) {
+  if constexpr (sizeof(E) == 2) {
+    if (written >= CACHE_BYTES) { f(std::true_type()); return; }
+  }
+  f(std::false_type());
 }
 template <int V> using Int = std::integral_constant<int, V>;
 
@@ -102,12 +111,13 @@ bool norm_ok(const qsl_norm* n) {
 }
 Memory weight_of(const qsl_norm* n) { return array(n->weight, static_cast<uint64_t>(n->cols) * elem_size(n->weight_dtype)); }
 
-// Blocks of the backward pass: each goes through many rows, so that their sums for dweight are few.
+// Blocks of the backward pass: each goes through many rows, so that their sums for dweight are few.  Two rows (or two for each group of threads) are
+// left to one block, whose sum is dweight: they take 1 to 2 us in it, another launch takes the host 4.
 uint32_t back_blocks(const qsl_norm* n) {
   uint32_t blocks = 0;
   pick_row_back(n->cols, [&](auto l, auto) {
     const uint64_t th = THREADS<l()>, per = th / l(), most = th == 256 ? (n->dtype == QSL_F32 ? 512 : 768) : 256 * 1024 / th;
-    blocks = static_cast<uint32_t>(std::min<uint64_t>((n->rows + per - 1) / per, most));
+    blocks = n->rows <= 2 * per ? (n->rows != 0) : static_cast<uint32_t>(std::min<uint64_t>((n->rows + per - 1) / per, most));
   });
   return blocks;
 }
@@ -129,8 +139,11 @@ extern "C" qsl_status qsl_dropout(uint32_t rows, uint32_t cols, uint32_t dtype, 
   if (drop && meet(array(drop->round_at, 8), at(my))) return QSL_ERR_INVALID_ARG;
   const uint32_t units = (cols + 7) / 8;
   const DropArgs a = {mx.data, mr.data, my.data, mx.stride, mr.stride, my.stride, rows, cols, units, drop_of(drop)};
-  const uint64_t each = 256 * DROP_EACH, blocks = (static_cast<uint64_t>(rows) * units + each - 1) / each;
-  pick_type(dtype, [&](auto e) { k_dropout<decltype(e)><<<grid_of(blocks), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+  const uint64_t blocks = (static_cast<uint64_t>(rows) * units + DROP_THREADS - 1) / DROP_THREADS;
+  pick_type(dtype, [&](auto e) {
+    typedef decltype(e) E;
+    pick_past<E>(rows * (cols * es), [&](auto past) { k_dropout<E, past()><<<grid_of(blocks), DROP_THREADS, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+  });
   return launched();
 }
 
@@ -164,15 +177,18 @@ extern "C" qsl_status qsl_rms_norm(const qsl_norm* norm, const qsl_rows* x, cons
     pick_row<E>(norm->cols, [&](auto l, auto u) {
       constexpr int th = THREADS<l()>, per = th / l();
       const dim3 grid = grid_of((rows + per - 1) / per);
-      if (bits8) k_rms_norm<E, l(), u(), true><<<grid, th, 0, stream>>>(a);
-      else k_rms_norm<E, l(), u(), false><<<grid, th, 0, stream>>>(a);
+      pick_past<E>(rows * cols * ((mt.data ? es : 0) + elem_size(out_dtype)), [&](auto past) {
+        if (bits8) k_rms_norm<E, l(), u(), true, past()><<<grid, th, 0, stream>>>(a);
+        else k_rms_norm<E, l(), u(), false, past()><<<grid, th, 0, stream>>>(a);
+      });
     });
   });
   return launched();
 }
 
 extern "C" size_t qsl_rms_norm_workspace_bytes(const qsl_norm* norm) {
-  return norm_ok(norm) ? align_up(4ull * back_blocks(norm) * norm->cols, 256) : 0;
+  const uint64_t blocks = norm_ok(norm) ? back_blocks(norm) : 0;
+  return blocks > 1 ? align_up(4 * blocks * norm->cols, 256) : 0;
 }
 
 extern "C" qsl_status qsl_rms_norm_backward(const qsl_norm* norm, const qsl_rows* total, const qsl_rows* dy, const qsl_rows* dtotal,
@@ -183,26 +199,32 @@ extern "C" qsl_status qsl_rms_norm_backward(const qsl_norm* norm, const qsl_rows
   const Matrix mt = of(total), my = of(dy), md = of(dtotal), mr = of(dresidual), mx = of(dx);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const uint32_t blocks = back_blocks(norm);
-  const uint64_t used = dweight ? 4ull * blocks * cols : 0;
+  const bool parts_apart = dweight && blocks > 1;
   if (rows != 0) {
     if (!mt.data || !my.data || (!mr.data && !mx.data && !dweight)) return QSL_ERR_INVALID_ARG;
     for (const Matrix& m : {mt, my, md, mr, mx}) if (!matrix_ok(m, rows, cols, norm->dtype)) return QSL_ERR_INVALID_ARG;
-    if (dweight && (!workspace || !aligned(workspace, 256))) return QSL_ERR_INVALID_ARG;
-    if (dweight && workspace_bytes < qsl_rms_norm_workspace_bytes(norm)) return QSL_ERR_BUFFER_TOO_SMALL;
+    if (parts_apart && (!workspace || !aligned(workspace, 256))) return QSL_ERR_INVALID_ARG;
+    if (parts_apart && workspace_bytes < qsl_rms_norm_workspace_bytes(norm)) return QSL_ERR_BUFFER_TOO_SMALL;
     auto at = [&](const Matrix& m) { return rows_at(m.data, rows, cols, m.stride, es); };
-    const Memory dw = array(dweight, 4 * cols), parts = array(workspace, used);
+    const Memory dw = array(dweight, 4 * cols), parts = array(workspace, parts_apart ? 4 * blocks * cols : 0);
     if (!apart({at(mr), at(mx), dw, parts}, {weight_of(norm), array(drop ? drop->round_at : nullptr, 8)})) return QSL_ERR_INVALID_ARG;
     for (const Matrix& m : {mt, my, md}) {
       if (!m.data) continue;
       for (const Matrix& o : {mr, mx}) if (o.data && !same(m, o, rows) && meet(at(m), at(o))) return QSL_ERR_INVALID_ARG;
       if (meet(at(m), dw) || meet(at(m), parts)) return QSL_ERR_INVALID_ARG;
     }
-    const BackArgs a = {mt.data, my.data, md.data, norm->weight, mr.data, mx.data, dweight ? static_cast<float*>(workspace) : nullptr, mt.stride,
+    const BackArgs a = {mt.data, my.data, md.data, norm->weight, mr.data, mx.data, parts_apart ? static_cast<float*>(workspace) : dweight, mt.stride,
                         my.stride, md.stride, mr.stride, mx.stride, rows, norm->cols, norm->weight_dtype == QSL_F32, norm->eps, drop_of(drop)};
     pick_type(norm->dtype, [&](auto e) {
-      pick_row_back(norm->cols, [&](auto l, auto u) { k_rms_norm_backward<decltype(e), l(), u()><<<blocks, THREADS<l()>, 0, stream>>>(a); });
+      typedef decltype(e) E;
+      pick_row_back(norm->cols, [&](auto l, auto u) {
+        pick_past<E>(rows * cols * es * ((mr.data != nullptr) + (mx.data != nullptr)), [&](auto past) {
+          k_rms_norm_backward<E, l(), u(), past()><<<blocks, THREADS<l()>, 0, stream>>>(a);
+        });
+      });
     });
   }
-  if (dweight) k_sum_parts<<<(norm->cols + SUM_COLS - 1) / SUM_COLS, SUM_COLS * SUM_PARTS, 0, stream>>>(static_cast<const float*>(workspace), rows ? blocks : 0, norm->cols, dweight);
+  if (parts_apart || (dweight && rows == 0))
+    k_sum_parts<<<(norm->cols + SUM_COLS - 1) / SUM_COLS, SUM_COLS * SUM_PARTS, 0, stream>>>(static_cast<const float*>(workspace), blocks, norm->cols, dweight);
   return rows || dweight ? launched() : QSL_OK;
 }

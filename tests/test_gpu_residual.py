@@ -299,6 +299,48 @@ def test_the_weights_gradient_over_many_rows(B, N, C, dtype):
     assert torch.equal(dw, dw2) and (space[-256:] == 7).all()
 
 
+@pytest.mark.parametrize("C", [5, 100, 400, 1000, 2000, 4000, 8000, 16000, 32768])
+def test_the_weights_gradient_of_few_rows(B, C):
+    """Where one block has all rows its sum is dweight, without a workspace; and the numbers of rows around that border."""
+    per = 16 if C <= 128 else 4 if C <= 1024 else 1
+    for N in (1, 2, 2 * per, 2 * per + 1):
+        h, dy = rows_of(N, C, "fp32", N), rows_of(N, C, "fp32", 50 + N)
+        dw = torch.full((C,), 77.0, device=dev)
+        assert (B.rms_norm_workspace_bytes(h) == 0) == (N <= 2 * per)
+        B.rms_norm_backward(h, dy, dweight=dw)
+        _, _, want, tol = X.backward(h, dy, None, 1e-6)
+        X.check(dw, want, tol, f"{N} x {C}")
+
+
+@pytest.mark.parametrize("N,C,dtype", [(70000, 2048, "bf16"), (16500, 8200, "fp16"), (17000, 4099, "bf16"), (300000, 513, "bf16"), (1100000, 127, "fp16")])
+def test_results_that_the_caches_do_not_hold(B, N, C, dtype):
+    """More than 256 MB written: the first and the last rows, and rows between, against the definitions; all of them against smaller calls."""
+    g = torch.Generator(device=dev).manual_seed(1)
+    x, res, dy = (torch.randn(N, C, generator=g, device=dev).to(X.TYPES[dtype]) for _ in range(3))
+    w, p = weight_of(C, "same", dtype), 0.2
+    y, t, dres, dx, d, dw = (torch.empty_like(x) for _ in range(6))
+    dw = torch.empty(C, device=dev)
+    B.rms_norm(x, y, weight=w, residual=res, total=t, p=p, seed=1)
+    B.rms_norm_backward(t, dy, weight=w, dtotal=res, dresidual=dres, dx=dx, dweight=dw, p=p, seed=1)
+    B.dropout(x, d, p, seed=1, residual=res)
+    assert torch.equal(d, t)
+    for a in (0, N // 2, N - 7):
+        keep = X.kept(7, C, p, seed=1, row0=a)
+        h, tol = X.total_of(x[a:a + 7], res[a:a + 7], keep, p)
+        want, tol_y = X.norm_of(h, tol, w, 1e-6)
+        X.check(t[a:a + 7], h, tol + X.rounding(h, tol, t.dtype), "total")
+        X.check(y[a:a + 7], want, tol_y + X.rounding(want, tol_y, y.dtype), "y")
+        want, tol, _, _ = X.backward(t[a:a + 7], dy[a:a + 7], w, 1e-6, res[a:a + 7])
+        X.check(dres[a:a + 7], want, tol + X.rounding(want, tol, y.dtype), "dresidual")
+    step = N // 7 + 1
+    for a in range(0, N, step):
+        part = [torch.empty_like(v[a:a + step]) for v in (y, t, dres, dx)]
+        kw = dict(p=p, seed=1, row0=a)
+        B.rms_norm(x[a:a + step], part[0], weight=w, residual=res[a:a + step], total=part[1], **kw)
+        B.rms_norm_backward(t[a:a + step], dy[a:a + step], weight=w, dtotal=res[a:a + step], dresidual=part[2], dx=part[3], **kw)
+        assert all(torch.equal(v[a:a + step], q) for v, q in zip((y, t, dres, dx), part)), a
+
+
 def test_no_rows(B):
     x, w = torch.empty(0, 100, device=dev), torch.ones(100, device=dev)
     dw = torch.full((100,), 5.0, device=dev)
@@ -553,9 +595,9 @@ def test_two_graphs_and_two_streams_at_once(B):
 
 
 def test_refusals_through_the_binding(B):
-    x, y = rows_of(4, 64, "bf16", 1), room(4, 64, "bf16")[0]
+    x, y = rows_of(40, 64, "bf16", 1), room(40, 64, "bf16")[0]
     for call in (lambda: B.dropout(x, y, 1.5), lambda: B.dropout(x, y, -0.1), lambda: B.rms_norm(x, y, eps=0.0), lambda: B.rms_norm(x, y, total=y), lambda: B.rms_norm(x, y, group=32),
-                 lambda: B.rms_norm(x, torch.empty(4, 64, dtype=torch.int8, device=dev)), lambda: B.rms_norm_backward(x, y), lambda: B.rms_norm_backward(x, y, dresidual=x, dx=x),
+                 lambda: B.rms_norm(x, torch.empty(40, 64, dtype=torch.int8, device=dev)), lambda: B.rms_norm_backward(x, y), lambda: B.rms_norm_backward(x, y, dresidual=x, dx=x),
                  lambda: B.rms_norm_backward(x, y, dweight=torch.empty(64, device=dev), workspace=torch.empty(256, dtype=torch.uint8, device=dev)[:0]),
                  lambda: B.rms_norm(rows_of(1, 32769, "bf16"), room(1, 32769, "bf16")[0])):
         with pytest.raises(B.QslError):

@@ -42,7 +42,7 @@ def lib():
     return l
 
 
-N, W, PITCH = 4, 1000, 1008                      # rows, columns, stride
+N, W, PITCH = 40, 1000, 1008                     # rows, columns, stride
 
 
 def at(k):                                       # addresses that are never looked at, far apart
@@ -167,6 +167,7 @@ def test_gradient_arguments_that_are_refused(lib):
     need = lib.qsl_rms_norm_workspace_bytes(a_norm())
     assert need >= 4 * W and need % 256 == 0
     assert back_call(lib, n=need - 1) == TOO_SMALL
+    assert [lib.qsl_rms_norm_workspace_bytes(a_norm(rows=n)) for n in (0, 1, 2)] == [0, 0, 0]      # one block, whose sum is dweight
     assert back_call(lib, norm=a_norm(rows=0), dw=None, ws=None, n=0, total=None, dy=None) == 0
 
 
