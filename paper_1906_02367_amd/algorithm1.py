@@ -15,7 +15,8 @@ can be checked along the run.
 
 `SoftmaxProblem.error` is the other axis of the plots of Section 5 (top-1 and top-5 error), `DistilledProblem` the same model
 trained on the labels and on a trained model's top log probabilities; both, and the gradients of the latter's local steps, come from the
-library's operators on logits.
+library's operators on logits.  `RegularisedProblem` is the model on normed features, which its local steps drop out: by the library's norm,
+with the random words of its other streams.
 
     python -m paper_1906_02367_amd.algorithm1        # loss against bits for a few operators
 """
@@ -128,6 +129,43 @@ class DistilledProblem(SoftmaxProblem):
         return g.reshape(R, D) + self.lam * w_local
 
 
+class RegularisedProblem(SoftmaxProblem):
+    """The same data and model on the samples' features x / rms(x), of which a local step drops a share `p` before they are normed.  The masks come
+    from (seed, step, worker, sample): a run that is repeated or resumed (`step`) has the same ones."""
+
+    def __init__(self, problem, p=0.2, eps=1e-6, seed=0):
+        self.device, self.R, self.n, self.lam = problem.device, problem.R, problem.n, problem.lam
+        self.x, self.y = problem.x, problem.y
+        self.gen = torch.Generator(device=self.device).manual_seed(7 + seed)
+        self.p, self.eps, self.seed, self.step = p, eps, seed, 0
+
+    def features(self, x, **drop):
+        out = torch.empty_like(x)
+        B.rms_norm(x, out, eps=self.eps, **drop)
+        return out
+
+    def logits(self, w):
+        return self.features(self.x.reshape(self.n, -1)) @ w.view(N_CLASSES, -1).t()
+
+    def loss(self, w):
+        logprob = torch.empty(self.n, device=self.device)
+        B.token_logprobs(self.logits(w), self.y.reshape(-1), logprob=logprob)
+        return float(-logprob.double().mean() + 0.5 * self.lam * (w.double() ** 2).sum())
+
+    def minibatch_grads(self, w_local, b):
+        R, F = self.R, N_FEATURES + 1
+        idx = torch.randint(0, self.x.shape[1], (R, b), generator=self.gen, device=self.device)
+        xb = torch.gather(self.x, 1, idx.unsqueeze(-1).expand(R, b, F)).view(R * b, F)
+        yb = torch.gather(self.y, 1, idx).reshape(-1)
+        xb = self.features(xb, p=self.p, seed=self.seed, round=self.step).view(R, b, F)
+        self.step += 1
+        z = torch.bmm(xb, w_local.view(R, N_CLASSES, F).transpose(1, 2).contiguous()).view(R * b, N_CLASSES)
+        dz = torch.empty_like(z)
+        B.token_logprobs_backward(z, yb, dz, grad_logprob=torch.full((R * b,), -1.0 / b, device=self.device))
+        g = torch.bmm(dz.view(R, b, N_CLASSES).transpose(1, 2).contiguous(), xb)
+        return g.reshape(R, D) + self.lam * w_local
+
+
 @dataclasses.dataclass
 class Operator:
     k: int = 40
@@ -228,8 +266,8 @@ def main():
             ("SignTop_k, H=8", Operator(quantizer=B.SIGN_L1), 8)]
     print(f"{'scheme':34s} {'final loss':>10s} {'top-1 error':>11s} {'top-5':>7s} {'log2(bits)':>11s} {'identity err':>13s}")
 
-    def line(name, res, ident):
-        top1, top5 = prob.error(res["x"])
+    def line(name, res, ident, model=prob):
+        top1, top5 = model.error(res["x"])
         print(f"{name:34s} {res['loss'][-1]:10.4f} {top1:11.4f} {top5:7.4f} {math.log2(res['bits'][-1]):11.2f} {ident:>13s}")
 
     teacher = None
@@ -241,6 +279,9 @@ def main():
     line("SignTop_k, asynchronous, H<=4", run_async(prob, Operator(quantizer=B.SIGN_L1), H=4, T=800), "")
     res = run_sync(DistilledProblem(prob, teacher), Operator(quantizer=B.SIGN_L1), H=4, T=800)
     line("SignTop_k, H=4, taught by that one", res, f"{res['identity_err']:.2e}")
+    model = RegularisedProblem(prob)
+    res = run_sync(model, Operator(quantizer=B.SIGN_L1), H=4, T=800)
+    line("SignTop_k, H=4, normed, dropout 0.2", res, f"{res['identity_err']:.2e}", model)
 
 
 if __name__ == "__main__":
