@@ -364,7 +364,7 @@ enum { QSL_E4M3 = 3, QSL_I8 = 4 };      /* 8 bits: e4m3 without infinities (larg
  * T = floor((1 - p) 65536 + 1/2).  The mask is stored nowhere: the backward pass forms it again from the same numbers, and a part of a batch has
  * the masks that it has in the whole (row0).  This is the library's third stream of random words (see qsl_compress for the others). */
 typedef struct {
-  double p;                  /* share that is dropped, 0 <= p <= 1, taken to a multiple of 2^-16 by T            */
+  double p;                  /* share that is dropped, 0 <= p <= 1, taken to a multiple of 2^-16 by T; with 0 the rest is not looked at */
   uint64_t seed;
   uint64_t round;            /* < 2^62: the step, for instance                                                   */
   const uint64_t *round_at;  /* device, 8-byte aligned, or NULL: added to round when the kernel runs (a replayed graph then has another mask each
@@ -372,16 +372,20 @@ typedef struct {
   uint32_t row0;             /* number of the first row; row0 + rows <= 2^32                                     */
 } qsl_drop;
 
-/* Rows of a matrix: row n starts at element n * stride, stride >= cols; aligned to the type's size.  data = NULL: not there. */
+/* Rows of a matrix: row n starts at element n * stride, stride >= cols; aligned to the type's size.  data = NULL: not there (zeros, where it is
+ * read). */
 typedef struct { void *data; uint64_t stride; } qsl_rows;
 
-/* y = residual + drop(x).  The gradient in x is the same call on the gradient in y, without the residual; the residual's is that in y.
- *   rows, cols    < 2^31 each; dtype QSL_F32, QSL_BF16, QSL_F16 of all three
- *   x, y          there;  y may be x or the residual
- *   residual      may be absent (zeros), or NULL
- *   drop          NULL: p = 0 */
-qsl_status qsl_dropout(uint32_t rows, uint32_t cols, uint32_t dtype, const qsl_rows *x, const qsl_rows *residual, const qsl_drop *drop,
-                       const qsl_rows *y, void *hip_stream);
+/* y = residual + drop(x).  The gradient in x is the same call on the gradient in y, without the residual; the residual's is that in y. */
+typedef struct {
+  uint32_t rows, cols;       /* < 2^31 each, cols >= 1                                                           */
+  uint32_t dtype;            /* of all three: QSL_F32, QSL_BF16, QSL_F16                                         */
+  qsl_rows x;                /* there                                                                            */
+  qsl_rows residual;         /* may be absent                                                                    */
+  qsl_rows y;                /* there; may be x or the residual                                                  */
+  qsl_drop drop;
+} qsl_dropout_args;
+qsl_status qsl_dropout(const qsl_dropout_args *args, void *hip_stream);
 
 /* What is normed and how. */
 typedef struct {
@@ -393,19 +397,23 @@ typedef struct {
   float eps;                 /* 2^-100 .. 2^100                                                                  */
 } qsl_norm;
 
-/* The norm.
- *   x, residual, drop   as above;  x is there
- *   total    may be absent; receives residual + drop(x); may be x or the residual
- *   y        there; with out_dtype = norm->dtype it may be x or the residual
- *   out_dtype  norm->dtype, or QSL_E4M3 or QSL_I8: y then has 8-bit codes, which stand for code * scale, and `scales` is there
- *   group    8 bits: columns that share a scale, 32, 64 or 128 (a row's last group may be shorter), or 0 for the whole row
- *   scales   device, float [rows, ceil(cols / group)] ([rows] with group = 0), 4-byte aligned:
- *              scale = max(a, 2^-100) / Q,  a = max |y| of the group, Q = 448 (QSL_E4M3) or 127 (QSL_I8),  code = y * (Q / max(a, 2^-100))
- *            rounded to the nearest, ties to even.  A NaN or an infinity among a group's y makes its scale NaN and its codes 0.
+/* The norm.  With out_dtype QSL_E4M3 or QSL_I8 y has 8-bit codes, which stand for code * scale:
+ *     scale = max(a, 2^-100) / Q,  a = max |y| of the group, Q = 448 (QSL_E4M3) or 127 (QSL_I8),  code = y Q / max(a, 2^-100)
+ * rounded to the nearest, ties to even.  A NaN or an infinity among a group's y makes its scale NaN and its codes 0.
  * A NaN in a total makes its whole row NaN; an infinity makes the row's finite values 0 and itself NaN, as the formula says.  (Finite totals
  * whose squares do not fit are normed all the same.)  A row of zeros gives zeros. */
-qsl_status qsl_rms_norm(const qsl_norm *norm, const qsl_rows *x, const qsl_rows *residual, const qsl_drop *drop, const qsl_rows *total,
-                        const qsl_rows *y, uint32_t out_dtype, uint32_t group, float *scales, void *hip_stream);
+typedef struct {
+  qsl_norm norm;
+  qsl_rows x;                /* there                                                                            */
+  qsl_rows residual;         /* may be absent                                                                    */
+  qsl_rows total;            /* may be absent; receives residual + drop(x); may be x or the residual             */
+  qsl_rows y;                /* there; with out_dtype = norm.dtype it may be x or the residual                   */
+  qsl_drop drop;
+  uint32_t out_dtype;        /* norm.dtype, or QSL_E4M3 or QSL_I8                                                */
+  uint32_t group;            /* 8 bits: columns that share a scale, 32, 64 or 128 (a row's last group may be shorter), or 0 for the whole row */
+  float *scales;             /* 8 bits: device, [rows, ceil(cols / group)] ([rows] with group = 0), 4-byte aligned; else NULL */
+} qsl_rms_norm_args;
+qsl_status qsl_rms_norm(const qsl_rms_norm_args *args, void *hip_stream);
 
 /* Bytes of device memory that qsl_rms_norm_backward needs as `workspace` for dweight, a multiple of 256; 0 where it needs none (very few rows), and for
  * invalid arguments. */
@@ -414,16 +422,21 @@ size_t qsl_rms_norm_workspace_bytes(const qsl_norm *norm);
 /* The gradient of qsl_rms_norm (of y before any rounding to 8 bits), from the totals as they were stored: with r = 1 / sqrt(mean total^2 + eps),
  * u = r total, g = weight dy,
  *     dresidual = r (g - u mean_j(g_j u_j)) + dtotal,      dx = drop(dresidual),      dweight = sum over the rows of dy u
- *   total      there (x itself where nothing was added and nothing dropped)
- *   dy         there; the gradient in y, of norm->dtype
- *   dtotal     may be absent; what arrives at the total from elsewhere (the layers that the residual stream goes on to)
- *   dresidual  may be absent; may be total, dy or dtotal
- *   dx         may be absent; may be total, dy or dtotal, but not dresidual
- *   dweight    device, float [cols], or NULL: written, not added to; zeros for rows = 0.  One of the three has to be there
- *   workspace  device, at least qsl_rms_norm_workspace_bytes() bytes, 256-byte aligned; looked at only with dweight, and where that is not 0 */
-qsl_status qsl_rms_norm_backward(const qsl_norm *norm, const qsl_rows *total, const qsl_rows *dy, const qsl_rows *dtotal, const qsl_drop *drop,
-                                 const qsl_rows *dresidual, const qsl_rows *dx, float *dweight, void *workspace, size_t workspace_bytes,
-                                 void *hip_stream);
+ * dresidual, dx and dweight: one of the three has to be there. */
+typedef struct {
+  qsl_norm norm;
+  qsl_rows total;            /* there (x itself where nothing was added and nothing dropped)                     */
+  qsl_rows dy;               /* there; the gradient in y, of norm.dtype                                          */
+  qsl_rows dtotal;           /* may be absent; what arrives at the total from elsewhere (where the residual stream goes on to) */
+  qsl_rows dresidual;        /* may be absent; may be total, dy or dtotal                                        */
+  qsl_rows dx;               /* may be absent; may be total, dy or dtotal, but not dresidual                     */
+  qsl_drop drop;             /* the forward pass's                                                               */
+  float *dweight;            /* device, [cols], or NULL: written, not added to; zeros for rows = 0               */
+  void *workspace;           /* device, at least qsl_rms_norm_workspace_bytes() bytes, 256-byte aligned; looked at only with dweight, and where
+                                that is not 0                                                                    */
+  size_t workspace_bytes;
+} qsl_rms_norm_backward_args;
+qsl_status qsl_rms_norm_backward(const qsl_rms_norm_backward_args *args, void *hip_stream);
 
 const char *qsl_status_string(qsl_status st);
 

@@ -54,8 +54,12 @@ class _Teacher(C.Structure):
     _fields_ = [("index", C.c_void_p), ("value", C.c_void_p), ("lse", C.c_void_p), ("top", C.c_uint32), ("scale", C.c_float)]
 
 
-# qsl_rows, qsl_drop, qsl_norm as bytes in the machine's own layout, which are handed over as they are (structures of ctypes cost 0.5 us each)
-_ROWS, _DROP, _NORM = (struct.Struct(f).pack for f in ("@PQ", "@dQQPI4x", "@IIIIPf4x"))
+# The structures of the operators on a residual stream as bytes in the machine's own layout, handed over as they are (a call by ctypes costs
+# 0.06 us for each argument, a structure of ctypes 0.5)
+_NORM_FIELDS, _DROP_FIELDS = "IIIIPf4x", "dQQPI4x"
+_PACK_NORM, _PACK_DROPOUT, _PACK_RMS_NORM, _PACK_RMS_NORM_BACKWARD = (struct.Struct("@" + f).pack for f in (
+    _NORM_FIELDS, "III4x" + 3 * "PQ" + _DROP_FIELDS, _NORM_FIELDS + 4 * "PQ" + _DROP_FIELDS + "IIP", _NORM_FIELDS + 5 * "PQ" + _DROP_FIELDS + "PPN"))
+_ABSENT, _KEEP_ALL = (0, 0), (0.0, 0, 0, 0, 0)
 
 
 def _load():
@@ -89,11 +93,10 @@ def _load():
     lib.qsl_token_logprobs_backward.restype = C.c_int
     lib.qsl_distill.argtypes = [zp, tp, vp, vp, vp, sz, vp]; lib.qsl_distill.restype = C.c_int
     lib.qsl_distill_backward.argtypes = [zp, tp, vp, vp, vp, vp, u64, vp, sz, vp]; lib.qsl_distill_backward.restype = C.c_int
-    st = C.c_char_p                                     # a structure's bytes, or None
-    lib.qsl_dropout.argtypes = [u32, u32, u32, st, st, st, st, vp]; lib.qsl_dropout.restype = C.c_int
-    lib.qsl_rms_norm.argtypes = [st, st, st, st, st, st, u32, u32, vp, vp]; lib.qsl_rms_norm.restype = C.c_int
-    lib.qsl_rms_norm_workspace_bytes.argtypes = [st]; lib.qsl_rms_norm_workspace_bytes.restype = sz
-    lib.qsl_rms_norm_backward.argtypes = [st, st, st, st, st, st, st, vp, vp, sz, vp]; lib.qsl_rms_norm_backward.restype = C.c_int
+    for name in ("qsl_dropout", "qsl_rms_norm", "qsl_rms_norm_backward"):
+        fn = getattr(lib, name)
+        fn.argtypes = [C.c_char_p, vp]; fn.restype = C.c_int          # a structure's bytes, the stream
+    lib.qsl_rms_norm_workspace_bytes.argtypes = [C.c_char_p]; lib.qsl_rms_norm_workspace_bytes.restype = sz
     return lib
 
 
@@ -282,53 +285,60 @@ def distill_backward(logits, teacher_index, teacher_value, dlogits, scale=1.0, t
                entries=True)
 
 
-def _matrix(t, what, device, dtype, shape):
-    """A `qsl_rows` of a [rows, cols] tensor on `device` (its index) whose rows are contiguous and do not overlap."""
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
-        raise ValueError(f"{what}: expected a {dtype} tensor {list(shape)} on cuda:{device}, got {t.dtype} {list(t.shape)} on {t.device}")
-    if t.is_contiguous():
-        return _ROWS(t.data_ptr(), shape[1])
+def _row_stride(t, what):
+    """The row stride of a [rows, cols] tensor that is not contiguous, whose rows have to be, and not to overlap."""
+    rows, cols = t.shape
     stride, step = t.stride()
-    rows, cols = shape
     if (step != 1 and cols != 1) or (rows > 1 and stride < cols):
         raise ValueError(f"{what}: expected contiguous rows that do not overlap, got strides {t.stride()}")
-    return _ROWS(t.data_ptr(), stride if rows > 1 else cols)
+    return stride if rows > 1 else cols
 
 
-def _residual_shape(x, what):
-    """Device, type and shape of the call, by its first array."""
+def _leading(x, what):
+    """Device (its index), type and shape of a call, by its first array, and that array's address and row stride."""
     dtype, shape, device = x.dtype, x.shape, x.get_device()
     if len(shape) != 2 or device < 0 or dtype not in DTYPES:
         raise ValueError(f"{what}: expected a device tensor [rows, cols] of float32, bfloat16 or float16")
     if shape[0] >= SIZE_END or shape[1] >= SIZE_END:                      # (32 bits would keep the lower half)
         raise ValueError(f"{what}: expected less than 2^31 rows and columns, got {list(shape)}")
-    return device, dtype, shape
+    return device, dtype, shape, (x.data_ptr(), shape[1] if x.is_contiguous() else _row_stride(x, what))
+
+
+def _matrix(t, what, device, dtype, shape):
+    """Address and row stride of an array of the call; of None: absent."""
+    if t is None:
+        return _ABSENT
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{what}: expected a {dtype} tensor {list(shape)} on cuda:{device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr(), shape[1] if t.is_contiguous() else _row_stride(t, what)
 
 
 def _drop(p, seed, round, row0, round_at, device):
-    """A `qsl_drop`, for a p that is not 0."""
+    """The fields of a `qsl_drop`, for a p that is not 0."""
     if not (0 <= seed < 1 << 64 and 0 <= round < 1 << 62 and 0 <= row0 < 1 << 32):
         raise ValueError(f"expected a seed below 2^64, a round below 2^62 and a first row below 2^32, got {seed}, {round}, {row0}")
-    return _DROP(p, seed, round, 0 if round_at is None else _beside(round_at.view(-1), "round_at", device, torch.int64, (1,)), row0)
+    return p, seed, round, 0 if round_at is None else _beside(round_at.view(-1), "round_at", device, torch.int64, (1,)), row0
 
 
 def _norm(shape, dtype, weight, eps, device):
+    """The fields of a `qsl_norm`."""
     rows, cols = shape
     code = DTYPES[dtype]
     if weight is None:
-        return _NORM(rows, cols, code, code, 0, eps)
+        return rows, cols, code, code, 0, eps
     kind = weight.dtype
-    return _NORM(rows, cols, code, 0 if kind is torch.float32 else code,
-                 _beside(weight, "weight", device, kind if kind is torch.float32 else dtype, (cols,)), eps)
+    if kind is torch.float32:
+        return rows, cols, code, 0, _beside(weight, "weight", device, kind, (cols,)), eps
+    return rows, cols, code, code, _beside(weight, "weight", device, dtype, (cols,)), eps
 
 
-def _on_device(where, fn, device, *args):
-    """Calls fn(*args, stream) on the device and its current stream."""
+def _on_device(where, fn, device, args):
+    """Calls fn(args, stream) on the device and its current stream."""
     if device == _current_device():
-        st = fn(*args, _raw_stream(device))
+        st = fn(args, _raw_stream(device))
     else:
         with torch.cuda.device(device):
-            st = fn(*args, _raw_stream(device))
+            st = fn(args, _raw_stream(device))
     if st != OK:
         raise QslError(st, where)
 
@@ -337,56 +347,59 @@ def dropout(x, y, p, seed=0, round=0, row0=0, residual=None, round_at=None):
     """`qsl_dropout`: y = residual + drop(x) of x [rows, cols]; y may be x or the residual.  The gradient in x is the same call, with the same
     numbers, on the gradient in y, without the residual.  round_at: an int64 tensor of one value on the device, added to `round` when the
     kernel runs."""
-    dev, dtype, shape = _residual_shape(x, "x")
-    _on_device("qsl_dropout", _lib.qsl_dropout, dev, shape[0], shape[1], DTYPES[dtype], _matrix(x, "x", dev, dtype, shape),
-               None if residual is None else _matrix(residual, "residual", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev) if p else None,
-               _matrix(y, "y", dev, dtype, shape))
+    dev, dtype, shape, at = _leading(x, "x")
+    _on_device("qsl_dropout", _lib.qsl_dropout, dev, _PACK_DROPOUT(
+        *shape, DTYPES[dtype], *at, *_matrix(residual, "residual", dev, dtype, shape), *_matrix(y, "y", dev, dtype, shape),
+        *(_drop(p, seed, round, row0, round_at, dev) if p else _KEEP_ALL)))
 
 
 def rms_norm(x, y, weight=None, eps=1e-6, residual=None, total=None, p=0.0, seed=0, round=0, row0=0, round_at=None, scales=None, group=0):
     """`qsl_rms_norm`: total = residual + drop(x), y = weight * total / sqrt(mean(total^2) + eps).  y has x's type, or is float8_e4m3fn or int8: codes
     with `scales` [rows, number of groups], a group being `group` (32, 64, 128) columns, or 0 for the whole row."""
-    dev, dtype, shape = _residual_shape(x, "x")
-    kind = y.dtype if y.dtype in CODES else dtype
-    at = None
+    dev, dtype, shape, at = _leading(x, "x")
+    kind, scales_at = y.dtype, 0
+    if kind in CODES:
+        out = CODES[kind]
+    else:
+        kind, out = dtype, DTYPES[dtype]
     if scales is not None or group:
         if not 0 <= group < SIZE_END:
             raise ValueError(f"group: expected 0, 32, 64 or 128, got {group}")
-        at = None if scales is None else _beside(scales, "scales", dev, torch.float32, (shape[0], -(-shape[1] // group) if group else 1))
-    _on_device("qsl_rms_norm", _lib.qsl_rms_norm, dev, _norm(shape, dtype, weight, eps, dev), _matrix(x, "x", dev, dtype, shape),
-               None if residual is None else _matrix(residual, "residual", dev, dtype, shape), _drop(p, seed, round, row0, round_at, dev) if p else None,
-               None if total is None else _matrix(total, "total", dev, dtype, shape), _matrix(y, "y", dev, kind, shape),
-               CODES[kind] if kind in CODES else DTYPES[kind], group, at)
+        if scales is not None:
+            scales_at = _beside(scales, "scales", dev, torch.float32, (shape[0], -(-shape[1] // group) if group else 1))
+    _on_device("qsl_rms_norm", _lib.qsl_rms_norm, dev, _PACK_RMS_NORM(
+        *_norm(shape, dtype, weight, eps, dev), *at, *_matrix(residual, "residual", dev, dtype, shape), *_matrix(total, "total", dev, dtype, shape),
+        *_matrix(y, "y", dev, kind, shape), *(_drop(p, seed, round, row0, round_at, dev) if p else _KEEP_ALL), out, group, scales_at))
 
 
 def rms_norm_workspace_bytes(total):
     """`qsl_rms_norm_workspace_bytes` of these rows: what `workspace=` of `rms_norm_backward` has to hold for dweight (it is allocated if it
     is not given)."""
-    dev, dtype, shape = _residual_shape(total, "total")
-    return int(_lib.qsl_rms_norm_workspace_bytes(_norm(shape, dtype, None, 1.0, dev)))
+    dev, dtype, shape, _ = _leading(total, "total")
+    return int(_lib.qsl_rms_norm_workspace_bytes(_PACK_NORM(*_norm(shape, dtype, None, 1.0, dev))))
 
 
 def rms_norm_backward(total, dy, weight=None, eps=1e-6, dtotal=None, dresidual=None, dx=None, dweight=None, p=0.0, seed=0, round=0, row0=0,
                       round_at=None, workspace=None):
     """`qsl_rms_norm_backward`: from the totals, the gradient dy in y and what else arrives at the total (`dtotal`), those of the residual, of x
     and of the weight (float32), into the tensors that are given."""
-    dev, dtype, shape = _residual_shape(total, "total")
+    dev, dtype, shape, at = _leading(total, "total")
     norm = _norm(shape, dtype, weight, eps, dev)
-    dw, at, size = None, None, 0
+    dw, work, size = 0, 0, 0
     if dweight is not None:
         dw = _beside(dweight, "dweight", dev, torch.float32, (shape[1],))
         if workspace is None:
-            size = _lib.qsl_rms_norm_workspace_bytes(norm)
+            size = _lib.qsl_rms_norm_workspace_bytes(_PACK_NORM(*norm))
             if size:
                 workspace = torch.empty(size, dtype=torch.uint8, device=total.device)
-                at = workspace.data_ptr()
-    if workspace is not None and at is None:
+                work = workspace.data_ptr()
+    if workspace is not None and not work:
         size = workspace.numel()
-        at = _beside(workspace, "workspace", dev, torch.uint8, (size,))
-    _on_device("qsl_rms_norm_backward", _lib.qsl_rms_norm_backward, dev, norm, _matrix(total, "total", dev, dtype, shape),
-               _matrix(dy, "dy", dev, dtype, shape), None if dtotal is None else _matrix(dtotal, "dtotal", dev, dtype, shape),
-               _drop(p, seed, round, row0, round_at, dev) if p else None, None if dresidual is None else _matrix(dresidual, "dresidual", dev, dtype, shape),
-               None if dx is None else _matrix(dx, "dx", dev, dtype, shape), dw, at, size)
+        work = _beside(workspace, "workspace", dev, torch.uint8, (size,))
+    _on_device("qsl_rms_norm_backward", _lib.qsl_rms_norm_backward, dev, _PACK_RMS_NORM_BACKWARD(
+        *norm, *at, *_matrix(dy, "dy", dev, dtype, shape), *_matrix(dtotal, "dtotal", dev, dtype, shape),
+        *_matrix(dresidual, "dresidual", dev, dtype, shape), *_matrix(dx, "dx", dev, dtype, shape),
+        *(_drop(p, seed, round, row0, round_at, dev) if p else _KEEP_ALL), dw, work, size))
 
 
 class Qsl:

@@ -20,22 +20,19 @@ constexpr uint64_t GRID_X = 1u << 20;              // blocks in a row of the gri
 
 uint32_t elem_size(uint32_t dtype) { return dtype == QSL_F32 ? 4 : dtype <= QSL_F16 ? 2 : 1; }
 
-// A matrix of a call: what is there, at which stride.
-struct Matrix { void* data; uint64_t stride; };
-Matrix of(const qsl_rows* r) { return r ? Matrix{r->data, r->stride} : Matrix{nullptr, 0}; }
-bool matrix_ok(const Matrix& m, uint64_t rows, uint64_t cols, uint32_t dtype) {
+bool rows_ok(const qsl_rows& m, uint64_t rows, uint64_t cols, uint32_t dtype) {
   return !m.data || (stride_ok(rows, cols, m.stride) && aligned(m.data, elem_size(dtype)));
 }
-bool same(const Matrix& a, const Matrix& b, uint64_t rows) { return a.data == b.data && (a.stride == b.stride || rows == 1); }
+bool same(const qsl_rows& a, const qsl_rows& b, uint64_t rows) { return a.data == b.data && (a.stride == b.stride || rows == 1); }
 
-bool drop_ok(const qsl_drop* d, uint64_t rows) {
-  return !d || (d->p >= 0.0 && d->p <= 1.0 && d->round < 1ull << 62 && aligned(d->round_at, 8) && d->row0 + rows <= 1ull << 32);
+bool drop_ok(const qsl_drop& d, uint64_t rows) {
+  return d.p == 0.0 || (d.p > 0.0 && d.p <= 1.0 && d.round < 1ull << 62 && aligned(d.round_at, 8) && d.row0 + rows <= 1ull << 32);
 }
-Drop drop_of(const qsl_drop* d) {
-  if (!d) return Drop{KEEP_ALL, 1.0f, 0, 0, 0, 0, nullptr};
-  const uint32_t T = static_cast<uint32_t>(floor((1.0 - d->p) * 65536.0 + 0.5));
-  return Drop{T, T ? static_cast<float>(65536.0 / T) : 0.0f, d->row0, static_cast<uint32_t>(d->seed), static_cast<uint32_t>(d->seed >> 32), d->round, d->round_at};
+Drop drop_of(const qsl_drop& d) {
+  const uint32_t T = static_cast<uint32_t>(floor((1.0 - d.p) * 65536.0 + 0.5));
+  return Drop{T, T ? static_cast<float>(65536.0 / T) : 0.0f, d.row0, static_cast<uint32_t>(d.seed), static_cast<uint32_t>(d.seed >> 32), d.round, d.round_at};
 }
+Memory round_of(const qsl_drop& d) { return array(d.p > 0.0 ? d.round_at : nullptr, 8); }
 
 // f(the element type) as a type
 template <class F>
@@ -122,62 +119,70 @@ uint32_t back_blocks(const qsl_norm* n) {
   return blocks;
 }
 
+// Narrow sums by blocks of 16 columns, of which there are more; wide ones by 32, whole lines of the caches, which else two compute dies read.  us behind a
+// kernel that writes them, 16 / 32 columns: 768 blocks of 1,024 3.4 / 4.7, of 2,048 6.0 / 5.6, 512 of 4,096 7.1 / 5.7, 256 of 12,289 13.1 / 10.3
+void sum_parts(const float* part, uint32_t blocks, uint32_t cols, float* dweight, hipStream_t stream) {
+  if (cols <= 1024) k_sum_parts<16, 64><<<(cols + 15) / 16, 1024, 0, stream>>>(part, blocks, cols, dweight);
+  else k_sum_parts<32, 32><<<(cols + 31) / 32, 1024, 0, stream>>>(part, blocks, cols, dweight);
+}
+
 qsl_status launched() { return hipGetLastError() == hipSuccess ? QSL_OK : QSL_ERR_DEVICE; }
 
 }  // namespace
 
-extern "C" qsl_status qsl_dropout(uint32_t rows, uint32_t cols, uint32_t dtype, const qsl_rows* x, const qsl_rows* residual,
-                                  const qsl_drop* drop, const qsl_rows* y, void* hip_stream) {
-  const Matrix mx = of(x), mr = of(residual), my = of(y);
-  if (dtype > QSL_F16 || rows >= 1u << 31 || cols == 0 || cols >= 1u << 31 || !drop_ok(drop, rows)) return QSL_ERR_INVALID_ARG;
+extern "C" qsl_status qsl_dropout(const qsl_dropout_args* args, void* hip_stream) {
+  if (!args) return QSL_ERR_INVALID_ARG;
+  const qsl_rows &x = args->x, &res = args->residual, &y = args->y;
+  const uint64_t rows = args->rows, cols = args->cols, es = elem_size(args->dtype);
+  if (args->dtype > QSL_F16 || rows >= 1u << 31 || cols == 0 || cols >= 1u << 31 || !drop_ok(args->drop, rows)) return QSL_ERR_INVALID_ARG;
   if (rows == 0) return QSL_OK;
-  if (!mx.data || !my.data) return QSL_ERR_INVALID_ARG;
-  for (const Matrix& m : {mx, mr, my}) if (!matrix_ok(m, rows, cols, dtype)) return QSL_ERR_INVALID_ARG;
-  const uint64_t es = elem_size(dtype);
-  auto at = [&](const Matrix& m) { return rows_at(m.data, rows, cols, m.stride, es); };
-  for (const Matrix& m : {mx, mr}) if (m.data && !same(m, my, rows) && meet(at(m), at(my))) return QSL_ERR_INVALID_ARG;
-  if (drop && meet(array(drop->round_at, 8), at(my))) return QSL_ERR_INVALID_ARG;
-  const uint32_t units = (cols + 7) / 8;
-  const DropArgs a = {mx.data, mr.data, my.data, mx.stride, mr.stride, my.stride, rows, cols, units, drop_of(drop)};
-  const uint64_t blocks = (static_cast<uint64_t>(rows) * units + DROP_THREADS - 1) / DROP_THREADS;
-  pick_type(dtype, [&](auto e) {
+  if (!x.data || !y.data) return QSL_ERR_INVALID_ARG;
+  for (const qsl_rows* m : {&x, &res, &y}) if (!rows_ok(*m, rows, cols, args->dtype)) return QSL_ERR_INVALID_ARG;
+  auto at = [&](const qsl_rows& m) { return rows_at(m.data, rows, cols, m.stride, es); };
+  for (const qsl_rows* m : {&x, &res}) if (m->data && !same(*m, y, rows) && meet(at(*m), at(y))) return QSL_ERR_INVALID_ARG;
+  if (meet(round_of(args->drop), at(y))) return QSL_ERR_INVALID_ARG;
+  const uint32_t units = static_cast<uint32_t>((cols + 7) / 8);
+  const DropArgs a = {x.data, res.data, y.data, x.stride, res.stride, y.stride, rows, args->cols, units, drop_of(args->drop)};
+  const uint64_t blocks = (rows * units + DROP_THREADS - 1) / DROP_THREADS;
+  pick_type(args->dtype, [&](auto e) {
     typedef decltype(e) E;
-    pick_past<E>(rows * (cols * es), [&](auto past) { k_dropout<E, past()><<<grid_of(blocks), DROP_THREADS, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+    pick_past<E>(rows * cols * es, [&](auto past) { k_dropout<E, past()><<<grid_of(blocks), DROP_THREADS, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
   });
   return launched();
 }
 
-extern "C" qsl_status qsl_rms_norm(const qsl_norm* norm, const qsl_rows* x, const qsl_rows* residual, const qsl_drop* drop,
-                                   const qsl_rows* total, const qsl_rows* y, uint32_t out_dtype, uint32_t group, float* scales,
-                                   void* hip_stream) {
-  if (!norm_ok(norm)) return QSL_ERR_INVALID_ARG;
+extern "C" qsl_status qsl_rms_norm(const qsl_rms_norm_args* args, void* hip_stream) {
+  if (!args || !norm_ok(&args->norm)) return QSL_ERR_INVALID_ARG;
+  const qsl_norm* norm = &args->norm;
+  const qsl_rows &x = args->x, &res = args->residual, &total = args->total, &y = args->y;
   const uint64_t rows = norm->rows, cols = norm->cols, es = elem_size(norm->dtype);
+  const uint32_t out_dtype = args->out_dtype, group = args->group;
   const bool bits8 = out_dtype == QSL_E4M3 || out_dtype == QSL_I8;
-  if (!drop_ok(drop, rows) || (!bits8 && out_dtype != norm->dtype)) return QSL_ERR_INVALID_ARG;
-  if (bits8 ? group != 0 && group != 32 && group != 64 && group != 128 : group != 0 || scales) return QSL_ERR_INVALID_ARG;
+  if (!drop_ok(args->drop, rows) || (!bits8 && out_dtype != norm->dtype)) return QSL_ERR_INVALID_ARG;
+  if (bits8 ? group != 0 && group != 32 && group != 64 && group != 128 : group != 0 || args->scales) return QSL_ERR_INVALID_ARG;
   if (rows == 0) return QSL_OK;
-  const Matrix mx = of(x), mr = of(residual), mt = of(total), my = of(y);
-  if (!mx.data || !my.data || (bits8 && (!scales || !aligned(scales, 4)))) return QSL_ERR_INVALID_ARG;
-  for (const Matrix& m : {mx, mr, mt}) if (!matrix_ok(m, rows, cols, norm->dtype)) return QSL_ERR_INVALID_ARG;
-  if (!matrix_ok(my, rows, cols, out_dtype)) return QSL_ERR_INVALID_ARG;
-  auto at = [&](const Matrix& m, uint64_t size) { return rows_at(m.data, rows, cols, m.stride, size); };
-  const Memory out_t = at(mt, es), out_y = at(my, elem_size(out_dtype)), out_s = array(scales, 4 * rows * (group ? (cols + group - 1) / group : 1));
-  if (!apart({out_t, out_y, out_s}, {weight_of(norm), array(drop ? drop->round_at : nullptr, 8)})) return QSL_ERR_INVALID_ARG;
-  for (const Matrix& m : {mx, mr}) {      // a thread reads x and the residual where it writes the total and y, all of the row before any of it
-    if (!m.data) continue;
-    if (!same(m, mt, rows) && meet(at(m, es), out_t)) return QSL_ERR_INVALID_ARG;
-    if ((bits8 || !same(m, my, rows)) && meet(at(m, es), out_y)) return QSL_ERR_INVALID_ARG;
-    if (meet(at(m, es), out_s)) return QSL_ERR_INVALID_ARG;
+  if (!x.data || !y.data || (bits8 && (!args->scales || !aligned(args->scales, 4)))) return QSL_ERR_INVALID_ARG;
+  for (const qsl_rows* m : {&x, &res, &total}) if (!rows_ok(*m, rows, cols, norm->dtype)) return QSL_ERR_INVALID_ARG;
+  if (!rows_ok(y, rows, cols, out_dtype)) return QSL_ERR_INVALID_ARG;
+  auto at = [&](const qsl_rows& m, uint64_t size) { return rows_at(m.data, rows, cols, m.stride, size); };
+  const Memory out_t = at(total, es), out_y = at(y, elem_size(out_dtype)), out_s = array(args->scales, 4 * rows * (group ? (cols + group - 1) / group : 1));
+  if (!apart({out_t, out_y, out_s}, {weight_of(norm), round_of(args->drop)})) return QSL_ERR_INVALID_ARG;
+  for (const qsl_rows* m : {&x, &res}) {      // a thread reads x and the residual where it writes the total and y, all of the row before any of it
+    if (!m->data) continue;
+    const Memory in = at(*m, es);
+    if (!same(*m, total, rows) && meet(in, out_t)) return QSL_ERR_INVALID_ARG;
+    if ((bits8 || !same(*m, y, rows)) && meet(in, out_y)) return QSL_ERR_INVALID_ARG;
+    if (meet(in, out_s)) return QSL_ERR_INVALID_ARG;
   }
-  const NormArgs a = {mx.data, mr.data, norm->weight, mt.data, my.data, scales, mx.stride, mr.stride, mt.stride, my.stride, rows, norm->cols,
-                      norm->weight_dtype == QSL_F32, out_dtype == QSL_E4M3, group, norm->eps, drop_of(drop)};
+  const NormArgs a = {x.data, res.data, norm->weight, total.data, y.data, args->scales, x.stride, res.stride, total.stride, y.stride, rows, norm->cols,
+                      norm->weight_dtype == QSL_F32, out_dtype == QSL_E4M3, group ? 31u - __builtin_clz(group) : 0u, norm->eps, drop_of(args->drop)};
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   pick_type(norm->dtype, [&](auto e) {
     typedef decltype(e) E;
     pick_row<E>(norm->cols, [&](auto l, auto u) {
       constexpr int th = THREADS<l()>, per = th / l();
       const dim3 grid = grid_of((rows + per - 1) / per);
-      pick_past<E>(rows * cols * ((mt.data ? es : 0) + elem_size(out_dtype)), [&](auto past) {
+      pick_past<E>(rows * cols * ((total.data ? es : 0) + elem_size(out_dtype)), [&](auto past) {
         if (bits8) k_rms_norm<E, l(), u(), true, past()><<<grid, th, 0, stream>>>(a);
         else k_rms_norm<E, l(), u(), false, past()><<<grid, th, 0, stream>>>(a);
       });
@@ -191,40 +196,40 @@ extern "C" size_t qsl_rms_norm_workspace_bytes(const qsl_norm* norm) {
   return blocks > 1 ? align_up(4 * blocks * norm->cols, 256) : 0;
 }
 
-extern "C" qsl_status qsl_rms_norm_backward(const qsl_norm* norm, const qsl_rows* total, const qsl_rows* dy, const qsl_rows* dtotal,
-                                            const qsl_drop* drop, const qsl_rows* dresidual, const qsl_rows* dx, float* dweight,
-                                            void* workspace, size_t workspace_bytes, void* hip_stream) {
-  if (!norm_ok(norm) || !drop_ok(drop, norm->rows) || !aligned(dweight, 4)) return QSL_ERR_INVALID_ARG;
+extern "C" qsl_status qsl_rms_norm_backward(const qsl_rms_norm_backward_args* args, void* hip_stream) {
+  if (!args || !norm_ok(&args->norm) || !drop_ok(args->drop, args->norm.rows) || !aligned(args->dweight, 4)) return QSL_ERR_INVALID_ARG;
+  const qsl_norm* norm = &args->norm;
+  const qsl_rows &total = args->total, &dy = args->dy, &dtotal = args->dtotal, &dres = args->dresidual, &dx = args->dx;
   const uint64_t rows = norm->rows, cols = norm->cols, es = elem_size(norm->dtype);
-  const Matrix mt = of(total), my = of(dy), md = of(dtotal), mr = of(dresidual), mx = of(dx);
+  float* const dweight = args->dweight;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const uint32_t blocks = back_blocks(norm);
   const bool parts_apart = dweight && blocks > 1;
   if (rows != 0) {
-    if (!mt.data || !my.data || (!mr.data && !mx.data && !dweight)) return QSL_ERR_INVALID_ARG;
-    for (const Matrix& m : {mt, my, md, mr, mx}) if (!matrix_ok(m, rows, cols, norm->dtype)) return QSL_ERR_INVALID_ARG;
-    if (parts_apart && (!workspace || !aligned(workspace, 256))) return QSL_ERR_INVALID_ARG;
-    if (parts_apart && workspace_bytes < qsl_rms_norm_workspace_bytes(norm)) return QSL_ERR_BUFFER_TOO_SMALL;
-    auto at = [&](const Matrix& m) { return rows_at(m.data, rows, cols, m.stride, es); };
-    const Memory dw = array(dweight, 4 * cols), parts = array(workspace, parts_apart ? 4 * blocks * cols : 0);
-    if (!apart({at(mr), at(mx), dw, parts}, {weight_of(norm), array(drop ? drop->round_at : nullptr, 8)})) return QSL_ERR_INVALID_ARG;
-    for (const Matrix& m : {mt, my, md}) {
-      if (!m.data) continue;
-      for (const Matrix& o : {mr, mx}) if (o.data && !same(m, o, rows) && meet(at(m), at(o))) return QSL_ERR_INVALID_ARG;
-      if (meet(at(m), dw) || meet(at(m), parts)) return QSL_ERR_INVALID_ARG;
+    if (!total.data || !dy.data || (!dres.data && !dx.data && !dweight)) return QSL_ERR_INVALID_ARG;
+    for (const qsl_rows* m : {&total, &dy, &dtotal, &dres, &dx}) if (!rows_ok(*m, rows, cols, norm->dtype)) return QSL_ERR_INVALID_ARG;
+    if (parts_apart && (!args->workspace || !aligned(args->workspace, 256))) return QSL_ERR_INVALID_ARG;
+    if (parts_apart && args->workspace_bytes < qsl_rms_norm_workspace_bytes(norm)) return QSL_ERR_BUFFER_TOO_SMALL;
+    auto at = [&](const qsl_rows& m) { return rows_at(m.data, rows, cols, m.stride, es); };
+    const Memory dw = array(dweight, 4 * cols), parts = array(args->workspace, parts_apart ? 4 * blocks * cols : 0);
+    if (!apart({at(dres), at(dx), dw, parts}, {weight_of(norm), round_of(args->drop)})) return QSL_ERR_INVALID_ARG;
+    for (const qsl_rows* m : {&total, &dy, &dtotal}) {
+      if (!m->data) continue;
+      for (const qsl_rows* o : {&dres, &dx}) if (o->data && !same(*m, *o, rows) && meet(at(*m), at(*o))) return QSL_ERR_INVALID_ARG;
+      if (meet(at(*m), dw) || meet(at(*m), parts)) return QSL_ERR_INVALID_ARG;
     }
-    const BackArgs a = {mt.data, my.data, md.data, norm->weight, mr.data, mx.data, parts_apart ? static_cast<float*>(workspace) : dweight, mt.stride,
-                        my.stride, md.stride, mr.stride, mx.stride, rows, norm->cols, norm->weight_dtype == QSL_F32, norm->eps, drop_of(drop)};
+    const BackArgs a = {total.data, dy.data, dtotal.data, norm->weight, dres.data, dx.data, parts_apart ? static_cast<float*>(args->workspace) : dweight,
+                        total.stride, dy.stride, dtotal.stride, dres.stride, dx.stride, rows, norm->cols, norm->weight_dtype == QSL_F32, norm->eps,
+                        drop_of(args->drop)};
     pick_type(norm->dtype, [&](auto e) {
       typedef decltype(e) E;
       pick_row_back(norm->cols, [&](auto l, auto u) {
-        pick_past<E>(rows * cols * es * ((mr.data != nullptr) + (mx.data != nullptr)), [&](auto past) {
+        pick_past<E>(rows * cols * es * ((dres.data != nullptr) + (dx.data != nullptr)), [&](auto past) {
           k_rms_norm_backward<E, l(), u(), past()><<<blocks, THREADS<l()>, 0, stream>>>(a);
         });
       });
     });
   }
-  if (parts_apart || (dweight && rows == 0))
-    k_sum_parts<<<(norm->cols + SUM_COLS - 1) / SUM_COLS, SUM_COLS * SUM_PARTS, 0, stream>>>(static_cast<const float*>(workspace), blocks, norm->cols, dweight);
+  if (parts_apart || (dweight && rows == 0)) sum_parts(static_cast<const float*>(args->workspace), blocks, norm->cols, dweight, stream);
   return rows || dweight ? launched() : QSL_OK;
 }

@@ -28,17 +28,30 @@ class Norm(C.Structure):
                 ("eps", C.c_float)]
 
 
+class DropoutArgs(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("cols", C.c_uint32), ("dtype", C.c_uint32), ("x", Rows), ("residual", Rows), ("y", Rows), ("drop", Drop)]
+
+
+class NormArgs(C.Structure):
+    _fields_ = [("norm", Norm), ("x", Rows), ("residual", Rows), ("total", Rows), ("y", Rows), ("drop", Drop), ("out_dtype", C.c_uint32), ("group", C.c_uint32),
+                ("scales", C.c_void_p)]
+
+
+class BackArgs(C.Structure):
+    _fields_ = [("norm", Norm), ("total", Rows), ("dy", Rows), ("dtotal", Rows), ("dresidual", Rows), ("dx", Rows), ("drop", Drop), ("dweight", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 @pytest.fixture(scope="module")
 def lib():
     if not os.path.exists(LIB_PATH):
         from paper_1906_02367_amd import build
         build.build()
     l = C.CDLL(LIB_PATH)
-    vp, u32, sz, rp = C.c_void_p, C.c_uint32, C.c_size_t, C.POINTER(Rows)
-    l.qsl_dropout.argtypes = [u32, u32, u32, rp, rp, C.POINTER(Drop), rp, vp]
-    l.qsl_rms_norm.argtypes = [C.POINTER(Norm), rp, rp, C.POINTER(Drop), rp, rp, u32, u32, vp, vp]
-    l.qsl_rms_norm_workspace_bytes.argtypes = [C.POINTER(Norm)]; l.qsl_rms_norm_workspace_bytes.restype = sz
-    l.qsl_rms_norm_backward.argtypes = [C.POINTER(Norm), rp, rp, rp, C.POINTER(Drop), rp, rp, vp, vp, sz, vp]
+    l.qsl_dropout.argtypes = [C.POINTER(DropoutArgs), C.c_void_p]
+    l.qsl_rms_norm.argtypes = [C.POINTER(NormArgs), C.c_void_p]
+    l.qsl_rms_norm_workspace_bytes.argtypes = [C.POINTER(Norm)]; l.qsl_rms_norm_workspace_bytes.restype = C.c_size_t
+    l.qsl_rms_norm_backward.argtypes = [C.POINTER(BackArgs), C.c_void_p]
     return l
 
 
@@ -49,36 +62,33 @@ def at(k):                                       # addresses that are never look
     return (1 << 40) + k * (1 << 24)
 
 
-def rows(a, stride=PITCH):
-    return None if a is None else C.byref(Rows(a, stride))
-
-
 def a_drop(**kw):
     d = dict(p=0.1, seed=1, round=2, round_at=None, row0=0)
     d.update(kw)
-    return C.byref(Drop(**d))
+    return Drop(**d)
 
 
 def a_norm(**kw):
     d = dict(rows=N, cols=W, dtype=0, weight_dtype=0, weight=at(50), eps=1e-5)
     d.update(kw)
-    return C.byref(Norm(**d))
+    return Norm(**d)
 
 
 def drop_call(lib, n=N, cols=W, dtype=0, x=at(1), res=at(2), drop=None, y=at(3), **st):
     s = lambda k: st.get("s" + k, PITCH)
-    return lib.qsl_dropout(n, cols, dtype, rows(x, s("x")), rows(res, s("res")), drop or a_drop(), rows(y, s("y")), None)
+    return lib.qsl_dropout(C.byref(DropoutArgs(n, cols, dtype, Rows(x, s("x")), Rows(res, s("res")), Rows(y, s("y")), drop or a_drop())), None)
 
 
 def norm_call(lib, norm=None, x=at(1), res=at(2), drop=None, total=at(3), y=at(4), out=0, group=0, scales=None, **st):
     s = lambda k: st.get("s" + k, PITCH)
-    return lib.qsl_rms_norm(norm or a_norm(), rows(x, s("x")), rows(res, s("res")), drop or a_drop(), rows(total, s("total")), rows(y, s("y")), out, group, scales, None)
+    return lib.qsl_rms_norm(C.byref(NormArgs(norm or a_norm(), Rows(x, s("x")), Rows(res, s("res")), Rows(total, s("total")), Rows(y, s("y")), drop or a_drop(), out, group, scales)),
+                            None)
 
 
 def back_call(lib, norm=None, total=at(1), dy=at(2), dtotal=at(3), drop=None, dres=at(4), dx=at(5), dw=at(6), ws=at(7), n=1 << 20, **st):
     s = lambda k: st.get("s" + k, PITCH)
-    return lib.qsl_rms_norm_backward(norm or a_norm(), rows(total, s("total")), rows(dy, s("dy")), rows(dtotal, s("dtotal")), drop or a_drop(), rows(dres, s("dres")),
-                                     rows(dx, s("dx")), dw, ws, n, None)
+    return lib.qsl_rms_norm_backward(C.byref(BackArgs(norm or a_norm(), Rows(total, s("total")), Rows(dy, s("dy")), Rows(dtotal, s("dtotal")), Rows(dres, s("dres")), Rows(dx, s("dx")),
+                                                      drop or a_drop(), dw, ws, n)), None)
 
 
 def test_the_words_are_those_of_the_known_answers():
@@ -109,7 +119,7 @@ def test_the_gradient_of_the_definition():
 
 
 def test_drops_that_are_refused(lib):
-    for kw in (dict(p=-0.1), dict(p=1.0001), dict(p=float("nan")), dict(p=float("inf")), dict(round=1 << 62), dict(round_at=at(9) + 4), dict(row0=2 ** 32 - N + 1)):
+    for kw in (dict(p=-0.1), dict(p=-1e-300), dict(p=1.0001), dict(p=float("nan")), dict(p=float("inf")), dict(round=1 << 62), dict(round_at=at(9) + 4), dict(row0=2 ** 32 - N + 1)):
         d = a_drop(**kw)
         assert drop_call(lib, drop=d) == INVALID and norm_call(lib, drop=d) == INVALID and back_call(lib, drop=d) == INVALID, kw
 
@@ -118,7 +128,7 @@ def test_dropout_arguments_that_are_refused(lib):
     for kw in (dict(x=None), dict(y=None), dict(dtype=3), dict(dtype=4), dict(n=1 << 31), dict(cols=0), dict(cols=1 << 31, sx=1 << 32, sres=1 << 32, sy=1 << 32), dict(x=at(1) + 2),
                dict(res=at(2) + 1), dict(y=at(3) + 2), dict(x=at(1) + 1, dtype=1), dict(sx=999), dict(sy=999), dict(sres=0), dict(sx=1 << 48)):
         assert drop_call(lib, **kw) == INVALID, kw
-    assert lib.qsl_dropout(N, W, 0, None, None, None, rows(at(3)), None) == INVALID
+    assert lib.qsl_dropout(None, None) == INVALID and lib.qsl_rms_norm(None, None) == INVALID and lib.qsl_rms_norm_backward(None, None) == INVALID
     # y over a part of x or of the residual, or over them with another stride, or over the round
     for kw in (dict(y=at(1) + 4), dict(y=at(2) - 4 * PITCH), dict(y=at(1), sy=PITCH + 1), dict(y=at(2), sy=PITCH - 1), dict(drop=a_drop(round_at=at(3) + 4 * PITCH + 8))):
         assert drop_call(lib, **kw) == INVALID, kw
@@ -136,7 +146,7 @@ def test_norms_that_are_refused(lib, kw):
     assert norm_call(lib, norm=n, **wide) == INVALID
     assert back_call(lib, norm=n, n=1 << 40, stotal=1 << 16, sdy=1 << 16, sdtotal=1 << 16, sdres=1 << 16, sdx=1 << 16) == INVALID
     assert lib.qsl_rms_norm_workspace_bytes(n) == 0
-    assert lib.qsl_rms_norm_workspace_bytes(None) == 0 and lib.qsl_rms_norm(None, rows(at(1)), None, None, None, rows(at(2)), 0, 0, None, None) == INVALID
+    assert lib.qsl_rms_norm_workspace_bytes(None) == 0
 
 
 def test_norm_arguments_that_are_refused(lib):
@@ -182,6 +192,21 @@ def test_gradient_arrays_that_share_memory(lib):
 
 
 # ---- the binding ---------------------------------------------------------------------------------------------------------------
+def test_the_bindings_structures_have_the_headers_layout(B):
+    """What the binding packs, read back field by field by ctypes."""
+    norm, drop = (3, 5, 1, 0, 1 << 40, 0.25), (0.5, 7, 9, 1 << 41, 11)
+    m = [(k << 20, 100 + k) for k in range(1, 6)]
+    flat = [v for pair in m for v in pair]
+
+    def fields(s):
+        return [x for f, _ in s._fields_ for x in (fields(getattr(s, f)) if isinstance(getattr(s, f), C.Structure) else [getattr(s, f)])]
+
+    for cls, pack, values in ((Norm, B._PACK_NORM, [*norm]), (DropoutArgs, B._PACK_DROPOUT, [3, 5, 1, *flat[:6], *drop]), (NormArgs, B._PACK_RMS_NORM, [*norm, *flat[:8], *drop, 3, 64, 1 << 42]),
+                              (BackArgs, B._PACK_RMS_NORM_BACKWARD, [*norm, *flat, *drop, 1 << 43, 1 << 44, 1 << 33])):
+        raw = pack(*values)
+        assert len(raw) == C.sizeof(cls) and fields(cls.from_buffer_copy(raw)) == values, cls
+
+
 @pytest.fixture(scope="module")
 def B():
     from paper_1906_02367_amd import binding
