@@ -497,15 +497,17 @@ struct BackArgs {
   Drop drop;
 };
 
-// A block goes through rows that lie a grid apart and keeps its sum for dw in registers.
-// Where 1024 threads leave a thread 128 registers, the weights are held in LDS, every thread's own; where that is not enough, what else arrives at
-// the totals is loaded where it is added.
+// A block goes through rows that lie a grid apart and keeps its sum for dw in registers.  A unit's registers take the next row's as soon as this row's is
+// unpacked for its results, so that these loads are under way beside the masks and the stores and few waves are enough (us, bf16, loads at a row's
+// beginning / ahead: 16,384 rows of 4,096 128.8 / 120.7, of 2,048 70 / 65, 2,047 rows of 12,288 58.8 / 56.3).
+// Where 1024 threads leave a thread 128 registers, the weights are held in LDS, every thread's own; where that is not enough (TIGHT), nothing is loaded
+// ahead, and what else arrives at the totals is loaded where it is added (fp32, 2,047 rows of 12,288: ahead 118, not 107, without either 120).
 template <int L, int U> constexpr bool WEIGHT_IN_LDS = L * U >= 2048;
-template <class E, int L, int U> constexpr bool LATE_DTOTAL = L * U * sizeof(E) >= 8192;
+template <class E, int L, int U> constexpr bool TIGHT_ROW = L * U * sizeof(E) >= 8192;
 template <class E, int L, int U, bool PAST>
 __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   constexpr int ROWS = THREADS<L> / L;
-  constexpr bool LDS = WEIGHT_IN_LDS<L, U>, LATE = LATE_DTOTAL<E, L, U>;
+  constexpr bool LDS = WEIGHT_IN_LDS<L, U>, TIGHT = TIGHT_ROW<E, L, U>;
   typedef float quad __attribute__((ext_vector_type(4)));
   __shared__ quad weights[LDS ? 2 * U : 1][LDS ? L : 1];
   __shared__ Two sums[2][2][WAVES<L>];
@@ -534,21 +536,32 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   };
 #pragma unroll
   for (int i = 0; i < 8 * U; ++i) dw[i] = 0.0f;
-  uint32_t turn = 0;             // a row's sums go where those before last stood: there is a barrier between reading these and writing them
-  for (uint64_t base = static_cast<uint64_t>(blockIdx.x) * ROWS; base < a.rows; base += static_cast<uint64_t>(gridDim.x) * ROWS) {
-    const uint64_t row = base + row_in_block<L>();
+  Unit<E> hq[U], dyq[U], dtq[TIGHT ? 1 : U];
+  auto load_unit = [&](uint64_t row, int u) {
+    const uint32_t c = c0 + u * L * 8;
     const bool live = row < a.rows;
-    const uint32_t end = live ? a.cols : 0;
-    const E* dt_row = a.dtotal ? static_cast<const E*>(a.dtotal) + row * a.dtotal_stride : nullptr;
-    Unit<E> hq[U], dyq[U], dtq[LATE ? 1 : U];
-    load_units<E, U, TINY<L>, PAST>(static_cast<const E*>(a.total) + row * a.total_stride, c0, L * 8, a.cols, live, hq);
-    load_units<E, U, TINY<L>, PAST>(static_cast<const E*>(a.dy) + row * a.dy_stride, c0, L * 8, a.cols, live, dyq);
-    if constexpr (!LATE)
-      if (dt_row) load_units<E, U, TINY<L>, PAST>(dt_row, c0, L * 8, a.cols, live, dtq);
+    load_units<E, 1, TINY<L>, PAST>(static_cast<const E*>(a.total) + row * a.total_stride, c, 0, a.cols, live, hq + u);
+    load_units<E, 1, TINY<L>, PAST>(static_cast<const E*>(a.dy) + row * a.dy_stride, c, 0, a.cols, live, dyq + u);
+    if constexpr (!TIGHT)
+      if (a.dtotal) load_units<E, 1, TINY<L>, PAST>(static_cast<const E*>(a.dtotal) + row * a.dtotal_stride, c, 0, a.cols, live, dtq + u);
+  };
+  const uint64_t step = static_cast<uint64_t>(gridDim.x) * ROWS;
+  uint64_t row = static_cast<uint64_t>(blockIdx.x) * ROWS + row_in_block<L>();
+  if constexpr (!TIGHT) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_unit(row, u);
+  }
+  uint32_t turn = 0;             // a row's sums go where those before last stood: there is a barrier between reading these and writing them
+  for (uint64_t base = static_cast<uint64_t>(blockIdx.x) * ROWS; base < a.rows; base += step, row += step) {
+    const uint32_t end = row < a.rows ? a.cols : 0;
+    if constexpr (TIGHT) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_unit(row, u);
+    }
     cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, hq);
     cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, dyq);
-    if constexpr (!LATE)
-      if (dt_row) cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, dtq);
+    if constexpr (!TIGHT)
+      if (a.dtotal) cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, dtq);
     auto sum = [&]() {
       Two s = {0.0f, 0.0f};
 #pragma unroll
@@ -591,19 +604,20 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
       unpack(hq[u], h);
       unpack(dyq[u], d);
       weight_of(u, w);
-      if (dt_row) {
-        if constexpr (LATE) {
-          load_units<E, 1, false, PAST>(dt_row, c0 + u * L * 8, 0, a.cols, live, dtq);
+      if (a.dtotal) {
+        if constexpr (TIGHT) {
+          load_units<E, 1, false, PAST>(static_cast<const E*>(a.dtotal) + row * a.dtotal_stride, c0 + u * L * 8, 0, a.cols, end != 0, dtq);
           cut_units<E, 1, false>(c0 + u * L * 8, 0, a.cols, dtq);
         }
-        unpack(dtq[LATE ? 0 : u], t);
+        unpack(dtq[TIGHT ? 0 : u], t);
       }
+      if constexpr (!TIGHT) load_unit(row + step, u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float un = h[i] * r;
         dw[8 * u + i] = __builtin_fmaf(d[i], un, dw[8 * u + i]);
         d[i] = rf * (d[i] * w[i] - un * mean);
-        if (dt_row) d[i] += t[i];
+        if (a.dtotal) d[i] += t[i];
       }
       if (a.dres) store_unit<PAST>(static_cast<E*>(a.dres) + row * a.dres_stride, c0 + u * L * 8, end, d);
       if (a.dx) {

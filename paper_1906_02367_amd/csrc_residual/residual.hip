@@ -77,14 +77,14 @@ void pick_row(uint32_t cols, F&& f) {
     else f(Int<1024>(), Int<1>());
   }
 }
-// The gradient's, which holds three arrays and the sum for dweight.  us with all of them, a mask and k_sum_parts, bf16 / fp32, by blocks for a compute unit (of 256
-// threads 2, 3, 4; of 512 1, 2; of 1,024 1):
-//   32,768 rows of 512     64 x 1 38, 37, 39 / 67, 69, 70
-//   30,000 rows of 785     64 x 2 68, 56, 71 / 97, 100, 116
-//   16,384 rows of 2,048   256 x 1 72, 71, 71 / 126, 131, 135;  128 x 2 (bf16) 74, 72, 78
-//   16,384 rows of 4,096   512 x 1 155, 129 / 252, 250;  256 x 2 129, 133, 148 / 251, 256, 258
-//   8,192 rows of 8,192    1024 x 1 132 / 246;  512 x 2 (bf16) 133, 137
-//   2,047 rows of 12,288   1024 x 2 61 / 110;  4,096 of 16,384 138 / 262;  2,048 of 32,768  1024 x 4 259 / 359
+// The gradient's, which holds three arrays and the sum for dweight.  us with all of them, a mask and k_sum_parts, bf16 / fp32, with waves on a SIMD unit:
+//   131,072 rows of 128    16 x 1  1: 44 / 89, 2: 36 / 68, 3: 37 / 67, 4: 39 / 70
+//   32,768 rows of 512     64 x 1  1: 44 / 66, 2: 37 / 67, 3: 37 / 70, 4: 39 / 70
+//   30,000 rows of 785     64 x 2  1: 78 / 102, 2: 56 / 102, 3: 54 / 115, 4: 62 / 104;  128 x 1  2: 75 / 100, 3: 65 / 105
+//   16,384 rows of 2,048   256 x 1  1: 84 / 121, 2: 65 / 127, 3: 69 / 130, 4: 71 / 134;  128 x 2  2: 69 / 135
+//   16,384 rows of 4,096   512 x 1  2: 121 / 247, 4: 132 / 250;  256 x 2  2: 133 / 247, 3: 135 / 247
+//   8,192 rows of 8,192    512 x 2  2: 128 / 250, 4: 131 / 252;  1024 x 1  4: 131 / 249
+//   4,096 rows of 16,384   1024 x 2  4: 130 / 262;  512 x 4  2: 132 / 268;  2,048 of 32,768  1024 x 4  4: 259 / 347
 template <class F>
 void pick_row_back(uint32_t cols, F&& f) {
   if (cols <= 16 * 8) f(Int<16>(), Int<1>());
@@ -92,7 +92,7 @@ void pick_row_back(uint32_t cols, F&& f) {
   else if (cols <= 64 * 16) f(Int<64>(), Int<2>());
   else if (cols <= 256 * 8) f(Int<256>(), Int<1>());
   else if (cols <= 512 * 8) f(Int<512>(), Int<1>());
-  else if (cols <= 1024 * 8) f(Int<1024>(), Int<1>());
+  else if (cols <= 512 * 16) f(Int<512>(), Int<2>());
   else if (cols <= 1024 * 16) f(Int<1024>(), Int<2>());
   else f(Int<1024>(), Int<4>());
 }
@@ -113,7 +113,7 @@ Memory weight_of(const qsl_norm* n) { return array(n->weight, static_cast<uint64
 uint32_t back_blocks(const qsl_norm* n) {
   uint32_t blocks = 0;
   pick_row_back(n->cols, [&](auto l, auto) {
-    const uint64_t th = THREADS<l()>, per = th / l(), most = th == 256 ? (n->dtype == QSL_F32 ? 512 : 768) : 256 * 1024 / th;
+    const uint64_t th = THREADS<l()>, per = th / l(), most = th == 256 ? 512 : 256;
     blocks = n->rows <= 2 * per ? (n->rows != 0) : static_cast<uint32_t>(std::min<uint64_t>((n->rows + per - 1) / per, most));
   });
   return blocks;
