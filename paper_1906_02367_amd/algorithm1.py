@@ -15,8 +15,8 @@ can be checked along the run.
 
 `SoftmaxProblem.error` is the other axis of the plots of Section 5 (top-1 and top-5 error), `DistilledProblem` the same model
 trained on the labels and on a trained model's top log probabilities; both, and the gradients of the latter's local steps, come from the
-library's operators on logits.  `RegularisedProblem` is the model on normed features, which its local steps drop out: by the library's norm,
-with the random words of its other streams.
+library's operators on logits.  `RegularisedProblem` is the model on normed features, a share of which its local steps drop, by the library's
+norm and dropout.
 
     python -m paper_1906_02367_amd.algorithm1        # loss against bits for a few operators
 """

@@ -448,6 +448,74 @@ def test_results_in_the_place_of_what_is_read(B, C, dtype):
         assert torch.equal(v[first], a) and torch.equal(v[second], b), (first, second)
 
 
+@pytest.mark.parametrize("C", [1, 13, 129, 785, 2001, 4100])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_rows_that_stand_in_turn(B, C, dtype):
+    """Every array's rows among the others', at all offsets an element's alignment allows; what lies between stays as it was."""
+    N, p = 17, 0.3
+    parts = [rows_of(N, C, dtype, k) for k in range(5)]
+    w = weight_of(C, "same", dtype)
+    apart = [room(N, C, dtype)[0] for _ in range(5)]
+    B.rms_norm(parts[0], apart[0], weight=w, residual=parts[1], total=apart[1], p=p, seed=1)
+    B.rms_norm_backward(apart[1], parts[2], weight=w, dtotal=parts[3], dresidual=apart[2], dx=apart[3], p=p, seed=1)
+    B.dropout(parts[0], apart[4], p, seed=2, residual=parts[4])
+    held = torch.full((N, 11 * (C + 1) + 1), 7.0, dtype=X.TYPES[dtype], device=dev)
+    place = [held[:, 1 + k * (C + 1): 1 + k * (C + 1) + C] for k in range(10)]
+    for v, q in zip(place, parts):
+        v.copy_(q)
+    x, res, dy, dt, res2, y, t, dres, dx, d = place
+    wide = torch.full((C + 1,), 7.0, dtype=w.dtype, device=dev)
+    w2 = wide[1:].copy_(w)
+    B.rms_norm(x, y, weight=w2, residual=res, total=t, p=p, seed=1)
+    B.rms_norm_backward(t, dy, weight=w2, dtotal=dt, dresidual=dres, dx=dx, p=p, seed=1)
+    B.dropout(x, d, p, seed=2, residual=res2)
+    assert all(torch.equal(a, b) for a, b in zip((y, t, dres, dx, d), apart)) and all(torch.equal(a, b) for a, b in zip(place, parts))
+    between = held.clone()
+    for v in (between[:, 1 + k * (C + 1): 1 + k * (C + 1) + C] for k in range(10)):
+        v.fill_(7.0)
+    assert (between == 7.0).all()
+    # codes in turn with codes, at every byte
+    q, s = room(N, C, torch.int8)[0], torch.empty(N, 1, device=dev)
+    B.rms_norm(x, q, weight=w2, residual=res, p=p, seed=1, scales=s)
+    bytes_ = torch.full((N, 3 * C + 5), 9, dtype=torch.int8, device=dev)
+    for k in (0, C + 2):
+        B.rms_norm(x, bytes_[:, k:k + C], weight=w2, residual=res, p=p, seed=1, scales=s)
+        assert torch.equal(bytes_[:, k:k + C], q)
+    assert (bytes_[:, C:C + 2] == 9).all() and (bytes_[:, 2 * C + 2:] == 9).all()
+
+
+def test_two_host_threads_at_once(B):
+    import threading
+    N, C = 300, 1500
+    xs = [rows_of(N, C, "bf16", s) for s in (1, 2)]
+    dy = rows_of(N, C, "bf16", 3)
+
+    def calls(x, o):
+        for _ in range(20):
+            B.rms_norm(x, o[0], p=0.1, seed=1, total=o[1])
+            B.rms_norm_backward(o[1], dy, dx=o[2], dweight=o[3], p=0.1, seed=1)
+            B.dropout(x, o[4], 0.1, seed=1)
+
+    outputs = lambda: [torch.zeros_like(dy) for _ in range(3)] + [torch.zeros(C, device=dev), torch.zeros_like(dy)]
+    want, got = [outputs() for _ in xs], [outputs() for _ in xs]
+    for x, o in zip(xs, want):
+        calls(x, o)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+
+    def run(x, o, s):
+        with torch.cuda.stream(s):
+            calls(x, o)
+
+    threads = [threading.Thread(target=run, args=a) for a in zip(xs, got, streams)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for w, g in zip(want, got) for a, b in zip(w, g))
+
+
 def test_one_array_read_twice(B):
     x = rows_of(9, 300, "bf16", 1)
     y, t = (room(9, 300, "bf16")[0] for _ in range(2))
