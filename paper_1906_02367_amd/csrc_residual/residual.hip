@@ -119,11 +119,18 @@ uint32_t back_blocks(const qsl_norm* n) {
   return blocks;
 }
 
+// Launches kernel(args...).  (<<<...>>> takes the host 0.43 us more: it hands the launch's shape over by two calls of its own.)
+template <class... A>
+void launch(void (*kernel)(A...), dim3 grid, uint32_t threads, hipStream_t stream, std::common_type_t<A>... args) {
+  void* at[] = {&args...};
+  (void)hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, 0, stream);      // what fails is the last error
+}
+
 // Narrow sums by blocks of 16 columns, of which there are more; wide ones by 32, whole lines of the caches, which else two compute dies read.  us behind a
 // kernel that writes them, 16 / 32 columns: 768 blocks of 1,024 3.4 / 4.7, of 2,048 6.0 / 5.6, 512 of 4,096 7.1 / 5.7, 256 of 12,289 13.1 / 10.3
 void sum_parts(const float* part, uint32_t blocks, uint32_t cols, float* dweight, hipStream_t stream) {
-  if (cols <= 1024) k_sum_parts<16, 64><<<(cols + 15) / 16, 1024, 0, stream>>>(part, blocks, cols, dweight);
-  else k_sum_parts<32, 32><<<(cols + 31) / 32, 1024, 0, stream>>>(part, blocks, cols, dweight);
+  if (cols <= 1024) launch(k_sum_parts<16, 64>, dim3((cols + 15) / 16), 1024, stream, part, blocks, cols, dweight);
+  else launch(k_sum_parts<32, 32>, dim3((cols + 31) / 32), 1024, stream, part, blocks, cols, dweight);
 }
 
 qsl_status launched() { return hipGetLastError() == hipSuccess ? QSL_OK : QSL_ERR_DEVICE; }
@@ -146,7 +153,7 @@ extern "C" qsl_status qsl_dropout(const qsl_dropout_args* args, void* hip_stream
   const uint64_t blocks = (rows * units + DROP_THREADS - 1) / DROP_THREADS;
   pick_type(args->dtype, [&](auto e) {
     typedef decltype(e) E;
-    pick_past<E>(rows * cols * es, [&](auto past) { k_dropout<E, past()><<<grid_of(blocks), DROP_THREADS, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+    pick_past<E>(rows * cols * es, [&](auto past) { launch(k_dropout<E, past()>, grid_of(blocks), DROP_THREADS, static_cast<hipStream_t>(hip_stream), a); });
   });
   return launched();
 }
@@ -183,8 +190,8 @@ extern "C" qsl_status qsl_rms_norm(const qsl_rms_norm_args* args, void* hip_stre
       constexpr int th = THREADS<l()>, per = th / l();
       const dim3 grid = grid_of((rows + per - 1) / per);
       pick_past<E>(rows * cols * ((total.data ? es : 0) + elem_size(out_dtype)), [&](auto past) {
-        if (bits8) k_rms_norm<E, l(), u(), true, past()><<<grid, th, 0, stream>>>(a);
-        else k_rms_norm<E, l(), u(), false, past()><<<grid, th, 0, stream>>>(a);
+        if (bits8) launch(k_rms_norm<E, l(), u(), true, past()>, grid, th, stream, a);
+        else launch(k_rms_norm<E, l(), u(), false, past()>, grid, th, stream, a);
       });
     });
   });
@@ -225,7 +232,7 @@ extern "C" qsl_status qsl_rms_norm_backward(const qsl_rms_norm_backward_args* ar
       typedef decltype(e) E;
       pick_row_back(norm->cols, [&](auto l, auto u) {
         pick_past<E>(rows * cols * es * ((dres.data != nullptr) + (dx.data != nullptr)), [&](auto past) {
-          k_rms_norm_backward<E, l(), u(), past()><<<blocks, THREADS<l()>, 0, stream>>>(a);
+          launch(k_rms_norm_backward<E, l(), u(), past()>, dim3(blocks), THREADS<l()>, stream, a);
         });
       });
     });
