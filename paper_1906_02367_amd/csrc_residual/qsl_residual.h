@@ -12,6 +12,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "qsl_device.h"
 
 using namespace qsl;
@@ -21,37 +23,39 @@ namespace {
 __device__ __forceinline__ uint64_t block_number() { return static_cast<uint64_t>(blockIdx.y) * gridDim.x + blockIdx.x; }
 
 // ---------------------------------------------------------------------------------------------
-// units: eight columns of a row, the values that one Philox block decides on, 16 bytes of 16-bit values or 32 of floats.  They begin at
-// every eighth column of the row, wherever that lies: the loads need no more than the elements' alignment.
+// units: N columns of a row, 16 bytes of the arrays' type E, eight 16-bit values or four floats: lanes side by side read 16 bytes side by side.  (Eight
+// floats a lane in two loads: the norm of 6,000 fp32 rows of 785, without a residual, 9.7 us instead of 7.9.)  They begin at every N-th column of the row, wherever
+// that lies: the loads need no more than the elements' alignment.  Weights and sums in floats beside 16-bit arrays have units of eight too.
 // ---------------------------------------------------------------------------------------------
-template <class E> struct Unit { uint32_t w[2 * sizeof(E)]; };
+template <class E> constexpr int COLS = 16 / sizeof(E);
+template <class W, int N> struct Unit { uint32_t w[N * sizeof(W) / 4]; };
 
-__device__ __forceinline__ void unpack(const Unit<float>& q, float* v) {
+template <int N> __device__ __forceinline__ void unpack(const Unit<float, N>& q, float* v) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(q.w[i]);
+  for (int i = 0; i < N; ++i) v[i] = __uint_as_float(q.w[i]);
 }
-__device__ __forceinline__ void unpack(const Unit<__bf16>& q, float* v) {
+__device__ __forceinline__ void unpack(const Unit<__bf16, 8>& q, float* v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(q.w[i] << 16); v[2 * i + 1] = __uint_as_float(q.w[i] & 0xFFFF0000u); }
 }
-__device__ __forceinline__ void unpack(const Unit<_Float16>& q, float* v) {
+__device__ __forceinline__ void unpack(const Unit<_Float16, 8>& q, float* v) {
   typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 #pragma unroll
   for (int i = 0; i < 4; ++i) { const h2 x = __builtin_bit_cast(h2, q.w[i]); v[2 * i] = static_cast<float>(x[0]); v[2 * i + 1] = static_cast<float>(x[1]); }
 }
 // rounded once, to nearest even
-__device__ __forceinline__ void pack(const float* v, Unit<float>& q) {
+template <int N> __device__ __forceinline__ void pack(const float* v, Unit<float, N>& q) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q.w[i] = __float_as_uint(v[i]);
+  for (int i = 0; i < N; ++i) q.w[i] = __float_as_uint(v[i]);
 }
-template <class E> __device__ __forceinline__ void pack(const float* v, Unit<E>& q) {
-  typedef E e2 __attribute__((ext_vector_type(2)));
+template <class W, class = typename std::enable_if<sizeof(W) == 2>::type> __device__ __forceinline__ void pack(const float* v, Unit<W, 8>& q) {
+  typedef W w2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { const e2 x = {static_cast<E>(v[2 * i]), static_cast<E>(v[2 * i + 1])}; q.w[i] = __builtin_bit_cast(uint32_t, x); }
+  for (int i = 0; i < 4; ++i) { const w2 x = {static_cast<W>(v[2 * i]), static_cast<W>(v[2 * i + 1])}; q.w[i] = __builtin_bit_cast(uint32_t, x); }
 }
 
 // 16 bytes with the elements' alignment, and the parts of a unit that is short of columns; an element's bits
-template <class E> struct Raw {
+template <class W> struct Raw {
   typedef uint32_t mem __attribute__((ext_vector_type(4), aligned(2)));
   typedef uint32_t four __attribute__((ext_vector_type(2), aligned(2)));
   typedef uint32_t two __attribute__((aligned(2)));
@@ -63,26 +67,26 @@ template <> struct Raw<float> {
   typedef uint32_t two __attribute__((ext_vector_type(2), aligned(4)));
   typedef uint32_t bits;
 };
-// the first n of a unit's elements away, zeros behind the rest
-template <class E> __device__ __forceinline__ void shift_out(Unit<E>& q, uint32_t n) {
-  constexpr int W = 2 * sizeof(E), STEP = W / 8;      // words, words of an element
+// the first n < N of a unit's elements away, zeros behind the rest
+template <class W, int N> __device__ __forceinline__ void shift_out(Unit<W, N>& q, uint32_t n) {
+  constexpr int WORDS = N * sizeof(W) / 4;
   auto away = [&](int words) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) q.w[i] = i + words < W ? q.w[i + words] : 0;
+    for (int i = 0; i < WORDS; ++i) q.w[i] = i + words < WORDS ? q.w[i + words] : 0;
   };
-  if (n & 4) away(W / 2);
-  if (n & 2) away(W / 4);
+  if (N == 8 && n & 4) away(WORDS / 2);
+  if (n & 2) away(2 * sizeof(W) / 4);
   if (n & 1) {
-    if constexpr (STEP == 1) away(1);
+    if constexpr (sizeof(W) == 4) away(1);
     else {
 #pragma unroll
-      for (int i = 0; i < W; ++i) q.w[i] = __builtin_amdgcn_alignbit(i + 1 < W ? q.w[i + 1] : 0, q.w[i], 16);
+      for (int i = 0; i < WORDS; ++i) q.w[i] = __builtin_amdgcn_alignbit(i + 1 < WORDS ? q.w[i + 1] : 0, q.w[i], 16);
     }
   }
 }
 // PAST: what is read or written is more than the caches hold, so that nothing of it is found there by what runs next: it need not pass through
-// them.  us for 16,384 rows of 4,096 bf16: the norm 91.5 / 88.1, and with a reader of its results behind it 161 / 158; the gradient 130 / 119.  (Of
-// 8,192 rows 81 / 83 with the reader, and fp32, whose lanes read 32 bytes in two loads, loses in any case: 248 / 278.)
+// them.  us for 16,384 rows of 4,096, through them / past them: the norm bf16 91 / 88, fp32 182 / 175, and bf16 with a reader of its results behind it
+// 161 / 158 (of 8,192 rows, which the caches hold, 81 / 83); the gradient bf16 125.5 / 120, fp32 246 / 230; dropout with a residual fp32 135.5 / 128.
 template <bool PAST, class M> __device__ __forceinline__ M load16(const M* p) {
   if constexpr (PAST) return __builtin_nontemporal_load(p);
   else return *p;
@@ -92,77 +96,78 @@ template <bool PAST, class M> __device__ __forceinline__ void store16(M* p, M m)
   else *p = m;
 }
 // U units of a row of `cols` columns, from column c0 on, `step` columns apart; zeros where there is no row (`live`) or none of it left.  A row's last
-// unit, where it is short, is cut from the row's last eight columns, so that its load is one with the others (by single elements: the gradient
+// unit, where it is short, is cut from the row's last N columns, so that its load is one with the others (by single elements: the gradient
 // of 30,000 rows of 785 bf16 71 instead of 61 us): cut_units has to follow.  It waits for the values, so it follows when all
-// arrays' loads are under way (else 2,047 rows of 12,289 70 instead of 64 us).  TINY: rows of less than eight are taken by elements.
-template <class E, int U, bool TINY, bool PAST> __device__ __forceinline__ void load_units(const E* row, uint32_t c0, uint32_t step, uint32_t cols, bool live, Unit<E>* q) {
-  constexpr int W = 2 * sizeof(E);
+// arrays' loads are under way (else 2,047 rows of 12,289 70 instead of 64 us).  TINY: rows of less than N are taken by elements.
+template <int U, bool TINY, bool PAST, class W, int N>
+__device__ __forceinline__ void load_units(const W* row, uint32_t c0, uint32_t step, uint32_t cols, bool live, Unit<W, N>* q) {
+  constexpr int WORDS = N * sizeof(W) / 4;
   const uint32_t end = live ? cols : 0;
-  if (!TINY || cols >= 8) {
+  if (!TINY || cols >= N) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t c = c0 + u * step;
-      const E* p = row + min(c, cols - 8);
+      const W* p = row + min(c, cols - N);
 #pragma unroll
-      for (int k = 0; k < W / 4; ++k) {
-        typename Raw<E>::mem m = {0, 0, 0, 0};
-        if (c < end) m = load16<PAST>(reinterpret_cast<const typename Raw<E>::mem*>(p) + k);
+      for (int k = 0; k < WORDS / 4; ++k) {
+        typename Raw<W>::mem m = {0, 0, 0, 0};
+        if (c < end) m = load16<PAST>(reinterpret_cast<const typename Raw<W>::mem*>(p) + k);
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[u].w[4 * k + i] = m[i];
       }
     }
   } else {
-    typedef typename Raw<E>::bits bits;
+    typedef typename Raw<W>::bits bits;
     const bits* p = reinterpret_cast<const bits*>(row);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int i = 0; i < W; ++i) q[u].w[i] = 0;
+      for (int i = 0; i < WORDS; ++i) q[u].w[i] = 0;
     }
     if (c0 < end) {                                                         // (c0 = 0)
 #pragma unroll
-      for (uint32_t i = 0; i < 7; ++i) {
+      for (uint32_t i = 0; i < N - 1; ++i) {
         const uint32_t x = i < cols ? static_cast<uint32_t>(p[i]) : 0u;
-        if constexpr (sizeof(E) == 4) q[0].w[i] = x;
+        if constexpr (sizeof(W) == 4) q[0].w[i] = x;
         else q[0].w[i / 2] |= x << 16 * (i & 1);
       }
     }
   }
 }
-template <class E, int U, bool TINY> __device__ __forceinline__ void cut_units(uint32_t c0, uint32_t step, uint32_t cols, Unit<E>* q) {
-  if ((cols & 7) == 0 || (TINY && cols < 8)) return;
+template <int U, bool TINY, class W, int N> __device__ __forceinline__ void cut_units(uint32_t c0, uint32_t step, uint32_t cols, Unit<W, N>* q) {
+  if ((cols & (N - 1)) == 0 || (TINY && cols < N)) return;
 #pragma unroll
   for (int u = 0; u < U; ++u)
-    if (c0 + u * step < cols && c0 + u * step + 8 > cols) shift_out(q[u], 8 - (cols & 7));      // (no row: zeros stay zeros)
+    if (c0 + u * step < cols && c0 + u * step + N > cols) shift_out(q[u], N - (cols & (N - 1)));      // (no row: zeros stay zeros)
 }
 // a unit's columns below `end`: cols, or 0 where there is no row
-template <bool PAST, class E> __device__ __forceinline__ void store_unit(E* row, uint32_t c, uint32_t end, const float* v) {
-  Unit<E> q;
+template <bool PAST, int N, class W> __device__ __forceinline__ void store_unit(W* row, uint32_t c, uint32_t end, const float* v) {
+  Unit<W, N> q;
   pack(v, q);
-  if (c + 8 <= end) {
+  if (c + N <= end) {
 #pragma unroll
-    for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) {
-      typename Raw<E>::mem m = {q.w[4 * k], q.w[4 * k + 1], q.w[4 * k + 2], q.w[4 * k + 3]};
-      store16<PAST>(reinterpret_cast<typename Raw<E>::mem*>(row + c) + k, m);
+    for (int k = 0; k < N * static_cast<int>(sizeof(W)) / 16; ++k) {
+      typename Raw<W>::mem m = {q.w[4 * k], q.w[4 * k + 1], q.w[4 * k + 2], q.w[4 * k + 3]};
+      store16<PAST>(reinterpret_cast<typename Raw<W>::mem*>(row + c) + k, m);
     }
   } else if (c < end) {                                                     // four, two, one
     uint32_t n = end - c;
-    E* p = row + c;
-    if (n & 4) {
-      typename Raw<E>::four m;
+    W* p = row + c;
+    if (N == 8 && n & 4) {
+      typename Raw<W>::four m;
       __builtin_memcpy(&m, q.w, sizeof(m));
-      *reinterpret_cast<typename Raw<E>::four*>(p) = m;
+      *reinterpret_cast<typename Raw<W>::four*>(p) = m;
       shift_out(q, 4);
       p += 4;
     }
     if (n & 2) {
-      typename Raw<E>::two m;
+      typename Raw<W>::two m;
       __builtin_memcpy(&m, q.w, sizeof(m));
-      *reinterpret_cast<typename Raw<E>::two*>(p) = m;
+      *reinterpret_cast<typename Raw<W>::two*>(p) = m;
       shift_out(q, 2);
       p += 2;
     }
-    if (n & 1) *reinterpret_cast<typename Raw<E>::bits*>(p) = static_cast<typename Raw<E>::bits>(q.w[0]);
+    if (n & 1) *reinterpret_cast<typename Raw<W>::bits*>(p) = static_cast<typename Raw<W>::bits>(q.w[0]);
   }
 }
 
@@ -196,12 +201,14 @@ __device__ __forceinline__ Words4 random_words(uint32_t c0, uint32_t c1, uint32_
   }
   return Words4{{c0, c1, c2, c3}};
 }
-// v <- drop(v) of a row's unit: one Philox block, eight pieces of 16 bits.  (A word of 32 bits for each: those 175.5 us become 200.  The share that is kept
-// is a multiple of 2^-16, and the factor belongs to that share, so that what is kept has the right mean.)
-__device__ __forceinline__ void drop_unit(const Drop& d, const Key& k, uint32_t row, uint32_t unit, float* v) {
-  const Words4 o = random_words(unit, d.row0 + row, k.lo, k.hi, d.seed_lo, d.seed_hi);
+// v <- drop(v) of a row's unit: 16-bit pieces of the Philox block of its eight columns, of which a unit of four takes its half.  (A word of 32 bits for
+// each: those 175.5 us become 200.  The share that is kept is a multiple of 2^-16, and the factor belongs to that share, so that what is kept has the
+// right mean.)
+template <int N> __device__ __forceinline__ void drop_unit(const Drop& d, const Key& k, uint32_t row, uint32_t unit, float* v) {
+  Words4 o = random_words(N == 8 ? unit : unit / 2, d.row0 + row, k.lo, k.hi, d.seed_lo, d.seed_hi);
+  if (N == 4 && unit & 1) { o.w[0] = o.w[2]; o.w[1] = o.w[3]; }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < N; ++i) {
     const uint32_t piece = i & 1 ? o.w[i / 2] >> 16 : o.w[i / 2] & 0xFFFFu;
     v[i] = piece < d.T ? v[i] * d.factor : 0.0f;
   }
@@ -256,12 +263,13 @@ template <int L> __device__ __forceinline__ Two row_sums(Two x, Two* at) {
   x = at[threadIdx.x % (L / 64)];
   return Two{join_sum<L / 64>(x.a), join_sum<L / 64>(x.b)};
 }
-// over 4, 8 or 16 neighbouring lanes
+// over 4, 8, 16 or 32 neighbouring lanes
 __device__ __forceinline__ uint32_t max_of_lanes(uint32_t x, uint32_t lanes) {
   x = max(x, dpp_move<DPP_XOR1>(x));
   x = max(x, dpp_move<DPP_XOR2>(x));
   if (lanes >= 8) x = max(x, dpp_move<DPP_HALF_MIRROR>(x));
   if (lanes >= 16) x = max(x, dpp_move<DPP_ROW_ROR + 8>(x));
+  if (lanes >= 32) x = max(x, static_cast<uint32_t>(__builtin_amdgcn_ds_swizzle(static_cast<int>(x), 0x401F)));      // from lane ^ 16
   return x;
 }
 template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t x, uint32_t* at) {
@@ -285,7 +293,7 @@ constexpr float SMALLER = 0x1p-72f;
 constexpr float INF = __builtin_inff();
 
 template <int L> constexpr int THREADS = L <= 64 ? 256 : L;      // rows of a wave and less share a block
-template <int L> constexpr bool TINY = L == 16;                  // rows of less than eight columns go there
+template <int L> constexpr bool TINY = L == 16;                  // rows of less than a unit's columns go there
 template <int L> constexpr int WAVES = L <= 64 ? 1 : L / 64;     // of a row
 // a row's number within the block, for the compiler the same in a wave where it is
 template <int L> __device__ __forceinline__ uint32_t row_in_block() {
@@ -307,29 +315,30 @@ struct DropArgs {
 constexpr int DROP_THREADS = 256;
 
 // Read and written once each, bound by memory: 8,192 rows of 4,096 bf16 with a residual 37.6 us, 5.35 TB/s (a copy of 1 GiB: 5.2).
-// A unit a thread, the rows' units one behind the other: the shortest way from a load to a store, eight waves on a SIMD unit.  (Four a thread, whose loads are under way together: 8,192 rows of 4,096 bf16 28.7 us instead of 25.3, 4,095 of 11,009 40.9 / 34.2, fp32
-// 53.4 / 48.9; eight: 30.5.)
+// A unit a thread, the rows' units one behind the other: the shortest way from a load to a store, eight waves on a
+// SIMD unit.  (Four a thread, whose loads are under way together: 8,192 rows of 4,096 bf16 28.7 us instead of 25.3, 4,095 of 11,009 40.9 / 34.2; eight 30.5.)
 template <class E, bool PAST> __global__ __launch_bounds__(DROP_THREADS) void k_dropout(DropArgs a) {
   const uint64_t first = block_number() * DROP_THREADS, row_b = first / a.units;
   const uint32_t i = static_cast<uint32_t>(first - row_b * a.units) + threadIdx.x, r = i / a.units;
   const uint64_t row = row_b + r;
-  const uint32_t c = (i - r * a.units) * 8;
+  constexpr int N = COLS<E>;
+  const uint32_t unit = i - r * a.units, c = unit * N;
   if (row >= a.rows) return;
-  Unit<E> x, res;
-  load_units<E, 1, true, PAST>(static_cast<const E*>(a.x) + row * a.x_stride, c, 0, a.cols, true, &x);
-  if (a.res) load_units<E, 1, true, PAST>(static_cast<const E*>(a.res) + row * a.res_stride, c, 0, a.cols, true, &res);
-  cut_units<E, 1, true>(c, 0, a.cols, &x);
-  float v[8];
+  Unit<E, N> x, res;
+  load_units<1, true, PAST>(static_cast<const E*>(a.x) + row * a.x_stride, c, 0, a.cols, true, &x);
+  if (a.res) load_units<1, true, PAST>(static_cast<const E*>(a.res) + row * a.res_stride, c, 0, a.cols, true, &res);
+  cut_units<1, true>(c, 0, a.cols, &x);
+  float v[N];
   unpack(x, v);
-  if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key_of(a.drop), static_cast<uint32_t>(row), c / 8, v);
+  if (a.drop.T != KEEP_ALL) drop_unit<N>(a.drop, key_of(a.drop), static_cast<uint32_t>(row), unit, v);
   if (a.res) {
-    float b[8];
-    cut_units<E, 1, true>(c, 0, a.cols, &res);
+    float b[N];
+    cut_units<1, true>(c, 0, a.cols, &res);
     unpack(res, b);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += b[k];
+    for (int k = 0; k < N; ++k) v[k] += b[k];
   }
-  store_unit<PAST>(static_cast<E*>(a.y) + row * a.y_stride, c, a.cols, v);
+  store_unit<PAST, N>(static_cast<E*>(a.y) + row * a.y_stride, c, a.cols, v);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -346,62 +355,63 @@ struct NormArgs {
 };
 
 template <class E, int U, bool TINY> __device__ __forceinline__ void load_weight(const void* weight, uint32_t is_float, uint32_t c0, uint32_t step, uint32_t cols, float* w) {
+  constexpr int N = COLS<E>;
+  auto load = [&](auto* at) {
+    Unit<typename std::remove_const<typename std::remove_reference<decltype(*at)>::type>::type, N> q[U];
+    load_units<U, TINY, false>(at, c0, step, cols, true, q);
+    cut_units<U, TINY>(c0, step, cols, q);
+#pragma unroll
+    for (int u = 0; u < U; ++u) unpack(q[u], w + N * u);
+  };
   if (!weight) {
 #pragma unroll
-    for (int i = 0; i < 8 * U; ++i) w[i] = 1.0f;
+    for (int i = 0; i < N * U; ++i) w[i] = 1.0f;
   } else if (sizeof(E) == 4 || is_float) {
-    Unit<float> q[U];
-    load_units<float, U, TINY, false>(static_cast<const float*>(weight), c0, step, cols, true, q);
-    cut_units<float, U, TINY>(c0, step, cols, q);
-#pragma unroll
-    for (int u = 0; u < U; ++u) unpack(q[u], w + 8 * u);
+    load(static_cast<const float*>(weight));
   } else {
-    Unit<E> q[U];
-    load_units<E, U, TINY, false>(static_cast<const E*>(weight), c0, step, cols, true, q);
-    cut_units<E, U, TINY>(c0, step, cols, q);
-#pragma unroll
-    for (int u = 0; u < U; ++u) unpack(q[u], w + 8 * u);
+    load(static_cast<const E*>(weight));
   }
 }
-// 8-bit codes of a unit, eight bytes.  y = r t with t = w h, whose rounding error is t_lo; `most`: the bits of the group's largest |t|.  y Q / a =
+// 8-bit codes of a unit, N bytes.  y = r t with t = w h, whose rounding error is t_lo; `most`: the bits of the group's largest |t|.  y Q / a =
 // t Q / max |t|: r does not enter, and with the errors of t and of the quotient the code is that of the exact value for all that h allows.  (Of 24.6 million
 // e4m3 codes of rows of 4,096 with a residual 48 are not those of 64 bits, by elementary operations in 32 bits 67; fp32 8 and 16.)
-__device__ __forceinline__ void store_codes(uint8_t* row, uint32_t c, uint32_t cols, const float* t, const float* t_lo, uint32_t most, float r, bool is_e4m3,
+template <int N> __device__ __forceinline__ void store_codes(uint8_t* row, uint32_t c, uint32_t cols, const float* t, const float* t_lo, uint32_t most, float r, bool is_e4m3,
                                             float* scale_at) {
   const float Q = is_e4m3 ? 448.0f : 127.0f, t_max = __uint_as_float(most), y_max = t_max * r, a = fmaxf(y_max, 0x1p-100f);
   const bool bad = !(y_max < INF);                                // an infinity or a NaN
   const bool plain = !(t_max >= 0x1p-100f && y_max >= 0x1p-100f);      // next to nothing: by y itself
   const float div = plain ? a : t_max, q = Q / div, inv = plain ? q * r : q, lo_inv = plain ? 0.0f : q, inv_lo = __builtin_fmaf(-q, div, Q) * (lo_inv / Q);
-  float v[8];
+  float v[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(t[i], inv, __builtin_fmaf(t[i], inv_lo, t_lo[i] * lo_inv));
-  uint32_t lo = 0, hi = 0;
-  if (is_e4m3) {
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], lo, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], hi, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
-  } else {
+  for (int i = 0; i < N; ++i) v[i] = __builtin_fmaf(t[i], inv, __builtin_fmaf(t[i], inv_lo, t_lo[i] * lo_inv));
+  uint32_t code[N / 4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lo |= (static_cast<uint32_t>(static_cast<int>(rintf(v[i]))) & 0xFFu) << 8 * i;
-      hi |= (static_cast<uint32_t>(static_cast<int>(rintf(v[4 + i]))) & 0xFFu) << 8 * i;
+  for (int k = 0; k < N / 4; ++k) {
+    const float* f = v + 4 * k;
+    uint32_t x = 0;
+    if (is_e4m3) {
+      x = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], x, false);
+      x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], x, true);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x |= (static_cast<uint32_t>(static_cast<int>(rintf(f[i]))) & 0xFFu) << 8 * i;
     }
+    code[k] = bad ? 0 : x;
   }
-  if (bad) lo = hi = 0;
   if (scale_at) *scale_at = bad ? __builtin_nanf("") : a / Q;
   typedef uint32_t eight __attribute__((ext_vector_type(2), aligned(1)));
   typedef uint32_t four __attribute__((aligned(1)));
   typedef uint16_t two __attribute__((aligned(1)));
-  if (c + 8 <= cols) {
-    const eight q = {lo, hi};
-    *reinterpret_cast<eight*>(row + c) = q;
+  uint8_t* p = row + c;
+  if (c + N <= cols) {
+    if constexpr (N == 8) { const eight q = {code[0], code[1]}; *reinterpret_cast<eight*>(p) = q; }
+    else *reinterpret_cast<four*>(p) = code[0];
   } else {
     const uint32_t n = cols - c;
-    uint8_t* p = row + c;
-    if (n & 4) { *reinterpret_cast<four*>(p) = lo; lo = hi; p += 4; }
-    if (n & 2) { *reinterpret_cast<two*>(p) = static_cast<uint16_t>(lo); lo >>= 16; p += 2; }
-    if (n & 1) *p = static_cast<uint8_t>(lo);
+    uint32_t x = code[0];
+    if (N == 8 && n & 4) { *reinterpret_cast<four*>(p) = x; x = code[N / 4 - 1]; p += 4; }
+    if (n & 2) { *reinterpret_cast<two*>(p) = static_cast<uint16_t>(x); x >>= 16; p += 2; }
+    if (n & 1) *p = static_cast<uint8_t>(x);
   }
 }
 
@@ -412,32 +422,33 @@ template <class E, int L, int U, bool BITS8, bool PAST>
 __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
   __shared__ float sums[2][WAVES<L>];
   __shared__ uint32_t maxima[WAVES<L>];
+  constexpr int N = COLS<E>;
+  constexpr bool LATE_WEIGHT = L * U * N > 16384;      // (the registers do not hold them beside the rest)
   const uint64_t row = block_number() * (THREADS<L> / L) + row_in_block<L>();
-  const uint32_t lane = threadIdx.x % L, cols = row < a.rows ? a.cols : 0;
-  Unit<E> x[U], res[U];
-  load_units<E, U, TINY<L>, PAST>(static_cast<const E*>(a.x) + row * a.x_stride, lane * 8, L * 8, a.cols, cols != 0, x);
-  if (a.res) load_units<E, U, TINY<L>, PAST>(static_cast<const E*>(a.res) + row * a.res_stride, lane * 8, L * 8, a.cols, cols != 0, res);
-  float h[8 * U], w[8 * U];
-  // (four units a thread: the registers do not hold them beside the rest)
-  if constexpr (U <= 2) load_weight<E, U, TINY<L>>(a.weight, a.weight_is_float, lane * 8, L * 8, a.cols, w);
+  const uint32_t lane = threadIdx.x % L, c0 = lane * N, end = row < a.rows ? a.cols : 0;
+  Unit<E, N> x[U], res[U];
+  load_units<U, TINY<L>, PAST>(static_cast<const E*>(a.x) + row * a.x_stride, c0, L * N, a.cols, end != 0, x);
+  if (a.res) load_units<U, TINY<L>, PAST>(static_cast<const E*>(a.res) + row * a.res_stride, c0, L * N, a.cols, end != 0, res);
+  float h[N * U], w[N * U];
+  if constexpr (!LATE_WEIGHT) load_weight<E, U, TINY<L>>(a.weight, a.weight_is_float, c0, L * N, a.cols, w);
   const Key key = key_of(a.drop);
-  cut_units<E, U, TINY<L>>(lane * 8, L * 8, a.cols, x);
-  if (a.res) cut_units<E, U, TINY<L>>(lane * 8, L * 8, a.cols, res);
+  cut_units<U, TINY<L>>(c0, L * N, a.cols, x);
+  if (a.res) cut_units<U, TINY<L>>(c0, L * N, a.cols, res);
   float ss = 0.0f;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    float* v = h + 8 * u;
+    float* v = h + N * u;
     unpack(x[u], v);
-    if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key, static_cast<uint32_t>(row), u * L + lane, v);
+    if (a.drop.T != KEEP_ALL) drop_unit<N>(a.drop, key, static_cast<uint32_t>(row), u * L + lane, v);
     if (a.res) {
-      float b[8];
+      float b[N];
       unpack(res[u], b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += b[i];
+      for (int i = 0; i < N; ++i) v[i] += b[i];
     }
-    if (a.total) store_unit<PAST>(static_cast<E*>(a.total) + row * a.total_stride, lane * 8 + u * L * 8, cols, v);
+    if (a.total) store_unit<PAST, N>(static_cast<E*>(a.total) + row * a.total_stride, c0 + u * L * N, end, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(v[i], v[i], ss);
+    for (int i = 0; i < N; ++i) ss = __builtin_fmaf(v[i], v[i], ss);
   }
   ss = row_sum<L>(ss, sums[0]);
   float eps = a.eps;
@@ -445,17 +456,17 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
     const float f = ss == INF ? SMALLER : 1.0f;
     ss = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8 * U; ++i) { h[i] *= f; ss = __builtin_fmaf(h[i], h[i], ss); }
+    for (int i = 0; i < N * U; ++i) { h[i] *= f; ss = __builtin_fmaf(h[i], h[i], ss); }
     ss = row_sum<L>(ss, sums[1]);
     eps = f == 1.0f ? eps : 0.0f;
   }
   const float r = 1.0f / sqrtf(ss / static_cast<float>(a.cols) + eps);
-  float lo[BITS8 ? 8 * U : 1];
+  float lo[BITS8 ? N * U : 1];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if constexpr (U > 2) load_weight<E, 1, false>(a.weight, a.weight_is_float, lane * 8 + u * L * 8, 0, a.cols, w + 8 * u);
+    if constexpr (LATE_WEIGHT) load_weight<E, 1, false>(a.weight, a.weight_is_float, c0 + u * L * N, 0, a.cols, w + N * u);
 #pragma unroll
-    for (int k = 8 * u; k < 8 * u + 8; ++k) {
+    for (int k = N * u; k < N * u + N; ++k) {
       if constexpr (BITS8) {
         const float t = h[k] * w[k];
         lo[k] = __builtin_fmaf(h[k], w[k], -t);
@@ -467,25 +478,25 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
   }
   if constexpr (!BITS8) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) store_unit<PAST>(static_cast<E*>(a.y) + row * a.y_stride, lane * 8 + u * L * 8, cols, h + 8 * u);
+    for (int u = 0; u < U; ++u) store_unit<PAST, N>(static_cast<E*>(a.y) + row * a.y_stride, c0 + u * L * N, end, h + N * u);
   } else {
     uint32_t most[U], all = 0;      // of the bits of |t|: a NaN is above the infinities; 0 behind the row
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       most[u] = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) most[u] = max(most[u], __float_as_uint(h[8 * u + i]) & 0x7FFFFFFFu);
-      if (a.group_bits) most[u] = max_of_lanes(most[u], 1u << a.group_bits >> 3);
+      for (int i = 0; i < N; ++i) most[u] = max(most[u], __float_as_uint(h[N * u + i]) & 0x7FFFFFFFu);
+      if (a.group_bits) most[u] = max_of_lanes(most[u], (1u << a.group_bits) / N);
       all = max(all, most[u]);
     }
     if (!a.group_bits) all = row_max<L>(all, maxima);
     const uint32_t in_group = (1u << a.group_bits) - 1, of_row = a.group_bits ? (a.cols + in_group) >> a.group_bits : 1;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t c = lane * 8 + u * L * 8;
+      const uint32_t c = c0 + u * L * N;
       float* const scale_at = a.scales + row * of_row + (a.group_bits ? c >> a.group_bits : 0);
-      if (c < cols) store_codes(static_cast<uint8_t*>(a.y) + row * a.y_stride, c, cols, h + 8 * u, lo + 8 * u, a.group_bits ? most[u] : all, r, a.is_e4m3,
-                                (a.group_bits ? (c & in_group) == 0 : c == 0) ? scale_at : nullptr);
+      if (c < end) store_codes<N>(static_cast<uint8_t*>(a.y) + row * a.y_stride, c, end, h + N * u, lo + N * u, a.group_bits ? most[u] : all, r, a.is_e4m3,
+                                  (a.group_bits ? (c & in_group) == 0 : c == 0) ? scale_at : nullptr);
     }
   }
 }
@@ -510,49 +521,53 @@ struct BackArgs {
 // unpacked for its results, so that these loads are under way beside the masks and the stores and few waves are enough (us, bf16, loads at a row's
 // beginning / ahead: 16,384 rows of 4,096 128.8 / 120.7, of 2,048 70 / 65, 2,047 rows of 12,288 58.8 / 56.3).
 // Where 1024 threads leave a thread 128 registers, the weights are held in LDS, every thread's own; where that is not enough (TIGHT), nothing is loaded
-// ahead, and what else arrives at the totals is loaded where it is added (fp32, 2,047 rows of 12,288: ahead 118, not 107, without either 120).
-template <int L, int U> constexpr bool WEIGHT_IN_LDS = L * U >= 2048;
-template <class E, int L, int U> constexpr bool TIGHT_ROW = L * U * sizeof(E) >= 8192;
+// ahead, and what else arrives at the totals is loaded where it is added (fp32, 2,047 rows of 12,288: 104 us, with loads ahead 127).
+template <class E, int L, int U> constexpr bool WEIGHT_IN_LDS = L * U * COLS<E> >= 16384;
+template <int L, int U> constexpr bool TIGHT_ROW = L * U >= 4096;
 template <class E, int L, int U, bool PAST>
 __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   constexpr int ROWS = THREADS<L> / L;
-  constexpr bool LDS = WEIGHT_IN_LDS<L, U>, TIGHT = TIGHT_ROW<E, L, U>;
+  constexpr int N = COLS<E>;
+  constexpr bool LDS = WEIGHT_IN_LDS<E, L, U>, TIGHT = TIGHT_ROW<L, U>;
   typedef float quad __attribute__((ext_vector_type(4)));
-  __shared__ quad weights[LDS ? 2 * U : 1][LDS ? L : 1];
+  __shared__ quad weights[LDS ? N / 4 * U : 1][LDS ? L : 1];
   __shared__ Two sums[2][2][WAVES<L>];
-  __shared__ float joined[ROWS > 1 ? ROWS * 8 * U * L : 1];
-  const uint32_t lane = threadIdx.x % L, c0 = lane * 8;
+  __shared__ float joined[ROWS > 1 ? ROWS * N * U * L : 1];
+  const uint32_t lane = threadIdx.x % L, c0 = lane * N;
   const Key key = key_of(a.drop);
-  float w_all[LDS ? 8 : 8 * U], dw[8 * U];
+  float w_all[LDS ? N : N * U], dw[N * U];
   if constexpr (LDS) {
     for (int u = 0; u < U; ++u) {
-      load_weight<E, 1, false>(a.weight, a.weight_is_float, c0 + u * L * 8, 0, a.cols, w_all);
-      weights[2 * u][lane] = quad{w_all[0], w_all[1], w_all[2], w_all[3]};
-      weights[2 * u + 1][lane] = quad{w_all[4], w_all[5], w_all[6], w_all[7]};
+      load_weight<E, 1, false>(a.weight, a.weight_is_float, c0 + u * L * N, 0, a.cols, w_all);
+#pragma unroll
+      for (int k = 0; k < N / 4; ++k) weights[N / 4 * u + k][lane] = quad{w_all[4 * k], w_all[4 * k + 1], w_all[4 * k + 2], w_all[4 * k + 3]};
     }
   } else {
-    load_weight<E, U, TINY<L>>(a.weight, a.weight_is_float, c0, L * 8, a.cols, w_all);
+    load_weight<E, U, TINY<L>>(a.weight, a.weight_is_float, c0, L * N, a.cols, w_all);
   }
   auto weight_of = [&](int u, float* w) {
     if constexpr (LDS) {
-      const quad a0 = weights[2 * u][lane], a1 = weights[2 * u + 1][lane];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { w[i] = a0[i]; w[4 + i] = a1[i]; }
+      for (int k = 0; k < N / 4; ++k) {
+        const quad q = weights[N / 4 * u + k][lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[4 * k + i] = q[i];
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = w_all[8 * u + i];
+      for (int i = 0; i < N; ++i) w[i] = w_all[N * u + i];
     }
   };
 #pragma unroll
-  for (int i = 0; i < 8 * U; ++i) dw[i] = 0.0f;
-  Unit<E> hq[U], dyq[U], dtq[TIGHT ? 1 : U];
+  for (int i = 0; i < N * U; ++i) dw[i] = 0.0f;
+  Unit<E, N> hq[U], dyq[U], dtq[TIGHT ? 1 : U];
   auto load_unit = [&](uint64_t row, int u) {
-    const uint32_t c = c0 + u * L * 8;
+    const uint32_t c = c0 + u * L * N;
     const bool live = row < a.rows;
-    load_units<E, 1, TINY<L>, PAST>(static_cast<const E*>(a.total) + row * a.total_stride, c, 0, a.cols, live, hq + u);
-    load_units<E, 1, TINY<L>, PAST>(static_cast<const E*>(a.dy) + row * a.dy_stride, c, 0, a.cols, live, dyq + u);
+    load_units<1, TINY<L>, PAST>(static_cast<const E*>(a.total) + row * a.total_stride, c, 0, a.cols, live, hq + u);
+    load_units<1, TINY<L>, PAST>(static_cast<const E*>(a.dy) + row * a.dy_stride, c, 0, a.cols, live, dyq + u);
     if constexpr (!TIGHT)
-      if (a.dtotal) load_units<E, 1, TINY<L>, PAST>(static_cast<const E*>(a.dtotal) + row * a.dtotal_stride, c, 0, a.cols, live, dtq + u);
+      if (a.dtotal) load_units<1, TINY<L>, PAST>(static_cast<const E*>(a.dtotal) + row * a.dtotal_stride, c, 0, a.cols, live, dtq + u);
   };
   const uint64_t step = static_cast<uint64_t>(gridDim.x) * ROWS;
   uint64_t row = static_cast<uint64_t>(blockIdx.x) * ROWS + row_in_block<L>();
@@ -567,20 +582,20 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) load_unit(row, u);
     }
-    cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, hq);
-    cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, dyq);
+    cut_units<U, TINY<L>>(c0, L * N, a.cols, hq);
+    cut_units<U, TINY<L>>(c0, L * N, a.cols, dyq);
     if constexpr (!TIGHT)
-      if (a.dtotal) cut_units<E, U, TINY<L>>(c0, L * 8, a.cols, dtq);
+      if (a.dtotal) cut_units<U, TINY<L>>(c0, L * N, a.cols, dtq);
     auto sum = [&]() {
       Two s = {0.0f, 0.0f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        float h[8], d[8], w[8];
+        float h[N], d[N], w[N];
         unpack(hq[u], h);
         unpack(dyq[u], d);
         weight_of(u, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
           s.a = __builtin_fmaf(h[i], h[i], s.a);
           s.b = __builtin_fmaf(d[i] * w[i], h[i], s.b);
         }
@@ -595,10 +610,10 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
         eps = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          float h[8];
+          float h[N];
           unpack(hq[u], h);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) h[i] *= f;
+          for (int i = 0; i < N; ++i) h[i] *= f;
           pack(h, hq[u]);
         }
       }
@@ -609,29 +624,29 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
     const float mean = s.b * r / static_cast<float>(a.cols), rf = r * f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float h[8], d[8], t[8], w[8];
+      float h[N], d[N], t[N], w[N];
       unpack(hq[u], h);
       unpack(dyq[u], d);
       weight_of(u, w);
       if (a.dtotal) {
         if constexpr (TIGHT) {
-          load_units<E, 1, false, PAST>(static_cast<const E*>(a.dtotal) + row * a.dtotal_stride, c0 + u * L * 8, 0, a.cols, end != 0, dtq);
-          cut_units<E, 1, false>(c0 + u * L * 8, 0, a.cols, dtq);
+          load_units<1, false, PAST>(static_cast<const E*>(a.dtotal) + row * a.dtotal_stride, c0 + u * L * N, 0, a.cols, end != 0, dtq);
+          cut_units<1, false>(c0 + u * L * N, 0, a.cols, dtq);
         }
         unpack(dtq[TIGHT ? 0 : u], t);
       }
       if constexpr (!TIGHT) load_unit(row + step, u);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < N; ++i) {
         const float un = h[i] * r;
-        dw[8 * u + i] = __builtin_fmaf(d[i], un, dw[8 * u + i]);
+        dw[N * u + i] = __builtin_fmaf(d[i], un, dw[N * u + i]);
         d[i] = rf * (d[i] * w[i] - un * mean);
         if (a.dtotal) d[i] += t[i];
       }
-      if (a.dres) store_unit<PAST>(static_cast<E*>(a.dres) + row * a.dres_stride, c0 + u * L * 8, end, d);
+      if (a.dres) store_unit<PAST, N>(static_cast<E*>(a.dres) + row * a.dres_stride, c0 + u * L * N, end, d);
       if (a.dx) {
-        if (a.drop.T != KEEP_ALL) drop_unit(a.drop, key, static_cast<uint32_t>(row), u * L + lane, d);
-        store_unit<PAST>(static_cast<E*>(a.dx) + row * a.dx_stride, c0 + u * L * 8, end, d);
+        if (a.drop.T != KEEP_ALL) drop_unit<N>(a.drop, key, static_cast<uint32_t>(row), u * L + lane, d);
+        store_unit<PAST, N>(static_cast<E*>(a.dx) + row * a.dx_stride, c0 + u * L * N, end, d);
       }
     }
   }
@@ -639,18 +654,18 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   float* out = a.part + static_cast<uint64_t>(blockIdx.x) * a.cols;
   if constexpr (ROWS == 1) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) store_unit<false>(out, c0 + u * L * 8, a.cols, dw + 8 * u);
+    for (int u = 0; u < U; ++u) store_unit<false, N>(out, c0 + u * L * N, a.cols, dw + N * u);
   } else {
     const uint32_t mine = row_in_block<L>();
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) joined[mine * (8 * U * L) + c0 + u * L * 8 + i] = dw[8 * u + i];
+      for (int i = 0; i < N; ++i) joined[mine * (N * U * L) + c0 + u * L * N + i] = dw[N * u + i];
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < a.cols; c += THREADS<L>) {
       float s = joined[c];
 #pragma unroll
-      for (int k = 1; k < ROWS; ++k) s += joined[k * (8 * U * L) + c];
+      for (int k = 1; k < ROWS; ++k) s += joined[k * (N * U * L) + c];
       out[c] = s;
     }
   }

@@ -41,60 +41,65 @@ void pick_type(uint32_t dtype, F&& f) {
   else if (dtype == QSL_BF16) f(__bf16());
   else f(_Float16());
 }
-// f(whether `written` bytes go past the caches): those of 16-bit types, if the caches do not hold them
-template <class E, class F>
+// f(whether what is read and written goes past the caches), which has to be more than they hold
+template <class F>
 void pick_past(uint64_t written, F&& f) {
-  if constexpr (sizeof(E) == 2) {
-    if (written >= CACHE_BYTES) { f(std::true_type()); return; }
-  }
-  f(std::false_type());
+  if (written >= CACHE_BYTES) f(std::true_type());
+  else f(std::false_type());
 }
+// What the norm writes may do so in rows of up to 32 KiB, in 8 bits of up to 8,192 columns (a lane with longer ones waits at its stores).  us through the
+// caches / past them, whole and in 8 bits: bf16 16,384 rows of 8,192 180 / 175 and 161 / 158.5, 8,192 of 16,384 186 / 175 and 164 / 179, 3,000 of 32,768
+// 151 / 166 and 158 / 185; fp32 8,192 of 8,192 188 / 176 and 158 / 150, 4,096 of 16,384 192 / 206 and 170 / 169.
+template <class E, int L, int U, bool BITS8>
+constexpr bool NORM_MAY_PASS = L * U * 16 <= 32768 && (!BITS8 || L * U * COLS<E> <= 8192);
 template <int V> using Int = std::integral_constant<int, V>;
 
-// f(lanes that hold a row, units each of them holds).  us, residual added, total and y written, bf16 / fp32:
-//   131,072 rows of 128    16 x 1 26 / 51, 64 x 1 48 / 64
-//   32,768 rows of 512     64 x 1 25 / 50, 128 x 1 27 / 54, 256 x 1 42 / 57
-//   30,000 rows of 1,024   64 x 2 44.5 / 95, 128 x 1 44 / 90, 256 x 1 47 / 92;  of 785  64 x 2 38 / 77, 128 x 1 46 / 78
-//   16,384 rows of 2,048   128 x 2 46.5 / 103, 256 x 1 49 / 97.5, 512 x 1 51 / 99
-//   16,384 rows of 4,096   256 x 2 91 / 194, 512 x 1 91.5 / 185, 1024 x 1 101 / 201
-//   8,192 rows of 8,192    512 x 2 91.5 / 192, 1024 x 1 92 / 187
-//   4,096 rows of 16,384   512 x 4 98.5 / 207, 1024 x 2 99 / 198
-// 32 bytes of an array in a thread do best, whatever the type, but for rows of a wave (fp32 64 x 2: the form for 16 bits serves both)
+// f(lanes that hold a row, units each of them holds).  us, residual added, total and y written, through the caches, bf16 / fp32 (of which an array's unit is
+// four columns: twice the lanes or units):
+//   131,072 rows of 128    bf16 16 x 1 26, 64 x 1 48;                   fp32 16 x 2 47.6, 64 x 1 48.7
+//   32,768 rows of 512     bf16 64 x 1 25, 128 x 1 27, 256 x 1 42;      fp32 64 x 2 48.5, 128 x 1 47.5, 256 x 1 49
+//   30,000 rows of 1,024   bf16 64 x 2 44.5, 128 x 1 44, 256 x 1 47;    fp32 64 x 4 88, 128 x 2 85.6, 256 x 1 84, 512 x 1 84.6
+//   30,000 rows of 785     bf16 64 x 2 38, 128 x 1 46;                  fp32 64 x 4 75, 128 x 2 71, 256 x 1 68, 256 x 2 74
+//   16,384 rows of 2,048   bf16 128 x 2 46.5, 256 x 1 49, 512 x 1 51;   fp32 128 x 4 94, 256 x 2 92, 512 x 1 91.5, 1024 x 1 89 (with a mask 96)
+//   16,384 rows of 4,096   bf16 256 x 2 91, 512 x 1 91.5, 1024 x 1 101; fp32 256 x 4 183, 512 x 2 184, 1024 x 1 179 (y alone 109, by 512 x 2 91)
+//   8,192 rows of 8,192    bf16 512 x 2 91.5, 1024 x 1 92;              fp32 512 x 4 189, 1024 x 2 189
+//   4,096 rows of 16,384   bf16 512 x 4 98.5, 1024 x 2 99;              fp32 1024 x 4 191, 1024 x 8 196
+// So two units a lane, from 64 lanes to 1024, then more; short rows take eight columns a lane.
 template <class E, class F>
 void pick_row(uint32_t cols, F&& f) {
-  if (cols <= 16 * 8) f(Int<16>(), Int<1>());
-  else if (cols <= 64 * 8) f(Int<64>(), Int<1>());
-  else if (cols <= 64 * 16) f(Int<64>(), Int<2>());
-  else if (cols > 1024 * 16) f(Int<1024>(), Int<4>());
-  else if (cols > 1024 * 8) f(Int<1024>(), Int<2>());
-  else if constexpr (sizeof(E) == 2) {
-    if (cols <= 128 * 16) f(Int<128>(), Int<2>());
-    else if (cols <= 256 * 16) f(Int<256>(), Int<2>());
-    else f(Int<512>(), Int<2>());
-  } else {
-    if (cols <= 256 * 8) f(Int<256>(), Int<1>());
-    else if (cols <= 512 * 8) f(Int<512>(), Int<1>());
-    else f(Int<1024>(), Int<1>());
-  }
+  constexpr uint32_t N = COLS<E>, K = 8 / N;      // K units: eight columns
+  if (cols <= 16 * 8) f(Int<16>(), Int<K>());
+  else if (cols <= 64 * 8) f(Int<64>(), Int<K>());
+  else if (cols <= 64 * 2 * N) f(Int<64>(), Int<2>());
+  else if (cols <= 128 * 2 * N) f(Int<128>(), Int<2>());
+  else if (cols <= 256 * 2 * N) f(Int<256>(), Int<2>());
+  else if (cols <= 512 * 2 * N) f(Int<512>(), Int<2>());
+  else if (cols <= 1024 * 2 * N) f(Int<1024>(), Int<2>());
+  else if (cols <= 1024 * 16) f(Int<1024>(), Int<2 * K>());
+  else f(Int<1024>(), Int<4 * K>());
 }
-// The gradient's, which holds three arrays and the sum for dweight.  us with all of them, a mask and k_sum_parts, bf16 / fp32, with waves on a SIMD unit:
-//   131,072 rows of 128    16 x 1  1: 44 / 89, 2: 36 / 68, 3: 37 / 67, 4: 39 / 70
-//   32,768 rows of 512     64 x 1  1: 44 / 66, 2: 37 / 67, 3: 37 / 70, 4: 39 / 70
-//   30,000 rows of 785     64 x 2  1: 78 / 102, 2: 56 / 102, 3: 54 / 115, 4: 62 / 104;  128 x 1  2: 75 / 100, 3: 65 / 105
-//   16,384 rows of 2,048   256 x 1  1: 84 / 121, 2: 65 / 127, 3: 69 / 130, 4: 71 / 134;  128 x 2  2: 69 / 135
-//   16,384 rows of 4,096   512 x 1  2: 121 / 247, 4: 132 / 250;  256 x 2  2: 133 / 247, 3: 135 / 247
-//   8,192 rows of 8,192    512 x 2  2: 128 / 250, 4: 131 / 252;  1024 x 1  4: 131 / 249
-//   4,096 rows of 16,384   1024 x 2  4: 130 / 262;  512 x 4  2: 132 / 268;  2,048 of 32,768  1024 x 4  4: 259 / 347
-template <class F>
+// The gradient's, which holds three arrays and the sum for dweight.  us with all of them, a mask and k_sum_parts, through the caches, with 1, 2, 3, 4 waves on
+// a SIMD unit (1024 lanes: 4):
+//   131,072 rows of 128    bf16 16 x 1 44, 36, 37, 39;                               fp32 16 x 2 98, 69, 66, 68
+//   32,768 rows of 512     bf16 64 x 1 44, 37, 37, 39;                               fp32 64 x 2 69, 67, 67, 70
+//   30,000 rows of 785     bf16 64 x 2 78, 56, 54, 62;  128 x 1 -, 75, 65;           fp32 64 x 4 103, 98, 108, 101;  256 x 1 157, 102, 97, 101
+//   120 rows of 785                                                                  fp32 64 x 4 7.9;  256 x 1 6.6 (but up to 8 rows one launch, not two)
+//   16,384 rows of 2,048   bf16 256 x 1 84, 65, 69, 71;  128 x 2 -, 69;              fp32 512 x 1 -, 122, -, 130;  256 x 2 136, 131, 132, 134
+//   16,384 rows of 4,096   bf16 512 x 1 -, 121, -, 132;  256 x 2 -, 133, 135;        fp32 512 x 2 -, 247, -, 250;  1024 x 1 248
+//   8,192 rows of 8,192    bf16 512 x 2 -, 128, -, 131;  1024 x 1 131;               fp32 512 x 4 -, 246, -, 250;  1024 x 2 243
+//   4,096 rows of 16,384   bf16 1024 x 2 130;  512 x 4 -, 132;                       fp32 1024 x 4 263;  1024 x 8 407
+//   2,048 rows of 32,768   bf16 1024 x 4 229;                                        fp32 1024 x 8 368
+template <class E, class F>
 void pick_row_back(uint32_t cols, F&& f) {
-  if (cols <= 16 * 8) f(Int<16>(), Int<1>());
-  else if (cols <= 64 * 8) f(Int<64>(), Int<1>());
-  else if (cols <= 64 * 16) f(Int<64>(), Int<2>());
-  else if (cols <= 256 * 8) f(Int<256>(), Int<1>());
-  else if (cols <= 512 * 8) f(Int<512>(), Int<1>());
-  else if (cols <= 512 * 16) f(Int<512>(), Int<2>());
-  else if (cols <= 1024 * 16) f(Int<1024>(), Int<2>());
-  else f(Int<1024>(), Int<4>());
+  constexpr uint32_t K = 8 / COLS<E>;
+  if (cols <= 16 * 8) f(Int<16>(), Int<K>());
+  else if (cols <= 64 * 8) f(Int<64>(), Int<K>());
+  else if (cols <= 64 * 16) f(Int<64>(), Int<2 * K>());
+  else if (cols <= 256 * 8) f(Int<256 * K>(), Int<1>());
+  else if (cols <= 512 * 8) f(Int<512>(), Int<K>());
+  else if (cols <= 512 * 16) f(Int<512 * K>(), Int<2>());
+  else if (cols <= 1024 * 16) f(Int<1024>(), Int<2 * K>());
+  else f(Int<1024>(), Int<4 * K>());
 }
 
 dim3 grid_of(uint64_t blocks) {
@@ -112,9 +117,11 @@ Memory weight_of(const qsl_norm* n) { return array(n->weight, static_cast<uint64
 // left to one block, whose sum is dweight: they take 1 to 2 us in it, another launch takes the host 4.
 uint32_t back_blocks(const qsl_norm* n) {
   uint32_t blocks = 0;
-  pick_row_back(n->cols, [&](auto l, auto) {
-    const uint64_t th = THREADS<l()>, per = th / l(), most = th == 256 ? 512 : 256;
-    blocks = n->rows <= 2 * per ? (n->rows != 0) : static_cast<uint32_t>(std::min<uint64_t>((n->rows + per - 1) / per, most));
+  pick_type(n->dtype, [&](auto e) {
+    pick_row_back<decltype(e)>(n->cols, [&](auto l, auto) {
+      const uint64_t th = THREADS<l()>, per = th / l(), most = th == 256 ? 512 : 256;
+      blocks = n->rows <= 2 * per ? (n->rows != 0) : static_cast<uint32_t>(std::min<uint64_t>((n->rows + per - 1) / per, most));
+    });
   });
   return blocks;
 }
@@ -148,12 +155,12 @@ extern "C" qsl_status qsl_dropout(const qsl_dropout_args* args, void* hip_stream
   auto at = [&](const qsl_rows& m) { return rows_at(m.data, rows, cols, m.stride, es); };
   for (const qsl_rows* m : {&x, &res}) if (m->data && !same(*m, y, rows) && meet(at(*m), at(y))) return QSL_ERR_INVALID_ARG;
   if (meet(round_of(args->drop), at(y))) return QSL_ERR_INVALID_ARG;
-  const uint32_t units = static_cast<uint32_t>((cols + 7) / 8);
+  const uint32_t units = static_cast<uint32_t>((cols * es + 15) / 16);
   const DropArgs a = {x.data, res.data, y.data, x.stride, res.stride, y.stride, rows, args->cols, units, drop_of(args->drop)};
   const uint64_t blocks = (rows * units + DROP_THREADS - 1) / DROP_THREADS;
   pick_type(args->dtype, [&](auto e) {
     typedef decltype(e) E;
-    pick_past<E>(rows * cols * es, [&](auto past) { launch(k_dropout<E, past()>, grid_of(blocks), DROP_THREADS, static_cast<hipStream_t>(hip_stream), a); });
+    pick_past(rows * cols * es, [&](auto past) { launch(k_dropout<E, past()>, grid_of(blocks), DROP_THREADS, static_cast<hipStream_t>(hip_stream), a); });
   });
   return launched();
 }
@@ -184,15 +191,18 @@ extern "C" qsl_status qsl_rms_norm(const qsl_rms_norm_args* args, void* hip_stre
   const NormArgs a = {x.data, res.data, norm->weight, total.data, y.data, args->scales, x.stride, res.stride, total.stride, y.stride, rows, norm->cols,
                       norm->weight_dtype == QSL_F32, out_dtype == QSL_E4M3, group ? 31u - __builtin_clz(group) : 0u, norm->eps, drop_of(args->drop)};
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const uint64_t written = rows * cols * ((total.data ? es : 0) + elem_size(out_dtype));
   pick_type(norm->dtype, [&](auto e) {
     typedef decltype(e) E;
     pick_row<E>(norm->cols, [&](auto l, auto u) {
       constexpr int th = THREADS<l()>, per = th / l();
       const dim3 grid = grid_of((rows + per - 1) / per);
-      pick_past<E>(rows * cols * ((total.data ? es : 0) + elem_size(out_dtype)), [&](auto past) {
-        if (bits8) launch(k_rms_norm<E, l(), u(), true, past()>, grid, th, stream, a);
-        else launch(k_rms_norm<E, l(), u(), false, past()>, grid, th, stream, a);
-      });
+      auto norm_of = [&](auto b8) {
+        if constexpr (NORM_MAY_PASS<E, l(), u(), b8()>) pick_past(written, [&](auto past) { launch(k_rms_norm<E, l(), u(), b8(), past()>, grid, th, stream, a); });
+        else launch(k_rms_norm<E, l(), u(), b8(), false>, grid, th, stream, a);
+      };
+      if (bits8) norm_of(std::true_type());
+      else norm_of(std::false_type());
     });
   });
   return launched();
@@ -230,8 +240,8 @@ extern "C" qsl_status qsl_rms_norm_backward(const qsl_rms_norm_backward_args* ar
                         drop_of(args->drop)};
     pick_type(norm->dtype, [&](auto e) {
       typedef decltype(e) E;
-      pick_row_back(norm->cols, [&](auto l, auto u) {
-        pick_past<E>(rows * cols * es * ((dres.data != nullptr) + (dx.data != nullptr)), [&](auto past) {
+      pick_row_back<E>(norm->cols, [&](auto l, auto u) {
+        pick_past(rows * cols * es * ((dres.data != nullptr) + (dx.data != nullptr)), [&](auto past) {
           launch(k_rms_norm_backward<E, l(), u(), past()>, dim3(blocks), THREADS<l()>, stream, a);
         });
       });
