@@ -514,9 +514,9 @@ struct BackArgs {
   Drop drop;
 };
 
-// Both sums over a row at once, then the results from registers.  Bound by memory: 16,384 rows of 4,096 bf16 with a mask (five arrays) 110 us, 6.1 TB/s, and
+// Both sums over a row at once, then the results from registers.  Bound by memory: 16,384 rows of 4,096 bf16 with a mask (five arrays) 112 us, 6.0 TB/s, and
 // 4.5 for k_sum_parts; rows of more than 8,192 columns, a block to a compute unit, by the way from loads to stores that little else runs beside
-// (2,047 rows of 12,289 fp16, four arrays, 44 us, 4.6 TB/s, and 5.3).
+// (2,047 rows of 12,289 fp16, four arrays, 44.5 us, 4.5 TB/s, and 5.3).
 // A block goes through rows that lie a grid apart and keeps its sum for dw in registers.  A unit's registers take the next row's as soon as this row's is
 // unpacked for its results, so that these loads are under way beside the masks and the stores and few waves are enough (us, bf16, loads at a row's
 // beginning / ahead: 16,384 rows of 4,096 128.8 / 120.7, of 2,048 70 / 65, 2,047 rows of 12,288 58.8 / 56.3).
