@@ -188,8 +188,10 @@ extern "C" qsl_status qsl_rms_norm(const qsl_rms_norm_args* args, void* hip_stre
     if ((bits8 || !same(*m, y, rows)) && meet(in, out_y)) return QSL_ERR_INVALID_ARG;
     if (meet(in, out_s)) return QSL_ERR_INVALID_ARG;
   }
+  // a group that holds the row is the row: so no group has more than the 16 lanes of a short one
+  const uint32_t group_bits = group && group < cols ? 31u - __builtin_clz(group) : 0u;
   const NormArgs a = {x.data, res.data, norm->weight, total.data, y.data, args->scales, x.stride, res.stride, total.stride, y.stride, rows, norm->cols,
-                      norm->weight_dtype == QSL_F32, out_dtype == QSL_E4M3, group ? 31u - __builtin_clz(group) : 0u, norm->eps, drop_of(args->drop)};
+                      norm->weight_dtype == QSL_F32, out_dtype == QSL_E4M3, group_bits, norm->eps, drop_of(args->drop)};
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const uint64_t written = rows * cols * ((total.data ? es : 0) + elem_size(out_dtype));
   pick_type(norm->dtype, [&](auto e) {

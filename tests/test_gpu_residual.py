@@ -156,29 +156,43 @@ def test_rms_norm(B, C, dtype):
         assert untouched(held, C) and untouched(held_t, C)
 
 
+def check_8_bits(B, C, code, dtype, pad, group, wk, p, x, res):
+    N, Q = x.shape[0], 448.0 if code is torch.float8_e4m3fn else 127.0
+    w = weight_of(C, wk, dtype)
+    G = -(-C // group) if group else 1
+    q, held = room(N, C, code, pad)
+    t, s = room(N, C, dtype)[0], torch.full((N, G), 77.0, device=dev)
+    B.rms_norm(x, q, weight=w, residual=res, total=t, p=p, seed=2, scales=s, group=group)
+    h, tol = X.total_of(x, res, X.kept(N, C, p, seed=2) if p else None, p)
+    y, tol_y = X.norm_of(h, tol, w, 1e-6)
+    want_s, tol_s, spread = X.scales_of(y, tol_y, group, Q)
+    X.check(s, want_s, tol_s, f"{C}: scales, group {group}")
+    v = y / spread
+    t_v = 1.01 * (tol_y / spread + v.abs() * (tol_s / want_s).repeat_interleave(group or C, 1)[:, :C] + 3 * X.U * v.abs())
+    half = torch.full_like(v, 0.5) if code is torch.int8 else X.rounding(v, t_v, code)
+    X.check(q.float(), v, half + t_v, f"{C}: codes, group {group}")
+    X.check(t, h, tol + X.rounding(h, tol, t.dtype), f"{C}: total")
+    assert float(q.float().abs().max()) <= Q and untouched(held, C)
+
+
 @pytest.mark.parametrize("code", [torch.float8_e4m3fn, torch.int8])
 @pytest.mark.parametrize("C", [1, 8, 9, 31, 32, 33, 128, 130, 500, 512, 785, 1024, 1100, 2048, 3000, 4096, 8192, 9001, 16384, 20000, 32768])
 def test_rms_norm_in_8_bits(B, C, code):
     """Every code is nearest to y / scale: half a step of e4m3 is 2^-4 of the value or 2^-10, of whole numbers 1/2; y and the scale are off by their
     tolerances (the scale's moves a value by as much relative), and Q / a, its product and the division for the scale by 3 u."""
     N = rows_for(C)
-    Q = 448.0 if code is torch.float8_e4m3fn else 127.0
     for k, (dtype, pad, group, wk, p) in enumerate((("bf16", 0, 0, "same", 0.0), ("fp32", 3, 32, "none", 0.2), ("fp16", 1, 64, "fp32", 0.0), ("bf16", 5, 128, "fp32", 0.1))):
-        x, res, w = rows_of(N, C, dtype, k, pad), rows_of(N, C, dtype, 9, 0, 2.0), weight_of(C, wk, dtype)
-        G = -(-C // group) if group else 1
-        q, held = room(N, C, code, pad)
-        t, s = room(N, C, dtype)[0], torch.full((N, G), 77.0, device=dev)
-        B.rms_norm(x, q, weight=w, residual=res, total=t, p=p, seed=2, scales=s, group=group)
-        h, tol = X.total_of(x, res, X.kept(N, C, p, seed=2) if p else None, p)
-        y, tol_y = X.norm_of(h, tol, w, 1e-6)
-        want_s, tol_s, spread = X.scales_of(y, tol_y, group, Q)
-        X.check(s, want_s, tol_s, f"{C}: scales, group {group}")
-        v = y / spread
-        t_v = 1.01 * (tol_y / spread + v.abs() * (tol_s / want_s).repeat_interleave(group or C, 1)[:, :C] + 3 * X.U * v.abs())
-        half = torch.full_like(v, 0.5) if code is torch.int8 else X.rounding(v, t_v, code)
-        X.check(q.float(), v, half + t_v, f"{C}: codes, group {group}")
-        X.check(t, h, tol + X.rounding(h, tol, t.dtype), f"{C}: total")
-        assert float(q.float().abs().max()) <= Q and untouched(held, C)
+        check_8_bits(B, C, code, dtype, pad, group, wk, p, rows_of(N, C, dtype, k, pad), rows_of(N, C, dtype, 9, 0, 2.0))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("C", [3, 20, 64, 65, 100, 127, 128, 129, 200, 512, 1000, 2047, 4096, 5001])
+def test_groups_of_every_type(B, C, dtype):
+    """Every size of a group with every type, by the same tolerances."""
+    N = rows_for(C)
+    for code in (torch.float8_e4m3fn, torch.int8):
+        for group in (0, 32, 64, 128):
+            check_8_bits(B, C, code, dtype, 0, group, "same", 0.0, rows_of(N, C, dtype, group), None)
 
 
 def test_codes_of_known_values(B):
@@ -312,7 +326,8 @@ def test_the_weights_gradient_of_few_rows(B, C):
         X.check(dw, want, tol, f"{N} x {C}")
 
 
-@pytest.mark.parametrize("N,C,dtype", [(70000, 2048, "bf16"), (16500, 8200, "fp16"), (17000, 4099, "bf16"), (300000, 513, "bf16"), (1100000, 127, "fp16")])
+@pytest.mark.parametrize("N,C,dtype", [(70000, 2048, "bf16"), (16500, 8200, "fp16"), (17000, 4099, "bf16"), (300000, 513, "bf16"), (1100000, 127, "fp16"),
+                                        (600000, 127, "fp32"), (33000, 2100, "fp32"), (8300, 8200, "fp32"), (4200, 16390, "fp32"), (8300, 16400, "bf16")])
 def test_results_that_the_caches_do_not_hold(B, N, C, dtype):
     """More than 256 MB written: the first and the last rows, and rows between, against the definitions; all of them against smaller calls."""
     g = torch.Generator(device=dev).manual_seed(1)
