@@ -522,6 +522,8 @@ struct BackArgs {
 // beginning / ahead: 16,384 rows of 4,096 128.8 / 120.7, of 2,048 70 / 65, 2,047 rows of 12,288 58.8 / 56.3).
 // Where 1024 threads leave a thread 128 registers, the weights are held in LDS, every thread's own; where that is not enough (TIGHT), nothing is loaded
 // ahead, and what else arrives at the totals is loaded where it is added (fp32, 2,047 rows of 12,288: 104 us, with loads ahead 127).
+// There too the compiler is kept from holding what it can form again: offsets and the first rounds of the masks, which depend on the lane alone, and unpacked
+// 16-bit values (4,096 rows of 32,768 bf16 456 us without, 333 without the last, 272; 2,048 of fp32 368 / 275).
 template <class E, int L, int U> constexpr bool WEIGHT_IN_LDS = L * U * COLS<E> >= 16384;
 template <int L, int U> constexpr bool TIGHT_ROW = L * U >= 4096;
 template <class E, int L, int U, bool PAST>
@@ -533,7 +535,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   __shared__ quad weights[LDS ? N / 4 * U : 1][LDS ? L : 1];
   __shared__ Two sums[2][2][WAVES<L>];
   __shared__ float joined[ROWS > 1 ? ROWS * N * U * L : 1];
-  const uint32_t lane = threadIdx.x % L, c0 = lane * N;
+  uint32_t lane = threadIdx.x % L, c0 = lane * N;
   const Key key = key_of(a.drop);
   float w_all[LDS ? N : N * U], dw[N * U];
   if constexpr (LDS) {
@@ -545,6 +547,13 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   } else {
     load_weight<E, U, TINY<L>>(a.weight, a.weight_is_float, c0, L * N, a.cols, w_all);
   }
+  // what is formed of the lane's number is formed again behind this, not held in registers from row to row
+  auto lane_again = [&]() {
+    if constexpr (TIGHT) {
+      asm volatile("" : "+v"(lane));
+      c0 = lane * N;
+    }
+  };
   auto weight_of = [&](int u, float* w) {
     if constexpr (LDS) {
 #pragma unroll
@@ -578,6 +587,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
   uint32_t turn = 0;             // a row's sums go where those before last stood: there is a barrier between reading these and writing them
   for (uint64_t base = static_cast<uint64_t>(blockIdx.x) * ROWS; base < a.rows; base += step, row += step) {
     const uint32_t end = row < a.rows ? a.cols : 0;
+    lane_again();
     if constexpr (TIGHT) {
 #pragma unroll
       for (int u = 0; u < U; ++u) load_unit(row, u);
@@ -598,6 +608,10 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
         for (int i = 0; i < N; ++i) {
           s.a = __builtin_fmaf(h[i], h[i], s.a);
           s.b = __builtin_fmaf(d[i] * w[i], h[i], s.b);
+        }
+        if constexpr (TIGHT && sizeof(E) == 2) {      // (unpacked again for the results)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(hq[u].w[i]), "+v"(dyq[u].w[i]));
         }
       }
       return s;
@@ -622,6 +636,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
     turn ^= 1;
     const float r = 1.0f / sqrtf(s.a / static_cast<float>(a.cols) + eps);
     const float mean = s.b * r / static_cast<float>(a.cols), rf = r * f;
+    lane_again();
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float h[N], d[N], t[N], w[N];
