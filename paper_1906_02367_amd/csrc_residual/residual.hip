@@ -88,7 +88,7 @@ void pick_row(uint32_t cols, F&& f) {
 //   16,384 rows of 4,096   bf16 512 x 1 -, 121, -, 132;  256 x 2 -, 133, 135;        fp32 512 x 2 -, 247, -, 250;  1024 x 1 248
 //   8,192 rows of 8,192    bf16 512 x 2 -, 128, -, 131;  1024 x 1 131;               fp32 512 x 4 -, 246, -, 250;  1024 x 2 243
 //   4,096 rows of 16,384   bf16 1024 x 2 130;  512 x 4 -, 132;                       fp32 1024 x 4 263;  1024 x 8 407
-//   2,048 rows of 32,768   bf16 1024 x 4 229;                                        fp32 1024 x 8 368
+//   2,048 rows of 32,768   bf16 1024 x 4 150;                                        fp32 1024 x 8 275
 template <class E, class F>
 void pick_row_back(uint32_t cols, F&& f) {
   constexpr uint32_t K = 8 / COLS<E>;
