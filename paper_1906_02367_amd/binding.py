@@ -366,7 +366,8 @@ def rms_norm(x, y, weight=None, eps=1e-6, residual=None, total=None, p=0.0, seed
         if scales is not None:
             scales_at = _beside(scales, "scales", dev, torch.float32, (shape[0], -(-shape[1] // group) if group else 1))
     _on_device("qsl_rms_norm", _lib.qsl_rms_norm, dev, _PACK_RMS_NORM(
-        *_norm(shape, dtype, weight, eps, dev), *at, *(_ABSENT if residual is None else _matrix(residual, "residual", dev, dtype, shape)), *(_ABSENT if total is None else _matrix(total, "total", dev, dtype, shape)),
+        *_norm(shape, dtype, weight, eps, dev), *at, *(_ABSENT if residual is None else _matrix(residual, "residual", dev, dtype, shape)),
+        *(_ABSENT if total is None else _matrix(total, "total", dev, dtype, shape)),
         *_matrix(y, "y", dev, kind, shape), *(_drop(p, seed, round, row0, round_at, dev) if p else _KEEP_ALL), out, group, scales_at))
 
 
