@@ -379,11 +379,15 @@ template <int N> __device__ __forceinline__ void store_codes(uint8_t* row, uint3
                                             float* scale_at) {
   const float Q = is_e4m3 ? 448.0f : 127.0f, t_max = __uint_as_float(most), y_max = t_max * r, a = fmaxf(y_max, 0x1p-100f);
   const bool bad = !(y_max < INF);                                // an infinity or a NaN
-  const bool plain = !(t_max >= 0x1p-100f && y_max >= 0x1p-100f);      // next to nothing: by y itself
-  const float div = plain ? a : t_max, q = Q / div, inv = plain ? q * r : q, lo_inv = plain ? 0.0f : q, inv_lo = __builtin_fmaf(-q, div, Q) * (lo_inv / Q);
+  // next to nothing: by y itself, t r before its product with Q / a, since |y| Q / a <= Q where r Q / a may be infinite
+  const bool plain = !(t_max >= 0x1p-100f && y_max >= 0x1p-100f);
+  const float first = plain ? r : 1.0f, div = plain ? a : t_max, inv = Q / div, lo_inv = plain ? 0.0f : inv, inv_lo = __builtin_fmaf(-inv, div, Q) * (lo_inv / Q);
   float v[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = __builtin_fmaf(t[i], inv, __builtin_fmaf(t[i], inv_lo, t_lo[i] * lo_inv));
+  for (int i = 0; i < N; ++i) {
+    const float f = t[i] * first;
+    v[i] = __builtin_fmaf(f, inv, __builtin_fmaf(f, inv_lo, t_lo[i] * lo_inv));
+  }
   uint32_t code[N / 4];
 #pragma unroll
   for (int k = 0; k < N / 4; ++k) {
