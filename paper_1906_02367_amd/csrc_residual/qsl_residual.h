@@ -288,7 +288,8 @@ template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t x, uint32_
   return x;
 }
 
-// Squares of totals from 2^64 on do not fit into a float: such rows are taken times this.  2^56 squared times QSL_NORM_COLS_MAX does.
+// Squares of totals from 2^64 on do not fit into a float: such rows are taken times this, eps times its square.  (2^56 squared times QSL_NORM_COLS_MAX fits.  Of
+// a usual eps nothing is left, but 2^100 counts beside a mean of 2^113, from where on a sum over QSL_NORM_COLS_MAX columns may not fit.)
 constexpr float SMALLER = 0x1p-72f;
 constexpr float INF = __builtin_inff();
 
@@ -455,16 +456,15 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
     for (int i = 0; i < N; ++i) ss = __builtin_fmaf(v[i], v[i], ss);
   }
   ss = row_sum<L>(ss, sums[0]);
-  float eps = a.eps;
+  float f = 1.0f;
   if (__any(ss == INF)) {      // (the same answer in all waves of a row)
-    const float f = ss == INF ? SMALLER : 1.0f;
+    f = ss == INF ? SMALLER : 1.0f;
     ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < N * U; ++i) { h[i] *= f; ss = __builtin_fmaf(h[i], h[i], ss); }
     ss = row_sum<L>(ss, sums[1]);
-    eps = f == 1.0f ? eps : 0.0f;
   }
-  const float r = 1.0f / sqrtf(ss / static_cast<float>(a.cols) + eps);
+  const float r = 1.0f / sqrtf(ss / static_cast<float>(a.cols) + a.eps * f * f);
   float lo[BITS8 ? N * U : 1];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -621,11 +621,10 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
       return s;
     };
     Two s = row_sums<L>(sum(), sums[turn][0]);
-    float f = 1.0f, eps = a.eps;
+    float f = 1.0f;
     if (__any(s.a == INF)) {
       if (s.a == INF) {      // the totals times f, in their type: what that rounds is nothing beside the row's largest
         f = SMALLER;
-        eps = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           float h[N];
@@ -638,7 +637,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
       s = row_sums<L>(sum(), sums[turn][1]);
     }
     turn ^= 1;
-    const float r = 1.0f / sqrtf(s.a / static_cast<float>(a.cols) + eps);
+    const float r = 1.0f / sqrtf(s.a / static_cast<float>(a.cols) + a.eps * f * f);
     const float mean = s.b * r / static_cast<float>(a.cols), rf = r * f;
     lane_again();
 #pragma unroll

@@ -58,3 +58,26 @@ def test_codes_of_rows_next_to_nothing(B, C, code):
                 assert not q[1].any() and (s[1] == least).all() and not q[4, 32:64].any()
                 if group and C > 32:
                     assert s[4, 1] == least
+
+
+# ---- rows whose squares do not fit ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", [100, 1000, 2048, 4096, 8192, 16384, 32768])
+def test_rows_whose_squares_hardly_fit_beside_a_large_eps(B, C, dtype):
+    """eps counts on both sides of the border: a mean of 2^128 / C, where the sum no longer fits, is not far enough above 2^100 to leave it out."""
+    eps, border = 2.0 ** 100, 2.0 ** 64 / math.sqrt(C)
+    x, dy, w = rows_of(8, C, dtype, 1), rows_of(8, C, dtype, 2), rows_of(1, C, "fp32", 3)[0] * 0.3 + 1.0
+    for n, f in {1: 0.9, 2: 0.97, 3: 1.03, 4: 1.2, 6: 8.0, 7: 2.0 ** -10}.items():
+        x[n] = (torch.sign(x[n].double()) * border * f).to(x.dtype)
+    h = x.cpu().double()
+    fits = (h * h).sum(1) < 2.0 ** 128 * (1 - 2.0 ** -12)
+    assert not bool(fits[3]) and not bool(fits[6]) and bool(fits[1]) and bool(fits[7])
+    y, dres, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(C, device=dev)
+    B.rms_norm(x, y, weight=w, eps=eps)
+    want, tol = X.norm_of(h, torch.zeros_like(h), w, eps)
+    X.check(y, want, tol + X.rounding(want, tol, y.dtype), f"{C}: y")
+    B.rms_norm_backward(x, dy, weight=w, eps=eps, dresidual=dres, dweight=dw)
+    want, tol, want_w, tol_w = X.backward(x, dy, w, eps)
+    X.check(dres, want, tol + X.rounding(want, tol, y.dtype), f"{C}: gradient")
+    X.check(dw, want_w, tol_w, f"{C}: dweight")
+    check_codes(B, x, w, eps, E4M3, 0)
