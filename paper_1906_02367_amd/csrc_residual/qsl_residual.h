@@ -373,22 +373,19 @@ template <class E, int U, bool TINY> __device__ __forceinline__ void load_weight
     load(static_cast<const E*>(weight));
   }
 }
-// 8-bit codes of a unit, N bytes.  y = r t with t = w h, whose rounding error is t_lo; `most`: the bits of the group's largest |t|.  y Q / a =
-// t Q / max |t|: r does not enter, and with the errors of t and of the quotient the code is that of the exact value for all that h allows.  (Of 24.6 million
+// 8-bit codes of a unit, N bytes.  y = m t with t = w (h 2^e), r = m 2^e, 1 <= m < 2, and the product's rounding error t_lo: that power of two is exact, and
+// t fits where y does, large weights and small ones; `most`: the bits of the group's largest |t|.  y Q / a =
+// t Q / max |t|: m does not enter, and with the errors of t and of the quotient the code is that of the exact value for all that h allows.  (Of 24.6 million
 // e4m3 codes of rows of 4,096 with a residual 48 are not those of 64 bits, by elementary operations in 32 bits 67; fp32 8 and 16.)
-template <int N> __device__ __forceinline__ void store_codes(uint8_t* row, uint32_t c, uint32_t cols, const float* t, const float* t_lo, uint32_t most, float r, bool is_e4m3,
+template <int N> __device__ __forceinline__ void store_codes(uint8_t* row, uint32_t c, uint32_t cols, const float* t, const float* t_lo, uint32_t most, float m, bool is_e4m3,
                                             float* scale_at) {
-  const float Q = is_e4m3 ? 448.0f : 127.0f, t_max = __uint_as_float(most), y_max = t_max * r, a = fmaxf(y_max, 0x1p-100f);
-  const bool bad = !(y_max < INF);                                // an infinity or a NaN
-  // next to nothing: by y itself, t r before its product with Q / a, since |y| Q / a <= Q where r Q / a may be infinite
-  const bool plain = !(t_max >= 0x1p-100f && y_max >= 0x1p-100f);
-  const float first = plain ? r : 1.0f, div = plain ? a : t_max, inv = Q / div, lo_inv = plain ? 0.0f : inv, inv_lo = __builtin_fmaf(-inv, div, Q) * (lo_inv / Q);
+  const float Q = is_e4m3 ? 448.0f : 127.0f, t_max = __uint_as_float(most), y_max = t_max * m, a = fmaxf(y_max, 0x1p-100f);
+  const bool bad = !(y_max < INF);                    // an infinity or a NaN
+  const bool plain = !(y_max >= 0x1p-100f);           // next to nothing: by y itself, |y| Q / a <= Q
+  const float div = plain ? a : t_max, q = Q / div, inv = plain ? q * m : q, lo_inv = plain ? 0.0f : q, inv_lo = __builtin_fmaf(-q, div, Q) * (lo_inv / Q);
   float v[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float f = t[i] * first;
-    v[i] = __builtin_fmaf(f, inv, __builtin_fmaf(f, inv_lo, t_lo[i] * lo_inv));
-  }
+  for (int i = 0; i < N; ++i) v[i] = __builtin_fmaf(t[i], inv, __builtin_fmaf(t[i], inv_lo, t_lo[i] * lo_inv));
   uint32_t code[N / 4];
 #pragma unroll
   for (int k = 0; k < N / 4; ++k) {
@@ -465,6 +462,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
     ss = row_sum<L>(ss, sums[1]);
   }
   const float r = 1.0f / sqrtf(ss / static_cast<float>(a.cols) + a.eps * f * f);
+  const float two_e = __uint_as_float(__float_as_uint(r) & 0x7F800000u), m = __uint_as_float((__float_as_uint(r) & 0x007FFFFFu) | 0x3F800000u);      // (r NaN: 2^e infinite)
   float lo[BITS8 ? N * U : 1];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -472,8 +470,8 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
 #pragma unroll
     for (int k = N * u; k < N * u + N; ++k) {
       if constexpr (BITS8) {
-        const float t = h[k] * w[k];
-        lo[k] = __builtin_fmaf(h[k], w[k], -t);
+        const float x2 = h[k] * two_e, t = x2 * w[k];
+        lo[k] = __builtin_fmaf(x2, w[k], -t);
         h[k] = t;
       } else {
         h[k] = h[k] * r * w[k];
@@ -499,7 +497,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm(NormArgs a) {
     for (int u = 0; u < U; ++u) {
       const uint32_t c = c0 + u * L * N;
       float* const scale_at = a.scales + row * of_row + (a.group_bits ? c >> a.group_bits : 0);
-      if (c < end) store_codes<N>(static_cast<uint8_t*>(a.y) + row * a.y_stride, c, end, h + N * u, lo + N * u, a.group_bits ? most[u] : all, r, a.is_e4m3,
+      if (c < end) store_codes<N>(static_cast<uint8_t*>(a.y) + row * a.y_stride, c, end, h + N * u, lo + N * u, a.group_bits ? most[u] : all, m, a.is_e4m3,
                                   (a.group_bits ? (c & in_group) == 0 : c == 0) ? scale_at : nullptr);
     }
   }

@@ -60,6 +60,33 @@ def test_codes_of_rows_next_to_nothing(B, C, code):
                     assert s[4, 1] == least
 
 
+@pytest.mark.parametrize("code", [E4M3, I8])
+@pytest.mark.parametrize("C", [20, 130, 1000, 4100, 9000, 20000])
+def test_codes_with_weights_far_from_one(B, C, code):
+    """y fits where weight times total does not, and is above the least scale where that product has lost bits: fp32 weights of 2^70 and 2^-60 on rows up to
+    2^62 and down to 2^-75, in one row as well.  (Products of the row's own power of two are exact, so no tolerance more.)"""
+    for dtype, eps in (("fp32", 1e-6), ("bf16", 1e-12), ("fp32", 2.0 ** -100)):
+        x = rows_of(9, C, dtype, 1)
+        for n, f in {1: 2.0 ** 50, 2: 2.0 ** 62 / math.sqrt(C), 4: 2.0 ** 80, 5: 2.0 ** -30, 6: 2.0 ** -60, 7: 2.0 ** -75}.items():
+            x[n] = rows_of(1, C, dtype, n, f)[0]
+        w = rows_of(1, C, "fp32", 9)[0] * 0.3 + 1.0
+        for size in (2.0 ** 70, 2.0 ** 110, 2.0 ** -60, 2.0 ** -90):
+            check_codes(B, x, w * size, eps, code, 0)
+            check_codes(B, x, w * size, eps, code, 32)
+        mixed = w.clone()
+        mixed[::3], mixed[1::5] = w[::3] * 2.0 ** 70, w[1::5] * 2.0 ** -60
+        check_codes(B, x, mixed, eps, code, 0)
+        check_codes(B, x, mixed, eps, code, 64)
+    # what y itself does not fit into makes its group NaN, as it makes the whole type's y infinite
+    x, w = torch.ones(2, C, device=dev), torch.ones(C, device=dev)
+    x[0, 3], w[3], w[C - 1] = 8.0, 2.0 ** 127, 2.0 ** 100
+    q, s, y = torch.ones(2, C, device=dev).to(code), torch.empty(2, 1, device=dev), torch.empty_like(x)
+    B.rms_norm(x, q, weight=w, scales=s)
+    B.rms_norm(x, y, weight=w)
+    want = torch.isinf(y).any(1)
+    assert bool(want[0]) and not bool(want[1]) and torch.equal(torch.isnan(s[:, 0]), want) and not q.float()[0].any()
+
+
 # ---- rows whose squares do not fit ---------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("C", [100, 1000, 2048, 4096, 8192, 16384, 32768])
