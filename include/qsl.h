@@ -422,7 +422,7 @@ size_t qsl_rms_norm_workspace_bytes(const qsl_norm *norm);
 /* The gradient of qsl_rms_norm (of y before any rounding to 8 bits), from the totals as they were stored: with r = 1 / sqrt(mean total^2 + eps),
  * u = r total, g = weight dy,
  *     dresidual = r (g - u mean_j(g_j u_j)) + dtotal,      dx = drop(dresidual),      dweight = sum over the rows of dy u
- * dresidual, dx and dweight: one of the three has to be there. */
+ * dresidual, dx and dweight: one of the three has to be there.  Finite totals whose squares, or whose products with g, do not fit are taken all the same. */
 typedef struct {
   qsl_norm norm;
   qsl_rows total;            /* there (x itself where nothing was added and nothing dropped)                     */

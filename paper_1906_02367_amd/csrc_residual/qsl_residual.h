@@ -291,6 +291,9 @@ template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t x, uint32_
 // Squares of totals from 2^64 on do not fit into a float: such rows are taken times this, eps times its square.  (2^56 squared times QSL_NORM_COLS_MAX fits.  Of
 // a usual eps nothing is left, but 2^100 counts beside a mean of 2^113, from where on a sum over QSL_NORM_COLS_MAX columns may not fit.)
 constexpr float SMALLER = 0x1p-72f;
+// Totals below 2^64, or taken times that, times gradients below 2^128 divided by this fit, and their sums.  (What is lost below 2^-149 is nothing beside the
+// sum of sizes, 2^-40 and more where the products themselves do not fit.)
+constexpr float LARGER = 0x1p96f;
 constexpr float INF = __builtin_inff();
 
 template <int L> constexpr int THREADS = L <= 64 ? 256 : L;      // rows of a wave and less share a block
@@ -598,7 +601,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
     cut_units<U, TINY<L>>(c0, L * N, a.cols, dyq);
     if constexpr (!TIGHT)
       if (a.dtotal) cut_units<U, TINY<L>>(c0, L * N, a.cols, dtq);
-    auto sum = [&]() {
+    auto sum = [&](auto&& g_of) {
       Two s = {0.0f, 0.0f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -609,7 +612,7 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           s.a = __builtin_fmaf(h[i], h[i], s.a);
-          s.b = __builtin_fmaf(d[i] * w[i], h[i], s.b);
+          s.b = __builtin_fmaf(g_of(d[i] * w[i]), h[i], s.b);
         }
         if constexpr (TIGHT && sizeof(E) == 2) {      // (unpacked again for the results)
 #pragma unroll
@@ -618,9 +621,9 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
       }
       return s;
     };
-    Two s = row_sums<L>(sum(), sums[turn][0]);
-    float f = 1.0f;
-    if (__any(s.a == INF)) {
+    Two s = row_sums<L>(sum([](float g) { return g; }), sums[turn][0]);
+    float f = 1.0f, up = 1.0f;
+    if (__any(!(s.a + fabsf(s.b) < INF))) {
       if (s.a == INF) {      // the totals times f, in their type: what that rounds is nothing beside the row's largest
         f = SMALLER;
 #pragma unroll
@@ -632,11 +635,12 @@ __global__ __launch_bounds__(THREADS<L>) void k_rms_norm_backward(BackArgs a) {
           pack(h, hq[u]);
         }
       }
-      s = row_sums<L>(sum(), sums[turn][1]);
+      if (!(fabsf(s.b) < INF)) up = LARGER;
+      s = row_sums<L>(sum([down = up == 1.0f ? 1.0f : 1.0f / LARGER](float g) { return g * down; }), sums[turn][1]);
     }
     turn ^= 1;
     const float r = 1.0f / sqrtf(s.a / static_cast<float>(a.cols) + a.eps * f * f);
-    const float mean = s.b * r / static_cast<float>(a.cols), rf = r * f;
+    const float mean = s.b * r / static_cast<float>(a.cols) * up, rf = r * f;
     lane_again();
 #pragma unroll
     for (int u = 0; u < U; ++u) {

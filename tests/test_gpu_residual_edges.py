@@ -108,3 +108,31 @@ def test_rows_whose_squares_hardly_fit_beside_a_large_eps(B, C, dtype):
     X.check(dres, want, tol + X.rounding(want, tol, y.dtype), f"{C}: gradient")
     X.check(dw, want_w, tol_w, f"{C}: dweight")
     check_codes(B, x, w, eps, E4M3, 0)
+
+
+# ---- the gradient --------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", [4, 100, 500, 1000, 2000, 4000, 8000, 16000, 32768])
+def test_gradients_whose_products_with_the_totals_do_not_fit(B, C, dtype):
+    """dy times a total passes the largest float, dy and the gradient do not.  (2^-126 and less does not occur, so no tolerance more.)"""
+    N = 20
+    x, dy, dt, w = rows_of(N, C, dtype, 1), rows_of(N, C, dtype, 2), rows_of(N, C, dtype, 3), rows_of(1, C, "fp32", 4)[0] * 0.3 + 1.0
+    for n, (a, b) in {2: (2.0 ** 55, 2.0 ** 75), 3: (2.0 ** 55, 2.0 ** 120), 7: (1.0, 2.0 ** 118), 8: (2.0 ** 12, 2.0 ** 118), 11: (2.0 ** 56, 2.0 ** -30), 13: (2.0 ** 100, 2.0 ** 118),
+                      16: (2.0 ** -20, 2.0 ** 112)}.items():
+        x[n], dy[n] = rows_of(1, C, dtype, 10 + n, a)[0], rows_of(1, C, dtype, 40 + n, b)[0]
+    dres, dx = torch.empty_like(x), torch.empty_like(x)
+    B.rms_norm_backward(x, dy, weight=w, eps=1e-6, dtotal=dt, dresidual=dres, dx=dx)
+    want, tol, _, _ = X.backward(x, dy, w, 1e-6, dt)
+    X.check(dres, want, tol + X.rounding(want, tol, x.dtype), f"{C}: gradient")
+    assert torch.equal(dres, dx)
+    # such rows change no others, and what is no number stays none
+    plain, dw = torch.empty_like(x), torch.empty(C, device=dev)
+    quiet, loud = dy.clone(), dy.clone()
+    for n in (2, 3, 7, 8, 13, 16):
+        quiet[n] = 0.0
+    loud[3, C // 2], loud[7, C - 1] = float("nan"), float("inf")
+    B.rms_norm_backward(x, quiet, weight=w, eps=1e-6, dtotal=dt, dresidual=plain)
+    B.rms_norm_backward(x, loud, weight=w, eps=1e-6, dtotal=dt, dresidual=dx)
+    others = [n for n in range(N) if n not in (2, 3, 7, 8, 13, 16)]
+    assert torch.equal(plain[others], dres[others]) and torch.equal(dx[others], dres[others])
+    assert torch.isnan(dx[3]).all() and not torch.isfinite(dx[7]).any() and torch.equal(dx[[2, 8, 13, 16]], dres[[2, 8, 13, 16]])
