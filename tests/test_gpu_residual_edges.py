@@ -136,3 +136,57 @@ def test_gradients_whose_products_with_the_totals_do_not_fit(B, C, dtype):
     others = [n for n in range(N) if n not in (2, 3, 7, 8, 13, 16)]
     assert torch.equal(plain[others], dres[others]) and torch.equal(dx[others], dres[others])
     assert torch.isnan(dx[3]).all() and not torch.isfinite(dx[7]).any() and torch.equal(dx[[2, 8, 13, 16]], dres[[2, 8, 13, 16]])
+
+
+# ---- results that the caches do not hold ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,C", [(t, c) for t in ("fp32", "bf16", "fp16") for c in (120, 500, 1000, 2047, 4096, 8191)])
+def test_codes_that_the_caches_do_not_hold(B, dtype, C):
+    """More than 256 MB of totals and codes: some rows against the definitions, all of them against smaller calls, bit for bit."""
+    N = (2 ** 28 // (C * (5 if dtype == "fp32" else 3))) * 21 // 20 + 3
+    g = torch.Generator(device=dev).manual_seed(1)
+    x, res = (torch.randn(N, C, generator=g, device=dev).to(X.TYPES[dtype]) for _ in range(2))
+    w, p = (rows_of(1, C, "fp32", 3)[0] * 0.3 + 1.0).to(x.dtype), 0.2
+    step = N // 7 + 1
+    for code, group in ((E4M3, 0), (I8, 128), (E4M3, 32)):
+        G = -(-C // group) if group else 1
+        made = lambda n: (torch.empty(n, C, dtype=x.dtype, device=dev), torch.empty(n, C, dtype=code, device=dev), torch.empty(n, G, device=dev))
+        t, q, s = made(N)
+        assert t.numel() * t.element_size() + q.numel() > 2 ** 28
+        B.rms_norm(x, q, weight=w, residual=res, total=t, p=p, seed=1, scales=s, group=group)
+        for a in range(0, N, step):
+            t2, q2, s2 = made(len(x[a:a + step]))
+            B.rms_norm(x[a:a + step], q2, weight=w, residual=res[a:a + step], total=t2, p=p, seed=1, row0=a, scales=s2, group=group)
+            assert torch.equal(t[a:a + step], t2) and torch.equal(q[a:a + step].view(torch.uint8), q2.view(torch.uint8)) and torch.equal(s[a:a + step], s2), (code, group, a)
+        Q = 448.0 if code is E4M3 else 127.0
+        for a in (0, N // 2, N - 5):
+            h, tol = X.total_of(x[a:a + 5], res[a:a + 5], X.kept(5, C, p, seed=1, row0=a), p)
+            y, tol_y = X.norm_of(h, tol, w, 1e-6)
+            want_s, tol_s, spread = X.scales_of(y, tol_y, group, Q)
+            X.check(s[a:a + 5], want_s, tol_s, "scales")
+            v = y / spread
+            t_v = 1.01 * (tol_y / spread + v.abs() * (tol_s / want_s).repeat_interleave(group or C, 1)[:, :C] + 3 * X.U * v.abs())
+            X.check(q[a:a + 5].float(), v, t_v + (torch.full_like(v, 0.5) if code is I8 else X.rounding(v, t_v, code)), "codes")
+            X.check(t[a:a + 5], h, tol + X.rounding(h, tol, t.dtype), "total")
+
+
+@pytest.mark.parametrize("N,C,dtype,past", [(70000, 2048, "bf16", True), (16500, 8200, "fp16", True), (17000, 4099, "bf16", True), (300000, 513, "bf16", True), (1100000, 127, "fp16", True),
+                                            (600000, 127, "fp32", True), (33000, 2100, "fp32", True), (8300, 8200, "fp32", True), (4200, 16390, "fp32", True), (8300, 16400, "bf16", True),
+                                            (600, 16384, "fp32", False), (300, 32768, "fp32", False)])
+def test_the_weights_gradient_of_large_calls(B, N, C, dtype, past):
+    """Against the sum in 64 bits.  A term's roundings: the root's SUM / 2 + 3, the product with the total, that with dy: SUM / 2 + 6; its sums: at most
+    ceil(N / 256) rows one after the other (there are at least 256 blocks), then 16 groups of a block and the blocks, 112 steps."""
+    g = torch.Generator(device=dev).manual_seed(2)
+    h, dy = (torch.randn(N, C, generator=g, device=dev).to(X.TYPES[dtype]) for _ in range(2))
+    w = (rows_of(1, C, "fp32", 3)[0] * 0.3 + 1.0).to(h.dtype)
+    dres, dx, dw = torch.empty_like(h), torch.empty_like(h), torch.empty(C, device=dev)
+    assert (2 * h.numel() * h.element_size() > 2 ** 28) == past
+    B.rms_norm_backward(h, dy, weight=w, eps=1e-5, dresidual=dres, dx=dx, dweight=dw)
+    assert torch.equal(dres, dx)
+    want, size = torch.zeros(C, dtype=torch.float64, device=dev), torch.zeros(C, dtype=torch.float64, device=dev)
+    step = max(1, 2 ** 25 // C)
+    for a in range(0, N, step):
+        k = h[a:a + step].double()
+        terms = dy[a:a + step].double() * k / torch.sqrt((k * k).mean(1, keepdim=True) + 1e-5)
+        want += terms.sum(0)
+        size += terms.abs().sum(0)
+    X.check(dw, want.cpu(), (X.U * (X.SUM / 2 + 6 + math.ceil(N / 256) + 112) * size).cpu(), f"{N} x {C}")
