@@ -130,8 +130,9 @@ class DistilledProblem(SoftmaxProblem):
 
 
 class RegularisedProblem(SoftmaxProblem):
-    """The same data and model on the samples' features x / rms(x), of which a local step drops a share `p` before they are normed.  The masks come
-    from (seed, step, worker, sample): a run that is repeated or resumed (`step`) has the same ones."""
+    """The same data and model on the samples' features x / rms(x), of which a local step drops a share `p` before they are normed.  A mask comes
+    from (seed, step, the sample's place among all workers' mini-batches), whichever sample is drawn there.  A new object repeats a run; one that takes over
+    `step` and the state of `gen`, which draws the samples, goes on with it."""
 
     def __init__(self, problem, p=0.2, eps=1e-6, seed=0):
         self.device, self.R, self.n, self.lam = problem.device, problem.R, problem.n, problem.lam

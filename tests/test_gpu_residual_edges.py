@@ -190,3 +190,24 @@ def test_the_weights_gradient_of_large_calls(B, N, C, dtype, past):
         want += terms.sum(0)
         size += terms.abs().sum(0)
     X.check(dw, want.cpu(), (X.U * (X.SUM / 2 + 6 + math.ceil(N / 256) + 112) * size).cpu(), f"{N} x {C}")
+
+
+# ---- where the training harness uses them --------------------------------------------------------------------------------------
+def test_a_run_that_goes_on_or_is_repeated_has_the_same_gradients():
+    from paper_1906_02367_amd import algorithm1 as A
+    data = A.SoftmaxProblem(seed=4, n_per_worker=20, R=3)
+    new = lambda: A.RegularisedProblem(data, p=0.3, seed=11)
+    w = 0.1 * torch.randn(3, A.D, generator=torch.Generator().manual_seed(2)).to(dev)
+    first, whole, states = new(), [], []
+    for _ in range(6):
+        states.append((first.step, first.gen.get_state()))
+        whole.append(first.minibatch_grads(w, 5))
+    again = new()
+    assert all(torch.equal(again.minibatch_grads(w, 5), g) for g in whole)
+    later = new()
+    later.step = states[4][0]
+    later.gen.set_state(states[4][1])
+    assert all(torch.equal(later.minibatch_grads(w, 5), g) for g in whole[4:])
+    # the mask belongs to the place: the same sample at every place of a mini-batch has another mask at each
+    rows = first.features(data.x[0, :1].expand(15, -1).contiguous(), p=0.3, seed=11, round=0)
+    assert all(not torch.equal(rows[i] == 0, rows[j] == 0) for i in range(15) for j in range(i))
