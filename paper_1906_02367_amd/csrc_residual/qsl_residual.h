@@ -84,8 +84,8 @@ template <class W, int N> __device__ __forceinline__ void shift_out(Unit<W, N>& 
     }
   }
 }
-// PAST: what is read or written is more than the caches hold, so that nothing of it is found there by what runs next: it need not pass through
-// them.  us for 16,384 rows of 4,096, through them / past them: the norm bf16 91 / 88, fp32 182 / 175, and bf16 with a reader of its results behind it
+// PAST: what is written is all that the caches hold, or more, and what is read comes on top, so that little of it is found there by what runs next: it need
+// not pass through them.  us for 16,384 rows of 4,096, through them / past them: the norm bf16 91 / 88, fp32 182 / 175, and bf16 with a reader of its results behind it
 // 161 / 158 (of 8,192 rows, which the caches hold, 81 / 83); the gradient bf16 125.5 / 120, fp32 246 / 230; dropout with a residual fp32 135.5 / 128.
 template <bool PAST, class M> __device__ __forceinline__ M load16(const M* p) {
   if constexpr (PAST) return __builtin_nontemporal_load(p);
@@ -528,7 +528,8 @@ struct BackArgs {
 // Where 1024 threads leave a thread 128 registers, the weights are held in LDS, every thread's own; where that is not enough (TIGHT), nothing is loaded
 // ahead, and what else arrives at the totals is loaded where it is added (fp32, 2,047 rows of 12,288: 104 us, with loads ahead 127).
 // There too the compiler is kept from holding what it can form again: offsets and the first rounds of the masks, which depend on the lane alone, and unpacked
-// 16-bit values (4,096 rows of 32,768 bf16 456 us without, 333 without the last, 272; 2,048 of fp32 368 / 275).
+// 16-bit values (4,096 rows of 32,768 bf16 456 us without, 333 without the last, 272; 2,048 of fp32 368 / 275).  Rows of more than 16,384 columns still have 12
+// (fp32), 20 (bf16) and 32 bytes (fp16) of a lane's registers in memory: 2,048 of 32,768 fp32 260 us (floor 258), bf16 145 (129).
 template <class E, int L, int U> constexpr bool WEIGHT_IN_LDS = L * U * COLS<E> >= 16384;
 template <int L, int U> constexpr bool TIGHT_ROW = L * U >= 4096;
 template <class E, int L, int U, bool PAST>

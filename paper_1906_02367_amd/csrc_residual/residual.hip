@@ -41,7 +41,8 @@ void pick_type(uint32_t dtype, F&& f) {
   else if (dtype == QSL_BF16) f(__bf16());
   else f(_Float16());
 }
-// f(whether what is read and written goes past the caches), which has to be more than they hold
+// f(whether what is read and written goes past the caches).  From what they hold written on: every call reads half as much beside it at least, so that its
+// arrays together are more than that.
 template <class F>
 void pick_past(uint64_t written, F&& f) {
   if (written >= CACHE_BYTES) f(std::true_type());
